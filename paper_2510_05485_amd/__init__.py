@@ -2,6 +2,7 @@
 
 The computation lives in `libtensorbleu.so` (hand-written HIP for gfx950, built from `csrc/` by
 `python -m paper_2510_05485_amd.build`); `binding` marshals PyTorch device tensors into it.
+`losses` holds what a training loop does with such rewards: losses over a policy's logits.
 """
 from .binding import (  # noqa: F401
     LIB_PATH, TB_DEV_LENGTH_RANGE, TB_DEV_TABLE_OVERFLOW, TB_DEV_TOKEN_RANGE, Stats, TensorBLEUError, allocate_workspace, load_library, make_config,
@@ -13,4 +14,8 @@ from .binding import (  # noqa: F401
 from .api import (  # noqa: F401
     BleuScorer, corpus_bleu, lengths_from_padding, pack_reference_lists, pad_references, rouge_n,
     sentence_bleu,
+)
+from .losses import (  # noqa: F401
+    DistillationLoss, PolicyLoss, PreferenceLoss, distillation_loss, distillation_loss_grad,
+    policy_loss, policy_loss_grad, preference_loss, preference_loss_grad, token_logprobs,
 )

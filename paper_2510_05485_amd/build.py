@@ -34,14 +34,15 @@ FLAGS = [
 
 
 def sources():
-    return sorted(glob.glob(os.path.join(CSRC, "*.hip")))
+    return sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "loss", "*.hip")))
 
 
 def needs_build() -> bool:
     if not os.path.exists(LIB) or not os.path.exists(HOST_LIB):
         return True
     t = min(os.path.getmtime(LIB), os.path.getmtime(HOST_LIB))
-    deps = sources() + [HOST_SRC] + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(INCLUDE, "*.h"))
+    deps = sources() + [HOST_SRC] + glob.glob(os.path.join(CSRC, "*.h")) + \
+        glob.glob(os.path.join(CSRC, "loss", "*.h")) + glob.glob(os.path.join(INCLUDE, "*.h"))
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -1,0 +1,239 @@
+// What the kernels of the losses share: arguments, rows of logits in chunks of 16 bytes, sums over
+// wavefronts and workgroups.
+#pragma once
+
+#include <hip/hip_bfloat16.h>
+#include <hip/hip_fp16.h>
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "tensorloss.h"
+
+namespace tb {
+namespace loss {
+
+constexpr int kWave = 64;
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// What a row's workgroup does behind the softmax statistics.
+enum Op { kScore, kPolicy, kDistill };
+
+struct Rows {
+  const void* x;
+  int64_t x_seq, x_pos;
+  void* g;  // null: no gradient
+  int64_t g_seq, g_pos;
+  const void* tokens;
+  int64_t token_seq;
+  const int32_t* lengths;
+  const uint8_t* mask;
+  int32_t* status;
+  int B, T, V;
+  int long_tokens;
+  float inv_temp;
+  float g_scale;
+};
+
+struct RowOut {  // per position; any may be null but where an Op says otherwise
+  float *logprobs, *entropy;
+  float4* state;  // largest logit, sum of exponentials, entropy, log-probability
+  float *d_logprobs, *d_entropy;
+  float4* terms;  // of the position, without its weight
+};
+
+struct Policy {
+  const float *old_lp, *ref_lp, *advantages;
+  const float* weight;  // [B]
+  int each;
+  float low, high, kl_coef, entropy_coef;
+};
+
+struct Teacher {
+  const void *ids, *logits;
+  const float* weight;  // [B]
+  int K, long_ids, type;
+  float tau;
+};
+
+struct Given {  // the backward pass: cotangents of lp and H (or of the row's divergence)
+  const float4* state;
+  const float *d_lp, *d_entropy, *upstream;
+  int64_t d_seq, d_pos;
+};
+
+// ---- types ------------------------------------------------------------------------------------
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));  // a 16-byte access at any address of a value
+
+struct F32 {
+  using type = float;
+  static constexpr int kPer = 4;  // values of a chunk
+  static __device__ __forceinline__ float load(const float* p) { return *p; }
+  static __device__ __forceinline__ void store(float* p, float v) { *p = v; }
+  static __device__ __forceinline__ void unpack(u32x4 c, float* v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(c[i]);
+  }
+  static __device__ __forceinline__ u32x4 pack(const float* v) {
+    u32x4 c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = __float_as_uint(v[i]);
+    return c;
+  }
+};
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+struct BF16 {
+  using type = uint16_t;
+  static constexpr int kPer = 8;
+  static __device__ __forceinline__ uint32_t round2(float a, float b) {  // to nearest, ties to even
+    const bf16x2 r = __builtin_convertvector(f32x2{a, b}, bf16x2);
+    uint32_t u;
+    __builtin_memcpy(&u, &r, 4);
+    return u;
+  }
+  static __device__ __forceinline__ float load(const uint16_t* p) { return __uint_as_float(uint32_t(*p) << 16); }
+  static __device__ __forceinline__ void store(uint16_t* p, float v) { *p = uint16_t(round2(v, v)); }
+  static __device__ __forceinline__ void unpack(u32x4 c, float* v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(c[i] << 16);
+      v[2 * i + 1] = __uint_as_float(c[i] & 0xFFFF0000u);
+    }
+  }
+  static __device__ __forceinline__ u32x4 pack(const float* v) {
+    u32x4 c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = round2(v[2 * i], v[2 * i + 1]);
+    return c;
+  }
+};
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+struct F16 {
+  using type = _Float16;
+  static constexpr int kPer = 8;
+  static __device__ __forceinline__ float load(const _Float16* p) { return float(*p); }
+  static __device__ __forceinline__ void store(_Float16* p, float v) { *p = _Float16(v); }
+  static __device__ __forceinline__ void unpack(u32x4 c, float* v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f16x2 h;
+      const uint32_t u = c[i];
+      __builtin_memcpy(&h, &u, 4);
+      v[2 * i] = float(h[0]);
+      v[2 * i + 1] = float(h[1]);
+    }
+  }
+  static __device__ __forceinline__ u32x4 pack(const float* v) {
+    u32x4 c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f16x2 h = {_Float16(v[2 * i]), _Float16(v[2 * i + 1])};  // to nearest, ties to even
+      uint32_t u;
+      __builtin_memcpy(&u, &h, 4);
+      c[i] = u;
+    }
+    return c;
+  }
+};
+
+// 2^x; the hardware's instruction is within one unit in the last place, and gives 0 below 2^-126 (a
+// probability that no type of gradient holds beside one of its row's others)
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// ---- rows -------------------------------------------------------------------------------------
+
+// A row's values in the order of memory: `head` values up to the first address that is a multiple of
+// 16, `chunks` chunks of 16 bytes, and the rest.  Head and rest are less than 16 values together;
+// thread j takes the j-th of them.
+template <typename X>
+struct Span {
+  using T = typename X::type;
+  const T* x;
+  int V, head, chunks;
+  __device__ __forceinline__ Span(const T* row, int values) : x(row), V(values) {
+    head = int((-reinterpret_cast<uintptr_t>(row)) & 15) / int(sizeof(T));
+    if (head > values) head = values;
+    chunks = (values - head) / X::kPer;
+  }
+  __device__ __forceinline__ int at(int chunk) const { return head + chunk * X::kPer; }
+  __device__ __forceinline__ u32x4 chunk(int i) const { return *reinterpret_cast<const u32x4*>(x + at(i)); }
+  // the value of head and rest that thread j takes, or -1
+  __device__ __forceinline__ int edge(int j) const {
+    if (j < head) return j;
+    const int i = j + chunks * X::kPer;
+    return i < V ? i : -1;
+  }
+  // the thread of `threads` that writes value i of the gradient
+  __device__ __forceinline__ int owner(int i, int threads) const {
+    if (i < head) return i;
+    const int c = (i - head) / X::kPer;
+    return c < chunks ? c % threads : i - chunks * X::kPer;
+  }
+};
+
+template <typename X>
+__device__ __forceinline__ const typename X::type* row_of(const Rows& r, int b, int t) {
+  return static_cast<const typename X::type*>(r.x) + b * r.x_seq + t * r.x_pos;
+}
+template <typename X>
+__device__ __forceinline__ typename X::type* gradient_of(const Rows& r, int b, int t) {
+  return static_cast<typename X::type*>(r.g) + b * r.g_seq + t * r.g_pos;
+}
+__device__ __forceinline__ int64_t load_id(const void* ids, int wide, int64_t i) {
+  return wide ? static_cast<const int64_t*>(ids)[i] : int64_t(static_cast<const int32_t*>(ids)[i]);
+}
+
+__device__ __forceinline__ int held_length(int length, int T, int32_t* status) {
+  if (length >= 0 && length <= T) return length;
+  if (status) atomicOr(status, TB_DEV_LENGTH_RANGE);
+  return length < 0 ? 0 : T;
+}
+__device__ __forceinline__ bool counts(const Rows& r, int b, int t) {
+  if (r.lengths && t >= r.lengths[b]) return false;
+  return !r.mask || r.mask[int64_t(b) * r.T + t] != 0;
+}
+
+// ---- sums -------------------------------------------------------------------------------------
+
+template <typename V>
+__device__ __forceinline__ V wave_sum(V v) {
+#pragma unroll
+  for (int d = kWave / 2; d; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int d = kWave / 2; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+
+// Softmax statistics of a part of a row, of a = (x - m) k with k = log2(e) / temperature: the largest
+// value m (the lowest finite one at least, so that no difference of two -inf is formed), s = sum 2^a,
+// and for the entropy t = sum 2^a a.
+struct Stats {
+  float m, s, t;
+};
+
+// a without -inf, whose product with its weight 0 would be NaN
+__device__ __forceinline__ float finite(float a) { return fmaxf(a, -1e30f); }
+
+template <bool kEntropy>
+__device__ __forceinline__ Stats joined(const Stats& p, const Stats& q, float k) {
+  Stats r;
+  r.m = fmaxf(p.m, q.m);
+  const float dp = (p.m - r.m) * k, dq = (q.m - r.m) * k;
+  const float ep = exp2_fast(dp), eq = exp2_fast(dq);
+  r.s = ep * p.s + eq * q.s;
+  r.t = kEntropy ? ep * (p.t + finite(dp) * p.s) + eq * (q.t + finite(dq) * q.s) : 0.f;
+  return r;
+}
+
+}  // namespace loss
+}  // namespace tb
