@@ -14,10 +14,11 @@ namespace loss {
 
 constexpr int kWave = 64;
 constexpr float kLowest = -3.402823466e38f;
+constexpr float kExtreme = 1e37f;  // a row's largest logit beyond it: products with log2(e) might overflow
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // What a row's workgroup does behind the softmax statistics.
-enum Op { kScore, kPolicy, kDistill };
+enum Op { kScore, kPolicy, kDistill, kGiven };  // (kGiven: the gradient alone)
 
 struct Rows {
   const void* x;
@@ -35,23 +36,26 @@ struct Rows {
   float g_scale;
 };
 
-struct RowOut {  // per position; any may be null but where an Op says otherwise
+struct RowOut {  // per position, any may be null
   float *logprobs, *entropy;
   float4* state;  // largest logit, sum of exponentials, entropy, log-probability
   float *d_logprobs, *d_entropy;
-  float4* terms;  // of the position, without its weight
+  double* partial;  // [workgroup][4]: the weighted terms of its rows
+};
+
+struct Mean {
+  const float* weight;  // [B], or null: from the lengths
+  int average;
 };
 
 struct Policy {
   const float *old_lp, *ref_lp, *advantages;
-  const float* weight;  // [B]
   int each;
   float low, high, kl_coef, entropy_coef;
 };
 
 struct Teacher {
   const void *ids, *logits;
-  const float* weight;  // [B]
   int K, long_ids, type;
   float tau;
 };
@@ -68,6 +72,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));  // a 16-byte access at any address of a value
 
 struct F32 {
+  static constexpr uint32_t kNone = 0xFF800000u;  // -inf
   using type = float;
   static constexpr int kPer = 4;  // values of a chunk
   static __device__ __forceinline__ float load(const float* p) { return *p; }
@@ -88,6 +93,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 struct BF16 {
+  static constexpr uint32_t kNone = 0xFF80FF80u;  // -inf
   using type = uint16_t;
   static constexpr int kPer = 8;
   static __device__ __forceinline__ uint32_t round2(float a, float b) {  // to nearest, ties to even
@@ -116,6 +122,7 @@ struct BF16 {
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 struct F16 {
+  static constexpr uint32_t kNone = 0xFC00FC00u;  // -inf
   using type = _Float16;
   static constexpr int kPer = 8;
   static __device__ __forceinline__ float load(const _Float16* p) { return float(*p); }
@@ -150,8 +157,11 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // ---- rows -------------------------------------------------------------------------------------
 
 // A row's values in the order of memory: `head` values up to the first address that is a multiple of
-// 16, `chunks` chunks of 16 bytes, and the rest.  Head and rest are less than 16 values together;
-// thread j takes the j-th of them.
+// 16, `chunks` chunks of 16 bytes, and the rest.  Head and rest are at most kEdge values together;
+// chunk i and the i-th of them are thread i's (of a workgroup, or of the lanes that share a row).
+template <typename X>
+constexpr int kEdge = 2 * (X::kPer - 1);
+
 template <typename X>
 struct Span {
   using T = typename X::type;
@@ -164,17 +174,16 @@ struct Span {
   }
   __device__ __forceinline__ int at(int chunk) const { return head + chunk * X::kPer; }
   __device__ __forceinline__ u32x4 chunk(int i) const { return *reinterpret_cast<const u32x4*>(x + at(i)); }
-  // the value of head and rest that thread j takes, or -1
+  // the j-th value of head and rest, or -1
   __device__ __forceinline__ int edge(int j) const {
     if (j < head) return j;
     const int i = j + chunks * X::kPer;
     return i < V ? i : -1;
   }
-  // the thread of `threads` that writes value i of the gradient
+  // which of `threads` writes value i of the gradient
   __device__ __forceinline__ int owner(int i, int threads) const {
-    if (i < head) return i;
     const int c = (i - head) / X::kPer;
-    return c < chunks ? c % threads : i - chunks * X::kPer;
+    return (i < head ? i : c < chunks ? c : i - chunks * X::kPer) % threads;
   }
 };
 

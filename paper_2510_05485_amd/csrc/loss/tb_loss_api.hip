@@ -6,13 +6,22 @@ namespace tb {
 namespace loss {
 namespace {
 
+hipError_t run_rows(Op op, Call& c) {
+  return c.type == TB_FLOAT32 ? rows_of<F32>(op, c) : c.type == TB_BFLOAT16 ? rows_of<BF16>(op, c) : rows_of<F16>(op, c);
+}
+hipError_t run_gradient(Op op, const Call& c) {
+  return c.type == TB_FLOAT32    ? gradient_of<F32>(op, c)
+         : c.type == TB_BFLOAT16 ? gradient_of<BF16>(op, c)
+                                 : gradient_of<F16>(op, c);
+}
+
 size_t value_bytes(int type) { return type == TB_FLOAT32 ? 4 : 2; }
 
 constexpr size_t kAlign = 256;
 size_t aligned(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
 
 struct Workspace {
-  size_t counts, weight, partial, terms, state, d_sequence, bytes;
+  size_t counts, weight, more, partial, state, d_sequence, bytes;
 };
 Workspace workspace_of(int64_t B, int64_t T) {
   Workspace w;
@@ -24,9 +33,10 @@ Workspace workspace_of(int64_t B, int64_t T) {
   };
   w.counts = take(4 * B);
   w.weight = take(4 * B);
-  w.partial = take(8 * 4 * size_t(kPartials > B ? kPartials : B));
-  w.terms = take(16 * B * T);
-  w.state = w.terms;  // (the policy loss and distillation need the one, pairs the other)
+  w.more = take(8 * 4 * kMoreSums);
+  const int64_t groups = B * T < kMostGroups ? B * T : kMostGroups;
+  w.partial = take(8 * 4 * size_t(groups > B ? groups : B));
+  w.state = take(16 * B * T);  // (of pairs only)
   w.d_sequence = take(4 * B);
   w.bytes = at;
   return w;
@@ -100,6 +110,16 @@ int check_workspace(const Rows& r, void* workspace, size_t bytes) {
 template <typename T>
 T* in(void* workspace, size_t offset) {
   return reinterpret_cast<T*>(static_cast<char*>(workspace) + offset);
+}
+// Lengths of few sequences are added up by every workgroup while its row is on its way, and a launch or
+// two less (4 us each) is worth that; masks and many lengths are counted before.
+constexpr int kMostLengths = 2048;
+hipError_t set_mean(Call& c, int average, const Workspace& w, void* workspace) {
+  c.mean = {nullptr, average};
+  if (!c.rows.mask && (!c.rows.lengths || c.rows.B <= kMostLengths)) return hipSuccess;
+  float* weight = in<float>(workspace, w.weight);
+  c.mean.weight = weight;
+  return run_weights(c.rows, average, in<int32_t>(workspace, w.counts), weight, c.stream);
 }
 int done(hipError_t e) { return e == hipSuccess ? TB_OK : TB_ERR_HIP; }
 bool average_known(int a) { return a >= TB_MEAN_TOKENS && a <= TB_SUM; }
@@ -179,19 +199,16 @@ extern "C" int tensorloss_policy(const tb_logits_t* logits, const tb_positions_t
     return TB_ERR_INVALID_ARG;
   if (int rc = check_workspace(r, workspace, workspace_bytes)) return rc;
   const Workspace w = workspace_of(r.B, r.T);
-  float* weight = in<float>(workspace, w.weight);
-  float4* row_terms = in<float4>(workspace, w.terms);
-  double* partial = in<double>(workspace, w.partial);
-  if (empty(r)) return done(run_terms(r, row_terms, weight, partial, terms, 4, c.stream));
+  double *partial = in<double>(workspace, w.partial), *more = in<double>(workspace, w.more);
+  if (empty(r)) return done(run_terms(0, partial, more, terms, 4, c.stream));
   c.rows.status = status;
-  c.out = {logprobs, nullptr, reinterpret_cast<float4*>(row_state), d_logprobs, d_entropy, row_terms};
-  c.policy = {policy->old_logprobs, policy->ref_logprobs, policy->advantages, weight, policy->each, policy->clip_low,
+  c.out = {logprobs, nullptr, reinterpret_cast<float4*>(row_state), d_logprobs, d_entropy, partial};
+  c.policy = {policy->old_logprobs, policy->ref_logprobs, policy->advantages, policy->each, policy->clip_low,
               policy->clip_high, policy->kl_coef, policy->entropy_coef};
   c.entropy = policy->entropy_coef != 0.f;
-  if (run_weights(r, policy->average, in<int32_t>(workspace, w.counts), weight, c.stream) != hipSuccess ||
-      run_rows(kPolicy, c) != hipSuccess)
+  if (set_mean(c, policy->average, w, workspace) != hipSuccess || run_rows(kPolicy, c) != hipSuccess)
     return TB_ERR_HIP;
-  return done(run_terms(r, row_terms, weight, partial, terms, 4, c.stream));
+  return done(run_terms(c.groups, partial, more, terms, 4, c.stream));
 }
 
 extern "C" int tensorloss_preference(const tb_logits_t* logits, const tb_positions_t* at,
@@ -241,18 +258,14 @@ extern "C" int tensorloss_distill(const tb_logits_t* logits, const tb_positions_
   c.stream = static_cast<hipStream_t>(hip_stream);
   if (int rc = check_workspace(r, workspace, workspace_bytes)) return rc;
   const Workspace w = workspace_of(r.B, r.T);
-  float* weight = in<float>(workspace, w.weight);
-  float4* row_terms = in<float4>(workspace, w.terms);
-  double* partial = in<double>(workspace, w.partial);
-  if (empty(r)) return done(run_terms(r, row_terms, weight, partial, terms, 1, c.stream));
+  double *partial = in<double>(workspace, w.partial), *more = in<double>(workspace, w.more);
+  if (empty(r)) return done(run_terms(0, partial, more, terms, 1, c.stream));
   c.rows.status = status;
-  c.out = {row_loss, nullptr, reinterpret_cast<float4*>(row_state), d_row, nullptr, row_terms};
+  c.out = {row_loss, nullptr, reinterpret_cast<float4*>(row_state), d_row, nullptr, partial};
   c.teacher = teacher_of(*teacher, r);
-  c.teacher.weight = weight;
-  if (run_weights(r, teacher->average, in<int32_t>(workspace, w.counts), weight, c.stream) != hipSuccess ||
-      run_rows(kDistill, c) != hipSuccess)
+  if (set_mean(c, teacher->average, w, workspace) != hipSuccess || run_rows(kDistill, c) != hipSuccess)
     return TB_ERR_HIP;
-  return done(run_terms(r, row_terms, weight, partial, terms, 1, c.stream));
+  return done(run_terms(c.groups, partial, more, terms, 1, c.stream));
 }
 
 extern "C" int tensorloss_distill_grad(const tb_logits_t* logits, const tb_positions_t* at, const tb_teacher_t* teacher,

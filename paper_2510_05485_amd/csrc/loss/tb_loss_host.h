@@ -10,26 +10,31 @@ struct Call {
   Rows rows;
   RowOut out;
   Policy policy;
+  Mean mean;
   Teacher teacher;
   Given given;
   int type;      // tb_type_t of the logits
   bool entropy;  // the operator needs it
   hipStream_t stream;
+  int groups;  // (set by rows_of) workgroups that have left their terms in out.partial
 };
 
+// A launch has less than 2^32 threads: from so many rows on, workgroups take several.
+constexpr int64_t kMostGroups = 1 << 22;
+
 // A pass over all rows: statistics, the operator's values, and the gradient where rows.g is set.
-hipError_t run_rows(Op op, const Call& c);
+template <typename X>
+hipError_t rows_of(Op op, Call& c);
 // The gradient alone, of rows whose statistics and cotangents are given.
-hipError_t run_gradient(Op op, const Call& c);
+template <typename X>
+hipError_t gradient_of(Op op, const Call& c);
 
 // weight[b] of every sequence's positions; counts [B] is scratch.
 hipError_t run_weights(const Rows& r, int average, int32_t* counts, float* weight, hipStream_t stream);
 
-// terms[i] = sum over positions of weight[b] row_terms[b, t][i], i < n; partial: scratch of
-// kPartials * 4 doubles.
-constexpr int kPartials = 512;
-hipError_t run_terms(const Rows& r, const float4* row_terms, const float* weight, double* partial, float* terms,
-                     int n, hipStream_t stream);
+// terms[i] = sum over workgroups of partial[workgroup][i], i < n; more: scratch of kMoreSums * 4 doubles.
+constexpr int kMoreSums = 256;
+hipError_t run_terms(int64_t groups, const double* partial, double* more, float* terms, int n, hipStream_t stream);
 
 struct Pairs {
   const float* ref_lp;

@@ -1,0 +1,863 @@
+// Passes over rows of logits: log-probabilities and entropies, the policy loss, the distillation loss,
+// and their gradients.  Each type of logits is instantiated in a file of its own.
+//
+// All are bound by HBM: a row is read once and its gradient written once, with two exponentials and about
+// fifteen other instructions a value in between.  Three kernels share the work by the length of a row:
+//   lanes_kernel     up to 512 values a lane's eight chunks hold: 4 to 64 lanes of a wavefront keep a row
+//   held_kernel      a workgroup keeps a row in its registers
+//   sweep_kernel     a workgroup reads the row from memory in each of two sweeps (any length)
+#pragma once
+
+#include "tb_loss_host.h"
+
+namespace tb {
+namespace loss {
+namespace {
+
+constexpr uint32_t kNan = 0x7FC00000u;
+
+// ---- what all kernels do for a row ------------------------------------------------------------
+
+// What the gradient of a row is made of: values 2^a (by_weight + by_log a), a = (x - m) k, and `token`
+// more at the row's token.
+struct Slope {
+  float by_weight, by_log, token;
+};
+
+// from the cotangents of lp and H
+__device__ __forceinline__ Slope slope_of(float s, float H, float d_lp, float d_H, float scale) {
+  const float f = scale / s;
+  return {f * (-d_lp - d_H * (H - logf(s))), -f * d_H * kLn2, scale * d_lp};
+}
+template <bool kEntropy>
+__device__ __forceinline__ float gradient_at(float a, Slope f) {
+  return exp2_fast(a) * (kEntropy ? f.by_weight + f.by_log * finite(a) : f.by_weight);
+}
+
+// Loss and cotangents of a position (every thread of the workgroup computes them).
+struct Position {
+  float4 terms;  // loss, kl, clipped, entropy
+  float d_lp, d_H;
+};
+__device__ __forceinline__ Position policy_position(const Policy& p, int b, int64_t r, float lp, float H, float w) {
+  const float ratio = expf(lp - p.old_lp[r]), A = p.each ? p.advantages[r] : p.advantages[b];
+  const bool clipped = (A > 0 && ratio > 1 + p.high) || (A < 0 && ratio < 1 - p.low);
+  const float held = A > 0 ? 1 + p.high : 1 - p.low;
+  Position o;
+  float loss = -(clipped ? held : ratio) * A, kl = 0.f;
+  o.d_lp = clipped ? 0.f : -ratio * A;
+  if (p.kl_coef != 0.f) {
+    const float d = p.ref_lp[r] - lp, e = expf(d);
+    // near 0 the difference of e^d and 1 + d is its series' next terms: d^2 (1/2 + d/6 + ...)
+    kl = fabsf(d) < 0.02f ? d * d * (0.5f + d * (1.f / 6 + d * (1.f / 24 + d * (1.f / 120)))) : e - d - 1.f;
+    loss += p.kl_coef * kl;
+    o.d_lp += p.kl_coef * (fabsf(d) < 0.02f ? -d * (1.f + d * (0.5f + d * (1.f / 6 + d * (1.f / 24)))) : 1.f - e);
+  }
+  if (p.entropy_coef != 0.f) loss -= p.entropy_coef * H;
+  o.terms = {loss, kl, clipped ? 1.f : 0.f, p.entropy_coef != 0.f ? H : 0.f};
+  o.d_lp *= w;
+  o.d_H = -p.entropy_coef * w;
+  return o;
+}
+
+__device__ __forceinline__ float teacher_value(const Teacher& q, int64_t i) {
+  if (q.type == TB_FLOAT32) return static_cast<const float*>(q.logits)[i];
+  return q.type == TB_BFLOAT16 ? BF16::load(static_cast<const uint16_t*>(q.logits) + i)
+                               : F16::load(static_cast<const _Float16*>(q.logits) + i);
+}
+
+// The row's token, or -1 (reported by the thread that has `tell`) for one outside the vocabulary.
+__device__ __forceinline__ int take_token(const Rows& r, int b, int t, bool tell) {
+  const int64_t token = load_id(r.tokens, r.long_tokens, b * r.token_seq + t);
+  if (token >= 0 && token < r.V) return int(token);
+  if (tell && r.status) atomicOr(r.status, TB_DEV_TOKEN_RANGE);
+  return -1;
+}
+
+// What the position that does not count leaves, but for its gradient.
+__device__ __forceinline__ void leave_nothing(const RowOut& o, int64_t at) {
+  if (o.logprobs) o.logprobs[at] = 0.f;
+  if (o.entropy) o.entropy[at] = 0.f;
+  if (o.state) o.state[at] = {};
+  if (o.d_logprobs) o.d_logprobs[at] = 0.f;
+  if (o.d_entropy) o.d_entropy[at] = 0.f;
+}
+
+// Weights from the lengths: the thread's share of what they are divided by, and a sequence's weight.
+__device__ __forceinline__ int share_of_total(const Rows& r, const Mean& mean) {
+  int n = 0;
+  if (!mean.weight && r.lengths && mean.average != TB_SUM)
+    for (int b = threadIdx.x; b < r.B; b += blockDim.x) {
+      const int length = held_length(r.lengths[b], r.T, nullptr);
+      n += mean.average == TB_MEAN_TOKENS ? length : length > 0;
+    }
+  return n;
+}
+__device__ __forceinline__ float weight_of(const Rows& r, const Mean& mean, int b, int total) {
+  if (mean.weight) return mean.weight[b];
+  if (mean.average == TB_SUM) return 1.f;
+  if (!r.lengths) total = mean.average == TB_MEAN_TOKENS ? r.B * r.T : r.B;
+  if (mean.average == TB_MEAN_TOKENS) return 1.f / float(total);
+  return 1.f / (float(total) * float(r.lengths ? held_length(r.lengths[b], r.T, nullptr) : r.T));
+}
+
+// Which row a workgroup takes: neighbouring workgroups go to different XCDs, neighbouring rows to one.
+__device__ __forceinline__ int64_t row_of_group(int64_t group, int64_t rows) {
+  constexpr int kXcds = 8, kRun = 4;
+  const int64_t block = group / (kXcds * kRun), in = group % (kXcds * kRun);
+  if ((block + 1) * kXcds * kRun > rows) return group;
+  return block * kXcds * kRun + in % kXcds * kRun + in / kXcds;
+}
+
+// Sum over the lanes that share a row (kLanes of a wavefront), in all of them.
+template <int kCtrl>
+__device__ __forceinline__ float dpp(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), kCtrl, 0xf, 0xf, true));
+}
+// The value of a lane whose group of kStep lanes is the neighbour of the own one; all lanes of a group
+// hold the same value.
+template <int kStep>
+__device__ __forceinline__ float neighbour(float v) {
+  if constexpr (kStep == 1) return dpp<0xB1>(v);        // quad_perm [1, 0, 3, 2]
+  else if constexpr (kStep == 2) return dpp<0x4E>(v);   // quad_perm [2, 3, 0, 1]
+  else if constexpr (kStep == 4) return dpp<0x141>(v);  // row_half_mirror
+  else if constexpr (kStep == 8) return dpp<0x140>(v);  // row_mirror
+  else return __shfl_xor(v, kStep);
+}
+template <bool kEntropy, int kLanes, int kStep = 1, typename Join>
+__device__ __forceinline__ Stats joined_lanes(const Stats& mine, Join join) {
+  if constexpr (kStep == kLanes) return mine;
+  else {
+    const Stats other = {neighbour<kStep>(mine.m), neighbour<kStep>(mine.s), kEntropy ? neighbour<kStep>(mine.t) : 0.f};
+    return joined_lanes<kEntropy, kLanes, kStep * 2>(join(mine, other), join);
+  }
+}
+
+// ---- rows in the registers of some lanes ------------------------------------------------------
+
+// The part of a row that a lane of kLanes holds; what lies beyond the row is -inf.
+template <typename X, int kLanes, int kChunks>
+struct Part {
+  static constexpr int kEdges = (kEdge<X> + kLanes - 1) / kLanes;
+  u32x4 c[kChunks];
+  float e[kEdges];
+  __device__ __forceinline__ void load(const Span<X>& row, int lane, bool live) {
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) {
+      c[k] = u32x4{X::kNone, X::kNone, X::kNone, X::kNone};
+      if (live && lane + k * kLanes < row.chunks) c[k] = row.chunk(lane + k * kLanes);
+    }
+#pragma unroll
+    for (int j = 0; j < kEdges; ++j) {
+      const int i = row.edge(lane + j * kLanes);
+      e[j] = live && i >= 0 ? X::load(row.x + i) : -INFINITY;
+    }
+  }
+};
+
+template <bool kEntropy, int kLanes, typename X, int kChunks>
+__device__ __forceinline__ Stats part_stats(const Part<X, kLanes, kChunks>& p, float k) {
+  Stats mine = {kLowest, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < kChunks; ++j) {
+    float v[X::kPer];
+    X::unpack(p.c[j], v);
+#pragma unroll
+    for (int i = 0; i < X::kPer; ++i) mine.m = fmaxf(mine.m, v[i]);
+  }
+#pragma unroll
+  for (int j = 0; j < p.kEdges; ++j) mine.m = fmaxf(mine.m, p.e[j]);
+  auto take = [&](float x) {
+    const float a = (x - mine.m) * k, w = exp2_fast(a);
+    mine.s += w;
+    if (kEntropy) mine.t += w * finite(a);
+  };
+#pragma unroll
+  for (int j = 0; j < kChunks; ++j) {
+    float v[X::kPer];
+    X::unpack(p.c[j], v);
+#pragma unroll
+    for (int i = 0; i < X::kPer; ++i) take(v[i]);
+  }
+#pragma unroll
+  for (int j = 0; j < p.kEdges; ++j) take(p.e[j]);
+  return joined_lanes<kEntropy, kLanes>(mine, [k](const Stats& a, const Stats& b) { return joined<kEntropy>(a, b, k); });
+}
+
+// Writes the gradient, zeros where `live` is false.
+template <bool kEntropy, int kLanes, typename X, int kChunks>
+__device__ __forceinline__ void write_part(const Span<X>& row, const Part<X, kLanes, kChunks>& p, typename X::type* g,
+                                           int lane, bool live, float m, float k, Slope f) {
+#pragma unroll
+  for (int j = 0; j < kChunks; ++j) {
+    float v[X::kPer];
+    X::unpack(p.c[j], v);
+#pragma unroll
+    for (int i = 0; i < X::kPer; ++i) v[i] = gradient_at<kEntropy>((v[i] - m) * k, f);
+    const u32x4 c = live ? X::pack(v) : u32x4{};
+    if (lane + j * kLanes < row.chunks) *reinterpret_cast<u32x4_any*>(g + row.at(lane + j * kLanes)) = c;
+  }
+#pragma unroll
+  for (int j = 0; j < p.kEdges; ++j) {
+    const int i = row.edge(lane + j * kLanes);
+    if (i >= 0) X::store(g + i, live ? gradient_at<kEntropy>((p.e[j] - m) * k, f) : 0.f);
+  }
+}
+
+constexpr int kLaneThreads = 256;
+
+// kLanes lanes of a wavefront a row, kLaneThreads / kLanes rows a workgroup at a time.  Nothing of it
+// needs a barrier, and a row's statistics meet in two to six steps between lanes.
+template <typename X, int kOp, bool kEntropy, int kLanes, int kChunks>
+__global__ __launch_bounds__(kLaneThreads) void lanes_kernel(Rows r, RowOut o, Policy p, Mean mean, Given v) {
+  constexpr int kTeams = kLaneThreads / kLanes, kWaves = kLaneThreads / kWave;
+  __shared__ double sums[kWaves][4];
+  __shared__ int totals[kWaves];
+  const int lane = threadIdx.x % kLanes;
+  const int64_t rows = int64_t(r.B) * r.T;
+  const float k = r.inv_temp * kLog2e;
+  int total = 0;
+  if (kOp == kPolicy) {
+    const int part = wave_sum(share_of_total(r, mean));
+    if (threadIdx.x % kWave == 0) totals[threadIdx.x / kWave] = part;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w) total += totals[w];
+  }
+  const float up = kOp == kGiven && v.upstream ? *v.upstream : 1.f;
+  double sum[4] = {};
+  for (int64_t from = int64_t(blockIdx.x) * kTeams; from < rows; from += int64_t(gridDim.x) * kTeams) {
+    const int64_t at = from + threadIdx.x / kLanes;
+    if (at >= rows) continue;  // (all lanes of a row)
+    const int b = int(uint32_t(at) / uint32_t(r.T)), t = int(uint32_t(at) % uint32_t(r.T));
+    if (kOp != kGiven && lane == 0 && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
+    const bool live = counts(r, b, t);
+    const Span<X> row(row_of<X>(r, b, t), r.V);
+    Part<X, kLanes, kChunks> part;
+    part.load(row, lane, live);
+    Slope f = {};
+    float m = 0.f, x = 0.f;
+    int token = -1;
+    if (live) {
+      token = take_token(r, b, t, kOp != kGiven && lane == 0);
+      x = token < 0 ? __uint_as_float(kNan) : X::load(row.x + token);
+      if constexpr (kOp == kGiven) {
+        const float4 state = v.state[at];
+        const float d = v.d_lp[b * v.d_seq + t * v.d_pos] * up;
+        const float d_H = kEntropy ? v.d_entropy[b * v.d_seq + t * v.d_pos] * up : 0.f;
+        m = state.x;
+        f = slope_of(state.y, state.z, token < 0 ? x : d, d_H, r.g_scale * r.inv_temp);
+      } else {
+        const Stats s = part_stats<kEntropy, kLanes>(part, k);
+        const float log_s = logf(s.s), lp = (x - s.m) * r.inv_temp - log_s;
+        const float H = kEntropy ? log_s - kLn2 * s.t / s.s : 0.f;
+        m = s.m;
+        if (lane == 0) {
+          if (o.logprobs) o.logprobs[at] = lp;
+          if (o.entropy) o.entropy[at] = H;
+          if (o.state) o.state[at] = {s.m, s.s, H, lp};
+        }
+        if constexpr (kOp == kPolicy) {
+          const float w = weight_of(r, mean, b, total);
+          const Position q = policy_position(p, b, at, lp, H, w);
+          if (lane == 0) {
+            if (o.d_logprobs) o.d_logprobs[at] = q.d_lp;
+            if (o.d_entropy) o.d_entropy[at] = q.d_H;
+            sum[0] += double(w) * q.terms.x;
+            sum[1] += double(w) * q.terms.y;
+            sum[2] += double(w) * q.terms.z;
+            sum[3] += double(w) * q.terms.w;
+          }
+          f = slope_of(s.s, H, q.d_lp, q.d_H, r.g_scale * r.inv_temp);
+        }
+      }
+    } else if (kOp != kGiven && lane == 0) {
+      leave_nothing(o, at);
+    }
+    if (kOp == kScore || (kOp == kPolicy && !r.g)) continue;
+    typename X::type* g = gradient_of<X>(r, b, t);
+    write_part<kEntropy>(row, part, g, lane, live, m, k, f);
+    if (token >= 0 && row.owner(token, kLanes) == lane)  // (stores of one thread to one address keep their order)
+      X::store(g + token, f.token + gradient_at<kEntropy>((x - m) * k, f));
+  }
+  if constexpr (kOp == kPolicy) {
+    for (int j = 0; j < 4; ++j) {
+      sum[j] = wave_sum(sum[j]);
+      if (threadIdx.x % kWave == 0) sums[threadIdx.x / kWave][j] = sum[j];
+    }
+    __syncthreads();
+    if (threadIdx.x < 4) {
+      double all = 0;
+      for (int w = 0; w < kWaves; ++w) all += sums[w][threadIdx.x];
+      o.partial[int64_t(blockIdx.x) * 4 + threadIdx.x] = all;
+    }
+  }
+}
+
+// ---- sweeps over a row in memory --------------------------------------------------------------
+
+// Statistics of a row, in every thread.  Reads the row once.
+template <typename X, bool kEntropy>
+__device__ __forceinline__ Stats row_stats(const Span<X>& row, float k, Stats* parts) {
+  Stats mine = {kLowest, 0.f, 0.f};
+  auto take = [&](const float* v, int n) {
+    float top = mine.m;
+#pragma unroll
+    for (int i = 0; i < X::kPer; ++i)
+      if (i < n) top = fmaxf(top, v[i]);
+    const float d = (mine.m - top) * k, e = exp2_fast(d);
+    mine.t = kEntropy ? e * (mine.t + finite(d) * mine.s) : 0.f;
+    mine.s *= e;
+    mine.m = top;
+#pragma unroll
+    for (int i = 0; i < X::kPer; ++i)
+      if (i < n) {
+        const float a = (v[i] - top) * k, w = exp2_fast(a);
+        mine.s += w;
+        if (kEntropy) mine.t += w * finite(a);
+      }
+  };
+  for (int c = threadIdx.x; c < row.chunks; c += blockDim.x) {
+    float v[X::kPer];
+    X::unpack(row.chunk(c), v);
+    take(v, X::kPer);
+  }
+  const int e = row.edge(threadIdx.x);
+  if (e >= 0) {
+    const float v[X::kPer] = {X::load(row.x + e)};
+    take(v, 1);
+  }
+  mine = joined_lanes<kEntropy, kWave>(mine, [k](const Stats& a, const Stats& b) { return joined<kEntropy>(a, b, k); });
+  if (threadIdx.x % kWave == 0) parts[threadIdx.x / kWave] = mine;
+  __syncthreads();
+  Stats all = parts[0];
+  for (int w = 1; w < int(blockDim.x / kWave); ++w) all = joined<kEntropy>(all, parts[w], k);
+  return all;
+}
+
+// The gradient of a row, but for the additions at the token.
+template <typename X, bool kEntropy>
+__device__ __forceinline__ void write_gradient(const Span<X>& row, typename X::type* g, float m, float k, Slope f) {
+  for (int c = threadIdx.x; c < row.chunks; c += blockDim.x) {
+    float v[X::kPer];
+    X::unpack(row.chunk(c), v);
+#pragma unroll
+    for (int i = 0; i < X::kPer; ++i) v[i] = gradient_at<kEntropy>((v[i] - m) * k, f);
+    *reinterpret_cast<u32x4_any*>(g + row.at(c)) = X::pack(v);
+  }
+  const int e = row.edge(threadIdx.x);
+  if (e >= 0) X::store(g + e, gradient_at<kEntropy>((X::load(row.x + e) - m) * k, f));
+}
+
+template <typename X>
+__device__ __forceinline__ void write_zeros(const Rows& r, int b, int t) {
+  const Span<X> row(gradient_of<X>(r, b, t), r.V);
+  typename X::type* g = gradient_of<X>(r, b, t);
+  for (int c = threadIdx.x; c < row.chunks; c += blockDim.x) *reinterpret_cast<u32x4*>(g + row.at(c)) = u32x4{};
+  const int e = row.edge(threadIdx.x);
+  if (e >= 0) X::store(g + e, 0.f);
+}
+
+// The token's value, added where its owner has just stored the rest (stores of one thread to one
+// address keep their order).
+template <typename X, bool kEntropy>
+__device__ __forceinline__ void add_token(const Span<X>& row, typename X::type* g, int token, float x, float m,
+                                          float k, Slope f) {
+  if (row.owner(token, blockDim.x) == int(threadIdx.x))
+    X::store(g + token, f.token + gradient_at<kEntropy>((x - m) * k, f));
+}
+
+// The teacher's entries of a row, in LDS: ids (-1: none, or one outside the vocabulary, which makes
+// the row NaN), their probabilities, and their sum by id.
+struct Entries {
+  int id[TB_TEACHER_MOST];
+  float q[TB_TEACHER_MOST], log_q[TB_TEACHER_MOST], x[TB_TEACHER_MOST];  // x: the row's logits there
+  float part[16];
+};
+
+template <typename V>
+__device__ __forceinline__ V block_sum(V v, V* part) {  // part: one a wavefront
+  v = wave_sum(v);
+  __syncthreads();
+  if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
+  __syncthreads();
+  v = 0;
+  for (int w = 0; w < int(blockDim.x / kWave); ++w) v += part[w];
+  return v;
+}
+__device__ __forceinline__ float block_max(float v, float* part) {
+  v = wave_max(v);
+  __syncthreads();
+  if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
+  __syncthreads();
+  v = part[0];
+  for (int w = 1; w < int(blockDim.x / kWave); ++w) v = fmaxf(v, part[w]);
+  return v;
+}
+
+// Fills `e`; the sum of exponentials: 0 for a row without entries, NaN for one with a wrong id.
+template <typename X>
+__device__ __forceinline__ float take_entries(const Rows& r, const Span<X>& row, const Teacher& q, int64_t at, float k,
+                                              Entries& e) {
+  float top = kLowest;
+  for (int j = threadIdx.x; j < q.K; j += blockDim.x) {
+    const float v = teacher_value(q, at * q.K + j);
+    int id = -1;
+    if (v != -INFINITY) {
+      const int64_t wide = load_id(q.ids, q.long_ids, at * q.K + j);
+      if (wide >= 0 && wide < r.V) id = int(wide);
+      else if (r.status) atomicOr(r.status, TB_DEV_TOKEN_RANGE);
+    }
+    e.id[j] = id;
+    e.x[j] = id < 0 ? 0.f : X::load(row.x + id);
+    e.log_q[j] = v != -INFINITY && id < 0 ? __uint_as_float(kNan) : v;
+    top = fmaxf(top, v);
+  }
+  top = block_max(top, e.part);
+  float sum = 0.f;
+  for (int j = threadIdx.x; j < q.K; j += blockDim.x) {
+    const float a = (e.log_q[j] - top) * k;
+    e.log_q[j] = a * kLn2;
+    e.q[j] = exp2_fast(a);
+    sum += e.q[j];
+  }
+  sum = block_sum(sum, e.part);
+  const float log_sum = logf(sum), by = sum == 0.f ? 0.f : 1.f / sum;
+  for (int j = threadIdx.x; j < q.K; j += blockDim.x) {
+    e.log_q[j] -= log_sum;
+    e.q[j] *= by;
+  }
+  __syncthreads();
+  return sum;
+}
+
+// The gradient at the teacher's entries, behind a barrier after everything else is stored.
+template <typename X>
+__device__ __forceinline__ void add_entries(const Span<X>& row, typename X::type* g, const Teacher& q,
+                                            const Entries& e, float m, float k, Slope f) {
+  for (int j = threadIdx.x; j < q.K; j += blockDim.x) {
+    const int id = e.id[j];
+    if (id < 0) continue;
+    float sum = 0.f;
+    for (int i = 0; i < q.K; ++i) sum += e.id[i] == id ? e.q[i] : 0.f;
+    X::store(g + id, exp2_fast((e.x[j] - m) * k) * f.by_weight - f.token * sum);
+  }
+}
+
+// The gradient of a row's divergence; m, s: the row's statistics, sum: of take_entries, w: cotangent.
+template <typename X>
+__device__ __forceinline__ void write_distilled(const Rows& r, const Span<X>& row, const Teacher& q, const Entries& e,
+                                                int b, int t, float m, float s, float sum, float w, float k) {
+  if (sum == 0.f) {
+    write_zeros<X>(r, b, t);
+    return;
+  }
+  typename X::type* g = gradient_of<X>(r, b, t);
+  Slope f = {0.f, 0.f, q.tau * w * r.g_scale};
+  f.by_weight = sum == sum ? f.token / s : sum;
+  write_gradient<X, false>(row, g, m, k, f);
+  __syncthreads();  // (what it has stored comes before what follows)
+  add_entries<X>(row, g, q, e, m, k, f);
+}
+
+template <int kOp>
+struct Shared {
+  Stats parts[8];
+  int totals[8];
+};
+template <>
+struct Shared<kDistill> {
+  Stats parts[8];
+  int totals[8];
+  Entries entries;
+};
+
+template <typename X, int kOp, bool kEntropy>
+__device__ __forceinline__ float4 sweep_row(const Rows& r, const RowOut& o, const Policy& p, const Teacher& q, float w,
+                                            int b, int t, int64_t at, Shared<kOp>& shared) {
+  const bool first = threadIdx.x == 0;
+  const Span<X> row(row_of<X>(r, b, t), r.V);
+  const float k = r.inv_temp * kLog2e;
+  if constexpr (kOp != kDistill) {
+    const int token = take_token(r, b, t, first);
+    const float x = token < 0 ? __uint_as_float(kNan) : X::load(row.x + token);
+    const Stats s = row_stats<X, kEntropy>(row, k, shared.parts);
+    const float log_s = logf(s.s), lp = (x - s.m) * r.inv_temp - log_s;
+    const float H = kEntropy ? log_s - kLn2 * s.t / s.s : 0.f;
+    Position v = {};
+    if (kOp == kPolicy) v = policy_position(p, b, at, lp, H, w);
+    if (first) {
+      if (o.logprobs) o.logprobs[at] = lp;
+      if (o.entropy) o.entropy[at] = H;
+      if (o.state) o.state[at] = {s.m, s.s, H, lp};
+      if (o.d_logprobs) o.d_logprobs[at] = v.d_lp;
+      if (o.d_entropy) o.d_entropy[at] = v.d_H;
+    }
+    if (kOp == kPolicy && r.g) {
+      const Slope f = slope_of(s.s, H, v.d_lp, v.d_H, r.g_scale * r.inv_temp);
+      typename X::type* g = gradient_of<X>(r, b, t);
+      write_gradient<X, kEntropy>(row, g, s.m, k, f);
+      if (token >= 0) add_token<X, kEntropy>(row, g, token, x, s.m, k, f);
+    }
+    return v.terms;
+  } else {
+    Entries& e = shared.entries;
+    const float sum = take_entries<X>(r, row, q, at, k, e);
+    const Stats s = row_stats<X, false>(row, k, shared.parts);
+    const float log_s = logf(s.s);
+    float d = 0.f;
+    for (int j = threadIdx.x; j < q.K; j += blockDim.x)
+      if (!(e.q[j] <= 0.f)) d += e.q[j] * (e.log_q[j] - ((e.x[j] - s.m) * r.inv_temp - log_s));
+    d = block_sum(d, e.part) * q.tau * q.tau;
+    if (sum == 0.f) w = 0.f;
+    if (first) {
+      if (o.state) o.state[at] = {s.m, s.s, 0.f, d};
+      if (o.d_logprobs) o.d_logprobs[at] = w;
+      if (o.logprobs) o.logprobs[at] = d;
+    }
+    if (r.g) write_distilled<X>(r, row, q, e, b, t, s.m, s.s, sum, w, k);
+    return {d, 0.f, 0.f, 0.f};
+  }
+}
+
+// One workgroup a row; the row is read from memory in every sweep over it.
+template <typename X, int kOp, bool kEntropy>
+__global__ __launch_bounds__(512) void sweep_kernel(Rows r, RowOut o, Policy p, Mean mean, Teacher q) {
+  __shared__ Shared<kOp> shared;
+  const int64_t rows = int64_t(r.B) * r.T;
+  int total = 0;
+  if (kOp != kScore) {
+    const int part = wave_sum(share_of_total(r, mean));
+    if (threadIdx.x % kWave == 0) shared.totals[threadIdx.x / kWave] = part;
+    __syncthreads();
+    for (int w = 0; w < int(blockDim.x / kWave); ++w) total += shared.totals[w];
+  }
+  double sum[4] = {};
+  for (int64_t i = blockIdx.x; i < rows; i += gridDim.x) {
+    const int64_t at = row_of_group(i, rows);
+    const int b = int(uint32_t(at) / uint32_t(r.T)), t = int(uint32_t(at) % uint32_t(r.T));
+    if (threadIdx.x == 0 && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
+    if (counts(r, b, t)) {
+      const float w = kOp == kScore ? 0.f : weight_of(r, mean, b, total);
+      const float4 v = sweep_row<X, kOp, kEntropy>(r, o, p, q, w, b, t, at, shared);
+      sum[0] += double(w) * v.x;
+      sum[1] += double(w) * v.y;
+      sum[2] += double(w) * v.z;
+      sum[3] += double(w) * v.w;
+    } else {
+      if (threadIdx.x == 0) leave_nothing(o, at);
+      if (r.g) write_zeros<X>(r, b, t);
+    }
+    __syncthreads();  // (before the next row takes the shared memory)
+  }
+  if (kOp != kScore && threadIdx.x == 0)
+    for (int j = 0; j < 4; ++j) o.partial[int64_t(blockIdx.x) * 4 + j] = sum[j];
+}
+
+// The gradient of a row whose statistics are given.
+template <typename X, int kOp, bool kEntropy>
+__device__ __forceinline__ void given_row(const Rows& r, const Given& v, const Teacher& q, int b, int t, int64_t at,
+                                          Shared<kOp>& shared) {
+  const Span<X> row(row_of<X>(r, b, t), r.V);
+  const float k = r.inv_temp * kLog2e, up = v.upstream ? *v.upstream : 1.f;
+  const float4 state = v.state[at];
+  const float d = v.d_lp[b * v.d_seq + t * v.d_pos] * up;
+  if constexpr (kOp != kDistill) {
+    const float d_H = kEntropy ? v.d_entropy[b * v.d_seq + t * v.d_pos] * up : 0.f;
+    const int token = take_token(r, b, t, false);
+    const float x = token < 0 ? __uint_as_float(kNan) : X::load(row.x + token);
+    __syncthreads();  // (the row may be the gradient's own memory)
+    const Slope f = slope_of(state.y, state.z, token < 0 ? x : d, d_H, r.g_scale * r.inv_temp);
+    typename X::type* g = gradient_of<X>(r, b, t);
+    write_gradient<X, kEntropy>(row, g, state.x, k, f);
+    if (token >= 0) add_token<X, kEntropy>(row, g, token, x, state.x, k, f);
+  } else {
+    const float sum = take_entries<X>(r, row, q, at, k, shared.entries);
+    write_distilled<X>(r, row, q, shared.entries, b, t, state.x, state.y, sum, d, k);
+  }
+}
+
+template <typename X, int kOp, bool kEntropy>
+__global__ __launch_bounds__(512) void gradient_kernel(Rows r, Given v, Teacher q) {
+  __shared__ Shared<kOp> shared;
+  const int64_t rows = int64_t(r.B) * r.T;
+  for (int64_t i = blockIdx.x; i < rows; i += gridDim.x) {
+    const int64_t at = row_of_group(i, rows);
+    const int b = int(uint32_t(at) / uint32_t(r.T)), t = int(uint32_t(at) % uint32_t(r.T));
+    if (counts(r, b, t)) given_row<X, kOp, kEntropy>(r, v, q, b, t, at, shared);
+    else write_zeros<X>(r, b, t);
+    __syncthreads();
+  }
+}
+
+// ---- rows in the registers of a workgroup -----------------------------------------------------
+
+constexpr int kHeldThreads = 512;
+
+// A row's chunks in registers of a workgroup, kChunks a thread: chunk k * kHeldThreads + thread.  All but
+// the last are there in every thread; what lies beyond the row is -inf.
+template <typename X, int kChunks>
+struct Held {
+  u32x4 c[kChunks];
+  float edge;
+  int edge_at;
+  __device__ __forceinline__ void load(const Span<X>& row) {
+    const char* from = reinterpret_cast<const char*>(row.x + row.head);
+    const uint32_t lane = threadIdx.x * 16u;
+#pragma unroll
+    for (int k = 0; k < kChunks - 1; ++k)
+      c[k] = *reinterpret_cast<const u32x4*>(from + k * (kHeldThreads * 16) + lane);
+    c[kChunks - 1] = u32x4{X::kNone, X::kNone, X::kNone, X::kNone};
+    if (last(row)) c[kChunks - 1] = *reinterpret_cast<const u32x4*>(from + (kChunks - 1) * (kHeldThreads * 16) + lane);
+    edge_at = row.edge(threadIdx.x);
+    edge = edge_at >= 0 ? X::load(row.x + edge_at) : -INFINITY;
+  }
+  __device__ __forceinline__ bool last(const Span<X>& row) const {
+    return int(threadIdx.x) + (kChunks - 1) * kHeldThreads < row.chunks;
+  }
+  // Keeps the compiler from holding the values that it has unpacked until they are used again, which
+  // would take twice the registers of the row itself.
+  __device__ __forceinline__ void keep_packed() {
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) asm volatile("" : "+v"(c[k]));
+  }
+};
+
+// M = m k of the weights 2^(x k - M): rounded, and the same wherever it is formed (the compiler must
+// not take the product into a fused multiply-add, whose M would be another one).
+__device__ __forceinline__ float scaled(float m, float k) {
+#pragma clang fp contract(off)
+  return m * k;
+}
+
+template <bool kEntropy>
+__device__ __forceinline__ Stats joined_held(const Stats& p, const Stats& q, float k) {
+  Stats r;
+  r.m = fmaxf(p.m, q.m);
+  const float M = scaled(r.m, k), dp = scaled(p.m, k) - M, dq = scaled(q.m, k) - M;
+  const float ep = exp2_fast(dp), eq = exp2_fast(dq);
+  r.s = ep * p.s + eq * q.s;
+  r.t = kEntropy ? ep * (p.t + finite(dp) * p.s) + eq * (q.t + finite(dq) * q.s) : 0.f;
+  return r;
+}
+
+template <typename X, bool kEntropy, int kChunks>
+__device__ __forceinline__ Stats wave_stats(Held<X, kChunks>& h, float k) {
+  Stats mine = {fmaxf(h.edge, -kExtreme), 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < kChunks; ++j) {
+    float v[X::kPer];
+    X::unpack(h.c[j], v);
+#pragma unroll
+    for (int i = 0; i < X::kPer; ++i) mine.m = fmaxf(mine.m, v[i]);
+  }
+  h.keep_packed();
+  const float M = scaled(mine.m, k);
+  auto take = [&](float x) {
+    const float a = fmaf(x, k, -M), w = exp2_fast(a);
+    mine.s += w;
+    if (kEntropy) mine.t += w * finite(a);
+  };
+#pragma unroll
+  for (int j = 0; j < kChunks; ++j) {
+    float v[X::kPer];
+    X::unpack(h.c[j], v);
+#pragma unroll
+    for (int i = 0; i < X::kPer; ++i) take(v[i]);
+  }
+  take(h.edge);
+  h.keep_packed();
+  return joined_lanes<kEntropy, kWave>(mine, [k](const Stats& a, const Stats& b) { return joined_held<kEntropy>(a, b, k); });
+}
+
+template <typename X, bool kEntropy, int kChunks>
+__device__ __forceinline__ void write_held(const Span<X>& row, const Held<X, kChunks>& h, typename X::type* g, float m,
+                                           float k, Slope f) {
+  const float M = scaled(m, k);
+  char* to = reinterpret_cast<char*>(g + row.head);
+  const uint32_t lane = threadIdx.x * 16u;
+  auto value = [&](float x) { return gradient_at<kEntropy>(fmaf(x, k, -M), f); };
+#pragma unroll
+  for (int j = 0; j < kChunks; ++j) {
+    float v[X::kPer];
+    X::unpack(h.c[j], v);
+#pragma unroll
+    for (int i = 0; i < X::kPer; ++i) v[i] = value(v[i]);
+    if (j < kChunks - 1 || h.last(row))
+      *reinterpret_cast<u32x4_any*>(to + j * (kHeldThreads * 16) + lane) = X::pack(v);
+  }
+  if (h.edge_at >= 0) X::store(g + h.edge_at, value(h.edge));
+}
+
+// Statistics of the row, in every thread; of the parts that its wavefronts leave.
+template <bool kEntropy>
+__device__ __forceinline__ Stats block_stats(const Stats* parts, float k) {
+  Stats all = parts[0];
+  for (int w = 1; w < kHeldThreads / kWave; ++w) all = joined_held<kEntropy>(all, parts[w], k);
+  return all;
+}
+
+// One workgroup a row; the score, and the policy loss.
+template <typename X, int kOp, bool kEntropy, int kChunks>
+__global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Policy p, Mean mean) {
+  constexpr int kWaves = kHeldThreads / kWave;
+  __shared__ Stats parts[kWaves];
+  __shared__ int totals[kWaves];
+  const int64_t at = row_of_group(blockIdx.x, int64_t(r.B) * r.T);
+  const int b = int(uint32_t(at) / uint32_t(r.T)), t = int(uint32_t(at) % uint32_t(r.T));
+  const bool first = threadIdx.x == 0;
+  if (first && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
+  if (!counts(r, b, t)) {
+    if (first) leave_nothing(o, at);
+    if (kOp == kPolicy && threadIdx.x < 4) o.partial[int64_t(blockIdx.x) * 4 + threadIdx.x] = 0.0;
+    if (r.g) write_zeros<X>(r, b, t);
+    return;
+  }
+  const Span<X> row(row_of<X>(r, b, t), r.V);
+  // (what comes first is waited for first: not behind the whole row)
+  const int token = take_token(r, b, t, first), share = kOp == kPolicy ? share_of_total(r, mean) : 0;
+  Held<X, kChunks> h;
+  h.load(row);
+  const float x = token < 0 ? __uint_as_float(kNan) : X::load(row.x + token);
+  const float k = r.inv_temp * kLog2e;
+  if (kOp == kPolicy) {
+    const int part = wave_sum(share);
+    if (threadIdx.x % kWave == 0) totals[threadIdx.x / kWave] = part;
+  }
+  const Stats part = wave_stats<X, kEntropy>(h, k);
+  if (threadIdx.x % kWave == 0) parts[threadIdx.x / kWave] = part;
+  __syncthreads();
+  Stats s = block_stats<kEntropy>(parts, k);
+  const bool extreme = !(fabsf(s.m) < kExtreme);
+  if (extreme) {
+    __syncthreads();
+    s = row_stats<X, kEntropy>(row, k, parts);
+  }
+  const float log_s = logf(s.s);
+  const float lp = (extreme ? (x - s.m) * r.inv_temp : fmaf(x, k, -scaled(s.m, k)) * kLn2) - log_s;
+  const float H = kEntropy ? log_s - kLn2 * s.t / s.s : 0.f;
+  Position v = {};
+  if constexpr (kOp == kPolicy) {
+    int total = 0;
+    for (int w = 0; w < kWaves; ++w) total += totals[w];
+    const float w = weight_of(r, mean, b, total);
+    v = policy_position(p, b, at, lp, H, w);
+    if (first) {
+      double* to = o.partial + int64_t(blockIdx.x) * 4;
+      to[0] = double(w) * v.terms.x;
+      to[1] = double(w) * v.terms.y;
+      to[2] = double(w) * v.terms.z;
+      to[3] = double(w) * v.terms.w;
+    }
+  }
+  if (first) {
+    if (o.logprobs) o.logprobs[at] = lp;
+    if (o.entropy) o.entropy[at] = H;
+    if (o.state) o.state[at] = {s.m, s.s, H, lp};
+    if (o.d_logprobs) o.d_logprobs[at] = v.d_lp;
+    if (o.d_entropy) o.d_entropy[at] = v.d_H;
+  }
+  if (kOp == kScore || !r.g) return;
+  const Slope f = slope_of(s.s, H, v.d_lp, v.d_H, r.g_scale * r.inv_temp);
+  typename X::type* g = gradient_of<X>(r, b, t);
+  if (extreme) {
+    write_gradient<X, kEntropy>(row, g, s.m, k, f);
+    if (token >= 0) add_token<X, kEntropy>(row, g, token, x, s.m, k, f);
+    return;
+  }
+  write_held<X, kEntropy>(row, h, g, s.m, k, f);
+  if (token >= 0 && row.owner(token, kHeldThreads) == int(threadIdx.x))
+    X::store(g + token, f.token + gradient_at<kEntropy>(fmaf(x, k, -scaled(s.m, k)), f));
+}
+
+// ---- launches ---------------------------------------------------------------------------------
+
+int grid_of(const Rows& r) {
+  const int64_t rows = int64_t(r.B) * r.T;
+  return int(rows < kMostGroups ? rows : kMostGroups);
+}
+int threads_of(const Rows& r, int per) {
+  const int chunks = (r.V + per - 1) / per;
+  const int t = (chunks + kWave - 1) / kWave * kWave;
+  return t > 512 ? 512 : t;
+}
+
+// Workgroups that the card holds at a time take all rows: 8 of 4 wavefronts on each of 256 units.
+constexpr int kLaneGroups = 2048;
+
+template <typename X, int kOp, bool kEntropy>
+bool launch_lanes(Call& c) {
+  const Rows& r = c.rows;
+  const int64_t rows = int64_t(r.B) * r.T;
+  auto go = [&](auto kernel, int lanes) {
+    const int64_t teams = kLaneThreads / lanes, groups = (rows + teams - 1) / teams;
+    c.groups = int(groups < kLaneGroups ? groups : kLaneGroups);
+    kernel<<<c.groups, kLaneThreads, 0, c.stream>>>(r, c.out, c.policy, c.mean, c.given);
+    return true;
+  };
+  const int chunks = (r.V + X::kPer - 1) / X::kPer;
+  if (chunks <= 8) return go(lanes_kernel<X, kOp, kEntropy, 4, 2>, 4);
+  if (chunks <= 16) return go(lanes_kernel<X, kOp, kEntropy, 8, 2>, 8);
+  if (chunks <= 32) return go(lanes_kernel<X, kOp, kEntropy, 16, 2>, 16);
+  if (chunks <= 64) return go(lanes_kernel<X, kOp, kEntropy, 32, 2>, 32);
+  if (chunks <= 128) return go(lanes_kernel<X, kOp, kEntropy, 64, 2>, 64);
+  if (chunks <= 256) return go(lanes_kernel<X, kOp, kEntropy, 64, 4>, 64);
+  if (chunks <= 512) return go(lanes_kernel<X, kOp, kEntropy, 64, 8>, 64);
+  return false;
+}
+
+template <typename X, int kOp, bool kEntropy>
+bool launch_held(Call& c) {
+  const Rows& r = c.rows;
+  const int64_t rows = int64_t(r.B) * r.T;
+  if (rows > kMostGroups || r.V < 2 * X::kPer) return false;
+  c.groups = int(rows);
+#define HELD(n) \
+  case n: held_kernel<X, kOp, kEntropy, n><<<int(rows), kHeldThreads, 0, c.stream>>>(r, c.out, c.policy, c.mean); return true;
+  switch ((r.V / X::kPer + kHeldThreads - 1) / kHeldThreads) {
+    HELD(1) HELD(2) HELD(3) HELD(4) HELD(5) HELD(6) HELD(7) HELD(8) HELD(9) HELD(10) HELD(11) HELD(12) HELD(13) HELD(14)
+    HELD(15) HELD(16) HELD(17) HELD(18) HELD(19) HELD(20) HELD(21) HELD(22) HELD(23) HELD(24) HELD(25) HELD(26) HELD(27)
+    HELD(28) HELD(29) HELD(30) HELD(31) HELD(32)
+  }
+#undef HELD
+  return false;
+}
+
+template <typename X, int kOp, bool kEntropy>
+void launch_sweep(Call& c) {
+  c.groups = grid_of(c.rows);
+  sweep_kernel<X, kOp, kEntropy>
+      <<<c.groups, threads_of(c.rows, X::kPer), 0, c.stream>>>(c.rows, c.out, c.policy, c.mean, c.teacher);
+}
+
+template <typename X, bool kEntropy>
+hipError_t launch_rows(Op op, Call& c) {
+  if (op == kDistill) launch_sweep<X, kDistill, false>(c);
+  else if (op == kPolicy)
+    launch_lanes<X, kPolicy, kEntropy>(c) || launch_held<X, kPolicy, kEntropy>(c) || (launch_sweep<X, kPolicy, kEntropy>(c), true);
+  else
+    launch_lanes<X, kScore, kEntropy>(c) || launch_held<X, kScore, kEntropy>(c) || (launch_sweep<X, kScore, kEntropy>(c), true);
+  return hipGetLastError();
+}
+template <typename X, bool kEntropy>
+hipError_t launch_gradient(Op op, Call c) {
+  const Rows& r = c.rows;
+  const int grid = grid_of(r), threads = threads_of(r, X::kPer);
+  if (op == kDistill) gradient_kernel<X, kDistill, false><<<grid, threads, 0, c.stream>>>(r, c.given, c.teacher);
+  else if (!launch_lanes<X, kGiven, kEntropy>(c))
+    gradient_kernel<X, kGiven, kEntropy><<<grid, threads, 0, c.stream>>>(r, c.given, c.teacher);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+template <typename X>
+hipError_t rows_of(Op op, Call& c) {
+  return c.entropy ? launch_rows<X, true>(op, c) : launch_rows<X, false>(op, c);
+}
+template <typename X>
+hipError_t gradient_of(Op op, const Call& c) {
+  return c.entropy ? launch_gradient<X, true>(op, c) : launch_gradient<X, false>(op, c);
+}
+
+}  // namespace loss
+}  // namespace tb

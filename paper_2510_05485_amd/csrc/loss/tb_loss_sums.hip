@@ -40,40 +40,27 @@ __global__ __launch_bounds__(1024) void weight_kernel(int B, int average, const 
   }
 }
 
-// A workgroup's part of the positions; partial[workgroup][4].  The sums have a fixed order.
-__global__ __launch_bounds__(kThreads) void partial_kernel(int64_t rows, int T, const float4* terms,
-                                                           const float* weight, double* partial) {
-  __shared__ double part[kWaves][4];
+// Sums of n columns of `parts` rows, in an order that only their number fixes.  Several workgroups leave a
+// row each in `to`, a single one the columns' sums times `by` in `terms`.
+__global__ __launch_bounds__(1024) void sum_kernel(int64_t parts, const double* partial, int n, int step, double by,
+                                                   double* to, float* terms) {
+  __shared__ double part[16][4];
   double sum[4] = {};
-  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < rows; i += int64_t(gridDim.x) * kThreads) {
-    const float w = weight[uint32_t(i) / uint32_t(T)];
-    const float4 v = terms[i];
-    if (w != 0.f) {
-      sum[0] += double(w) * v.x;
-      sum[1] += double(w) * v.y;
-      sum[2] += double(w) * v.z;
-      sum[3] += double(w) * v.w;
-    }
-  }
+  for (int64_t i = int64_t(blockIdx.x) * 1024 + threadIdx.x; i < parts; i += int64_t(gridDim.x) * 1024)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < n) sum[j] += partial[i * step + j];
+#pragma unroll
   for (int j = 0; j < 4; ++j) {
     sum[j] = wave_sum(sum[j]);
     if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave][j] = sum[j];
   }
   __syncthreads();
-  if (threadIdx.x < 4) {
+  if (int(threadIdx.x) < n) {
     double all = 0;
-    for (int w = 0; w < kWaves; ++w) all += part[w][threadIdx.x];
-    partial[blockIdx.x * 4 + threadIdx.x] = all;
-  }
-}
-
-__global__ __launch_bounds__(kWave) void terms_kernel(int parts, const double* partial, float* terms, int n, int step,
-                                                      double by) {
-  for (int j = 0; j < n; ++j) {
-    double sum = 0;
-    for (int i = threadIdx.x; i < parts; i += kWave) sum += partial[int64_t(i) * step + j];
-    sum = wave_sum(sum);
-    if (threadIdx.x == 0) terms[j] = float(sum * by);
+    for (int w = 0; w < 16; ++w) all += part[w][threadIdx.x];
+    if (terms) terms[threadIdx.x] = float(all * by);
+    else to[blockIdx.x * 4 + threadIdx.x] = all;
   }
 }
 
@@ -149,20 +136,20 @@ hipError_t run_weights(const Rows& r, int average, int32_t* counts, float* weigh
   return hipGetLastError();
 }
 
-hipError_t run_terms(const Rows& r, const float4* row_terms, const float* weight, double* partial, float* terms, int n,
-                     hipStream_t stream) {
-  const int64_t rows = int64_t(r.B) * r.T;
-  int64_t parts = (rows + kThreads * 4 - 1) / (kThreads * 4);
-  if (parts > kPartials) parts = kPartials;
-  if (parts) partial_kernel<<<int(parts), kThreads, 0, stream>>>(rows, r.T, row_terms, weight, partial);
-  terms_kernel<<<1, kWave, 0, stream>>>(int(parts), partial, terms, n, 4, 1.0);
+hipError_t run_terms(int64_t groups, const double* partial, double* more, float* terms, int n, hipStream_t stream) {
+  if (groups > 16 * 1024) {  // (one workgroup reads 512 KB in 6 us, several and then one take 9 for any number)
+    sum_kernel<<<kMoreSums, 1024, 0, stream>>>(groups, partial, n, 4, 1.0, more, nullptr);
+    partial = more;
+    groups = kMoreSums;
+  }
+  sum_kernel<<<1, 1024, 0, stream>>>(groups, partial, n, 4, 1.0, nullptr, terms);
   return hipGetLastError();
 }
 
 hipError_t run_pairs(const Rows& r, const Pairs& p, hipStream_t stream) {
   const int pairs = r.B / 2;
   if (pairs) pair_kernel<<<pairs, kThreads, 0, stream>>>(r, p);
-  terms_kernel<<<1, kWave, 0, stream>>>(pairs, p.partial, p.terms, 3, 3, pairs ? 1.0 / pairs : 0.0);
+  sum_kernel<<<1, 1024, 0, stream>>>(pairs, p.partial, 3, 3, pairs ? 1.0 / pairs : 0.0, nullptr, p.terms);
   return hipGetLastError();
 }
 
