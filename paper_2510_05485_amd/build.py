@@ -1,8 +1,8 @@
 """Build the gfx950 shared library (libtensorbleu.so) and the Python module that calls it in-tree.
 
 `python -m paper_2510_05485_amd.build` compiles every HIP translation unit under csrc/ for
-gfx950 and links them into one C-ABI library next to this file, and csrc/tb_host.cpp (host code,
-against PyTorch's headers) into the module _host.  hipcc cross-compiles without a GPU, so this runs
+gfx950 and links them into one C-ABI library next to this file, and csrc/tb_host.cpp and
+csrc/loss/tb_loss_py.cpp (host code, against PyTorch's headers) into the modules _host and _loss_host.  hipcc cross-compiles without a GPU, so this runs
 anywhere the ROCm toolchain is installed.
 """
 from __future__ import annotations
@@ -21,6 +21,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libtensorbleu.so")
 HOST_SRC = os.path.join(CSRC, "tb_host.cpp")
 HOST_LIB = os.path.join(PKG, "_host.so")
+HOST_MODULES = [(HOST_SRC, HOST_LIB),
+                (os.path.join(CSRC, "loss", "tb_loss_py.cpp"), os.path.join(PKG, "_loss_host.so"))]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 PRELOADED_WORDS = 14  # of a kernel's plain arguments
@@ -38,10 +40,11 @@ def sources():
 
 
 def needs_build() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(HOST_LIB):
+    built = [LIB] + [lib for _, lib in HOST_MODULES]
+    if not all(os.path.exists(f) for f in built):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(HOST_LIB))
-    deps = sources() + [HOST_SRC] + glob.glob(os.path.join(CSRC, "*.h")) + \
+    t = min(os.path.getmtime(f) for f in built)
+    deps = sources() + [src for src, _ in HOST_MODULES] + glob.glob(os.path.join(CSRC, "*.h")) + \
         glob.glob(os.path.join(CSRC, "loss", "*.h")) + glob.glob(os.path.join(INCLUDE, "*.h"))
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -62,12 +65,13 @@ def build(verbose: bool = True) -> str:
         list(pool.map(run, [[HIPCC, *FLAGS, *extra, *include, "-c", f, "-o", o] for f, o in zip(sources(), names)]))
         run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-fno-gpu-rdc", "-o", tmp, *names])
     os.replace(tmp, LIB)
-    build_host(verbose)
+    for src, lib in HOST_MODULES:
+        build_host(verbose, src, lib)
     return LIB
 
 
-def build_host(verbose: bool = True) -> str:
-    """The module _host: links against the library and PyTorch."""
+def build_host(verbose: bool = True, src: str = HOST_SRC, lib: str = HOST_LIB) -> str:
+    """A module that marshals calls (_host, _loss_host): links against the library and PyTorch."""
     import sysconfig
 
     import torch
@@ -76,18 +80,18 @@ def build_host(verbose: bool = True) -> str:
     torch_lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     include = [INCLUDE, *cpp_extension.include_paths(), os.path.join(rocm, "include"),
                sysconfig.get_paths()["include"]]
-    tmp = HOST_LIB + f".tmp{os.getpid()}"
+    tmp = lib + f".tmp{os.getpid()}"
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
            "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-           *[f"-isystem{d}" for d in include], "-o", tmp, HOST_SRC, "-L", PKG, "-ltensorbleu",
+           *[f"-isystem{d}" for d in include], "-o", tmp, src, "-L", PKG, "-ltensorbleu",
            "-L", torch_lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip",
            "-Wl,-rpath,$ORIGIN"]
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)
-    os.replace(tmp, HOST_LIB)
-    return HOST_LIB
+    os.replace(tmp, lib)
+    return lib
 
 
 EXAMPLE_SRC = os.path.join(PKG, "example", "c_caller.c")

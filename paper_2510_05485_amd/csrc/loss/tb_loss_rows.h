@@ -296,8 +296,10 @@ __global__ __launch_bounds__(kLaneThreads) void lanes_kernel(Rows r, RowOut o, P
 // ---- sweeps over a row in memory --------------------------------------------------------------
 
 // Statistics of a row, in every thread.  Reads the row once.
-template <typename X, bool kEntropy>
-__device__ __forceinline__ Stats row_stats(const Span<X>& row, float k, Stats* parts) {
+// (kThreads: threads of the workgroup, or of the wavefront that has the row to itself; 0: blockDim.x)
+template <typename X, bool kEntropy, int kThreads = 0>
+__device__ __forceinline__ Stats row_stats(const Span<X>& row, float k, int thread, Stats* parts) {
+  const int threads = kThreads ? kThreads : blockDim.x;
   Stats mine = {kLowest, 0.f, 0.f};
   auto take = [&](const float* v, int n) {
     float top = mine.m;
@@ -316,35 +318,37 @@ __device__ __forceinline__ Stats row_stats(const Span<X>& row, float k, Stats* p
         if (kEntropy) mine.t += w * finite(a);
       }
   };
-  for (int c = threadIdx.x; c < row.chunks; c += blockDim.x) {
+  for (int c = thread; c < row.chunks; c += threads) {
     float v[X::kPer];
     X::unpack(row.chunk(c), v);
     take(v, X::kPer);
   }
-  const int e = row.edge(threadIdx.x);
+  const int e = row.edge(thread);
   if (e >= 0) {
     const float v[X::kPer] = {X::load(row.x + e)};
     take(v, 1);
   }
   mine = joined_lanes<kEntropy, kWave>(mine, [k](const Stats& a, const Stats& b) { return joined<kEntropy>(a, b, k); });
-  if (threadIdx.x % kWave == 0) parts[threadIdx.x / kWave] = mine;
+  if constexpr (kThreads == kWave) return mine;
+  if (thread % kWave == 0) parts[thread / kWave] = mine;
   __syncthreads();
   Stats all = parts[0];
-  for (int w = 1; w < int(blockDim.x / kWave); ++w) all = joined<kEntropy>(all, parts[w], k);
+  for (int w = 1; w < threads / kWave; ++w) all = joined<kEntropy>(all, parts[w], k);
   return all;
 }
 
 // The gradient of a row, but for the additions at the token.
-template <typename X, bool kEntropy>
-__device__ __forceinline__ void write_gradient(const Span<X>& row, typename X::type* g, float m, float k, Slope f) {
-  for (int c = threadIdx.x; c < row.chunks; c += blockDim.x) {
+template <typename X, bool kEntropy, int kThreads = 0>
+__device__ __forceinline__ void write_gradient(const Span<X>& row, typename X::type* g, int thread, float m, float k,
+                                               Slope f) {
+  for (int c = thread; c < row.chunks; c += kThreads ? kThreads : blockDim.x) {
     float v[X::kPer];
     X::unpack(row.chunk(c), v);
 #pragma unroll
     for (int i = 0; i < X::kPer; ++i) v[i] = gradient_at<kEntropy>((v[i] - m) * k, f);
     *reinterpret_cast<u32x4_any*>(g + row.at(c)) = X::pack(v);
   }
-  const int e = row.edge(threadIdx.x);
+  const int e = row.edge(thread);
   if (e >= 0) X::store(g + e, gradient_at<kEntropy>((X::load(row.x + e) - m) * k, f));
 }
 
@@ -454,7 +458,7 @@ __device__ __forceinline__ void write_distilled(const Rows& r, const Span<X>& ro
   typename X::type* g = gradient_of<X>(r, b, t);
   Slope f = {0.f, 0.f, q.tau * w * r.g_scale};
   f.by_weight = sum == sum ? f.token / s : sum;
-  write_gradient<X, false>(row, g, m, k, f);
+  write_gradient<X, false>(row, g, threadIdx.x, m, k, f);
   __syncthreads();  // (what it has stored comes before what follows)
   add_entries<X>(row, g, q, e, m, k, f);
 }
@@ -480,7 +484,7 @@ __device__ __forceinline__ float4 sweep_row(const Rows& r, const RowOut& o, cons
   if constexpr (kOp != kDistill) {
     const int token = take_token(r, b, t, first);
     const float x = token < 0 ? __uint_as_float(kNan) : X::load(row.x + token);
-    const Stats s = row_stats<X, kEntropy>(row, k, shared.parts);
+    const Stats s = row_stats<X, kEntropy>(row, k, threadIdx.x, shared.parts);
     const float log_s = logf(s.s), lp = (x - s.m) * r.inv_temp - log_s;
     const float H = kEntropy ? log_s - kLn2 * s.t / s.s : 0.f;
     Position v = {};
@@ -495,14 +499,14 @@ __device__ __forceinline__ float4 sweep_row(const Rows& r, const RowOut& o, cons
     if (kOp == kPolicy && r.g) {
       const Slope f = slope_of(s.s, H, v.d_lp, v.d_H, r.g_scale * r.inv_temp);
       typename X::type* g = gradient_of<X>(r, b, t);
-      write_gradient<X, kEntropy>(row, g, s.m, k, f);
+      write_gradient<X, kEntropy>(row, g, threadIdx.x, s.m, k, f);
       if (token >= 0) add_token<X, kEntropy>(row, g, token, x, s.m, k, f);
     }
     return v.terms;
   } else {
     Entries& e = shared.entries;
     const float sum = take_entries<X>(r, row, q, at, k, e);
-    const Stats s = row_stats<X, false>(row, k, shared.parts);
+    const Stats s = row_stats<X, false>(row, k, threadIdx.x, shared.parts);
     const float log_s = logf(s.s);
     float d = 0.f;
     for (int j = threadIdx.x; j < q.K; j += blockDim.x)
@@ -568,7 +572,7 @@ __device__ __forceinline__ void given_row(const Rows& r, const Given& v, const T
     __syncthreads();  // (the row may be the gradient's own memory)
     const Slope f = slope_of(state.y, state.z, token < 0 ? x : d, d_H, r.g_scale * r.inv_temp);
     typename X::type* g = gradient_of<X>(r, b, t);
-    write_gradient<X, kEntropy>(row, g, state.x, k, f);
+    write_gradient<X, kEntropy>(row, g, threadIdx.x, state.x, k, f);
     if (token >= 0) add_token<X, kEntropy>(row, g, token, x, state.x, k, f);
   } else {
     const float sum = take_entries<X>(r, row, q, at, k, shared.entries);
@@ -593,26 +597,26 @@ __global__ __launch_bounds__(512) void gradient_kernel(Rows r, Given v, Teacher 
 
 constexpr int kHeldThreads = 512;
 
-// A row's chunks in registers of a workgroup, kChunks a thread: chunk k * kHeldThreads + thread.  All but
-// the last are there in every thread; what lies beyond the row is -inf.
-template <typename X, int kChunks>
+// A row's chunks in registers of kThreads threads, kChunks each: chunk k * kThreads + thread.  All but the
+// last are there in every thread; what lies beyond the row is -inf.
+template <typename X, int kThreads, int kChunks>
 struct Held {
   u32x4 c[kChunks];
   float edge;
   int edge_at;
-  __device__ __forceinline__ void load(const Span<X>& row) {
+  __device__ __forceinline__ void load(const Span<X>& row, int thread) {
     const char* from = reinterpret_cast<const char*>(row.x + row.head);
-    const uint32_t lane = threadIdx.x * 16u;
+    const uint32_t lane = thread * 16u;
 #pragma unroll
     for (int k = 0; k < kChunks - 1; ++k)
-      c[k] = *reinterpret_cast<const u32x4*>(from + k * (kHeldThreads * 16) + lane);
+      c[k] = *reinterpret_cast<const u32x4*>(from + k * (kThreads * 16) + lane);
     c[kChunks - 1] = u32x4{X::kNone, X::kNone, X::kNone, X::kNone};
-    if (last(row)) c[kChunks - 1] = *reinterpret_cast<const u32x4*>(from + (kChunks - 1) * (kHeldThreads * 16) + lane);
-    edge_at = row.edge(threadIdx.x);
+    if (last(row, thread)) c[kChunks - 1] = *reinterpret_cast<const u32x4*>(from + (kChunks - 1) * (kThreads * 16) + lane);
+    edge_at = row.edge(thread);
     edge = edge_at >= 0 ? X::load(row.x + edge_at) : -INFINITY;
   }
-  __device__ __forceinline__ bool last(const Span<X>& row) const {
-    return int(threadIdx.x) + (kChunks - 1) * kHeldThreads < row.chunks;
+  __device__ __forceinline__ bool last(const Span<X>& row, int thread) const {
+    return thread + (kChunks - 1) * kThreads < row.chunks;
   }
   // Keeps the compiler from holding the values that it has unpacked until they are used again, which
   // would take twice the registers of the row itself.
@@ -640,8 +644,8 @@ __device__ __forceinline__ Stats joined_held(const Stats& p, const Stats& q, flo
   return r;
 }
 
-template <typename X, bool kEntropy, int kChunks>
-__device__ __forceinline__ Stats wave_stats(Held<X, kChunks>& h, float k) {
+template <bool kEntropy, typename X, int kThreads, int kChunks>
+__device__ __forceinline__ Stats wave_stats(Held<X, kThreads, kChunks>& h, float k) {
   Stats mine = {fmaxf(h.edge, -kExtreme), 0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < kChunks; ++j) {
@@ -669,12 +673,12 @@ __device__ __forceinline__ Stats wave_stats(Held<X, kChunks>& h, float k) {
   return joined_lanes<kEntropy, kWave>(mine, [k](const Stats& a, const Stats& b) { return joined_held<kEntropy>(a, b, k); });
 }
 
-template <typename X, bool kEntropy, int kChunks>
-__device__ __forceinline__ void write_held(const Span<X>& row, const Held<X, kChunks>& h, typename X::type* g, float m,
-                                           float k, Slope f) {
+template <bool kEntropy, typename X, int kThreads, int kChunks>
+__device__ __forceinline__ void write_held(const Span<X>& row, const Held<X, kThreads, kChunks>& h,
+                                           typename X::type* g, int thread, float m, float k, Slope f) {
   const float M = scaled(m, k);
   char* to = reinterpret_cast<char*>(g + row.head);
-  const uint32_t lane = threadIdx.x * 16u;
+  const uint32_t lane = thread * 16u;
   auto value = [&](float x) { return gradient_at<kEntropy>(fmaf(x, k, -M), f); };
 #pragma unroll
   for (int j = 0; j < kChunks; ++j) {
@@ -682,17 +686,17 @@ __device__ __forceinline__ void write_held(const Span<X>& row, const Held<X, kCh
     X::unpack(h.c[j], v);
 #pragma unroll
     for (int i = 0; i < X::kPer; ++i) v[i] = value(v[i]);
-    if (j < kChunks - 1 || h.last(row))
-      *reinterpret_cast<u32x4_any*>(to + j * (kHeldThreads * 16) + lane) = X::pack(v);
+    if (j < kChunks - 1 || h.last(row, thread))
+      *reinterpret_cast<u32x4_any*>(to + j * (kThreads * 16) + lane) = X::pack(v);
   }
   if (h.edge_at >= 0) X::store(g + h.edge_at, value(h.edge));
 }
 
 // Statistics of the row, in every thread; of the parts that its wavefronts leave.
-template <bool kEntropy>
+template <bool kEntropy, int kWaves>
 __device__ __forceinline__ Stats block_stats(const Stats* parts, float k) {
   Stats all = parts[0];
-  for (int w = 1; w < kHeldThreads / kWave; ++w) all = joined_held<kEntropy>(all, parts[w], k);
+  for (int w = 1; w < kWaves; ++w) all = joined_held<kEntropy>(all, parts[w], k);
   return all;
 }
 
@@ -715,22 +719,22 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Po
   const Span<X> row(row_of<X>(r, b, t), r.V);
   // (what comes first is waited for first: not behind the whole row)
   const int token = take_token(r, b, t, first), share = kOp == kPolicy ? share_of_total(r, mean) : 0;
-  Held<X, kChunks> h;
-  h.load(row);
+  Held<X, kHeldThreads, kChunks> h;
+  h.load(row, threadIdx.x);
   const float x = token < 0 ? __uint_as_float(kNan) : X::load(row.x + token);
   const float k = r.inv_temp * kLog2e;
   if (kOp == kPolicy) {
     const int part = wave_sum(share);
     if (threadIdx.x % kWave == 0) totals[threadIdx.x / kWave] = part;
   }
-  const Stats part = wave_stats<X, kEntropy>(h, k);
+  const Stats part = wave_stats<kEntropy>(h, k);
   if (threadIdx.x % kWave == 0) parts[threadIdx.x / kWave] = part;
   __syncthreads();
-  Stats s = block_stats<kEntropy>(parts, k);
+  Stats s = block_stats<kEntropy, kWaves>(parts, k);
   const bool extreme = !(fabsf(s.m) < kExtreme);
   if (extreme) {
     __syncthreads();
-    s = row_stats<X, kEntropy>(row, k, parts);
+    s = row_stats<X, kEntropy>(row, k, threadIdx.x, parts);
   }
   const float log_s = logf(s.s);
   const float lp = (extreme ? (x - s.m) * r.inv_temp : fmaf(x, k, -scaled(s.m, k)) * kLn2) - log_s;
@@ -760,13 +764,198 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Po
   const Slope f = slope_of(s.s, H, v.d_lp, v.d_H, r.g_scale * r.inv_temp);
   typename X::type* g = gradient_of<X>(r, b, t);
   if (extreme) {
-    write_gradient<X, kEntropy>(row, g, s.m, k, f);
+    write_gradient<X, kEntropy>(row, g, threadIdx.x, s.m, k, f);
     if (token >= 0) add_token<X, kEntropy>(row, g, token, x, s.m, k, f);
     return;
   }
-  write_held<X, kEntropy>(row, h, g, s.m, k, f);
+  write_held<kEntropy>(row, h, g, threadIdx.x, s.m, k, f);
   if (token >= 0 && row.owner(token, kHeldThreads) == int(threadIdx.x))
     X::store(g + token, f.token + gradient_at<kEntropy>(fmaf(x, k, -scaled(s.m, k)), f));
+}
+
+// ---- distillation on rows in registers --------------------------------------------------------
+
+// A barrier of the threads that share a row: of a wavefront, whose accesses keep their order, it only
+// keeps the compiler from moving them.
+template <int kThreads>
+__device__ __forceinline__ void meet() {
+  if constexpr (kThreads == kWave) {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  } else {
+    __syncthreads();
+  }
+}
+
+// kThreads threads a row, kEntries entries of the teacher each: a workgroup, or one of four wavefronts
+// that then take several rows.  While the row is on its way to the registers, its threads look for ids
+// that come up twice; entry j's thread writes the gradient at id j behind the others' stores, with the
+// sum of the probabilities of this id if it does.
+template <typename X, int kThreads, int kChunks, int kEntries>
+__global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void distill_kernel(Rows r, RowOut o, Mean mean,
+                                                                                           Teacher q) {
+  constexpr int kTeams = kThreads == kWave ? 4 : 1, kWaves = kThreads / kWave, kRoom = kThreads * kEntries;
+  __shared__ __attribute__((aligned(16))) int ids[kTeams][kRoom];
+  __shared__ __attribute__((aligned(16))) float shares[kTeams][kRoom];
+  __shared__ Stats parts[kTeams][kWaves], teachers[kTeams][kWaves];
+  __shared__ float losses[kTeams][kWaves];
+  __shared__ int totals[kTeams * kWaves];
+  const int team = threadIdx.x / kThreads, thread = threadIdx.x % kThreads, wave = thread / kWave;
+  const bool first = thread == 0;
+  const int64_t rows = int64_t(r.B) * r.T;
+  const float k = r.inv_temp * kLog2e;
+  int total = 0;
+  if constexpr (kThreads == kWave) {
+    const int part = wave_sum(share_of_total(r, mean));
+    if (first) totals[team] = part;
+    __syncthreads();
+    for (int w = 0; w < kTeams; ++w) total += totals[w];
+  }
+  double sum = 0;
+  for (int64_t i = int64_t(blockIdx.x) * kTeams + team; i < rows; i += int64_t(gridDim.x) * kTeams) {
+    const int64_t at = kThreads == kWave ? i : row_of_group(i, rows);
+    const int b = int(uint32_t(at) / uint32_t(r.T)), t = int(uint32_t(at) % uint32_t(r.T));
+    if (first && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
+    typename X::type* g = r.g ? gradient_of<X>(r, b, t) : nullptr;
+    auto zeros = [&] {
+      if (!g) return;
+      const Span<X> row(g, r.V);
+      for (int c = thread; c < row.chunks; c += kThreads) *reinterpret_cast<u32x4*>(g + row.at(c)) = u32x4{};
+      const int e = row.edge(thread);
+      if (e >= 0) X::store(g + e, 0.f);
+    };
+    if (!counts(r, b, t)) {
+      if (first) leave_nothing(o, at);
+      zeros();
+      continue;
+    }
+    const Span<X> row(row_of<X>(r, b, t), r.V);
+    // (what comes first is waited for first: not behind the whole row)
+    float v[kEntries], x[kEntries];
+    int64_t wide[kEntries];
+    int id[kEntries];
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) {
+      const int j = thread + e * kThreads;
+      v[e] = -INFINITY;
+      wide[e] = -1;
+      if (j < q.K) {
+        v[e] = teacher_value(q, at * q.K + j);
+        wide[e] = load_id(q.ids, q.long_ids, at * q.K + j);
+      }
+    }
+    const int share = kThreads == kWave ? 0 : share_of_total(r, mean);
+    Held<X, kThreads, kChunks> h;
+    h.load(row, thread);
+    Stats teacher = {kLowest, 0.f, 0.f};
+    bool wrong = false;
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) {
+      const bool entry = v[e] != -INFINITY, fits = wide[e] >= 0 && wide[e] < r.V;
+      if (entry && !fits) {
+        wrong = true;
+        v[e] = __uint_as_float(kNan);
+      }
+      id[e] = entry && fits ? int(wide[e]) : -1;
+      x[e] = id[e] >= 0 ? X::load(row.x + id[e]) : 0.f;
+      const int j = thread + e * kThreads;
+      ids[team][j] = id[e] >= 0 ? id[e] : ~j;
+      teacher.m = fmaxf(teacher.m, v[e]);
+    }
+    if (wrong && r.status) atomicOr(r.status, TB_DEV_TOKEN_RANGE);
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) teacher.s += exp2_fast((v[e] - teacher.m) * k);
+    teacher = joined_lanes<false, kWave>(teacher, [k](const Stats& a, const Stats& c) { return joined<false>(a, c, k); });
+    if constexpr (kThreads != kWave) {
+      const int part = wave_sum(share);
+      if (thread % kWave == 0) {
+        totals[wave] = part;
+        teachers[team][wave] = teacher;
+      }
+    }
+    meet<kThreads>();
+    uint32_t twice = 0;  // (bit e: entry e's id has others)
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) {
+      const int j = thread + e * kThreads;
+      if (j >= q.K) continue;
+      int found = 0;
+      for (int c = 0; c < q.K; c += 4) {
+        const int4 u = *reinterpret_cast<const int4*>(&ids[team][c]);
+        found += (u.x == id[e]) + (u.y == id[e]) + (u.z == id[e]) + (u.w == id[e]);
+      }
+      if (found > 1) twice |= 1u << e;
+    }
+    const Stats mine = wave_stats<false>(h, k);
+    Stats s = mine;
+    if constexpr (kThreads != kWave) {
+      if (thread % kWave == 0) parts[team][wave] = mine;
+      __syncthreads();
+      s = block_stats<false, kWaves>(parts[team], k);
+      teacher = teachers[team][0];
+      for (int w = 1; w < kWaves; ++w) teacher = joined<false>(teacher, teachers[team][w], k);
+      total = 0;
+      for (int w = 0; w < kWaves; ++w) total += totals[w];
+    }
+    const bool extreme = !(fabsf(s.m) < kExtreme);
+    if (extreme) {
+      meet<kThreads>();
+      s = row_stats<X, false, kThreads>(row, k, thread, parts[team]);
+    }
+    const float log_s = logf(s.s), log_t = logf(teacher.s), by = teacher.s == 0.f ? 0.f : 1.f / teacher.s;
+    const float M = scaled(s.m, k);
+    float d = 0.f;
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) {
+      const float a = (v[e] - teacher.m) * k, share_e = exp2_fast(a) * by;
+      const float z = extreme ? (x[e] - s.m) * k : fmaf(x[e], k, -M);
+      if (!(share_e <= 0.f)) d += share_e * ((a - z) * kLn2 - (log_t - log_s));
+      v[e] = share_e;
+      x[e] = z;
+      shares[team][thread + e * kThreads] = share_e;
+    }
+    d = wave_sum(d);
+    if (thread % kWave == 0) losses[team][wave] = d;
+    const float w = teacher.s == 0.f ? 0.f : weight_of(r, mean, b, total);
+    Slope f = {0.f, 0.f, q.tau * w * r.g_scale};
+    f.by_weight = teacher.s == teacher.s ? f.token / s.s : teacher.s;
+    if (teacher.s == 0.f) zeros();
+    else if (g && extreme) write_gradient<X, false, kThreads>(row, g, thread, s.m, k, f);
+    else if (g) write_held<false>(row, h, g, thread, s.m, k, f);
+    meet<kThreads>();  // (what it has stored comes before what follows)
+    if (g && teacher.s != 0.f) {
+#pragma unroll
+      for (int e = 0; e < kEntries; ++e) {
+        if (id[e] < 0) continue;
+        float sum_e = v[e];
+        if (twice >> e & 1) {
+          sum_e = 0.f;
+          for (int c = 0; c < q.K; ++c) sum_e += ids[team][c] == id[e] ? shares[team][c] : 0.f;
+        }
+        X::store(g + id[e], exp2_fast(x[e]) * f.by_weight - f.token * sum_e);
+      }
+    }
+    d = 0.f;
+    for (int c = 0; c < kWaves; ++c) d += losses[team][c];
+    d *= q.tau * q.tau;
+    if (first) {
+      if (o.state) o.state[at] = {s.m, s.s, 0.f, d};
+      if (o.d_logprobs) o.d_logprobs[at] = w;
+      if (o.logprobs) o.logprobs[at] = d;
+    }
+    sum += double(w) * d;
+    meet<kThreads>();  // (before the next row takes the shared memory)
+  }
+  __shared__ double sums[kTeams];
+  if (first) sums[team] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kTeams; ++w) sum += sums[w];
+    double* to = o.partial + int64_t(blockIdx.x) * 4;
+    to[0] = sum;
+    to[1] = to[2] = to[3] = 0.0;
+  }
 }
 
 // ---- launches ---------------------------------------------------------------------------------
@@ -822,6 +1011,42 @@ bool launch_held(Call& c) {
   return false;
 }
 
+// A wavefront a row of up to 512 chunks, a workgroup one of more.
+template <typename X, int kEntries>
+bool launch_distill_wave(Call& c) {
+  const Rows& r = c.rows;
+  const int64_t groups = (int64_t(r.B) * r.T + 3) / 4;
+  c.groups = int(groups < kLaneGroups ? groups : kLaneGroups);
+#define HELD(n) \
+  case n: distill_kernel<X, kWave, n, kEntries><<<c.groups, 4 * kWave, 0, c.stream>>>(r, c.out, c.mean, c.teacher); return true;
+  switch ((r.V / X::kPer + kWave - 1) / kWave) { HELD(1) HELD(2) HELD(3) HELD(4) HELD(5) HELD(6) HELD(7) HELD(8) }
+#undef HELD
+  return false;
+}
+template <typename X, int kEntries>
+bool launch_distill_block(Call& c) {
+  const Rows& r = c.rows;
+  c.groups = grid_of(r);
+#define HELD(n) \
+  case n: distill_kernel<X, kHeldThreads, n, kEntries><<<c.groups, kHeldThreads, 0, c.stream>>>(r, c.out, c.mean, c.teacher); return true;
+  switch ((r.V / X::kPer + kHeldThreads - 1) / kHeldThreads) {
+    HELD(1) HELD(2) HELD(3) HELD(4) HELD(5) HELD(6) HELD(7) HELD(8) HELD(9) HELD(10) HELD(11) HELD(12) HELD(13) HELD(14)
+    HELD(15) HELD(16) HELD(17) HELD(18) HELD(19) HELD(20) HELD(21) HELD(22) HELD(23) HELD(24) HELD(25) HELD(26) HELD(27)
+    HELD(28) HELD(29) HELD(30) HELD(31) HELD(32)
+  }
+#undef HELD
+  return false;
+}
+template <typename X>
+bool launch_distill(Call& c) {
+  if (c.rows.V < 2 * X::kPer) return false;
+  const int K = c.teacher.K;
+  return K <= 64    ? launch_distill_wave<X, 1>(c) || launch_distill_block<X, 1>(c)
+         : K <= 256 ? launch_distill_wave<X, 4>(c) || launch_distill_block<X, 1>(c)
+         : K <= 512 ? launch_distill_wave<X, 16>(c) || launch_distill_block<X, 1>(c)
+                    : launch_distill_wave<X, 16>(c) || launch_distill_block<X, 2>(c);
+}
+
 template <typename X, int kOp, bool kEntropy>
 void launch_sweep(Call& c) {
   c.groups = grid_of(c.rows);
@@ -831,7 +1056,7 @@ void launch_sweep(Call& c) {
 
 template <typename X, bool kEntropy>
 hipError_t launch_rows(Op op, Call& c) {
-  if (op == kDistill) launch_sweep<X, kDistill, false>(c);
+  if (op == kDistill) launch_distill<X>(c) || (launch_sweep<X, kDistill, false>(c), true);
   else if (op == kPolicy)
     launch_lanes<X, kPolicy, kEntropy>(c) || launch_held<X, kPolicy, kEntropy>(c) || (launch_sweep<X, kPolicy, kEntropy>(c), true);
   else

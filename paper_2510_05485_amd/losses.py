@@ -135,6 +135,24 @@ def _library() -> ctypes.CDLL:
     return _lib
 
 
+_host = None
+
+
+def native():
+    """The native marshalling module (built with the library; raises if it has not been).  Its functions
+    return None for what they leave to the code here."""
+    global _host
+    if _host is None:
+        _library()
+        try:
+            from . import _loss_host as module
+        except ImportError as e:
+            raise TensorBLEUError("the module _loss_host does not load: run `python -m "
+                                  f"paper_2510_05485_amd.build` first ({e})") from e
+        _host = module
+    return _host
+
+
 def workspace_bytes(B: int, T: int) -> int:
     return int(_library().tensorloss_workspace_bytes(B, T))
 
@@ -310,6 +328,9 @@ def token_logprobs(logits, tokens, *, lengths=None, mask=None, temperature: floa
     the entropies of the rows.  Differentiable in the logits."""
     if _needs_grad(logits):
         return _TokenLogprobs.apply(logits, tokens, lengths, mask, temperature, want_entropy, status)
+    found = native().logprobs(logits, tokens, lengths, mask, temperature, status, want_entropy)
+    if found is not None:
+        return found
     lp, entropy, _ = _score(_Call(logits, tokens, lengths, mask, temperature, status), want_entropy, False)
     return (lp, entropy) if want_entropy else lp
 
@@ -380,6 +401,11 @@ def policy_loss_grad(logits, tokens, old_logprobs, advantages, *, ref_logprobs=N
                      grad_scale: float = 1.0, out: Optional[torch.Tensor] = None,
                      status: Optional[torch.Tensor] = None) -> PolicyLoss:
     """policy_loss and its gradient in the logits, in one pass over them."""
+    found = native().policy(logits, tokens, lengths, mask, temperature, status, out, grad_scale, old_logprobs,
+                            advantages, ref_logprobs, clip_low, clip_high, kl_coef, entropy_coef,
+                            AVERAGES.get(average))
+    if found is not None:
+        return PolicyLoss(*found)
     call = _Call(logits, tokens, lengths, mask, temperature, status)
     out, g = call.gradient(out, grad_scale)
     terms, lp, *_ = _policy(call, old_logprobs, advantages, ref_logprobs, clip_low, clip_high, kl_coef,
@@ -446,6 +472,10 @@ def preference_loss_grad(logits, tokens, ref_logprobs, *, lengths=None, mask=Non
                          grad_scale: float = 1.0, out: Optional[torch.Tensor] = None,
                          status: Optional[torch.Tensor] = None) -> PreferenceLoss:
     """preference_loss and its gradient in the logits."""
+    found = native().preference(logits, tokens, lengths, mask, temperature, status, out, grad_scale, ref_logprobs,
+                                beta, PAIRS.get(kind), label_smoothing)
+    if found is not None:
+        return PreferenceLoss(*found)
     call = _Call(logits, tokens, lengths, mask, temperature, status)
     out, g = call.gradient(out, grad_scale)
     terms, lp, margins, *_ = _preference(call, ref_logprobs, beta, kind, label_smoothing, g, False)
@@ -519,6 +549,10 @@ def distillation_loss_grad(logits, teacher_ids, teacher_logits, *, lengths=None,
                            out: Optional[torch.Tensor] = None,
                            status: Optional[torch.Tensor] = None) -> DistillationLoss:
     """distillation_loss and its gradient in the logits, in one pass over them."""
+    found = native().distill(logits, lengths, mask, temperature, status, out, grad_scale, teacher_ids,
+                             teacher_logits, AVERAGES.get(average))
+    if found is not None:
+        return DistillationLoss(*found)
     call = _Call(logits, None, lengths, mask, temperature, status)
     q = _teacher(call, teacher_ids, teacher_logits, average)
     out, g = call.gradient(out, grad_scale)
