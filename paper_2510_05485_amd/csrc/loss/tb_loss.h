@@ -43,9 +43,12 @@ struct RowOut {  // per position, any may be null
   double* partial;  // [workgroup][4]: the weighted terms of its rows
 };
 
+// How positions are averaged.  A weight is one over a total, which every workgroup adds up from `parts`
+// numbers: positions of the sequences (or, for TB_MEAN_TOKENS, of any parts), or sequences that have some.
 struct Mean {
-  const float* weight;  // [B], or null: from the lengths
-  int average;
+  const float* weight;  // [B]: the weights themselves, or null
+  const int32_t* n;     // [parts], or null: the lengths, and T without these
+  int parts, average;
 };
 
 struct Policy {
@@ -204,6 +207,7 @@ __device__ __forceinline__ int held_length(int length, int T, int32_t* status) {
   if (status) atomicOr(status, TB_DEV_LENGTH_RANGE);
   return length < 0 ? 0 : T;
 }
+__device__ __forceinline__ int clamped(int length, int T) { return min(max(length, 0), T); }
 __device__ __forceinline__ bool counts(const Rows& r, int b, int t) {
   if (r.lengths && t >= r.lengths[b]) return false;
   return !r.mask || r.mask[int64_t(b) * r.T + t] != 0;

@@ -21,7 +21,7 @@ constexpr size_t kAlign = 256;
 size_t aligned(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
 
 struct Workspace {
-  size_t counts, weight, more, partial, state, d_sequence, bytes;
+  size_t counts, weight, more, partial, state, lp, d_sequence, bytes;
 };
 Workspace workspace_of(int64_t B, int64_t T) {
   Workspace w;
@@ -31,12 +31,13 @@ Workspace workspace_of(int64_t B, int64_t T) {
     at += aligned(n);
     return from;
   };
-  w.counts = take(4 * B);
+  w.counts = take(4 * (B > kCountParts ? B : kCountParts));
   w.weight = take(4 * B);
   w.more = take(8 * 4 * kMoreSums);
   const int64_t groups = B * T < kMostGroups ? B * T : kMostGroups;
   w.partial = take(8 * 4 * size_t(groups > B ? groups : B));
-  w.state = take(16 * B * T);  // (of pairs only)
+  w.state = take(16 * B * T);  // (of pairs only, as what follows)
+  w.lp = take(4 * B * T);
   w.d_sequence = take(4 * B);
   w.bytes = at;
   return w;
@@ -111,15 +112,31 @@ template <typename T>
 T* in(void* workspace, size_t offset) {
   return reinterpret_cast<T*>(static_cast<char*>(workspace) + offset);
 }
-// Lengths of few sequences are added up by every workgroup while its row is on its way, and a launch or
-// two less (4 us each) is worth that; masks and many lengths are counted before.
-constexpr int kMostLengths = 2048;
+// What a mean divides by is added up by every workgroup while its row is on its way, from the lengths, or
+// from the numbers that a launch (4 us) counts in a mask; beyond so many numbers a launch more leaves the
+// weights.  (Policy loss on 4096 sequences of 512 positions of 64 logits: 12 us less.)
+constexpr int kMostParts = 8192;
 hipError_t set_mean(Call& c, int average, const Workspace& w, void* workspace) {
-  c.mean = {nullptr, average};
-  if (!c.rows.mask && (!c.rows.lengths || c.rows.B <= kMostLengths)) return hipSuccess;
-  float* weight = in<float>(workspace, w.weight);
-  c.mean.weight = weight;
-  return run_weights(c.rows, average, in<int32_t>(workspace, w.counts), weight, c.stream);
+  const Rows& r = c.rows;
+  int32_t* n = in<int32_t>(workspace, w.counts);
+  c.mean = {nullptr, nullptr, r.B, average};
+  if (average == TB_SUM || (!r.mask && !r.lengths)) return hipSuccess;
+  if (r.mask && (average == TB_MEAN_TOKENS || r.B == 1)) {
+    c.mean = {nullptr, n, kCountParts, TB_MEAN_TOKENS};  // (one sequence's mean is that of its positions)
+    return run_part_counts(r, n, c.stream);
+  }
+  if (r.mask) {
+    c.mean.n = n;
+    const hipError_t e = run_counts(r, n, c.stream);
+    if (e != hipSuccess || r.B <= kMostParts) return e;
+  } else if (r.B <= kMostParts) {
+    return hipSuccess;
+  } else {
+    const hipError_t e = run_counts(r, n, c.stream);
+    if (e != hipSuccess) return e;
+  }
+  c.mean.weight = in<float>(workspace, w.weight);
+  return run_weights(r.B, average, n, in<float>(workspace, w.weight), c.stream);
 }
 int done(hipError_t e) { return e == hipSuccess ? TB_OK : TB_ERR_HIP; }
 bool average_known(int a) { return a >= TB_MEAN_TOKENS && a <= TB_SUM; }
@@ -233,10 +250,10 @@ extern "C" int tensorloss_preference(const tb_logits_t* logits, const tb_positio
   if (!empty(r)) {
     r.g = nullptr;
     r.status = status;
-    c.out = {nullptr, nullptr, state, nullptr, nullptr, nullptr};
+    c.out = {in<float>(workspace, w.lp), nullptr, state, nullptr, nullptr, nullptr};
     if (run_rows(kScore, c) != hipSuccess) return TB_ERR_HIP;
   }
-  const Pairs pairs = {preference->ref_logprobs, state, terms, sequence_logprobs, margins, d_sequence,
+  const Pairs pairs = {preference->ref_logprobs, in<float>(workspace, w.lp), terms, sequence_logprobs, margins, d_sequence,
                        in<double>(workspace, w.partial), preference->kind, preference->beta, preference->label_smoothing};
   if (run_pairs(r, pairs, c.stream) != hipSuccess) return TB_ERR_HIP;
   if (!g || empty(r)) return TB_OK;

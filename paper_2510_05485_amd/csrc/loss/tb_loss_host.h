@@ -29,16 +29,19 @@ hipError_t rows_of(Op op, Call& c);
 template <typename X>
 hipError_t gradient_of(Op op, const Call& c);
 
-// weight[b] of every sequence's positions; counts [B] is scratch.
-hipError_t run_weights(const Rows& r, int average, int32_t* counts, float* weight, hipStream_t stream);
+// How many positions of each sequence count (n [B]), or of parts of all positions (n [kCountParts]).
+constexpr int kCountParts = 256;
+hipError_t run_counts(const Rows& r, int32_t* n, hipStream_t stream);
+hipError_t run_part_counts(const Rows& r, int32_t* n, hipStream_t stream);
+// weight[b] of the positions of every sequence, from their numbers.
+hipError_t run_weights(int B, int average, const int32_t* n, float* weight, hipStream_t stream);
 
 // terms[i] = sum over workgroups of partial[workgroup][i], i < n; more: scratch of kMoreSums * 4 doubles.
 constexpr int kMoreSums = 256;
 hipError_t run_terms(int64_t groups, const double* partial, double* more, float* terms, int n, hipStream_t stream);
 
 struct Pairs {
-  const float* ref_lp;
-  const float4* state;
+  const float *ref_lp, *lp;  // [B, T]
   float *terms, *sequence_lp, *margins, *d_sequence;
   double* partial;  // [B / 2, 3]
   int kind;

@@ -6,7 +6,10 @@
 #include <Python.h>
 
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/autograd/function.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/autograd/saved_variable.h>
 #include <ATen/ATen.h>
 
 #include "tensorloss.h"
@@ -44,6 +47,7 @@ struct Call {
   const at::Tensor* x = nullptr;
   tb_logits_t logits = {};
   tb_positions_t at = {};
+  const at::Tensor *tokens = nullptr, *lengths = nullptr, *mask = nullptr;
   bool packed = false;
   int32_t* status = nullptr;
   void* stream = nullptr;
@@ -82,6 +86,7 @@ struct Call {
       if (!here(t) || !id_type(t->scalar_type()) || t->dim() != x->dim() - 1 || t->size(-1) != T ||
           (!packed && t->size(0) != B) || (T > 1 && t->stride(-1) != 1))
         return false;
+      tokens = t;
       at.tokens = t->data_ptr();
       at.token_stride = packed ? T : t->stride(0);
       at.token_bytes = t->scalar_type() == at::kLong ? 8 : 4;
@@ -90,6 +95,7 @@ struct Call {
       const at::Tensor* t = tensor(lengths_);
       if (packed || !here(t) || t->scalar_type() != at::kInt || t->dim() != 1 || t->size(0) != B || !t->is_contiguous())
         return false;
+      lengths = t;
       at.lengths = t->data_ptr<int32_t>();
     }
     if (mask_ != Py_None) {
@@ -97,6 +103,7 @@ struct Call {
       if (!here(t) || (t->scalar_type() != at::kBool && t->scalar_type() != at::kByte) || t->dim() != x->dim() - 1 ||
           t->size(-1) != T || (!packed && t->size(0) != B) || !t->is_contiguous())
         return false;
+      mask = t;
       at.mask = static_cast<const uint8_t*>(t->data_ptr());
     }
     if (status_ != Py_None) {
@@ -109,6 +116,7 @@ struct Call {
   at::Tensor values(at::IntArrayRef shape) const {
     return at::empty(shape, at::TensorOptions().dtype(at::kFloat).device(x->device()));
   }
+  at::Tensor row_state() const { return values({logits.B, logits.T, TB_ROW_STATE}); }
   at::IntArrayRef positions() const { return x->sizes().slice(0, x->dim() - 1); }
   at::Tensor workspace(size_t* bytes) const {
     *bytes = tensorloss_workspace_bytes(logits.B, logits.T);
@@ -132,6 +140,74 @@ struct Call {
     return true;
   }
 };
+
+// The backward pass of all operators: the gradient of rows whose statistics and cotangents the forward
+// pass has left.  Incoming gradients are of the log-probabilities and entropies themselves (kValues), or
+// of a scalar loss that `d_lp`, `d_entropy` are the cotangents of.
+struct RowsBackward : public torch::autograd::Node {
+  using Saved = torch::autograd::SavedVariable;
+  enum Kind { kValues, kLoss, kSequences, kDistill } kind;
+  tb_logits_t logits_of;
+  tb_positions_t at;
+  tb_teacher_t teacher = {};
+  Saved logits, tokens, lengths, mask, state, d_lp, d_entropy, ids, teacher_logits;
+
+  static Saved kept(const at::Tensor* t) { return t && t->defined() ? Saved(*t, false) : Saved(); }
+  RowsBackward(Kind k, const Call& c, const at::Tensor& row_state) : kind(k), logits_of(c.logits), at(c.at) {
+    logits = kept(c.x);
+    tokens = kept(c.tokens);
+    lengths = kept(c.lengths);
+    mask = kept(c.mask);
+    state = kept(&row_state);
+    set_next_edges(torch::autograd::collect_next_edges(*c.x));
+  }
+  std::string name() const override { return "TensorLossBackward"; }
+  void release_variables() override {
+    std::lock_guard<std::mutex> lock(mutex_);
+    for (Saved* s : {&logits, &tokens, &lengths, &mask, &state, &d_lp, &d_entropy, &ids, &teacher_logits}) s->reset_data();
+  }
+  torch::autograd::variable_list apply(torch::autograd::variable_list&& in) override {
+    std::lock_guard<std::mutex> lock(mutex_);
+    TORCH_CHECK(!at::GradMode::is_enabled(), "the losses over logits cannot be differentiated twice");
+    if (!in[0].defined() && (in.size() < 2 || !in[1].defined())) return {at::Tensor()};
+    // (unpacking checks that nothing has been written over since)
+    const at::Tensor x = logits.unpack(), s = state.unpack(), held[] = {tokens.unpack(), lengths.unpack(), mask.unpack()};
+    at::Tensor d = d_lp.unpack(), dh = d_entropy.unpack(), up;
+    if (kind == kValues) {
+      if (in[0].defined()) d = in[0].to(at::kFloat).contiguous();
+      if (in.size() > 1 && in[1].defined()) dh = in[1].to(at::kFloat).contiguous();
+      if (!d.defined()) d = at::zeros_like(dh);
+    } else {
+      up = in[0].to(at::kFloat).contiguous();
+    }
+    const c10::DeviceGuard guard(x.device());
+    at::Tensor out = at::empty(x.sizes(), x.options().requires_grad(false));
+    tb_gradient_t g = {out.data_ptr(), x.dim() == 2 ? 0 : out.stride(0), out.stride(x.dim() - 2), 1.f};
+    void* stream = static_cast<void*>(c10::hip::getCurrentHIPStream().stream());
+    const float* upstream = up.defined() ? up.data_ptr<float>() : nullptr;
+    int rc;
+    if (kind == kDistill) {
+      const at::Tensor i = ids.unpack(), q = teacher_logits.unpack();
+      rc = tensorloss_distill_grad(&logits_of, &at, &teacher, s.data_ptr<float>(), d.data_ptr<float>(), upstream, &g, stream);
+    } else {
+      const bool each = kind != kSequences;
+      rc = tensorloss_token_logprobs_grad(&logits_of, &at, s.data_ptr<float>(), d.data_ptr<float>(),
+                                          dh.defined() ? dh.data_ptr<float>() : nullptr, each ? logits_of.T : 1, each,
+                                          upstream, &g, stream);
+    }
+    TORCH_CHECK(rc == TB_OK, "tensorloss gradient: ", tensorbleu_status_string(rc));
+    return {out};
+  }
+};
+std::shared_ptr<RowsBackward> backward_of(RowsBackward::Kind kind, const Call& c, const at::Tensor& state) {
+  return std::shared_ptr<RowsBackward>(new RowsBackward(kind, c, state), torch::autograd::deleteNode);
+}
+bool differentiated(const at::Tensor& x) { return at::GradMode::is_enabled() && x.requires_grad(); }
+// the loss, terms[0], as a tensor of its own that shares its memory
+at::Tensor first_of(const at::Tensor& terms) {
+  at::AutoDispatchBelowADInplaceOrView guard;
+  return terms.select(0, 0);
+}
 
 PyObject* results(std::initializer_list<at::Tensor> all, PyObject* out, int out_at) {
   PyObject* tuple = PyTuple_New(Py_ssize_t(all.size()));
@@ -159,20 +235,28 @@ PyObject* logprobs(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Call c;
   if (n != 7 || !c.take(args[0], args[1], args[2], args[3], args[4], args[5])) Py_RETURN_NONE;
   const bool entropy = args[6] == Py_True;
-  at::Tensor lp = c.values(c.positions()), h;
+  at::Tensor lp = c.values(c.positions()), h, state;
   if (entropy) h = c.values(c.positions());
+  const bool backward = differentiated(*c.x);
+  if (backward) state = c.row_state();
   int rc;
   Py_BEGIN_ALLOW_THREADS
-  rc = tensorloss_token_logprobs(&c.logits, &c.at, lp.data_ptr<float>(), entropy ? h.data_ptr<float>() : nullptr, nullptr,
-                                 c.status, c.stream);
+  rc = tensorloss_token_logprobs(&c.logits, &c.at, lp.data_ptr<float>(), entropy ? h.data_ptr<float>() : nullptr,
+                                 backward ? state.data_ptr<float>() : nullptr, c.status, c.stream);
   Py_END_ALLOW_THREADS
   if (rc != TB_OK) Py_RETURN_NONE;
+  if (backward) {
+    auto node = backward_of(RowsBackward::kValues, c, state);
+    torch::autograd::set_history(lp, node);
+    if (entropy) torch::autograd::set_history(h, node);
+  }
   if (!entropy) return THPVariable_Wrap(std::move(lp));
   return results({lp, h}, Py_None, -1);
 }
 
 // policy(logits, tokens, lengths, mask, temperature, status, out, grad_scale, old_logprobs, advantages,
-// ref_logprobs, clip_low, clip_high, kl_coef, entropy_coef, average): (terms, gradient, logprobs) or None
+// ref_logprobs, clip_low, clip_high, kl_coef, entropy_coef, average): (terms, gradient, logprobs) or None;
+// grad_scale None: the loss, for torch to differentiate, and out is not used
 PyObject* policy(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Call c;
   if (n != 16 || !c.take(args[0], args[1], args[2], args[3], args[4], args[5])) Py_RETURN_NONE;
@@ -191,23 +275,41 @@ PyObject* policy(PyObject*, PyObject* const* args, Py_ssize_t n) {
     if (a->dim() != 1 || a->size(0) != c.logits.B || a->scalar_type() != at::kFloat || !a->is_contiguous()) Py_RETURN_NONE;
     p.advantages = a->data_ptr<float>();
   }
-  at::Tensor out;
+  const bool scalar = args[7] == Py_None, backward = scalar && differentiated(*c.x), bonus = p.entropy_coef != 0.f;
+  at::Tensor out, state, d_lp, d_entropy;
   tb_gradient_t g = {};
-  if (!c.gradient(args[6], args[7], &out, &g)) Py_RETURN_NONE;
+  if (!scalar && !c.gradient(args[6], args[7], &out, &g)) Py_RETURN_NONE;
+  if (backward) {
+    state = c.row_state();
+    d_lp = c.values(c.positions());
+    if (bonus) d_entropy = c.values(c.positions());
+  }
   at::Tensor terms = c.values({4}), lp = c.values(c.positions());
   size_t bytes;
   at::Tensor workspace = c.workspace(&bytes);
   int rc;
   Py_BEGIN_ALLOW_THREADS
-  rc = tensorloss_policy(&c.logits, &c.at, &p, &g, terms.data_ptr<float>(), lp.data_ptr<float>(), nullptr, nullptr,
-                         nullptr, c.status, workspace.data_ptr(), bytes, c.stream);
+  rc = tensorloss_policy(&c.logits, &c.at, &p, scalar ? nullptr : &g, terms.data_ptr<float>(), lp.data_ptr<float>(),
+                         backward ? state.data_ptr<float>() : nullptr, backward ? d_lp.data_ptr<float>() : nullptr,
+                         backward && bonus ? d_entropy.data_ptr<float>() : nullptr, c.status, workspace.data_ptr(), bytes,
+                         c.stream);
   Py_END_ALLOW_THREADS
   if (rc != TB_OK) Py_RETURN_NONE;
+  if (scalar) {
+    at::Tensor loss = first_of(terms);
+    if (backward) {
+      auto node = backward_of(RowsBackward::kLoss, c, state);
+      node->d_lp = RowsBackward::kept(&d_lp);
+      node->d_entropy = RowsBackward::kept(&d_entropy);
+      torch::autograd::set_history(loss, node);
+    }
+    return THPVariable_Wrap(std::move(loss));
+  }
   return results({terms, out, lp}, args[6], 1);
 }
 
 // preference(logits, tokens, lengths, mask, temperature, status, out, grad_scale, ref_logprobs, beta, kind,
-// label_smoothing): (terms, gradient, sequence log-probabilities, margins) or None
+// label_smoothing): (terms, gradient, sequence log-probabilities, margins) or None; grad_scale None: the loss
 PyObject* preference(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Call c;
   if (n != 12 || !c.take(args[0], args[1], args[2], args[3], args[4], args[5]) || c.packed) Py_RETURN_NONE;
@@ -215,23 +317,39 @@ PyObject* preference(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (!c.over_positions(args[8], &p.ref_logprobs) || !take_float(args[9], &p.beta) || !take_int(args[10], &p.kind) ||
       !take_float(args[11], &p.label_smoothing))
     Py_RETURN_NONE;
-  at::Tensor out;
+  const bool scalar = args[7] == Py_None, backward = scalar && differentiated(*c.x);
+  at::Tensor out, state, d_sequence;
   tb_gradient_t g = {};
-  if (!c.gradient(args[6], args[7], &out, &g)) Py_RETURN_NONE;
+  if (!scalar && !c.gradient(args[6], args[7], &out, &g)) Py_RETURN_NONE;
+  if (backward) {
+    state = c.row_state();
+    d_sequence = c.values({c.logits.B});
+  }
   at::Tensor terms = c.values({3}), sums = c.values({c.logits.B}), margins = c.values({c.logits.B / 2});
   size_t bytes;
   at::Tensor workspace = c.workspace(&bytes);
   int rc;
   Py_BEGIN_ALLOW_THREADS
-  rc = tensorloss_preference(&c.logits, &c.at, &p, &g, terms.data_ptr<float>(), sums.data_ptr<float>(),
-                             margins.data_ptr<float>(), nullptr, nullptr, c.status, workspace.data_ptr(), bytes, c.stream);
+  rc = tensorloss_preference(&c.logits, &c.at, &p, scalar ? nullptr : &g, terms.data_ptr<float>(), sums.data_ptr<float>(),
+                             margins.data_ptr<float>(), backward ? state.data_ptr<float>() : nullptr,
+                             backward ? d_sequence.data_ptr<float>() : nullptr, c.status, workspace.data_ptr(), bytes,
+                             c.stream);
   Py_END_ALLOW_THREADS
   if (rc != TB_OK) Py_RETURN_NONE;
+  if (scalar) {
+    at::Tensor loss = first_of(terms);
+    if (backward) {
+      auto node = backward_of(RowsBackward::kSequences, c, state);
+      node->d_lp = RowsBackward::kept(&d_sequence);
+      torch::autograd::set_history(loss, node);
+    }
+    return THPVariable_Wrap(std::move(loss));
+  }
   return results({terms, out, sums, margins}, args[6], 1);
 }
 
 // distill(logits, lengths, mask, temperature, status, out, grad_scale, teacher_ids, teacher_logits, average):
-// (terms, gradient, row losses) or None
+// (terms, gradient, row losses) or None; grad_scale None: the loss
 PyObject* distill(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Call c;
   if (n != 10 || !c.take(args[0], nullptr, args[1], args[2], args[3], args[4])) Py_RETURN_NONE;
@@ -246,18 +364,36 @@ PyObject* distill(PyObject*, PyObject* const* args, Py_ssize_t n) {
   q.logits = t->data_ptr();
   q.id_bytes = ids->scalar_type() == at::kLong ? 8 : 4;
   q.K = int32_t(ids->size(-1));
-  at::Tensor out;
+  const bool scalar = args[6] == Py_None, backward = scalar && differentiated(*c.x);
+  at::Tensor out, state, d_row;
   tb_gradient_t g = {};
-  if (!c.gradient(args[5], args[6], &out, &g)) Py_RETURN_NONE;
+  if (!scalar && !c.gradient(args[5], args[6], &out, &g)) Py_RETURN_NONE;
+  if (backward) {
+    state = c.row_state();
+    d_row = c.values(c.positions());
+  }
   at::Tensor terms = c.values({1}), rows = c.values(c.positions());
   size_t bytes;
   at::Tensor workspace = c.workspace(&bytes);
   int rc;
   Py_BEGIN_ALLOW_THREADS
-  rc = tensorloss_distill(&c.logits, &c.at, &q, &g, terms.data_ptr<float>(), rows.data_ptr<float>(), nullptr, nullptr,
+  rc = tensorloss_distill(&c.logits, &c.at, &q, scalar ? nullptr : &g, terms.data_ptr<float>(), rows.data_ptr<float>(),
+                          backward ? state.data_ptr<float>() : nullptr, backward ? d_row.data_ptr<float>() : nullptr,
                           c.status, workspace.data_ptr(), bytes, c.stream);
   Py_END_ALLOW_THREADS
   if (rc != TB_OK) Py_RETURN_NONE;
+  if (scalar) {
+    at::Tensor loss = first_of(terms);
+    if (backward) {
+      auto node = backward_of(RowsBackward::kDistill, c, state);
+      node->d_lp = RowsBackward::kept(&d_row);
+      node->ids = RowsBackward::kept(ids);
+      node->teacher_logits = RowsBackward::kept(t);
+      node->teacher = q;
+      torch::autograd::set_history(loss, node);
+    }
+    return THPVariable_Wrap(std::move(loss));
+  }
   return results({terms, out, rows}, args[5], 1);
 }
 

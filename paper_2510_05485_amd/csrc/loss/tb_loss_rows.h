@@ -83,22 +83,34 @@ __device__ __forceinline__ void leave_nothing(const RowOut& o, int64_t at) {
   if (o.d_entropy) o.d_entropy[at] = 0.f;
 }
 
-// Weights from the lengths: the thread's share of what they are divided by, and a sequence's weight.
+// The thread's share of the total, and the weight of a sequence's positions.
+__device__ __forceinline__ int positions_of(const Rows& r, const Mean& mean, int b) {
+  return mean.n ? mean.n[b] : r.lengths ? clamped(r.lengths[b], r.T) : r.T;
+}
 __device__ __forceinline__ int share_of_total(const Rows& r, const Mean& mean) {
+  constexpr int kAhead = 8;  // loads under way
+  const int32_t* from = mean.n ? mean.n : r.lengths;
   int n = 0;
-  if (!mean.weight && r.lengths && mean.average != TB_SUM)
-    for (int b = threadIdx.x; b < r.B; b += blockDim.x) {
-      const int length = held_length(r.lengths[b], r.T, nullptr);
-      n += mean.average == TB_MEAN_TOKENS ? length : length > 0;
+  if (mean.weight || mean.average == TB_SUM || !from) return n;
+  const int most = mean.n ? INT32_MAX : r.T, threads = blockDim.x;
+  for (int i = threadIdx.x; i < mean.parts; i += kAhead * threads) {
+    int m[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) m[j] = i + j * threads < mean.parts ? from[i + j * threads] : 0;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int c = clamped(m[j], most);
+      n += mean.average == TB_MEAN_TOKENS ? c : c > 0;
     }
+  }
   return n;
 }
 __device__ __forceinline__ float weight_of(const Rows& r, const Mean& mean, int b, int total) {
   if (mean.weight) return mean.weight[b];
   if (mean.average == TB_SUM) return 1.f;
-  if (!r.lengths) total = mean.average == TB_MEAN_TOKENS ? r.B * r.T : r.B;
+  if (!mean.n && !r.lengths) total = mean.average == TB_MEAN_TOKENS ? r.B * r.T : r.B;
   if (mean.average == TB_MEAN_TOKENS) return 1.f / float(total);
-  return 1.f / (float(total) * float(r.lengths ? held_length(r.lengths[b], r.T, nullptr) : r.T));
+  return 1.f / (float(total) * float(positions_of(r, mean, b)));
 }
 
 // Which row a workgroup takes: neighbouring workgroups go to different XCDs, neighbouring rows to one.

@@ -8,18 +8,41 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 
-// One wavefront a sequence: how many of its positions count.
+// kTeam threads a sequence (a workgroup or a wavefront): how many of its positions count.
+template <int kTeam>
 __global__ __launch_bounds__(kThreads) void count_kernel(Rows r, int32_t* n) {
-  const int lane = threadIdx.x % kWave;
-  for (int64_t b = int64_t(blockIdx.x) * kWaves + threadIdx.x / kWave; b < r.B; b += int64_t(gridDim.x) * kWaves) {
-    const int length = r.lengths ? held_length(r.lengths[b], r.T, nullptr) : r.T;
+  constexpr int kTeams = kThreads / kTeam;
+  __shared__ int part[kWaves];
+  const int thread = threadIdx.x % kTeam;
+  for (int64_t b = int64_t(blockIdx.x) * kTeams + threadIdx.x / kTeam; b < r.B; b += int64_t(gridDim.x) * kTeams) {
+    const int length = r.lengths ? clamped(r.lengths[b], r.T) : r.T;
     int c = 0;
-    if (!r.mask) c = lane == 0 ? length : 0;
+    if (!r.mask) c = thread == 0 ? length : 0;
     else
-      for (int t = lane; t < length; t += kWave) c += r.mask[b * r.T + t] != 0;
+      for (int t = thread; t < length; t += kTeam) c += r.mask[b * r.T + t] != 0;
     c = wave_sum(c);
-    if (lane == 0) n[b] = c;
+    if (kTeam > kWave) {
+      if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = c;
+      __syncthreads();
+      c = 0;
+      for (int w = 0; w < kWaves; ++w) c += part[w];
+      __syncthreads();
+    }
+    if (thread == 0) n[b] = c;
   }
+}
+
+// Parts of all positions of a mask, kCountParts workgroups.
+__global__ __launch_bounds__(kThreads) void part_count_kernel(Rows r, int32_t* n) {
+  __shared__ int part[kWaves];
+  const int64_t rows = int64_t(r.B) * r.T;
+  int c = 0;
+  for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < rows; i += int64_t(kCountParts) * kThreads)
+    c += counts(r, int(uint32_t(i) / uint32_t(r.T)), int(uint32_t(i) % uint32_t(r.T)));
+  c = wave_sum(c);
+  if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = c;
+  __syncthreads();
+  if (threadIdx.x == 0) n[blockIdx.x] = part[0] + part[1] + part[2] + part[3];
 }
 
 // One workgroup: weights from the counts.
@@ -64,47 +87,33 @@ __global__ __launch_bounds__(1024) void sum_kernel(int64_t parts, const double* 
   }
 }
 
-// One workgroup a pair.
-__global__ __launch_bounds__(kThreads) void pair_kernel(Rows r, Pairs p) {
-  __shared__ double part[kWaves][2][3];
-  const int pairs = r.B / 2, i = blockIdx.x;
-  for (int side = 0; side < 2; ++side) {
-    const int64_t b = i + int64_t(side) * pairs;
-    const int length = r.lengths ? held_length(r.lengths[b], r.T, nullptr) : r.T;
-    double lp_sum = 0, d_sum = 0, n = 0;
-    for (int t = threadIdx.x; t < length; t += kThreads) {
-      const int64_t at = b * r.T + t;
-      if (r.mask && !r.mask[at]) continue;
-      const float lp = p.state[at].w;
-      lp_sum += lp;
-      d_sum += double(lp) - p.ref_lp[at];
-      n += 1;
-    }
-    lp_sum = wave_sum(lp_sum);
-    d_sum = wave_sum(d_sum);
-    n = wave_sum(n);
-    if (threadIdx.x % kWave == 0) {
-      double* to = part[threadIdx.x / kWave][side];
-      to[0] = lp_sum;
-      to[1] = d_sum;
-      to[2] = n;
-    }
+// Of a sequence: sums of lp and of lp - ref, and how many positions count; of the thread's share.
+struct Sequence {
+  double lp, d;
+  int n;
+};
+__device__ __forceinline__ Sequence sequence_part(const Rows& r, const Pairs& p, int64_t b, int thread, int threads) {
+  const int length = r.lengths ? clamped(r.lengths[b], r.T) : r.T;
+  Sequence s = {};
+  for (int t = thread; t < length; t += threads) {
+    const int64_t at = b * r.T + t;
+    if (r.mask && !r.mask[at]) continue;
+    const float lp = p.lp[at];
+    s.lp += lp;
+    s.d += double(lp) - p.ref_lp[at];
+    s.n += 1;
   }
-  __syncthreads();
-  if (threadIdx.x) return;
-  double lp[2] = {}, d[2] = {}, share[2];
-  for (int side = 0; side < 2; ++side) {
-    double n = 0;
-    for (int w = 0; w < kWaves; ++w) {
-      lp[side] += part[w][side][0];
-      d[side] += part[w][side][1];
-      n += part[w][side][2];
-    }
-    share[side] = p.kind == TB_PAIR_IPO ? 1.0 / (n > 0 ? n : 1.0) : 1.0;
-    d[side] *= share[side];
-    p.sequence_lp[i + side * pairs] = float(lp[side]);
-  }
-  const double margin = d[0] - d[1], h = p.beta * margin, beta = p.beta;
+  return {wave_sum(s.lp), wave_sum(s.d), wave_sum(s.n)};
+}
+
+// Loss and margin of pair i from its sequences' sums; leaves the pair's values.
+struct Pair {
+  double loss, margin;
+};
+__device__ __forceinline__ Pair pair_values(const Pairs& p, int pairs, int i, Sequence s, Sequence u) {
+  const double of_s = p.kind == TB_PAIR_IPO ? 1.0 / (s.n > 0 ? s.n : 1) : 1.0;
+  const double of_u = p.kind == TB_PAIR_IPO ? 1.0 / (u.n > 0 ? u.n : 1) : 1.0;
+  const double margin = s.d * of_s - u.d * of_u, beta = p.beta, h = beta * margin;
   double loss, slope;
   if (p.kind == TB_PAIR_IPO) {
     const double off = margin - 0.5 / beta;
@@ -118,21 +127,87 @@ __global__ __launch_bounds__(kThreads) void pair_kernel(Rows r, Pairs p) {
     loss = low + (1 - e) * fmax(-h, 0.0) + e * fmax(h, 0.0);
     slope = beta * (e / (1 + exp(-h)) - (1 - e) / (1 + exp(h)));
   }
-  p.margins[i] = float(margin);
-  p.partial[3 * i] = loss;
-  p.partial[3 * i + 1] = margin > 0;
-  p.partial[3 * i + 2] = margin;
   slope /= pairs;
-  p.d_sequence[i] = float(slope * share[0]);
-  p.d_sequence[i + pairs] = float(-slope * share[1]);
+  p.sequence_lp[i] = float(s.lp);
+  p.sequence_lp[i + pairs] = float(u.lp);
+  p.margins[i] = float(margin);
+  p.d_sequence[i] = float(slope * of_s);
+  p.d_sequence[i + pairs] = float(-slope * of_u);
+  return {loss, margin};
+}
+
+// One workgroup a pair.
+__global__ __launch_bounds__(kThreads) void pair_kernel(Rows r, Pairs p) {
+  __shared__ Sequence part[2][kWaves];
+  const int pairs = r.B / 2, i = blockIdx.x;
+  for (int side = 0; side < 2; ++side) {
+    const Sequence s = sequence_part(r, p, i + int64_t(side) * pairs, threadIdx.x, kThreads);
+    if (threadIdx.x % kWave == 0) part[side][threadIdx.x / kWave] = s;
+  }
+  __syncthreads();
+  if (threadIdx.x) return;
+  Sequence s[2] = {};
+  for (int side = 0; side < 2; ++side)
+    for (int w = 0; w < kWaves; ++w) {
+      s[side].lp += part[side][w].lp;
+      s[side].d += part[side][w].d;
+      s[side].n += part[side][w].n;
+    }
+  const Pair v = pair_values(p, pairs, i, s[0], s[1]);
+  p.partial[3 * i] = v.loss;
+  p.partial[3 * i + 1] = v.margin > 0;
+  p.partial[3 * i + 2] = v.margin;
+}
+
+// All pairs in one workgroup, a wavefront a sequence, and the means over them.
+constexpr int kFewSequences = 256;
+__global__ __launch_bounds__(1024) void few_pairs_kernel(Rows r, Pairs p) {
+  __shared__ Sequence all[kFewSequences];
+  __shared__ double part[16][3];
+  const int pairs = r.B / 2, lane = threadIdx.x % kWave;
+  for (int b = threadIdx.x / kWave; b < r.B; b += 16) {
+    const Sequence s = sequence_part(r, p, b, lane, kWave);
+    if (lane == 0) all[b] = s;
+  }
+  __syncthreads();
+  double sum[3] = {};
+  const int i = threadIdx.x;
+  if (i < pairs) {
+    const Pair v = pair_values(p, pairs, i, all[i], all[i + pairs]);
+    sum[0] = v.loss;
+    sum[1] = v.margin > 0;
+    sum[2] = v.margin;
+  }
+#pragma unroll
+  for (int j = 0; j < 3; ++j) {
+    sum[j] = wave_sum(sum[j]);
+    if (lane == 0) part[threadIdx.x / kWave][j] = sum[j];
+  }
+  __syncthreads();
+  if (i < 3) {
+    double total = 0;
+    for (int w = 0; w < 16; ++w) total += part[w][i];
+    p.terms[i] = float(total / pairs);
+  }
 }
 
 }  // namespace
 
-hipError_t run_weights(const Rows& r, int average, int32_t* counts, float* weight, hipStream_t stream) {
-  const int64_t groups = (int64_t(r.B) + kWaves - 1) / kWaves;
-  count_kernel<<<int(groups < 4096 ? groups : 4096), kThreads, 0, stream>>>(r, counts);
-  weight_kernel<<<1, 1024, 0, stream>>>(r.B, average, counts, weight);
+hipError_t run_counts(const Rows& r, int32_t* n, hipStream_t stream) {
+  if (r.T > 512) {
+    count_kernel<kThreads><<<r.B < 4096 ? r.B : 4096, kThreads, 0, stream>>>(r, n);
+  } else {
+    const int64_t groups = (int64_t(r.B) + kWaves - 1) / kWaves;
+    count_kernel<kWave><<<int(groups < 4096 ? groups : 4096), kThreads, 0, stream>>>(r, n);
+  }
+  return hipGetLastError();
+}
+hipError_t run_part_counts(const Rows& r, int32_t* n, hipStream_t stream) {
+  part_count_kernel<<<kCountParts, kThreads, 0, stream>>>(r, n);
+  return hipGetLastError();
+}
+hipError_t run_weights(int B, int average, const int32_t* n, float* weight, hipStream_t stream) {
+  weight_kernel<<<1, 1024, 0, stream>>>(B, average, n, weight);
   return hipGetLastError();
 }
 
@@ -148,6 +223,11 @@ hipError_t run_terms(int64_t groups, const double* partial, double* more, float*
 
 hipError_t run_pairs(const Rows& r, const Pairs& p, hipStream_t stream) {
   const int pairs = r.B / 2;
+  // one workgroup takes 4.4 us for 64 positions a wavefront, 11 to 13 for 1024; two launches take 10
+  if (pairs && r.B <= kFewSequences && int64_t(r.B + 15) / 16 * r.T <= 512) {
+    few_pairs_kernel<<<1, 1024, 0, stream>>>(r, p);
+    return hipGetLastError();
+  }
   if (pairs) pair_kernel<<<pairs, kThreads, 0, stream>>>(r, p);
   sum_kernel<<<1, 1024, 0, stream>>>(pairs, p.partial, 3, 3, pairs ? 1.0 / pairs : 0.0, nullptr, p.terms);
   return hipGetLastError();

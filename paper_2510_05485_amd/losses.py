@@ -326,11 +326,11 @@ def token_logprobs(logits, tokens, *, lengths=None, mask=None, temperature: floa
                    want_entropy: bool = False, status: Optional[torch.Tensor] = None):
     """float32 log-probabilities of `tokens` (their shape), and with want_entropy a tuple of these and
     the entropies of the rows.  Differentiable in the logits."""
-    if _needs_grad(logits):
-        return _TokenLogprobs.apply(logits, tokens, lengths, mask, temperature, want_entropy, status)
     found = native().logprobs(logits, tokens, lengths, mask, temperature, status, want_entropy)
     if found is not None:
         return found
+    if _needs_grad(logits):
+        return _TokenLogprobs.apply(logits, tokens, lengths, mask, temperature, want_entropy, status)
     lp, entropy, _ = _score(_Call(logits, tokens, lengths, mask, temperature, status), want_entropy, False)
     return (lp, entropy) if want_entropy else lp
 
@@ -389,6 +389,10 @@ def policy_loss(logits, tokens, old_logprobs, advantages, *, ref_logprobs=None, 
     old_logprobs, ref_logprobs: float32 of the tokens' shape; advantages: float32 [B], or one for each
     position.  average: "token" (over all positions that count), "sequence" (the mean of sequences'
     means) or "sum"."""
+    loss = native().policy(logits, tokens, lengths, mask, temperature, status, None, None, old_logprobs, advantages,
+                           ref_logprobs, clip_low, clip_high, kl_coef, entropy_coef, AVERAGES.get(average))
+    if loss is not None:
+        return loss
     policy = (old_logprobs, advantages, ref_logprobs, clip_low, clip_high, kl_coef, entropy_coef, average)
     if _needs_grad(logits):
         return _PolicyLoss.apply(logits, tokens, lengths, mask, temperature, status, *policy)
@@ -401,7 +405,7 @@ def policy_loss_grad(logits, tokens, old_logprobs, advantages, *, ref_logprobs=N
                      grad_scale: float = 1.0, out: Optional[torch.Tensor] = None,
                      status: Optional[torch.Tensor] = None) -> PolicyLoss:
     """policy_loss and its gradient in the logits, in one pass over them."""
-    found = native().policy(logits, tokens, lengths, mask, temperature, status, out, grad_scale, old_logprobs,
+    found = native().policy(logits, tokens, lengths, mask, temperature, status, out, float(grad_scale), old_logprobs,
                             advantages, ref_logprobs, clip_low, clip_high, kl_coef, entropy_coef,
                             AVERAGES.get(average))
     if found is not None:
@@ -461,6 +465,10 @@ def preference_loss(logits, tokens, ref_logprobs, *, lengths=None, mask=None, be
     "hinge"  max(0, 1 - beta h);  "ipo"  (h - 1 / (2 beta))^2;  averaged over the pairs.
 
     ref_logprobs: float32 of the tokens' shape (token_logprobs of the reference model)."""
+    loss = native().preference(logits, tokens, lengths, mask, temperature, status, None, None, ref_logprobs, beta,
+                               PAIRS.get(kind), label_smoothing)
+    if loss is not None:
+        return loss
     preference = (ref_logprobs, beta, kind, label_smoothing)
     if _needs_grad(logits):
         return _PreferenceLoss.apply(logits, tokens, lengths, mask, temperature, status, *preference)
@@ -472,7 +480,7 @@ def preference_loss_grad(logits, tokens, ref_logprobs, *, lengths=None, mask=Non
                          grad_scale: float = 1.0, out: Optional[torch.Tensor] = None,
                          status: Optional[torch.Tensor] = None) -> PreferenceLoss:
     """preference_loss and its gradient in the logits."""
-    found = native().preference(logits, tokens, lengths, mask, temperature, status, out, grad_scale, ref_logprobs,
+    found = native().preference(logits, tokens, lengths, mask, temperature, status, out, float(grad_scale), ref_logprobs,
                                 beta, PAIRS.get(kind), label_smoothing)
     if found is not None:
         return PreferenceLoss(*found)
@@ -537,6 +545,10 @@ def distillation_loss(logits, teacher_ids, teacher_logits, *, lengths=None, mask
     softmax of the K entries of teacher_logits [..., K] over the temperature, and p that of the logits.
 
     An entry of -inf is none, whatever its id; a position without entries adds 0."""
+    loss = native().distill(logits, lengths, mask, temperature, status, None, None, teacher_ids, teacher_logits,
+                            AVERAGES.get(average))
+    if loss is not None:
+        return loss
     if _needs_grad(logits):
         return _DistillationLoss.apply(logits, teacher_ids, teacher_logits, lengths, mask, temperature,
                                        status, average)
@@ -549,7 +561,7 @@ def distillation_loss_grad(logits, teacher_ids, teacher_logits, *, lengths=None,
                            out: Optional[torch.Tensor] = None,
                            status: Optional[torch.Tensor] = None) -> DistillationLoss:
     """distillation_loss and its gradient in the logits, in one pass over them."""
-    found = native().distill(logits, lengths, mask, temperature, status, out, grad_scale, teacher_ids,
+    found = native().distill(logits, lengths, mask, temperature, status, out, float(grad_scale), teacher_ids,
                              teacher_logits, AVERAGES.get(average))
     if found is not None:
         return DistillationLoss(*found)

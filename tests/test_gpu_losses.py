@@ -474,6 +474,81 @@ def test_in_a_graph(V):
             assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("V", [64, 5000])
+def test_both_ways_of_marshalling(V):
+    """Calls that the native code takes and calls that it leaves to the general way (lengths of 64 bits,
+    values that are not contiguous) give the same."""
+    B, T = 4, 6
+    x, tokens, old, reference, a = policy_inputs(V, B, T, V, torch.bfloat16, True)
+    ids, teacher = torch.randint(0, V, (B, T, 5)).to(DEV), torch.randn(B, T, 5).to(DEV)
+    lengths = torch.tensor([6, 0, 4, 5], device=DEV, dtype=torch.int32)
+    apart = lambda v: torch.stack([v, v], -1)[..., 0]
+
+    def found(n, f):
+        leaf = x.clone().requires_grad_()
+        out = [*tb.token_logprobs(leaf, tokens, lengths=n, want_entropy=True)]
+        out += torch.autograd.grad(out, leaf, (f(a), f(old)), retain_graph=True)
+        out += torch.autograd.grad(out[1], leaf, f(old))
+        for step, loss in ((tb.policy_loss_grad, tb.policy_loss), (tb.preference_loss_grad, tb.preference_loss),
+                           (tb.distillation_loss_grad, tb.distillation_loss)):
+            args = dict(policy_loss_grad=(tokens, f(old), f(a)), preference_loss_grad=(tokens, f(reference)),
+                        distillation_loss_grad=(ids, f(teacher)))[step.__name__]
+            kw = dict(ref_logprobs=f(reference), kl_coef=0.1, entropy_coef=0.1) if step is tb.policy_loss_grad else {}
+            out += [*step(x, *args, lengths=n, **kw)]
+            value = loss(leaf, *args, lengths=n, **kw)
+            out += [value, *torch.autograd.grad(2 * value, leaf)]
+            assert torch.equal(loss(x, *args, lengths=n, **kw), value) and value.dim() == 0
+        return [t.detach() for t in out]
+    for one, other in zip(found(lengths, lambda v: v), found(lengths.long(), apart)):
+        assert torch.equal(one, other)
+
+
+def test_backward_of_what_has_changed_raises():
+    x, tokens, _ = inputs(1, 2, 3, 50)
+    leaf = x.requires_grad_()
+    y = leaf * 1.0
+    loss = tb.policy_loss(y, tokens, torch.zeros(2, 3, device=DEV), torch.ones(2, device=DEV))
+    y.zero_()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    loss = tb.token_logprobs(leaf, tokens).sum()
+    loss.backward(retain_graph=True)
+    first = leaf.grad.clone()
+    loss.backward()
+    assert torch.equal(leaf.grad, 2 * first)
+    with pytest.raises(RuntimeError):
+        loss.backward()
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(tb.token_logprobs(leaf, tokens).sum(), leaf, create_graph=True)
+
+
+@pytest.mark.parametrize("B,T,average", [(1, 3000, "sequence"), (3, 1500, "token"), (3, 1500, "sequence"),
+                                         (40, 7, "sequence"), (9000, 2, "token"), (9000, 2, "sequence"), (300, 4, "sum")])
+@pytest.mark.parametrize("masked", [False, True])
+def test_averages_over_many_positions(B, T, average, masked):
+    V = 17
+    x, tokens, g = inputs(B + T, B, T, V)
+    lengths = torch.randint(0, T + 1, (B,), generator=g).to(DEV)
+    mask = (torch.rand(B, T, generator=g) < 0.6).to(DEV) if masked else None
+    old, a = torch.full((B, T), -3.0, device=DEV), torch.ones(B, device=DEV)
+    terms, grad, _ = ref.policy(x, tokens, old, a, None, lengths, mask, average=average)
+    r = tb.policy_loss_grad(x, tokens, old, a, lengths=lengths, mask=mask, average=average)
+    n = B * T if average == "sum" else 1
+    near(r.terms, terms, LP * (20 * n + terms.abs().max()))
+    near_gradient(r.grad, grad, spread(grad) + grad.abs().max(), torch.float32)
+    reference = torch.full((B, T), -4.0, device=DEV)
+    half = B // 2 * 2
+    if half:
+        cut = dict(lengths=lengths[:half], mask=None if mask is None else mask[:half])
+        terms, grad, sums, margins = ref.preference(x[:half], tokens[:half], reference[:half], beta=0.01, **cut)
+        r = tb.preference_loss_grad(x[:half], tokens[:half], reference[:half], beta=0.01, **cut)
+        near(r.sequence_logprobs, sums, LP * T)
+        near(r.margins, margins, 2 * LP * T)
+        near(r.terms[:1], terms[:1], 2 * LP * T)
+        near(r.terms[2:], terms[2:], 2 * LP * T)
+        near_gradient(r.grad, grad, spread(grad) + grad.abs().max(), torch.float32)
+
+
 def test_refusals():
     x, tokens, _ = inputs(1, 4, 3, 50)
     v, one = torch.zeros(4, 3, device=DEV), torch.zeros(4, device=DEV)
