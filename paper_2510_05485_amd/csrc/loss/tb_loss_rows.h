@@ -150,10 +150,11 @@ __device__ __forceinline__ Stats joined_lanes(const Stats& mine, Join join) {
 // The part of a row that a lane of kLanes holds; what lies beyond the row is -inf.
 template <typename X, int kLanes, int kChunks>
 struct Part {
-  static constexpr int kEdges = (kEdge<X> + kLanes - 1) / kLanes;
+  using Row = Span<X, 16>;
+  static constexpr int kEdges = (Row::kEdge + kLanes - 1) / kLanes;
   u32x4 c[kChunks];
   float e[kEdges];
-  __device__ __forceinline__ void load(const Span<X>& row, int lane, bool live) {
+  __device__ __forceinline__ void load(const Row& row, int lane, bool live) {
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
       c[k] = u32x4{X::kNone, X::kNone, X::kNone, X::kNone};
@@ -198,7 +199,7 @@ __device__ __forceinline__ Stats part_stats(const Part<X, kLanes, kChunks>& p, f
 
 // Writes the gradient, zeros where `live` is false.
 template <bool kEntropy, int kLanes, typename X, int kChunks>
-__device__ __forceinline__ void write_part(const Span<X>& row, const Part<X, kLanes, kChunks>& p, typename X::type* g,
+__device__ __forceinline__ void write_part(const Span<X, 16>& row, const Part<X, kLanes, kChunks>& p, typename X::type* g,
                                            int lane, bool live, float m, float k, Slope f) {
 #pragma unroll
   for (int j = 0; j < kChunks; ++j) {
@@ -243,7 +244,7 @@ __global__ __launch_bounds__(kLaneThreads) void lanes_kernel(Rows r, RowOut o, P
     const int b = int(uint32_t(at) / uint32_t(r.T)), t = int(uint32_t(at) % uint32_t(r.T));
     if (kOp != kGiven && lane == 0 && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
     const bool live = counts(r, b, t);
-    const Span<X> row(row_of<X>(r, b, t), r.V);
+    const Span<X, 16> row(row_of<X>(r, b, t), r.V);
     Part<X, kLanes, kChunks> part;
     part.load(row, lane, live);
     Slope f = {};
@@ -309,8 +310,8 @@ __global__ __launch_bounds__(kLaneThreads) void lanes_kernel(Rows r, RowOut o, P
 
 // Statistics of a row, in every thread.  Reads the row once.
 // (kThreads: threads of the workgroup, or of the wavefront that has the row to itself; 0: blockDim.x)
-template <typename X, bool kEntropy, int kThreads = 0>
-__device__ __forceinline__ Stats row_stats(const Span<X>& row, float k, int thread, Stats* parts) {
+template <typename X, bool kEntropy, int kThreads = 0, typename Row>
+__device__ __forceinline__ Stats row_stats(const Row& row, float k, int thread, Stats* parts) {
   const int threads = kThreads ? kThreads : blockDim.x;
   Stats mine = {kLowest, 0.f, 0.f};
   auto take = [&](const float* v, int n) {
@@ -335,8 +336,9 @@ __device__ __forceinline__ Stats row_stats(const Span<X>& row, float k, int thre
     X::unpack(row.chunk(c), v);
     take(v, X::kPer);
   }
-  const int e = row.edge(thread);
-  if (e >= 0) {
+  for (int j = thread; j < row.kEdge; j += threads) {
+    const int e = row.edge(j);
+    if (e < 0) break;
     const float v[X::kPer] = {X::load(row.x + e)};
     take(v, 1);
   }
@@ -350,33 +352,39 @@ __device__ __forceinline__ Stats row_stats(const Span<X>& row, float k, int thre
 }
 
 // The gradient of a row, but for the additions at the token.
-template <typename X, bool kEntropy, int kThreads = 0>
-__device__ __forceinline__ void write_gradient(const Span<X>& row, typename X::type* g, int thread, float m, float k,
+template <typename X, bool kEntropy, int kThreads = 0, typename Row>
+__device__ __forceinline__ void write_gradient(const Row& row, typename X::type* g, int thread, float m, float k,
                                                Slope f) {
-  for (int c = thread; c < row.chunks; c += kThreads ? kThreads : blockDim.x) {
+  const int threads = kThreads ? kThreads : blockDim.x;
+  for (int c = thread; c < row.chunks; c += threads) {
     float v[X::kPer];
     X::unpack(row.chunk(c), v);
 #pragma unroll
     for (int i = 0; i < X::kPer; ++i) v[i] = gradient_at<kEntropy>((v[i] - m) * k, f);
     *reinterpret_cast<u32x4_any*>(g + row.at(c)) = X::pack(v);
   }
-  const int e = row.edge(thread);
-  if (e >= 0) X::store(g + e, gradient_at<kEntropy>((X::load(row.x + e) - m) * k, f));
+  for (int j = thread; j < row.kEdge; j += threads) {
+    const int e = row.edge(j);
+    if (e >= 0) X::store(g + e, gradient_at<kEntropy>((X::load(row.x + e) - m) * k, f));
+  }
 }
 
+// Zeros for a gradient's row.
 template <typename X>
-__device__ __forceinline__ void write_zeros(const Rows& r, int b, int t) {
-  const Span<X> row(gradient_of<X>(r, b, t), r.V);
+__device__ __forceinline__ void write_zeros(const Rows& r, int b, int t, int thread, int threads) {
   typename X::type* g = gradient_of<X>(r, b, t);
-  for (int c = threadIdx.x; c < row.chunks; c += blockDim.x) *reinterpret_cast<u32x4*>(g + row.at(c)) = u32x4{};
-  const int e = row.edge(threadIdx.x);
-  if (e >= 0) X::store(g + e, 0.f);
+  const Line<X> row(g, r.V);
+  for (int c = thread; c < row.chunks; c += threads) *reinterpret_cast<u32x4*>(g + row.at(c)) = u32x4{};
+  for (int j = thread; j < row.kEdge; j += threads) {
+    const int e = row.edge(j);
+    if (e >= 0) X::store(g + e, 0.f);
+  }
 }
 
 // The token's value, added where its owner has just stored the rest (stores of one thread to one
 // address keep their order).
 template <typename X, bool kEntropy>
-__device__ __forceinline__ void add_token(const Span<X>& row, typename X::type* g, int token, float x, float m,
+__device__ __forceinline__ void add_token(const Line<X>& row, typename X::type* g, int token, float x, float m,
                                           float k, Slope f) {
   if (row.owner(token, blockDim.x) == int(threadIdx.x))
     X::store(g + token, f.token + gradient_at<kEntropy>((x - m) * k, f));
@@ -412,7 +420,7 @@ __device__ __forceinline__ float block_max(float v, float* part) {
 
 // Fills `e`; the sum of exponentials: 0 for a row without entries, NaN for one with a wrong id.
 template <typename X>
-__device__ __forceinline__ float take_entries(const Rows& r, const Span<X>& row, const Teacher& q, int64_t at, float k,
+__device__ __forceinline__ float take_entries(const Rows& r, const Line<X>& row, const Teacher& q, int64_t at, float k,
                                               Entries& e) {
   float top = kLowest;
   for (int j = threadIdx.x; j < q.K; j += blockDim.x) {
@@ -448,7 +456,7 @@ __device__ __forceinline__ float take_entries(const Rows& r, const Span<X>& row,
 
 // The gradient at the teacher's entries, behind a barrier after everything else is stored.
 template <typename X>
-__device__ __forceinline__ void add_entries(const Span<X>& row, typename X::type* g, const Teacher& q,
+__device__ __forceinline__ void add_entries(const Line<X>& row, typename X::type* g, const Teacher& q,
                                             const Entries& e, float m, float k, Slope f) {
   for (int j = threadIdx.x; j < q.K; j += blockDim.x) {
     const int id = e.id[j];
@@ -461,10 +469,10 @@ __device__ __forceinline__ void add_entries(const Span<X>& row, typename X::type
 
 // The gradient of a row's divergence; m, s: the row's statistics, sum: of take_entries, w: cotangent.
 template <typename X>
-__device__ __forceinline__ void write_distilled(const Rows& r, const Span<X>& row, const Teacher& q, const Entries& e,
+__device__ __forceinline__ void write_distilled(const Rows& r, const Line<X>& row, const Teacher& q, const Entries& e,
                                                 int b, int t, float m, float s, float sum, float w, float k) {
   if (sum == 0.f) {
-    write_zeros<X>(r, b, t);
+    write_zeros<X>(r, b, t, threadIdx.x, blockDim.x);
     return;
   }
   typename X::type* g = gradient_of<X>(r, b, t);
@@ -491,7 +499,7 @@ template <typename X, int kOp, bool kEntropy>
 __device__ __forceinline__ float4 sweep_row(const Rows& r, const RowOut& o, const Policy& p, const Teacher& q, float w,
                                             int b, int t, int64_t at, Shared<kOp>& shared) {
   const bool first = threadIdx.x == 0;
-  const Span<X> row(row_of<X>(r, b, t), r.V);
+  const Line<X> row(row_of<X>(r, b, t), r.V);
   const float k = r.inv_temp * kLog2e;
   if constexpr (kOp != kDistill) {
     const int token = take_token(r, b, t, first);
@@ -561,7 +569,7 @@ __global__ __launch_bounds__(512) void sweep_kernel(Rows r, RowOut o, Policy p, 
       sum[3] += double(w) * v.w;
     } else {
       if (threadIdx.x == 0) leave_nothing(o, at);
-      if (r.g) write_zeros<X>(r, b, t);
+      if (r.g) write_zeros<X>(r, b, t, threadIdx.x, blockDim.x);
     }
     __syncthreads();  // (before the next row takes the shared memory)
   }
@@ -573,7 +581,7 @@ __global__ __launch_bounds__(512) void sweep_kernel(Rows r, RowOut o, Policy p, 
 template <typename X, int kOp, bool kEntropy>
 __device__ __forceinline__ void given_row(const Rows& r, const Given& v, const Teacher& q, int b, int t, int64_t at,
                                           Shared<kOp>& shared) {
-  const Span<X> row(row_of<X>(r, b, t), r.V);
+  const Line<X> row(row_of<X>(r, b, t), r.V);
   const float k = r.inv_temp * kLog2e, up = v.upstream ? *v.upstream : 1.f;
   const float4 state = v.state[at];
   const float d = v.d_lp[b * v.d_seq + t * v.d_pos] * up;
@@ -600,7 +608,7 @@ __global__ __launch_bounds__(512) void gradient_kernel(Rows r, Given v, Teacher 
     const int64_t at = row_of_group(i, rows);
     const int b = int(uint32_t(at) / uint32_t(r.T)), t = int(uint32_t(at) % uint32_t(r.T));
     if (counts(r, b, t)) given_row<X, kOp, kEntropy>(r, v, q, b, t, at, shared);
-    else write_zeros<X>(r, b, t);
+    else write_zeros<X>(r, b, t, threadIdx.x, blockDim.x);
     __syncthreads();
   }
 }
@@ -609,26 +617,31 @@ __global__ __launch_bounds__(512) void gradient_kernel(Rows r, Given v, Teacher 
 
 constexpr int kHeldThreads = 512;
 
-// A row's chunks in registers of kThreads threads, kChunks each: chunk k * kThreads + thread.  All but the
-// last are there in every thread; what lies beyond the row is -inf.
+// A row's chunks in registers of kThreads threads, kChunks each: chunk k * kThreads + thread.  With
+// kChunks = V / kPer / kThreads rounded up, all but the last two are there in every thread (the row's head
+// takes up to eight chunks from the last but one); what lies beyond the row is -inf.
 template <typename X, int kThreads, int kChunks>
 struct Held {
+  // (a wavefront's lanes would have two values of head and rest each if it read whole lines)
+  using Row = Span<X, kThreads == kWave ? 16 : kLine>;
+  static_assert(Row::kEdge <= kThreads);
+  static constexpr int kSure = kChunks - 2;
   u32x4 c[kChunks];
   float edge;
   int edge_at;
-  __device__ __forceinline__ void load(const Span<X>& row, int thread) {
+  __device__ __forceinline__ void load(const Row& row, int thread) {
     const char* from = reinterpret_cast<const char*>(row.x + row.head);
     const uint32_t lane = thread * 16u;
 #pragma unroll
-    for (int k = 0; k < kChunks - 1; ++k)
-      c[k] = *reinterpret_cast<const u32x4*>(from + k * (kThreads * 16) + lane);
-    c[kChunks - 1] = u32x4{X::kNone, X::kNone, X::kNone, X::kNone};
-    if (last(row, thread)) c[kChunks - 1] = *reinterpret_cast<const u32x4*>(from + (kChunks - 1) * (kThreads * 16) + lane);
+    for (int k = 0; k < kChunks; ++k) {
+      if (k >= kSure) c[k] = u32x4{X::kNone, X::kNone, X::kNone, X::kNone};
+      if (k < kSure || there(row, thread, k)) c[k] = *reinterpret_cast<const u32x4*>(from + k * (kThreads * 16) + lane);
+    }
     edge_at = row.edge(thread);
     edge = edge_at >= 0 ? X::load(row.x + edge_at) : -INFINITY;
   }
-  __device__ __forceinline__ bool last(const Span<X>& row, int thread) const {
-    return thread + (kChunks - 1) * kThreads < row.chunks;
+  static __device__ __forceinline__ bool there(const Row& row, int thread, int k) {
+    return thread + k * kThreads < row.chunks;
   }
   // Keeps the compiler from holding the values that it has unpacked until they are used again, which
   // would take twice the registers of the row itself.
@@ -686,7 +699,7 @@ __device__ __forceinline__ Stats wave_stats(Held<X, kThreads, kChunks>& h, float
 }
 
 template <bool kEntropy, typename X, int kThreads, int kChunks>
-__device__ __forceinline__ void write_held(const Span<X>& row, const Held<X, kThreads, kChunks>& h,
+__device__ __forceinline__ void write_held(const typename Held<X, kThreads, kChunks>::Row& row, const Held<X, kThreads, kChunks>& h,
                                            typename X::type* g, int thread, float m, float k, Slope f) {
   const float M = scaled(m, k);
   char* to = reinterpret_cast<char*>(g + row.head);
@@ -698,7 +711,7 @@ __device__ __forceinline__ void write_held(const Span<X>& row, const Held<X, kTh
     X::unpack(h.c[j], v);
 #pragma unroll
     for (int i = 0; i < X::kPer; ++i) v[i] = value(v[i]);
-    if (j < kChunks - 1 || h.last(row, thread))
+    if (j < h.kSure || h.there(row, thread, j))
       *reinterpret_cast<u32x4_any*>(to + j * (kThreads * 16) + lane) = X::pack(v);
   }
   if (h.edge_at >= 0) X::store(g + h.edge_at, value(h.edge));
@@ -725,10 +738,10 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Po
   if (!counts(r, b, t)) {
     if (first) leave_nothing(o, at);
     if (kOp == kPolicy && threadIdx.x < 4) o.partial[int64_t(blockIdx.x) * 4 + threadIdx.x] = 0.0;
-    if (r.g) write_zeros<X>(r, b, t);
+    if (r.g) write_zeros<X>(r, b, t, threadIdx.x, blockDim.x);
     return;
   }
-  const Span<X> row(row_of<X>(r, b, t), r.V);
+  const Line<X> row(row_of<X>(r, b, t), r.V);
   // (what comes first is waited for first: not behind the whole row)
   const int token = take_token(r, b, t, first), share = kOp == kPolicy ? share_of_total(r, mean) : 0;
   Held<X, kHeldThreads, kChunks> h;
@@ -831,18 +844,14 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
     if (first && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
     typename X::type* g = r.g ? gradient_of<X>(r, b, t) : nullptr;
     auto zeros = [&] {
-      if (!g) return;
-      const Span<X> row(g, r.V);
-      for (int c = thread; c < row.chunks; c += kThreads) *reinterpret_cast<u32x4*>(g + row.at(c)) = u32x4{};
-      const int e = row.edge(thread);
-      if (e >= 0) X::store(g + e, 0.f);
+      if (g) write_zeros<X>(r, b, t, thread, kThreads);
     };
     if (!counts(r, b, t)) {
       if (first) leave_nothing(o, at);
       zeros();
       continue;
     }
-    const Span<X> row(row_of<X>(r, b, t), r.V);
+    const typename Held<X, kThreads, kChunks>::Row row(row_of<X>(r, b, t), r.V);
     // (what comes first is waited for first: not behind the whole row)
     float v[kEntries], x[kEntries];
     int64_t wide[kEntries];
