@@ -31,9 +31,16 @@ struct Rows {
   const uint8_t* mask;
   int32_t* status;
   int B, T, V;
+  uint32_t t_magic, t_shift;  // of the division by T
   int long_tokens;
   float inv_temp;
   float g_scale;
+};
+
+// Positions are numbered b T + t.  n / T = (umulhi(n, magic) + n) >> shift for n < 2^31 with shift =
+// ceil(log2 T) and magic = floor(2^32 (2^shift - T) / T) + 1 (Granlund and Montgomery 1994).
+struct At {
+  int b, t;
 };
 
 struct RowOut {  // per position, any may be null
@@ -75,6 +82,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_any __attribute__((aligned(2)));  // a 16-byte access at any address of a value
 
 struct F32 {
+  template <int kFirst>
+  static __device__ __forceinline__ float upper(const u32x4* c);  // of the first kFirst chunks
   static constexpr uint32_t kNone = 0xFF800000u;  // -inf
   using type = float;
   static constexpr int kPer = 4;  // values of a chunk
@@ -96,6 +105,8 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 struct BF16 {
+  template <int kFirst>
+  static __device__ __forceinline__ float upper(const u32x4* c);  // of the first kFirst chunks
   static constexpr uint32_t kNone = 0xFF80FF80u;  // -inf
   using type = uint16_t;
   static constexpr int kPer = 8;
@@ -125,6 +136,8 @@ struct BF16 {
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 struct F16 {
+  template <int kFirst>
+  static __device__ __forceinline__ float upper(const u32x4* c);  // of the first kFirst chunks
   static constexpr uint32_t kNone = 0xFC00FC00u;  // -inf
   using type = _Float16;
   static constexpr int kPer = 8;
@@ -152,6 +165,54 @@ struct F16 {
     return c;
   }
 };
+
+// The largest of three; instruction and all, since the compiler would first quiet signalling NaNs, one
+// instruction a value (such a value makes the row NaN in any case).
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
+// The largest of packed values, as signed integers that order values from 0 on like the values themselves
+// and any of them behind those below 0 (which come the other way round).
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+template <int kFirst>
+__device__ __forceinline__ i16x2 upper_pair(const u32x4* c) {
+  i16x2 top = {-32768, -32768};
+#pragma unroll
+  for (int k = 0; k < kFirst; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t u = c[k][i];
+      i16x2 v;
+      __builtin_memcpy(&v, &u, 4);
+      top = __builtin_elementwise_max(top, v);
+    }
+  return top;
+}
+template <int kFirst>
+__device__ __forceinline__ float F32::upper(const u32x4* c) {
+  int top = INT32_MIN;
+#pragma unroll
+  for (int k = 0; k < kFirst; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = max(top, int(c[k][i]));
+  return __int_as_float(top);
+}
+template <int kFirst>
+__device__ __forceinline__ float BF16::upper(const u32x4* c) {
+  const i16x2 top = upper_pair<kFirst>(c);
+  return __uint_as_float(uint32_t(uint16_t(max(top[0], top[1]))) << 16);
+}
+template <int kFirst>
+__device__ __forceinline__ float F16::upper(const u32x4* c) {
+  const i16x2 top = upper_pair<kFirst>(c);
+  const short most = max(top[0], top[1]);
+  _Float16 h;
+  __builtin_memcpy(&h, &most, 2);
+  return float(h);
+}
 
 // 2^x; the hardware's instruction is within one unit in the last place, and gives 0 below 2^-126 (a
 // probability that no type of gradient holds beside one of its row's others)
@@ -210,6 +271,10 @@ __device__ __forceinline__ int held_length(int length, int T, int32_t* status) {
   if (status) atomicOr(status, TB_DEV_LENGTH_RANGE);
   return length < 0 ? 0 : T;
 }
+__device__ __forceinline__ At position(const Rows& r, int64_t at) {
+  const uint32_t n = uint32_t(at), b = (__umulhi(n, r.t_magic) + n) >> r.t_shift;
+  return {int(b), int(n - b * uint32_t(r.T))};
+}
 __device__ __forceinline__ int clamped(int length, int T) { return min(max(length, 0), T); }
 __device__ __forceinline__ bool counts(const Rows& r, int b, int t) {
   if (r.lengths && t >= r.lengths[b]) return false;
@@ -228,6 +293,45 @@ __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int d = kWave / 2; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
   return v;
+}
+
+// Sum over a wavefront, all lanes active: two butterflies' worth of steps inside rows of 16 lanes, then
+// each row's into the next ones'; the last lane has all of it.
+template <int kCtrl, int kRows = 0xf>
+__device__ __forceinline__ float dpp_or(float old, float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(v), kCtrl, kRows, 0xf, false));
+}
+__device__ __forceinline__ float last_lane(float v) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), kWave - 1));
+}
+__device__ __forceinline__ float full_wave_sum(float v) {
+  v += dpp_or<0xB1>(0.f, v);          // quad_perm [1, 0, 3, 2]
+  v += dpp_or<0x4E>(0.f, v);          // quad_perm [2, 3, 0, 1]
+  v += dpp_or<0x141>(0.f, v);         // row_half_mirror
+  v += dpp_or<0x140>(0.f, v);         // row_mirror
+  v += dpp_or<0x142, 0xa>(0.f, v);    // row_bcast:15 into rows 1 and 3
+  v += dpp_or<0x143, 0xc>(0.f, v);    // row_bcast:31 into rows 2 and 3
+  return last_lane(v);
+}
+__device__ __forceinline__ float full_wave_max(float v) {
+  v = fmaxf(v, dpp_or<0xB1>(v, v));
+  v = fmaxf(v, dpp_or<0x4E>(v, v));
+  v = fmaxf(v, dpp_or<0x141>(v, v));
+  v = fmaxf(v, dpp_or<0x140>(v, v));
+  v = fmaxf(v, dpp_or<0x142, 0xa>(v, v));
+  v = fmaxf(v, dpp_or<0x143, 0xc>(v, v));
+  return last_lane(v);
+}
+// Sum of 32-bit integers over a wavefront, all lanes active.
+__device__ __forceinline__ int full_wave_sum(int v) {
+  auto step = [](int a, int b) { return a + b; };
+  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, false));
+  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, false));
+  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x141, 0xf, 0xf, false));
+  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x140, 0xf, 0xf, false));
+  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false));
+  v = step(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(v, kWave - 1);
 }
 
 // Softmax statistics of a part of a row, of a = (x - m) k with k = log2(e) / temperature: the largest

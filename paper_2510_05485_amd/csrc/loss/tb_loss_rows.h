@@ -18,6 +18,24 @@ constexpr uint32_t kNan = 0x7FC00000u;
 
 // ---- what all kernels do for a row ------------------------------------------------------------
 
+// M = m k of the weights 2^(x k - M): rounded, and the same wherever it is formed (the compiler must
+// not take the product into a fused multiply-add, whose M would be another one).
+__device__ __forceinline__ float scaled(float m, float k) {
+#pragma clang fp contract(off)
+  return m * k;
+}
+// Kernels that form weights as 2^((x - m) k) have sums that differ from those of 2^(x k - M) by a factor
+// that rounds M; the state of a row that is kept for the backward pass is of the latter, where M can be
+// formed at all.
+__device__ __forceinline__ float to_scaled(float m, float k) {
+  return fabsf(m) < kExtreme ? exp2_fast(fmaf(m, k, -scaled(m, k))) : 1.f;
+}
+__device__ __forceinline__ float from_scaled(float m, float k) {
+  return fabsf(m) < kExtreme ? exp2_fast(-fmaf(m, k, -scaled(m, k))) : 1.f;
+}
+// 1 / x, to 1 unit in the last place
+__device__ __forceinline__ float reciprocal(float x) { return __builtin_amdgcn_rcpf(x); }
+
 // What the gradient of a row is made of: values 2^a (by_weight + by_log a), a = (x - m) k, and `token`
 // more at the row's token.
 struct Slope {
@@ -26,7 +44,7 @@ struct Slope {
 
 // from the cotangents of lp and H
 __device__ __forceinline__ Slope slope_of(float s, float H, float d_lp, float d_H, float scale) {
-  const float f = scale / s;
+  const float f = scale * reciprocal(s);
   return {f * (-d_lp - d_H * (H - logf(s))), -f * d_H * kLn2, scale * d_lp};
 }
 template <bool kEntropy>
@@ -110,7 +128,7 @@ __device__ __forceinline__ float weight_of(const Rows& r, const Mean& mean, int 
   if (mean.average == TB_SUM) return 1.f;
   if (!mean.n && !r.lengths) total = mean.average == TB_MEAN_TOKENS ? r.B * r.T : r.B;
   if (mean.average == TB_MEAN_TOKENS) return 1.f / float(total);
-  return 1.f / (float(total) * float(positions_of(r, mean, b)));
+  return reciprocal(float(total) * float(positions_of(r, mean, b)));
 }
 
 // Which row a workgroup takes: neighbouring workgroups go to different XCDs, neighbouring rows to one.
@@ -154,16 +172,22 @@ struct Part {
   static constexpr int kEdges = (Row::kEdge + kLanes - 1) / kLanes;
   u32x4 c[kChunks];
   float e[kEdges];
+  bool ragged;  // some row of the wavefront has a head or a rest
   __device__ __forceinline__ void load(const Row& row, int lane, bool live) {
+    ragged = __any(row.head != 0 || row.at(row.chunks) != row.V);
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
       c[k] = u32x4{X::kNone, X::kNone, X::kNone, X::kNone};
       if (live && lane + k * kLanes < row.chunks) c[k] = row.chunk(lane + k * kLanes);
     }
 #pragma unroll
-    for (int j = 0; j < kEdges; ++j) {
-      const int i = row.edge(lane + j * kLanes);
-      e[j] = live && i >= 0 ? X::load(row.x + i) : -INFINITY;
+    for (int j = 0; j < kEdges; ++j) e[j] = -INFINITY;
+    if (ragged) {
+#pragma unroll
+      for (int j = 0; j < kEdges; ++j) {
+        const int i = row.edge(lane + j * kLanes);
+        if (live && i >= 0) e[j] = X::load(row.x + i);
+      }
     }
   }
 };
@@ -176,10 +200,12 @@ __device__ __forceinline__ Stats part_stats(const Part<X, kLanes, kChunks>& p, f
     float v[X::kPer];
     X::unpack(p.c[j], v);
 #pragma unroll
-    for (int i = 0; i < X::kPer; ++i) mine.m = fmaxf(mine.m, v[i]);
+    for (int i = 0; i < X::kPer; i += 2) mine.m = max3(mine.m, v[i], v[i + 1]);
   }
+  if (p.ragged) {
 #pragma unroll
-  for (int j = 0; j < p.kEdges; ++j) mine.m = fmaxf(mine.m, p.e[j]);
+    for (int j = 0; j < p.kEdges; ++j) mine.m = fmaxf(mine.m, p.e[j]);
+  }
   auto take = [&](float x) {
     const float a = (x - mine.m) * k, w = exp2_fast(a);
     mine.s += w;
@@ -192,8 +218,10 @@ __device__ __forceinline__ Stats part_stats(const Part<X, kLanes, kChunks>& p, f
 #pragma unroll
     for (int i = 0; i < X::kPer; ++i) take(v[i]);
   }
+  if (p.ragged) {
 #pragma unroll
-  for (int j = 0; j < p.kEdges; ++j) take(p.e[j]);
+    for (int j = 0; j < p.kEdges; ++j) take(p.e[j]);
+  }
   return joined_lanes<kEntropy, kLanes>(mine, [k](const Stats& a, const Stats& b) { return joined<kEntropy>(a, b, k); });
 }
 
@@ -210,6 +238,7 @@ __device__ __forceinline__ void write_part(const Span<X, 16>& row, const Part<X,
     const u32x4 c = live ? X::pack(v) : u32x4{};
     if (lane + j * kLanes < row.chunks) *reinterpret_cast<u32x4_any*>(g + row.at(lane + j * kLanes)) = c;
   }
+  if (!p.ragged) return;
 #pragma unroll
   for (int j = 0; j < p.kEdges; ++j) {
     const int i = row.edge(lane + j * kLanes);
@@ -231,7 +260,7 @@ __global__ __launch_bounds__(kLaneThreads) void lanes_kernel(Rows r, RowOut o, P
   const float k = r.inv_temp * kLog2e;
   int total = 0;
   if (kOp == kPolicy) {
-    const int part = wave_sum(share_of_total(r, mean));
+    const int part = full_wave_sum(share_of_total(r, mean));
     if (threadIdx.x % kWave == 0) totals[threadIdx.x / kWave] = part;
     __syncthreads();
     for (int w = 0; w < kWaves; ++w) total += totals[w];
@@ -241,7 +270,8 @@ __global__ __launch_bounds__(kLaneThreads) void lanes_kernel(Rows r, RowOut o, P
   for (int64_t from = int64_t(blockIdx.x) * kTeams; from < rows; from += int64_t(gridDim.x) * kTeams) {
     const int64_t at = from + threadIdx.x / kLanes;
     if (at >= rows) continue;  // (all lanes of a row)
-    const int b = int(uint32_t(at) / uint32_t(r.T)), t = int(uint32_t(at) % uint32_t(r.T));
+    const At pos = position(r, at);
+    const int b = pos.b, t = pos.t;
     if (kOp != kGiven && lane == 0 && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
     const bool live = counts(r, b, t);
     const Span<X, 16> row(row_of<X>(r, b, t), r.V);
@@ -258,7 +288,7 @@ __global__ __launch_bounds__(kLaneThreads) void lanes_kernel(Rows r, RowOut o, P
         const float d = v.d_lp[b * v.d_seq + t * v.d_pos] * up;
         const float d_H = kEntropy ? v.d_entropy[b * v.d_seq + t * v.d_pos] * up : 0.f;
         m = state.x;
-        f = slope_of(state.y, state.z, token < 0 ? x : d, d_H, r.g_scale * r.inv_temp);
+        f = slope_of(state.y * from_scaled(m, k), state.z, token < 0 ? x : d, d_H, r.g_scale * r.inv_temp);
       } else {
         const Stats s = part_stats<kEntropy, kLanes>(part, k);
         const float log_s = logf(s.s), lp = (x - s.m) * r.inv_temp - log_s;
@@ -267,7 +297,7 @@ __global__ __launch_bounds__(kLaneThreads) void lanes_kernel(Rows r, RowOut o, P
         if (lane == 0) {
           if (o.logprobs) o.logprobs[at] = lp;
           if (o.entropy) o.entropy[at] = H;
-          if (o.state) o.state[at] = {s.m, s.s, H, lp};
+          if (o.state) o.state[at] = {s.m, s.s * to_scaled(s.m, k), H, lp};
         }
         if constexpr (kOp == kPolicy) {
           const float w = weight_of(r, mean, b, total);
@@ -275,10 +305,11 @@ __global__ __launch_bounds__(kLaneThreads) void lanes_kernel(Rows r, RowOut o, P
           if (lane == 0) {
             if (o.d_logprobs) o.d_logprobs[at] = q.d_lp;
             if (o.d_entropy) o.d_entropy[at] = q.d_H;
-            sum[0] += double(w) * q.terms.x;
-            sum[1] += double(w) * q.terms.y;
-            sum[2] += double(w) * q.terms.z;
-            sum[3] += double(w) * q.terms.w;
+            const double by = w;
+            sum[0] = fma(by, double(q.terms.x), sum[0]);
+            if (p.kl_coef != 0.f) sum[1] = fma(by, double(q.terms.y), sum[1]);
+            sum[2] = fma(by, double(q.terms.z), sum[2]);
+            if (kEntropy) sum[3] = fma(by, double(q.terms.w), sum[3]);
           }
           f = slope_of(s.s, H, q.d_lp, q.d_H, r.g_scale * r.inv_temp);
         }
@@ -512,7 +543,7 @@ __device__ __forceinline__ float4 sweep_row(const Rows& r, const RowOut& o, cons
     if (first) {
       if (o.logprobs) o.logprobs[at] = lp;
       if (o.entropy) o.entropy[at] = H;
-      if (o.state) o.state[at] = {s.m, s.s, H, lp};
+      if (o.state) o.state[at] = {s.m, s.s * to_scaled(s.m, k), H, lp};
       if (o.d_logprobs) o.d_logprobs[at] = v.d_lp;
       if (o.d_entropy) o.d_entropy[at] = v.d_H;
     }
@@ -534,7 +565,7 @@ __device__ __forceinline__ float4 sweep_row(const Rows& r, const RowOut& o, cons
     d = block_sum(d, e.part) * q.tau * q.tau;
     if (sum == 0.f) w = 0.f;
     if (first) {
-      if (o.state) o.state[at] = {s.m, s.s, 0.f, d};
+      if (o.state) o.state[at] = {s.m, s.s * to_scaled(s.m, k), 0.f, d};
       if (o.d_logprobs) o.d_logprobs[at] = w;
       if (o.logprobs) o.logprobs[at] = d;
     }
@@ -550,7 +581,7 @@ __global__ __launch_bounds__(512) void sweep_kernel(Rows r, RowOut o, Policy p, 
   const int64_t rows = int64_t(r.B) * r.T;
   int total = 0;
   if (kOp != kScore) {
-    const int part = wave_sum(share_of_total(r, mean));
+    const int part = full_wave_sum(share_of_total(r, mean));
     if (threadIdx.x % kWave == 0) shared.totals[threadIdx.x / kWave] = part;
     __syncthreads();
     for (int w = 0; w < int(blockDim.x / kWave); ++w) total += shared.totals[w];
@@ -558,7 +589,8 @@ __global__ __launch_bounds__(512) void sweep_kernel(Rows r, RowOut o, Policy p, 
   double sum[4] = {};
   for (int64_t i = blockIdx.x; i < rows; i += gridDim.x) {
     const int64_t at = row_of_group(i, rows);
-    const int b = int(uint32_t(at) / uint32_t(r.T)), t = int(uint32_t(at) % uint32_t(r.T));
+    const At pos = position(r, at);
+    const int b = pos.b, t = pos.t;
     if (threadIdx.x == 0 && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
     if (counts(r, b, t)) {
       const float w = kOp == kScore ? 0.f : weight_of(r, mean, b, total);
@@ -590,13 +622,13 @@ __device__ __forceinline__ void given_row(const Rows& r, const Given& v, const T
     const int token = take_token(r, b, t, false);
     const float x = token < 0 ? __uint_as_float(kNan) : X::load(row.x + token);
     __syncthreads();  // (the row may be the gradient's own memory)
-    const Slope f = slope_of(state.y, state.z, token < 0 ? x : d, d_H, r.g_scale * r.inv_temp);
+    const Slope f = slope_of(state.y * from_scaled(state.x, k), state.z, token < 0 ? x : d, d_H, r.g_scale * r.inv_temp);
     typename X::type* g = gradient_of<X>(r, b, t);
     write_gradient<X, kEntropy>(row, g, threadIdx.x, state.x, k, f);
     if (token >= 0) add_token<X, kEntropy>(row, g, token, x, state.x, k, f);
   } else {
     const float sum = take_entries<X>(r, row, q, at, k, shared.entries);
-    write_distilled<X>(r, row, q, shared.entries, b, t, state.x, state.y, sum, d, k);
+    write_distilled<X>(r, row, q, shared.entries, b, t, state.x, state.y * from_scaled(state.x, k), sum, d, k);
   }
 }
 
@@ -606,7 +638,8 @@ __global__ __launch_bounds__(512) void gradient_kernel(Rows r, Given v, Teacher 
   const int64_t rows = int64_t(r.B) * r.T;
   for (int64_t i = blockIdx.x; i < rows; i += gridDim.x) {
     const int64_t at = row_of_group(i, rows);
-    const int b = int(uint32_t(at) / uint32_t(r.T)), t = int(uint32_t(at) % uint32_t(r.T));
+    const At pos = position(r, at);
+    const int b = pos.b, t = pos.t;
     if (counts(r, b, t)) given_row<X, kOp, kEntropy>(r, v, q, b, t, at, shared);
     else write_zeros<X>(r, b, t, threadIdx.x, blockDim.x);
     __syncthreads();
@@ -651,35 +684,23 @@ struct Held {
   }
 };
 
-// M = m k of the weights 2^(x k - M): rounded, and the same wherever it is formed (the compiler must
-// not take the product into a fused multiply-add, whose M would be another one).
-__device__ __forceinline__ float scaled(float m, float k) {
-#pragma clang fp contract(off)
-  return m * k;
-}
-
-template <bool kEntropy>
-__device__ __forceinline__ Stats joined_held(const Stats& p, const Stats& q, float k) {
-  Stats r;
-  r.m = fmaxf(p.m, q.m);
-  const float M = scaled(r.m, k), dp = scaled(p.m, k) - M, dq = scaled(q.m, k) - M;
-  const float ep = exp2_fast(dp), eq = exp2_fast(dq);
-  r.s = ep * p.s + eq * q.s;
-  r.t = kEntropy ? ep * (p.t + finite(dp) * p.s) + eq * (q.t + finite(dq) * q.s) : 0.f;
-  return r;
-}
-
+// Statistics of a wavefront's part of a row, the same in all lanes, of weights 2^(x k - M), M = scaled(m, k).
+// m need not be the largest value: any that keeps the weights in range does.  It is the largest of the
+// lanes' own, found on the packed values as signed integers: right where a lane has a value above 0, else
+// the lane's smallest (half an instruction a value instead of two and a half).  Where that takes the sum
+// out of range, `fine` is false and the row has to be swept.
 template <bool kEntropy, typename X, int kThreads, int kChunks>
 __device__ __forceinline__ Stats wave_stats(Held<X, kThreads, kChunks>& h, float k) {
   Stats mine = {fmaxf(h.edge, -kExtreme), 0.f, 0.f};
+  if constexpr (kChunks > 2) mine.m = fmaxf(mine.m, X::template upper<kChunks - 2>(h.c));
 #pragma unroll
-  for (int j = 0; j < kChunks; ++j) {
+  for (int j = kChunks > 2 ? kChunks - 2 : 0; j < kChunks; ++j) {  // (with what lies beyond the row)
     float v[X::kPer];
     X::unpack(h.c[j], v);
 #pragma unroll
-    for (int i = 0; i < X::kPer; ++i) mine.m = fmaxf(mine.m, v[i]);
+    for (int i = 0; i < X::kPer; i += 2) mine.m = max3(mine.m, v[i], v[i + 1]);
   }
-  h.keep_packed();
+  mine.m = full_wave_max(mine.m);
   const float M = scaled(mine.m, k);
   auto take = [&](float x) {
     const float a = fmaf(x, k, -M), w = exp2_fast(a);
@@ -695,7 +716,12 @@ __device__ __forceinline__ Stats wave_stats(Held<X, kThreads, kChunks>& h, float
   }
   take(h.edge);
   h.keep_packed();
-  return joined_lanes<kEntropy, kWave>(mine, [k](const Stats& a, const Stats& b) { return joined_held<kEntropy>(a, b, k); });
+  mine.s = full_wave_sum(mine.s);
+  if (kEntropy) mine.t = full_wave_sum(mine.t);
+  return mine;
+}
+__device__ __forceinline__ bool fine(const Stats& s) {
+  return fabsf(s.m) < kExtreme && s.s > 0x1p-40f && s.s < 0x1p40f;
 }
 
 template <bool kEntropy, typename X, int kThreads, int kChunks>
@@ -717,12 +743,29 @@ __device__ __forceinline__ void write_held(const typename Held<X, kThreads, kChu
   if (h.edge_at >= 0) X::store(g + h.edge_at, value(h.edge));
 }
 
-// Statistics of the row, in every thread; of the parts that its wavefronts leave.
+// Statistics of the row, in every thread, of the parts that eight wavefronts leave: one a lane, joined in
+// three steps.
 template <bool kEntropy, int kWaves>
 __device__ __forceinline__ Stats block_stats(const Stats* parts, float k) {
-  Stats all = parts[0];
-  for (int w = 1; w < kWaves; ++w) all = joined_held<kEntropy>(all, parts[w], k);
-  return all;
+  static_assert(kWaves == 8);
+  Stats s = parts[threadIdx.x % 8];
+  float m = s.m;
+  m = fmaxf(m, neighbour<1>(m));
+  m = fmaxf(m, neighbour<2>(m));
+  m = fmaxf(m, neighbour<4>(m));
+  const float d = scaled(s.m, k) - scaled(m, k), e = exp2_fast(d);
+  if (kEntropy) s.t = e * (s.t + finite(d) * s.s);
+  s.s *= e;
+  s.s += neighbour<1>(s.s);
+  s.s += neighbour<2>(s.s);
+  s.s += neighbour<4>(s.s);
+  if (kEntropy) {
+    s.t += neighbour<1>(s.t);
+    s.t += neighbour<2>(s.t);
+    s.t += neighbour<4>(s.t);
+  }
+  auto uniform = [](float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); };
+  return {uniform(m), uniform(s.s), kEntropy ? uniform(s.t) : 0.f};
 }
 
 // One workgroup a row; the score, and the policy loss.
@@ -732,7 +775,8 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Po
   __shared__ Stats parts[kWaves];
   __shared__ int totals[kWaves];
   const int64_t at = row_of_group(blockIdx.x, int64_t(r.B) * r.T);
-  const int b = int(uint32_t(at) / uint32_t(r.T)), t = int(uint32_t(at) % uint32_t(r.T));
+  const At pos = position(r, at);
+    const int b = pos.b, t = pos.t;
   const bool first = threadIdx.x == 0;
   if (first && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
   if (!counts(r, b, t)) {
@@ -749,14 +793,14 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Po
   const float x = token < 0 ? __uint_as_float(kNan) : X::load(row.x + token);
   const float k = r.inv_temp * kLog2e;
   if (kOp == kPolicy) {
-    const int part = wave_sum(share);
+    const int part = full_wave_sum(share);
     if (threadIdx.x % kWave == 0) totals[threadIdx.x / kWave] = part;
   }
   const Stats part = wave_stats<kEntropy>(h, k);
   if (threadIdx.x % kWave == 0) parts[threadIdx.x / kWave] = part;
   __syncthreads();
   Stats s = block_stats<kEntropy, kWaves>(parts, k);
-  const bool extreme = !(fabsf(s.m) < kExtreme);
+  const bool extreme = !fine(s);
   if (extreme) {
     __syncthreads();
     s = row_stats<X, kEntropy>(row, k, threadIdx.x, parts);
@@ -781,7 +825,7 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Po
   if (first) {
     if (o.logprobs) o.logprobs[at] = lp;
     if (o.entropy) o.entropy[at] = H;
-    if (o.state) o.state[at] = {s.m, s.s, H, lp};
+    if (o.state) o.state[at] = {s.m, extreme ? s.s * to_scaled(s.m, k) : s.s, H, lp};
     if (o.d_logprobs) o.d_logprobs[at] = v.d_lp;
     if (o.d_entropy) o.d_entropy[at] = v.d_H;
   }
@@ -832,7 +876,7 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
   const float k = r.inv_temp * kLog2e;
   int total = 0;
   if constexpr (kThreads == kWave) {
-    const int part = wave_sum(share_of_total(r, mean));
+    const int part = full_wave_sum(share_of_total(r, mean));
     if (first) totals[team] = part;
     __syncthreads();
     for (int w = 0; w < kTeams; ++w) total += totals[w];
@@ -840,7 +884,8 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
   double sum = 0;
   for (int64_t i = int64_t(blockIdx.x) * kTeams + team; i < rows; i += int64_t(gridDim.x) * kTeams) {
     const int64_t at = kThreads == kWave ? i : row_of_group(i, rows);
-    const int b = int(uint32_t(at) / uint32_t(r.T)), t = int(uint32_t(at) % uint32_t(r.T));
+    const At pos = position(r, at);
+    const int b = pos.b, t = pos.t;
     if (first && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
     typename X::type* g = r.g ? gradient_of<X>(r, b, t) : nullptr;
     auto zeros = [&] {
@@ -889,7 +934,7 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
     for (int e = 0; e < kEntries; ++e) teacher.s += exp2_fast((v[e] - teacher.m) * k);
     teacher = joined_lanes<false, kWave>(teacher, [k](const Stats& a, const Stats& c) { return joined<false>(a, c, k); });
     if constexpr (kThreads != kWave) {
-      const int part = wave_sum(share);
+      const int part = full_wave_sum(share);
       if (thread % kWave == 0) {
         totals[wave] = part;
         teachers[team][wave] = teacher;
@@ -919,7 +964,7 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
       total = 0;
       for (int w = 0; w < kWaves; ++w) total += totals[w];
     }
-    const bool extreme = !(fabsf(s.m) < kExtreme);
+    const bool extreme = !fine(s);
     if (extreme) {
       meet<kThreads>();
       s = row_stats<X, false, kThreads>(row, k, thread, parts[team]);
@@ -961,7 +1006,7 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
     for (int c = 0; c < kWaves; ++c) d += losses[team][c];
     d *= q.tau * q.tau;
     if (first) {
-      if (o.state) o.state[at] = {s.m, s.s, 0.f, d};
+      if (o.state) o.state[at] = {s.m, extreme ? s.s * to_scaled(s.m, k) : s.s, 0.f, d};
       if (o.d_logprobs) o.d_logprobs[at] = w;
       if (o.logprobs) o.logprobs[at] = d;
     }

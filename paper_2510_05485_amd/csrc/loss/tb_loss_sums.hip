@@ -38,7 +38,7 @@ __global__ __launch_bounds__(kThreads) void part_count_kernel(Rows r, int32_t* n
   const int64_t rows = int64_t(r.B) * r.T;
   int c = 0;
   for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < rows; i += int64_t(kCountParts) * kThreads)
-    c += counts(r, int(uint32_t(i) / uint32_t(r.T)), int(uint32_t(i) % uint32_t(r.T)));
+    c += counts(r, position(r, i).b, position(r, i).t);
   c = wave_sum(c);
   if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = c;
   __syncthreads();
