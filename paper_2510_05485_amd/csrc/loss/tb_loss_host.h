@@ -4,6 +4,9 @@
 #include "tb_loss.h"
 
 namespace tb {
+
+hipError_t grant_dynamic_lds(const void* kernel, size_t bytes);  // (../tb_kernels.h)
+
 namespace loss {
 
 struct Call {

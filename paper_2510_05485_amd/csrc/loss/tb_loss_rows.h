@@ -8,6 +8,8 @@
 //   sweep_kernel     a workgroup reads the row from memory in each of two sweeps (any length)
 #pragma once
 
+#include <type_traits>
+
 #include "tb_loss_host.h"
 
 namespace tb {
@@ -132,11 +134,13 @@ __device__ __forceinline__ float weight_of(const Rows& r, const Mean& mean, int 
 }
 
 // Which row a workgroup takes: neighbouring workgroups go to different XCDs, neighbouring rows to one.
+// Which XCD begins changes from block to block, so that the ends of sequences, whose rows do not count, fall
+// to all of them alike (512 sequences of 32 positions, half of which count: 212 us without).
 __device__ __forceinline__ int64_t row_of_group(int64_t group, int64_t rows) {
   constexpr int kXcds = 8, kRun = 4;
   const int64_t block = group / (kXcds * kRun), in = group % (kXcds * kRun);
   if ((block + 1) * kXcds * kRun > rows) return group;
-  return block * kXcds * kRun + in % kXcds * kRun + in / kXcds;
+  return block * kXcds * kRun + (in + block) % kXcds * kRun + in / kXcds;
 }
 
 // Sum over the lanes that share a row (kLanes of a wavefront), in all of them.
@@ -345,33 +349,44 @@ template <typename X, bool kEntropy, int kThreads = 0, typename Row>
 __device__ __forceinline__ Stats row_stats(const Row& row, float k, int thread, Stats* parts) {
   const int threads = kThreads ? kThreads : blockDim.x;
   Stats mine = {kLowest, 0.f, 0.f};
-  auto take = [&](const float* v, int n) {
+  auto take = [&](const float* v, auto count) {
+    constexpr int n = decltype(count)::value;
     float top = mine.m;
 #pragma unroll
-    for (int i = 0; i < X::kPer; ++i)
-      if (i < n) top = fmaxf(top, v[i]);
+    for (int i = 0; i + 1 < n; i += 2) top = max3(top, v[i], v[i + 1]);
+    if (n % 2) top = fmaxf(top, v[n - 1]);
     const float d = (mine.m - top) * k, e = exp2_fast(d);
     mine.t = kEntropy ? e * (mine.t + finite(d) * mine.s) : 0.f;
     mine.s *= e;
     mine.m = top;
 #pragma unroll
-    for (int i = 0; i < X::kPer; ++i)
-      if (i < n) {
-        const float a = (v[i] - top) * k, w = exp2_fast(a);
-        mine.s += w;
-        if (kEntropy) mine.t += w * finite(a);
-      }
+    for (int i = 0; i < n; ++i) {
+      const float a = (v[i] - top) * k, w = exp2_fast(a);
+      mine.s += w;
+      if (kEntropy) mine.t += w * finite(a);
+    }
   };
-  for (int c = thread; c < row.chunks; c += threads) {
+  constexpr int kAhead = 4;  // chunks under way
+  int c = thread;
+  for (; c + (kAhead - 1) * threads < row.chunks; c += kAhead * threads) {
+    u32x4 u[kAhead];
+    float v[kAhead * X::kPer];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) u[j] = row.chunk(c + j * threads);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) X::unpack(u[j], v + j * X::kPer);
+    take(v, std::integral_constant<int, kAhead * X::kPer>());
+  }
+  for (; c < row.chunks; c += threads) {
     float v[X::kPer];
     X::unpack(row.chunk(c), v);
-    take(v, X::kPer);
+    take(v, std::integral_constant<int, X::kPer>());
   }
   for (int j = thread; j < row.kEdge; j += threads) {
     const int e = row.edge(j);
     if (e < 0) break;
-    const float v[X::kPer] = {X::load(row.x + e)};
-    take(v, 1);
+    const float v[1] = {X::load(row.x + e)};
+    take(v, std::integral_constant<int, 1>());
   }
   mine = joined_lanes<kEntropy, kWave>(mine, [k](const Stats& a, const Stats& b) { return joined<kEntropy>(a, b, k); });
   if constexpr (kThreads == kWave) return mine;
@@ -653,15 +668,19 @@ constexpr int kHeldThreads = 512;
 // A row's chunks in registers of kThreads threads, kChunks each: chunk k * kThreads + thread.  With
 // kChunks = V / kPer / kThreads rounded up, all but the last two are there in every thread (the row's head
 // takes up to eight chunks from the last but one); what lies beyond the row is -inf.
-template <typename X, int kThreads, int kChunks>
+// With kMore, chunks from kChunks on are in LDS, where they come without passing through registers: the
+// registers and the LDS of a compute unit hold 512 KB of a row together.
+extern __shared__ u32x4 more_chunks[];
+template <typename X, int kThreads, int kChunks, bool kMore = false>
 struct Held {
   // (a wavefront's lanes would have two values of head and rest each if it read whole lines)
   using Row = Span<X, kThreads == kWave ? 16 : kLine>;
   static_assert(Row::kEdge <= kThreads);
-  static constexpr int kSure = kChunks - 2;
+  static constexpr int kSure = kChunks - (kMore ? 1 : 2);
   u32x4 c[kChunks];
   float edge;
   int edge_at;
+  int more;  // chunks in LDS
   __device__ __forceinline__ void load(const Row& row, int thread) {
     const char* from = reinterpret_cast<const char*>(row.x + row.head);
     const uint32_t lane = thread * 16u;
@@ -670,8 +689,22 @@ struct Held {
       if (k >= kSure) c[k] = u32x4{X::kNone, X::kNone, X::kNone, X::kNone};
       if (k < kSure || there(row, thread, k)) c[k] = *reinterpret_cast<const u32x4*>(from + k * (kThreads * 16) + lane);
     }
+    more = 0;
+    if constexpr (kMore) {
+      more = (row.chunks + kThreads - 1) / kThreads - kChunks;
+      for (int j = 0; j < more; ++j)
+        if (there(row, thread, kChunks + j))
+          __builtin_amdgcn_global_load_lds(
+              (const __attribute__((address_space(1))) void*)(from + int64_t(kChunks + j) * (kThreads * 16) + lane),
+              (__attribute__((address_space(3))) void*)(more_chunks + j * kThreads + thread / kWave * kWave), 16, 0, 0);
+    }
     edge_at = row.edge(thread);
     edge = edge_at >= 0 ? X::load(row.x + edge_at) : -INFINITY;
+  }
+  // LDS chunk j of the thread, when all that has been loaded is there
+  __device__ __forceinline__ u32x4 chunk_in_lds(const Row& row, int thread, int j) const {
+    const u32x4 none = {X::kNone, X::kNone, X::kNone, X::kNone};
+    return there(row, thread, kChunks + j) ? more_chunks[j * kThreads + thread] : none;
   }
   static __device__ __forceinline__ bool there(const Row& row, int thread, int k) {
     return thread + k * kThreads < row.chunks;
@@ -689,8 +722,9 @@ struct Held {
 // lanes' own, found on the packed values as signed integers: right where a lane has a value above 0, else
 // the lane's smallest (half an instruction a value instead of two and a half).  Where that takes the sum
 // out of range, `fine` is false and the row has to be swept.
-template <bool kEntropy, typename X, int kThreads, int kChunks>
-__device__ __forceinline__ Stats wave_stats(Held<X, kThreads, kChunks>& h, float k) {
+template <bool kEntropy, typename X, int kThreads, int kChunks, bool kMore>
+__device__ __forceinline__ Stats wave_stats(const typename Held<X, kThreads, kChunks, kMore>::Row& row,
+                                            Held<X, kThreads, kChunks, kMore>& h, int thread, float k) {
   Stats mine = {fmaxf(h.edge, -kExtreme), 0.f, 0.f};
   if constexpr (kChunks > 2) mine.m = fmaxf(mine.m, X::template upper<kChunks - 2>(h.c));
 #pragma unroll
@@ -716,6 +750,15 @@ __device__ __forceinline__ Stats wave_stats(Held<X, kThreads, kChunks>& h, float
   }
   take(h.edge);
   h.keep_packed();
+  if constexpr (kMore) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // (what a wavefront has asked for is in LDS then)
+    for (int j = 0; j < h.more; ++j) {
+      float v[X::kPer];
+      X::unpack(h.chunk_in_lds(row, thread, j), v);
+#pragma unroll
+      for (int i = 0; i < X::kPer; ++i) take(v[i]);
+    }
+  }
   mine.s = full_wave_sum(mine.s);
   if (kEntropy) mine.t = full_wave_sum(mine.t);
   return mine;
@@ -724,9 +767,10 @@ __device__ __forceinline__ bool fine(const Stats& s) {
   return fabsf(s.m) < kExtreme && s.s > 0x1p-40f && s.s < 0x1p40f;
 }
 
-template <bool kEntropy, typename X, int kThreads, int kChunks>
-__device__ __forceinline__ void write_held(const typename Held<X, kThreads, kChunks>::Row& row, const Held<X, kThreads, kChunks>& h,
-                                           typename X::type* g, int thread, float m, float k, Slope f) {
+template <bool kEntropy, typename X, int kThreads, int kChunks, bool kMore>
+__device__ __forceinline__ void write_held(const typename Held<X, kThreads, kChunks, kMore>::Row& row,
+                                           const Held<X, kThreads, kChunks, kMore>& h, typename X::type* g, int thread,
+                                           float m, float k, Slope f) {
   const float M = scaled(m, k);
   char* to = reinterpret_cast<char*>(g + row.head);
   const uint32_t lane = thread * 16u;
@@ -740,6 +784,15 @@ __device__ __forceinline__ void write_held(const typename Held<X, kThreads, kChu
     if (j < h.kSure || h.there(row, thread, j))
       *reinterpret_cast<u32x4_any*>(to + j * (kThreads * 16) + lane) = X::pack(v);
   }
+  if constexpr (kMore)
+    for (int j = 0; j < h.more; ++j) {
+      float v[X::kPer];
+      X::unpack(h.chunk_in_lds(row, thread, j), v);
+#pragma unroll
+      for (int i = 0; i < X::kPer; ++i) v[i] = value(v[i]);
+      if (h.there(row, thread, kChunks + j))
+        *reinterpret_cast<u32x4_any*>(to + int64_t(kChunks + j) * (kThreads * 16) + lane) = X::pack(v);
+    }
   if (h.edge_at >= 0) X::store(g + h.edge_at, value(h.edge));
 }
 
@@ -769,7 +822,7 @@ __device__ __forceinline__ Stats block_stats(const Stats* parts, float k) {
 }
 
 // One workgroup a row; the score, and the policy loss.
-template <typename X, int kOp, bool kEntropy, int kChunks>
+template <typename X, int kOp, bool kEntropy, int kChunks, bool kMore = false>
 __global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Policy p, Mean mean) {
   constexpr int kWaves = kHeldThreads / kWave;
   __shared__ Stats parts[kWaves];
@@ -788,7 +841,7 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Po
   const Line<X> row(row_of<X>(r, b, t), r.V);
   // (what comes first is waited for first: not behind the whole row)
   const int token = take_token(r, b, t, first), share = kOp == kPolicy ? share_of_total(r, mean) : 0;
-  Held<X, kHeldThreads, kChunks> h;
+  Held<X, kHeldThreads, kChunks, kMore> h;
   h.load(row, threadIdx.x);
   const float x = token < 0 ? __uint_as_float(kNan) : X::load(row.x + token);
   const float k = r.inv_temp * kLog2e;
@@ -796,7 +849,7 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Po
     const int part = full_wave_sum(share);
     if (threadIdx.x % kWave == 0) totals[threadIdx.x / kWave] = part;
   }
-  const Stats part = wave_stats<kEntropy>(h, k);
+  const Stats part = wave_stats<kEntropy>(row, h, threadIdx.x, k);
   if (threadIdx.x % kWave == 0) parts[threadIdx.x / kWave] = part;
   __syncthreads();
   Stats s = block_stats<kEntropy, kWaves>(parts, k);
@@ -861,7 +914,7 @@ __device__ __forceinline__ void meet() {
 // that then take several rows.  While the row is on its way to the registers, its threads look for ids
 // that come up twice; entry j's thread writes the gradient at id j behind the others' stores, with the
 // sum of the probabilities of this id if it does.
-template <typename X, int kThreads, int kChunks, int kEntries>
+template <typename X, int kThreads, int kChunks, int kEntries, bool kMore = false>
 __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void distill_kernel(Rows r, RowOut o, Mean mean,
                                                                                            Teacher q) {
   constexpr int kTeams = kThreads == kWave ? 4 : 1, kWaves = kThreads / kWave, kRoom = kThreads * kEntries;
@@ -882,7 +935,7 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
     for (int w = 0; w < kTeams; ++w) total += totals[w];
   }
   double sum = 0;
-  for (int64_t i = int64_t(blockIdx.x) * kTeams + team; i < rows; i += int64_t(gridDim.x) * kTeams) {
+  auto take_row = [&](int64_t i) {
     const int64_t at = kThreads == kWave ? i : row_of_group(i, rows);
     const At pos = position(r, at);
     const int b = pos.b, t = pos.t;
@@ -894,9 +947,9 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
     if (!counts(r, b, t)) {
       if (first) leave_nothing(o, at);
       zeros();
-      continue;
+      return;
     }
-    const typename Held<X, kThreads, kChunks>::Row row(row_of<X>(r, b, t), r.V);
+    const typename Held<X, kThreads, kChunks, kMore>::Row row(row_of<X>(r, b, t), r.V);
     // (what comes first is waited for first: not behind the whole row)
     float v[kEntries], x[kEntries];
     int64_t wide[kEntries];
@@ -912,7 +965,7 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
       }
     }
     const int share = kThreads == kWave ? 0 : share_of_total(r, mean);
-    Held<X, kThreads, kChunks> h;
+    Held<X, kThreads, kChunks, kMore> h;
     h.load(row, thread);
     Stats teacher = {kLowest, 0.f, 0.f};
     bool wrong = false;
@@ -953,7 +1006,7 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
       }
       if (found > 1) twice |= 1u << e;
     }
-    const Stats mine = wave_stats<false>(h, k);
+    const Stats mine = wave_stats<false>(row, h, thread, k);
     Stats s = mine;
     if constexpr (kThreads != kWave) {
       if (thread % kWave == 0) parts[team][wave] = mine;
@@ -1011,7 +1064,15 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
       if (o.logprobs) o.logprobs[at] = d;
     }
     sum += double(w) * d;
-    meet<kThreads>();  // (before the next row takes the shared memory)
+  };
+  // (a workgroup takes one row: what lives from row to row would cost it registers)
+  if constexpr (kThreads == kWave) {
+    for (int64_t i = int64_t(blockIdx.x) * kTeams + team; i < rows; i += int64_t(gridDim.x) * kTeams) {
+      take_row(i);
+      meet<kThreads>();  // (before the next row takes the shared memory)
+    }
+  } else {
+    take_row(blockIdx.x);
   }
   __shared__ double sums[kTeams];
   if (first) sums[team] = sum;
@@ -1060,15 +1121,35 @@ bool launch_lanes(Call& c) {
   return false;
 }
 
+// Longer rows than 32 chunks a thread: 32 or 46 in registers and up to 18 in LDS, one workgroup a unit.
+// 2047 rows of 262144 values in bfloat16, distilled: 655 us with sweeps, 443 so (4.6 TB/s).
+constexpr int kMoreFrom = 32, kFewer = 32, kMostHeld = 46, kMostMore = 18;
+template <typename Kernel>
+bool more_in_lds(Kernel kernel, int chunks, size_t* bytes) {
+  *bytes = size_t(chunks) * kHeldThreads * sizeof(u32x4);
+  return grant_dynamic_lds(reinterpret_cast<const void*>(kernel), *bytes) == hipSuccess;
+}
+
 template <typename X, int kOp, bool kEntropy>
 bool launch_held(Call& c) {
   const Rows& r = c.rows;
   const int64_t rows = int64_t(r.B) * r.T;
   if (rows > kMostGroups || r.V < 2 * X::kPer) return false;
   c.groups = int(rows);
+  const int need = (r.V / X::kPer + kHeldThreads - 1) / kHeldThreads;
+  if (kOp == kPolicy && need > kMoreFrom) {
+    auto go = [&](auto kernel, int held) {
+      size_t bytes;
+      if (need - held > kMostMore || !more_in_lds(kernel, need - held, &bytes)) return false;
+      kernel<<<int(rows), kHeldThreads, bytes, c.stream>>>(r, c.out, c.policy, c.mean);
+      return true;
+    };
+    return need - kFewer <= kMostMore ? go(held_kernel<X, kPolicy, kEntropy, kFewer, true>, kFewer)
+                                      : go(held_kernel<X, kPolicy, kEntropy, kMostHeld, true>, kMostHeld);
+  }
 #define HELD(n) \
   case n: held_kernel<X, kOp, kEntropy, n><<<int(rows), kHeldThreads, 0, c.stream>>>(r, c.out, c.policy, c.mean); return true;
-  switch ((r.V / X::kPer + kHeldThreads - 1) / kHeldThreads) {
+  switch (need) {
     HELD(1) HELD(2) HELD(3) HELD(4) HELD(5) HELD(6) HELD(7) HELD(8) HELD(9) HELD(10) HELD(11) HELD(12) HELD(13) HELD(14)
     HELD(15) HELD(16) HELD(17) HELD(18) HELD(19) HELD(20) HELD(21) HELD(22) HELD(23) HELD(24) HELD(25) HELD(26) HELD(27)
     HELD(28) HELD(29) HELD(30) HELD(31) HELD(32)
@@ -1092,10 +1173,22 @@ bool launch_distill_wave(Call& c) {
 template <typename X, int kEntries>
 bool launch_distill_block(Call& c) {
   const Rows& r = c.rows;
+  if (int64_t(r.B) * r.T > kMostGroups) return false;
   c.groups = grid_of(r);
 #define HELD(n) \
   case n: distill_kernel<X, kHeldThreads, n, kEntries><<<c.groups, kHeldThreads, 0, c.stream>>>(r, c.out, c.mean, c.teacher); return true;
-  switch ((r.V / X::kPer + kHeldThreads - 1) / kHeldThreads) {
+  const int need = (r.V / X::kPer + kHeldThreads - 1) / kHeldThreads;
+  if (need > kMoreFrom) {
+    auto go = [&](auto kernel, int held) {
+      size_t bytes;
+      if (need - held > kMostMore || !more_in_lds(kernel, need - held, &bytes)) return false;
+      kernel<<<c.groups, kHeldThreads, bytes, c.stream>>>(r, c.out, c.mean, c.teacher);
+      return true;
+    };
+    return need - kFewer <= kMostMore ? go(distill_kernel<X, kHeldThreads, kFewer, kEntries, true>, kFewer)
+                                      : go(distill_kernel<X, kHeldThreads, kMostHeld, kEntries, true>, kMostHeld);
+  }
+  switch (need) {
     HELD(1) HELD(2) HELD(3) HELD(4) HELD(5) HELD(6) HELD(7) HELD(8) HELD(9) HELD(10) HELD(11) HELD(12) HELD(13) HELD(14)
     HELD(15) HELD(16) HELD(17) HELD(18) HELD(19) HELD(20) HELD(21) HELD(22) HELD(23) HELD(24) HELD(25) HELD(26) HELD(27)
     HELD(28) HELD(29) HELD(30) HELD(31) HELD(32)

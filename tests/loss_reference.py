@@ -39,7 +39,7 @@ def chosen(logp, tokens, valid):
 
 
 def entropies(logp, valid):
-    h = -torch.where(logp > -float("inf"), logp.exp() * logp, torch.zeros_like(logp)).sum(-1)
+    h = -(logp.exp() * logp.masked_fill(logp == -float("inf"), 0.0)).sum(-1)   # (0 log 0 is 0, its slope, too)
     return torch.where(valid, h, torch.zeros_like(h))
 
 

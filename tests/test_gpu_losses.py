@@ -191,6 +191,71 @@ def test_distillation_loss(dtype, V, K, kw):
     near_gradient(leaf.grad, 2 * grad, 2 * size, dtype, "backward")
 
 
+@pytest.mark.parametrize("dtype,V", [(d, v // (2 if d == torch.float32 else 1)) for d in TYPES
+                                     for v in (131064, 131072, 131082, 139264, 204802, 204820, 209001, 262144, 262152, 270003)])
+def test_long_rows(dtype, V):
+    """Rows that registers hold, that registers and LDS hold, and longer ones, at each boundary."""
+    B, T = 2, 2
+    base = torch.zeros(B, T, V + 9, dtype=dtype, device=DEV)
+    x, tokens, g = inputs(V, B, T, V, dtype)
+    tokens[0, 0], tokens[0, 1], tokens[1, 0] = 0, V - 1, V - 9
+    old = torch.full((B, T), -10.0, device=DEV)
+    a = torch.tensor([1.0, -0.5], device=DEV)
+    ids = torch.stack([torch.randint(0, V, (B, T), generator=g), torch.zeros(B, T, dtype=torch.long),
+                       torch.full((B, T), V - 1), torch.zeros(B, T, dtype=torch.long)], -1).to(DEV)
+    teacher = torch.randn(B, T, 4, generator=g).to(DEV)
+    kw = dict(kl_coef=0.1, entropy_coef=0.1)
+    terms, grad, lp = ref.policy(x, tokens, old, a, old, None, None, **kw)
+    d_terms, d_grad, rows = ref.distillation(x, ids, teacher)
+    size = 4 * float(grad.abs().amax() + 1)
+    for lo in (0, 3, 8):
+        view = base[..., lo:lo + V]
+        view.copy_(x)
+        out = torch.full_like(base, 7.0)
+        r = tb.policy_loss_grad(view, tokens, old, a, ref_logprobs=old, out=out[..., lo:lo + V], **kw)
+        near(r.logprobs, lp, LP)
+        near(r.terms, terms, LP * (20 + terms.abs().max()))
+        near_gradient(r.grad, grad, size, dtype)
+        assert (out[..., :lo] == 7).all() and (out[..., lo + V:] == 7).all()
+        out.fill_(7.0)
+        r = tb.distillation_loss_grad(view, ids, teacher, out=out[..., lo:lo + V])
+        near(r.row_loss, rows, 2 * LP)
+        near_gradient(r.grad, d_grad, 1.0, dtype)
+        assert (out[..., :lo] == 7).all() and (out[..., lo + V:] == 7).all()
+        near(tb.token_logprobs(view, tokens), lp, LP)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [64, 5000, 20011])
+@pytest.mark.parametrize("shift", [-200.0, -30.0, 60.0, 2000.0])
+def test_shifted_logits(dtype, V, shift):
+    """Softmax does not change with a constant: rows below 0 throughout (log-probabilities as logits), far
+    above, with tokens that cannot be among them."""
+    B, T = 2, 3
+    x, tokens, g = inputs(V, B, T, V)
+    x = (x + shift).to(dtype)
+    dead = (torch.rand(B, T, V, generator=g) < 0.3).to(DEV).scatter(-1, tokens.unsqueeze(-1), False)
+    for low in (None, -math.inf, torch.finfo(dtype).min):
+        y = x if low is None else torch.where(dead, torch.full_like(x, low), x)
+        old, a = torch.full((B, T), -8.0, device=DEV), torch.ones(B, device=DEV)
+        terms, grad, lp = ref.policy(y, tokens, old, a, None, None, None, entropy_coef=0.1)
+        r = tb.policy_loss_grad(y, tokens, old, a, entropy_coef=0.1)
+        # z - m is a difference of numbers of the shift's size, whose products with log2(e) are rounded
+        tol = LP + 4 * abs(shift) * 2.0 ** -24
+        near(r.logprobs, lp, tol)
+        near(r.terms, terms, tol * (20 + terms.abs().max()))
+        near(r.grad, grad, tol * 20 * (1 + float(grad.abs().max())) + grad.abs() * (ROUND[dtype] * 1.01) + STEP[dtype])
+        d_terms, d_grad, rows = ref.distillation(y, tokens.unsqueeze(-1), torch.zeros(B, T, 1))
+        r = tb.distillation_loss_grad(y, tokens.unsqueeze(-1), torch.zeros(B, T, 1, device=DEV))
+        near(r.row_loss, rows, tol)
+        near(r.grad, d_grad, tol * 20 + d_grad.abs() * (ROUND[dtype] * 1.01) + STEP[dtype])
+        leaf = y.clone().requires_grad_()
+        got, = torch.autograd.grad(tb.token_logprobs(leaf, tokens).sum(), leaf)
+        p = torch.log_softmax(y.cpu().double(), -1).exp()
+        want = torch.nn.functional.one_hot(tokens.cpu(), V) - p
+        near(got, want, tol * 20 + want.abs() * (ROUND[dtype] * 1.01) + STEP[dtype])
+
+
 def all_operators(x, tokens, where, seed=5, out=False):
     """Every operator on the same logits [B, T, V] (B even); a list of (name, tensor)."""
     g = torch.Generator().manual_seed(seed)
