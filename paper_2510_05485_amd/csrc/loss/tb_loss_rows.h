@@ -59,15 +59,16 @@ struct Position {
   float4 terms;  // loss, kl, clipped, entropy
   float d_lp, d_H;
 };
-__device__ __forceinline__ Position policy_position(const Policy& p, int b, int64_t r, float lp, float H, float w) {
-  const float ratio = expf(lp - p.old_lp[r]), A = p.each ? p.advantages[r] : p.advantages[b];
+__device__ __forceinline__ Position policy_position(const Policy& p, float old_lp, float ref_lp, float A, float lp,
+                                                    float H, float w) {
+  const float ratio = expf(lp - old_lp);
   const bool clipped = (A > 0 && ratio > 1 + p.high) || (A < 0 && ratio < 1 - p.low);
   const float held = A > 0 ? 1 + p.high : 1 - p.low;
   Position o;
   float loss = -(clipped ? held : ratio) * A, kl = 0.f;
   o.d_lp = clipped ? 0.f : -ratio * A;
   if (p.kl_coef != 0.f) {
-    const float d = p.ref_lp[r] - lp, e = expf(d);
+    const float d = ref_lp - lp, e = expf(d);
     // near 0 the difference of e^d and 1 + d is its series' next terms: d^2 (1/2 + d/6 + ...)
     kl = fabsf(d) < 0.02f ? d * d * (0.5f + d * (1.f / 6 + d * (1.f / 24 + d * (1.f / 120)))) : e - d - 1.f;
     loss += p.kl_coef * kl;
@@ -78,6 +79,9 @@ __device__ __forceinline__ Position policy_position(const Policy& p, int b, int6
   o.d_lp *= w;
   o.d_H = -p.entropy_coef * w;
   return o;
+}
+__device__ __forceinline__ Position policy_position(const Policy& p, int b, int64_t at, float lp, float H, float w) {
+  return policy_position(p, p.old_lp[at], p.kl_coef != 0.f ? p.ref_lp[at] : 0.f, p.advantages[p.each ? at : b], lp, H, w);
 }
 
 __device__ __forceinline__ float teacher_value(const Teacher& q, int64_t i) {
@@ -104,9 +108,6 @@ __device__ __forceinline__ void leave_nothing(const RowOut& o, int64_t at) {
 }
 
 // The thread's share of the total, and the weight of a sequence's positions.
-__device__ __forceinline__ int positions_of(const Rows& r, const Mean& mean, int b) {
-  return mean.n ? mean.n[b] : r.lengths ? clamped(r.lengths[b], r.T) : r.T;
-}
 __device__ __forceinline__ int share_of_total(const Rows& r, const Mean& mean) {
   constexpr int kAhead = 8;  // loads under way
   const int32_t* from = mean.n ? mean.n : r.lengths;
@@ -125,12 +126,15 @@ __device__ __forceinline__ int share_of_total(const Rows& r, const Mean& mean) {
   }
   return n;
 }
-__device__ __forceinline__ float weight_of(const Rows& r, const Mean& mean, int b, int total) {
+__device__ __forceinline__ float weight_of(const Rows& r, const Mean& mean, int b, int length, int total) {
   if (mean.weight) return mean.weight[b];
   if (mean.average == TB_SUM) return 1.f;
   if (!mean.n && !r.lengths) total = mean.average == TB_MEAN_TOKENS ? r.B * r.T : r.B;
   if (mean.average == TB_MEAN_TOKENS) return 1.f / float(total);
-  return reciprocal(float(total) * float(positions_of(r, mean, b)));
+  return reciprocal(float(total) * float(mean.n ? mean.n[b] : length));
+}
+__device__ __forceinline__ float weight_of(const Rows& r, const Mean& mean, int b, int total) {
+  return weight_of(r, mean, b, r.lengths ? clamped(r.lengths[b], r.T) : r.T, total);
 }
 
 // Which row a workgroup takes: neighbouring workgroups go to different XCDs, neighbouring rows to one.
@@ -167,37 +171,57 @@ __device__ __forceinline__ Stats joined_lanes(const Stats& mine, Join join) {
   }
 }
 
+// A barrier of the threads that share a row: of a wavefront, whose accesses keep their order, it only
+// keeps the compiler from moving them.
+template <int kThreads>
+__device__ __forceinline__ void meet() {
+  if constexpr (kThreads == kWave) {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  } else {
+    __syncthreads();
+  }
+}
+
 // ---- rows in the registers of some lanes ------------------------------------------------------
 
-// The part of a row that a lane of kLanes holds; what lies beyond the row is -inf.
+// The part of a row that a lane of kLanes holds: chunks lane + k kLanes of 16 bytes from the row's first
+// value on, at any address.  The last chunk ends with the row: where a row is not a whole number of chunks it
+// has values of the chunk before once more, which count once and get the same gradient twice.
 template <typename X, int kLanes, int kChunks>
 struct Part {
-  using Row = Span<X, 16>;
-  static constexpr int kEdges = (Row::kEdge + kLanes - 1) / kLanes;
   u32x4 c[kChunks];
-  float e[kEdges];
-  bool ragged;  // some row of the wavefront has a head or a rest
-  __device__ __forceinline__ void load(const Row& row, int lane, bool live) {
-    ragged = __any(row.head != 0 || row.at(row.chunks) != row.V);
+  // the first value of chunk k, or -1
+  static __device__ __forceinline__ int at(int V, int lane, int k) {
+    const int i = (lane + k * kLanes) * X::kPer;
+    return i < V ? min(i, V - X::kPer) : -1;
+  }
+  __device__ __forceinline__ void load(const typename X::type* row, int V, int lane, bool live) {
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
       c[k] = u32x4{X::kNone, X::kNone, X::kNone, X::kNone};
-      if (live && lane + k * kLanes < row.chunks) c[k] = row.chunk(lane + k * kLanes);
+      const int i = at(V, lane, k);
+      if (live && i >= 0) c[k] = *reinterpret_cast<const u32x4_any*>(row + i);
     }
+  }
+  // values of chunk k, those that count elsewhere as -inf
+  __device__ __forceinline__ void once(int V, int lane, int k, float* v) const {
+    X::unpack(c[k], v);
+    if (V % X::kPer == 0) return;  // (the same for all rows)
+    const int again = (lane + k * kLanes) * X::kPer - (V - X::kPer);
 #pragma unroll
-    for (int j = 0; j < kEdges; ++j) e[j] = -INFINITY;
-    if (ragged) {
+    for (int i = 0; i < X::kPer - 1; ++i)
+      if (i < again) v[i] = -INFINITY;
+  }
+  __device__ __forceinline__ void keep_packed() {  // (as in Held)
 #pragma unroll
-      for (int j = 0; j < kEdges; ++j) {
-        const int i = row.edge(lane + j * kLanes);
-        if (live && i >= 0) e[j] = X::load(row.x + i);
-      }
-    }
+    for (int k = 0; k < kChunks; ++k) asm volatile("" : "+v"(c[k]));
   }
 };
 
 template <bool kEntropy, int kLanes, typename X, int kChunks>
-__device__ __forceinline__ Stats part_stats(const Part<X, kLanes, kChunks>& p, float k) {
+__device__ __forceinline__ Stats part_stats(Part<X, kLanes, kChunks>& p, int V, int lane, float k) {
   Stats mine = {kLowest, 0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < kChunks; ++j) {
@@ -206,62 +230,127 @@ __device__ __forceinline__ Stats part_stats(const Part<X, kLanes, kChunks>& p, f
 #pragma unroll
     for (int i = 0; i < X::kPer; i += 2) mine.m = max3(mine.m, v[i], v[i + 1]);
   }
-  if (p.ragged) {
-#pragma unroll
-    for (int j = 0; j < p.kEdges; ++j) mine.m = fmaxf(mine.m, p.e[j]);
-  }
-  auto take = [&](float x) {
-    const float a = (x - mine.m) * k, w = exp2_fast(a);
-    mine.s += w;
-    if (kEntropy) mine.t += w * finite(a);
-  };
+  p.keep_packed();
 #pragma unroll
   for (int j = 0; j < kChunks; ++j) {
     float v[X::kPer];
-    X::unpack(p.c[j], v);
+    p.once(V, lane, j, v);
 #pragma unroll
-    for (int i = 0; i < X::kPer; ++i) take(v[i]);
+    for (int i = 0; i < X::kPer; ++i) {
+      const float a = (v[i] - mine.m) * k, w = exp2_fast(a);
+      mine.s += w;
+      if (kEntropy) mine.t += w * finite(a);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   }
-  if (p.ragged) {
-#pragma unroll
-    for (int j = 0; j < p.kEdges; ++j) take(p.e[j]);
-  }
+  p.keep_packed();
   return joined_lanes<kEntropy, kLanes>(mine, [k](const Stats& a, const Stats& b) { return joined<kEntropy>(a, b, k); });
 }
 
-// Writes the gradient, zeros where `live` is false.
+// Writes the gradients of a wavefront's rows, the first of which is row `from`; zeros where `live` is false.
+// Lanes that hold pieces of 16 or 32 bytes of a row would store as many pieces of lines; so the chunks go
+// through LDS, from where neighbouring lanes take neighbouring chunks (4096 x 512 rows of 64 values, the
+// gradient alone: 180 us without, 117 so).  `stage`: room for the wavefront's chunks.
 template <bool kEntropy, int kLanes, typename X, int kChunks>
-__device__ __forceinline__ void write_part(const Span<X, 16>& row, const Part<X, kLanes, kChunks>& p, typename X::type* g,
-                                           int lane, bool live, float m, float k, Slope f) {
+__device__ __forceinline__ void write_part(const Part<X, kLanes, kChunks>& p, const Rows& r, int64_t from, int V,
+                                           bool live, int token, float x, float m, float k, Slope f, u32x4* stage) {
+  using T = typename X::type;
+  constexpr int kSlots = kLanes * kChunks, kSpread = kSlots < 8 ? kSlots : 8;
+  const int lane = threadIdx.x % kLanes, thread = threadIdx.x % kWave, row = thread / kLanes;
+  auto slot_of = [](int row, int slot) { return row * kSlots + (slot ^ (row % kSpread)); };  // (other banks for other rows)
+  const bool any = __any(live);
 #pragma unroll
   for (int j = 0; j < kChunks; ++j) {
-    float v[X::kPer];
-    X::unpack(p.c[j], v);
+    u32x4 c = {};
+    if (any) {
+      float v[X::kPer];
+      X::unpack(p.c[j], v);
 #pragma unroll
-    for (int i = 0; i < X::kPer; ++i) v[i] = gradient_at<kEntropy>((v[i] - m) * k, f);
-    const u32x4 c = live ? X::pack(v) : u32x4{};
-    if (lane + j * kLanes < row.chunks) *reinterpret_cast<u32x4_any*>(g + row.at(lane + j * kLanes)) = c;
+      for (int i = 0; i < X::kPer; ++i) v[i] = gradient_at<kEntropy>((v[i] - m) * k, f);
+      if (live) c = X::pack(v);
+    }
+    stage[slot_of(row, lane + j * kLanes)] = c;
+    __builtin_amdgcn_sched_barrier(0);  // (one chunk's values in registers at a time)
   }
-  if (!p.ragged) return;
-#pragma unroll
-  for (int j = 0; j < p.kEdges; ++j) {
-    const int i = row.edge(lane + j * kLanes);
-    if (i >= 0) X::store(g + i, live ? gradient_at<kEntropy>((p.e[j] - m) * k, f) : 0.f);
+  meet<kWave>();
+  if (live && token >= 0 && lane == 0) {
+    const float v = f.token + gradient_at<kEntropy>((x - m) * k, f);
+    const int chunk = token / X::kPer, last = (V - 1) / X::kPer, tail = token - (V - X::kPer);
+    if (chunk < V / X::kPer) X::store(reinterpret_cast<T*>(stage + slot_of(row, chunk)) + token % X::kPer, v);
+    if (tail >= 0) X::store(reinterpret_cast<T*>(stage + slot_of(row, last)) + tail, v);
   }
+  meet<kWave>();
+  const int64_t rows = int64_t(r.B) * r.T;
+#pragma unroll 1
+  for (int j = 0; j < kChunks; ++j) {
+    const int q = j * kWave + thread, other = q / kSlots, slot = q % kSlots;
+    const int i = Part<X, kLanes, kChunks>::at(V, slot, 0);
+    if (i < 0 || from + other >= rows) continue;
+    const At pos = position(r, from + other);
+    *reinterpret_cast<u32x4_any*>(gradient_of<X>(r, pos.b, pos.t) + i) = stage[slot_of(other, slot)];
+  }
+  meet<kWave>();  // (before the next rows' chunks)
 }
 
 constexpr int kLaneThreads = 256;
 
+// What a position brings besides its row, on its way while the position before is worked on: with one
+// round trip after the other in front of every row (length, token, the token's logit, the sampling policy's
+// value ...) 4096 x 512 rows of 64 values took a sixth longer.
+template <int kOp, bool kEntropy>
+struct Ahead {
+  int64_t token;
+  float old_lp, ref_lp, advantage;  // kPolicy
+  float4 state;                     // kGiven
+  float d_lp, d_H;
+  int length, mask, b, t;
+
+  __device__ __forceinline__ void fetch(const Rows& r, const Policy& p, const Given& v, int64_t at) {
+    const At pos = position(r, at);
+    b = pos.b;
+    t = pos.t;
+    length = r.lengths ? r.lengths[b] : r.T;
+    mask = r.mask ? r.mask[at] : 1;
+    token = load_id(r.tokens, r.long_tokens, b * r.token_seq + t);
+    if constexpr (kOp == kPolicy) {
+      old_lp = p.old_lp[at];
+      ref_lp = p.kl_coef != 0.f ? p.ref_lp[at] : 0.f;
+      advantage = p.advantages[p.each ? at : b];
+    }
+    if constexpr (kOp == kGiven) {
+      state = v.state[at];
+      d_lp = v.d_lp[b * v.d_seq + t * v.d_pos];
+      d_H = kEntropy ? v.d_entropy[b * v.d_seq + t * v.d_pos] : 0.f;
+    }
+  }
+};
+
 // kLanes lanes of a wavefront a row, kLaneThreads / kLanes rows a workgroup at a time.  Nothing of it
-// needs a barrier, and a row's statistics meet in two to six steps between lanes.
+// needs a barrier, and a row's statistics meet in one to six steps between lanes.  Few lanes with four
+// chunks each share what is done once a row, a third of all instructions at 64 values.
 template <typename X, int kOp, bool kEntropy, int kLanes, int kChunks>
 __global__ __launch_bounds__(kLaneThreads) void lanes_kernel(Rows r, RowOut o, Policy p, Mean mean, Given v) {
   constexpr int kTeams = kLaneThreads / kLanes, kWaves = kLaneThreads / kWave;
   __shared__ double sums[kWaves][4];
   __shared__ int totals[kWaves];
+  __shared__ u32x4 stage[kOp == kScore ? 1 : kWaves * kWave * kChunks];
   const int lane = threadIdx.x % kLanes;
   const int64_t rows = int64_t(r.B) * r.T;
   const float k = r.inv_temp * kLog2e;
+  constexpr int kRows = kWave / kLanes;  // of a wavefront
+  const int wave = threadIdx.x / kWave, row_in_wave = threadIdx.x % kWave / kLanes;
+  // Round by round the workgroups take the next rows, each one's place in a round being its neighbour's in
+  // the round before: in the same place it would meet the same positions of every sequence, the ends of
+  // which do not count (161 us for the rows above, 121 so).
+  auto first_of = [&](uint32_t round) {
+    uint32_t place = blockIdx.x + round;
+    if (place >= gridDim.x) place %= gridDim.x;
+    return (int64_t(round) * gridDim.x + place) * kTeams + wave * kRows;
+  };
+  int64_t from = first_of(0);
+  auto within = [&](int64_t i) { return i < rows ? i : rows - 1; };
+  Ahead<kOp, kEntropy> next;
+  next.fetch(r, p, v, within(from + row_in_wave));
   int total = 0;
   if (kOp == kPolicy) {
     const int part = full_wave_sum(share_of_total(r, mean));
@@ -271,44 +360,41 @@ __global__ __launch_bounds__(kLaneThreads) void lanes_kernel(Rows r, RowOut o, P
   }
   const float up = kOp == kGiven && v.upstream ? *v.upstream : 1.f;
   double sum[4] = {};
-  for (int64_t from = int64_t(blockIdx.x) * kTeams; from < rows; from += int64_t(gridDim.x) * kTeams) {
-    const int64_t at = from + threadIdx.x / kLanes;
-    if (at >= rows) continue;  // (all lanes of a row)
-    const At pos = position(r, at);
-    const int b = pos.b, t = pos.t;
-    if (kOp != kGiven && lane == 0 && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
-    const bool live = counts(r, b, t);
-    const Span<X, 16> row(row_of<X>(r, b, t), r.V);
+  const int64_t a_round = int64_t(gridDim.x) * kTeams;
+  for (uint32_t round = 0; round * a_round < rows; ++round) {
+    const int64_t at = from + row_in_wave, follows = first_of(round + 1);
+    // (keeps the compiler from working out the lanes' masks once for all rows, for which there are no registers)
+    int V = r.V;
+    asm volatile("" : "+s"(V));
+    const Ahead<kOp, kEntropy> now = next;
+    next.fetch(r, p, v, within(follows + row_in_wave));
+    const bool inside = at < rows, live = inside && now.t < now.length && now.mask != 0;
+    const typename X::type* row = row_of<X>(r, now.b, now.t);
     Part<X, kLanes, kChunks> part;
-    part.load(row, lane, live);
+    part.load(row, V, lane, live);
+    const int token = live && now.token >= 0 && now.token < V ? int(now.token) : -1;
+    const float x = token < 0 ? __uint_as_float(kNan) : X::load(row + token);
+    if (kOp != kGiven && lane == 0 && inside && r.status) {
+      if (now.t == 0 && (now.length < 0 || now.length > r.T)) atomicOr(r.status, TB_DEV_LENGTH_RANGE);
+      if (live && token < 0) atomicOr(r.status, TB_DEV_TOKEN_RANGE);
+    }
     Slope f = {};
-    float m = 0.f, x = 0.f;
-    int token = -1;
+    float m = 0.f;
     if (live) {
-      token = take_token(r, b, t, kOp != kGiven && lane == 0);
-      x = token < 0 ? __uint_as_float(kNan) : X::load(row.x + token);
       if constexpr (kOp == kGiven) {
-        const float4 state = v.state[at];
-        const float d = v.d_lp[b * v.d_seq + t * v.d_pos] * up;
-        const float d_H = kEntropy ? v.d_entropy[b * v.d_seq + t * v.d_pos] * up : 0.f;
-        m = state.x;
-        f = slope_of(state.y * from_scaled(m, k), state.z, token < 0 ? x : d, d_H, r.g_scale * r.inv_temp);
+        m = now.state.x;
+        f = slope_of(now.state.y * from_scaled(m, k), now.state.z, token < 0 ? x : now.d_lp * up, now.d_H * up,
+                     r.g_scale * r.inv_temp);
       } else {
-        const Stats s = part_stats<kEntropy, kLanes>(part, k);
+        const Stats s = part_stats<kEntropy, kLanes>(part, V, lane, k);
         const float log_s = logf(s.s), lp = (x - s.m) * r.inv_temp - log_s;
         const float H = kEntropy ? log_s - kLn2 * s.t / s.s : 0.f;
         m = s.m;
-        if (lane == 0) {
-          if (o.logprobs) o.logprobs[at] = lp;
-          if (o.entropy) o.entropy[at] = H;
-          if (o.state) o.state[at] = {s.m, s.s * to_scaled(s.m, k), H, lp};
-        }
+        Position q = {};
         if constexpr (kOp == kPolicy) {
-          const float w = weight_of(r, mean, b, total);
-          const Position q = policy_position(p, b, at, lp, H, w);
+          const float w = weight_of(r, mean, now.b, clamped(now.length, r.T), total);
+          q = policy_position(p, now.old_lp, now.ref_lp, now.advantage, lp, H, w);
           if (lane == 0) {
-            if (o.d_logprobs) o.d_logprobs[at] = q.d_lp;
-            if (o.d_entropy) o.d_entropy[at] = q.d_H;
             const double by = w;
             sum[0] = fma(by, double(q.terms.x), sum[0]);
             if (p.kl_coef != 0.f) sum[1] = fma(by, double(q.terms.y), sum[1]);
@@ -317,15 +403,21 @@ __global__ __launch_bounds__(kLaneThreads) void lanes_kernel(Rows r, RowOut o, P
           }
           f = slope_of(s.s, H, q.d_lp, q.d_H, r.g_scale * r.inv_temp);
         }
+        if (lane == 0) {
+          if (o.logprobs) o.logprobs[at] = lp;
+          if (kOp == kScore && o.entropy) o.entropy[at] = H;
+          if (o.state) o.state[at] = {s.m, s.s * to_scaled(s.m, k), H, lp};
+          if (kOp == kPolicy && o.d_logprobs) o.d_logprobs[at] = q.d_lp;
+          if (kOp == kPolicy && o.d_entropy) o.d_entropy[at] = q.d_H;
+        }
       }
-    } else if (kOp != kGiven && lane == 0) {
+    } else if (kOp != kGiven && lane == 0 && inside) {
       leave_nothing(o, at);
     }
     if (kOp == kScore || (kOp == kPolicy && !r.g)) continue;
-    typename X::type* g = gradient_of<X>(r, b, t);
-    write_part<kEntropy>(row, part, g, lane, live, m, k, f);
-    if (token >= 0 && row.owner(token, kLanes) == lane)  // (stores of one thread to one address keep their order)
-      X::store(g + token, f.token + gradient_at<kEntropy>((x - m) * k, f));
+    if (kOp == kGiven || (kOp == kPolicy && r.g))
+      write_part<kEntropy>(part, r, from, V, live, token, x, m, k, f, stage + wave * (kWave * kChunks));
+    from = follows;
   }
   if constexpr (kOp == kPolicy) {
     for (int j = 0; j < 4; ++j) {
@@ -897,19 +989,6 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Po
 
 // ---- distillation on rows in registers --------------------------------------------------------
 
-// A barrier of the threads that share a row: of a wavefront, whose accesses keep their order, it only
-// keeps the compiler from moving them.
-template <int kThreads>
-__device__ __forceinline__ void meet() {
-  if constexpr (kThreads == kWave) {
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-  } else {
-    __syncthreads();
-  }
-}
-
 // kThreads threads a row, kEntries entries of the teacher each: a workgroup, or one of four wavefronts
 // that then take several rows.  While the row is on its way to the registers, its threads look for ids
 // that come up twice; entry j's thread writes the gradient at id j behind the others' stores, with the
@@ -1111,11 +1190,12 @@ bool launch_lanes(Call& c) {
     return true;
   };
   const int chunks = (r.V + X::kPer - 1) / X::kPer;
-  if (chunks <= 8) return go(lanes_kernel<X, kOp, kEntropy, 4, 2>, 4);
-  if (chunks <= 16) return go(lanes_kernel<X, kOp, kEntropy, 8, 2>, 8);
-  if (chunks <= 32) return go(lanes_kernel<X, kOp, kEntropy, 16, 2>, 16);
-  if (chunks <= 64) return go(lanes_kernel<X, kOp, kEntropy, 32, 2>, 32);
-  if (chunks <= 128) return go(lanes_kernel<X, kOp, kEntropy, 64, 2>, 64);
+  if (r.V < X::kPer) return false;
+  if (chunks <= 8) return go(lanes_kernel<X, kOp, kEntropy, 2, 4>, 2);
+  if (chunks <= 16) return go(lanes_kernel<X, kOp, kEntropy, 4, 4>, 4);
+  if (chunks <= 32) return go(lanes_kernel<X, kOp, kEntropy, 8, 4>, 8);
+  if (chunks <= 64) return go(lanes_kernel<X, kOp, kEntropy, 16, 4>, 16);
+  if (chunks <= 128) return go(lanes_kernel<X, kOp, kEntropy, 32, 4>, 32);
   if (chunks <= 256) return go(lanes_kernel<X, kOp, kEntropy, 64, 4>, 64);
   if (chunks <= 512) return go(lanes_kernel<X, kOp, kEntropy, 64, 8>, 64);
   return false;
