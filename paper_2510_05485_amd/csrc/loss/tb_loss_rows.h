@@ -171,11 +171,11 @@ __device__ __forceinline__ Stats joined_lanes(const Stats& mine, Join join) {
   }
 }
 
-// A barrier of the threads that share a row: of a wavefront, whose accesses keep their order, it only
+// A barrier of the threads that share a row: in a wavefront, whose accesses keep their order, it only
 // keeps the compiler from moving them.
 template <int kThreads>
 __device__ __forceinline__ void meet() {
-  if constexpr (kThreads == kWave) {
+  if constexpr (kThreads <= kWave) {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -208,7 +208,7 @@ struct Part {
   // values of chunk k, those that count elsewhere as -inf
   __device__ __forceinline__ void once(int V, int lane, int k, float* v) const {
     X::unpack(c[k], v);
-    if (V % X::kPer == 0) return;  // (the same for all rows)
+    if (V % X::kPer == 0 || k != (V - 1) / X::kPer / kLanes) return;  // (the same for all rows)
     const int again = (lane + k * kLanes) * X::kPer - (V - X::kPer);
 #pragma unroll
     for (int i = 0; i < X::kPer - 1; ++i)
@@ -255,7 +255,7 @@ template <bool kEntropy, int kLanes, typename X, int kChunks>
 __device__ __forceinline__ void write_part(const Part<X, kLanes, kChunks>& p, const Rows& r, int64_t from, int V,
                                            bool live, int token, float x, float m, float k, Slope f, u32x4* stage) {
   using T = typename X::type;
-  constexpr int kSlots = kLanes * kChunks, kSpread = kSlots < 8 ? kSlots : 8;
+  constexpr int kSlots = kLanes * kChunks, kSpread = kSlots % 8 == 0 ? 8 : kSlots % 4 == 0 ? 4 : 2;
   const int lane = threadIdx.x % kLanes, thread = threadIdx.x % kWave, row = thread / kLanes;
   auto slot_of = [](int row, int slot) { return row * kSlots + (slot ^ (row % kSpread)); };  // (other banks for other rows)
   const bool any = __any(live);
@@ -480,8 +480,9 @@ __device__ __forceinline__ Stats row_stats(const Row& row, float k, int thread, 
     const float v[1] = {X::load(row.x + e)};
     take(v, std::integral_constant<int, 1>());
   }
-  mine = joined_lanes<kEntropy, kWave>(mine, [k](const Stats& a, const Stats& b) { return joined<kEntropy>(a, b, k); });
-  if constexpr (kThreads == kWave) return mine;
+  constexpr int kLanes = kThreads && kThreads < kWave ? kThreads : kWave;
+  mine = joined_lanes<kEntropy, kLanes>(mine, [k](const Stats& a, const Stats& b) { return joined<kEntropy>(a, b, k); });
+  if constexpr (kThreads && kThreads <= kWave) return mine;
   if (thread % kWave == 0) parts[thread / kWave] = mine;
   __syncthreads();
   Stats all = parts[0];
@@ -766,7 +767,7 @@ extern __shared__ u32x4 more_chunks[];
 template <typename X, int kThreads, int kChunks, bool kMore = false>
 struct Held {
   // (a wavefront's lanes would have two values of head and rest each if it read whole lines)
-  using Row = Span<X, kThreads == kWave ? 16 : kLine>;
+  using Row = Span<X, kThreads <= kWave ? 16 : kLine>;
   static_assert(Row::kEdge <= kThreads);
   static constexpr int kSure = kChunks - (kMore ? 1 : 2);
   u32x4 c[kChunks];
@@ -809,6 +810,25 @@ struct Held {
   }
 };
 
+// Over the lanes of a wavefront that share a row, all of them or 16.
+template <int kThreads>
+__device__ __forceinline__ float lanes_max(float v) {
+  static_assert(kThreads == 16 || kThreads >= kWave);
+  if constexpr (kThreads >= kWave) return full_wave_max(v);
+  v = fmaxf(v, neighbour<1>(v));
+  v = fmaxf(v, neighbour<2>(v));
+  v = fmaxf(v, neighbour<4>(v));
+  return fmaxf(v, neighbour<8>(v));
+}
+template <int kThreads>
+__device__ __forceinline__ float lanes_sum(float v) {
+  if constexpr (kThreads >= kWave) return full_wave_sum(v);
+  v += neighbour<1>(v);
+  v += neighbour<2>(v);
+  v += neighbour<4>(v);
+  return v + neighbour<8>(v);
+}
+
 // Statistics of a wavefront's part of a row, the same in all lanes, of weights 2^(x k - M), M = scaled(m, k).
 // m need not be the largest value: any that keeps the weights in range does.  It is the largest of the
 // lanes' own, found on the packed values as signed integers: right where a lane has a value above 0, else
@@ -826,7 +846,7 @@ __device__ __forceinline__ Stats wave_stats(const typename Held<X, kThreads, kCh
 #pragma unroll
     for (int i = 0; i < X::kPer; i += 2) mine.m = max3(mine.m, v[i], v[i + 1]);
   }
-  mine.m = full_wave_max(mine.m);
+  mine.m = lanes_max<kThreads>(mine.m);
   const float M = scaled(mine.m, k);
   auto take = [&](float x) {
     const float a = fmaf(x, k, -M), w = exp2_fast(a);
@@ -851,8 +871,8 @@ __device__ __forceinline__ Stats wave_stats(const typename Held<X, kThreads, kCh
       for (int i = 0; i < X::kPer; ++i) take(v[i]);
     }
   }
-  mine.s = full_wave_sum(mine.s);
-  if (kEntropy) mine.t = full_wave_sum(mine.t);
+  mine.s = lanes_sum<kThreads>(mine.s);
+  if (kEntropy) mine.t = lanes_sum<kThreads>(mine.t);
   return mine;
 }
 __device__ __forceinline__ bool fine(const Stats& s) {
@@ -888,35 +908,35 @@ __device__ __forceinline__ void write_held(const typename Held<X, kThreads, kChu
   if (h.edge_at >= 0) X::store(g + h.edge_at, value(h.edge));
 }
 
-// Statistics of the row, in every thread, of the parts that eight wavefronts leave: one a lane, joined in
-// three steps.
+// Statistics of the row, in every thread, of the parts that four or eight wavefronts leave: one a lane,
+// joined in two or three steps.
 template <bool kEntropy, int kWaves>
 __device__ __forceinline__ Stats block_stats(const Stats* parts, float k) {
-  static_assert(kWaves == 8);
-  Stats s = parts[threadIdx.x % 8];
+  static_assert(kWaves == 8 || kWaves == 4);
+  Stats s = parts[threadIdx.x % kWaves];
   float m = s.m;
   m = fmaxf(m, neighbour<1>(m));
   m = fmaxf(m, neighbour<2>(m));
-  m = fmaxf(m, neighbour<4>(m));
+  if (kWaves == 8) m = fmaxf(m, neighbour<4>(m));
   const float d = scaled(s.m, k) - scaled(m, k), e = exp2_fast(d);
   if (kEntropy) s.t = e * (s.t + finite(d) * s.s);
   s.s *= e;
   s.s += neighbour<1>(s.s);
   s.s += neighbour<2>(s.s);
-  s.s += neighbour<4>(s.s);
+  if (kWaves == 8) s.s += neighbour<4>(s.s);
   if (kEntropy) {
     s.t += neighbour<1>(s.t);
     s.t += neighbour<2>(s.t);
-    s.t += neighbour<4>(s.t);
+    if (kWaves == 8) s.t += neighbour<4>(s.t);
   }
   auto uniform = [](float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); };
   return {uniform(m), uniform(s.s), kEntropy ? uniform(s.t) : 0.f};
 }
 
 // One workgroup a row; the score, and the policy loss.
-template <typename X, int kOp, bool kEntropy, int kChunks, bool kMore = false>
-__global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Policy p, Mean mean) {
-  constexpr int kWaves = kHeldThreads / kWave;
+template <typename X, int kOp, bool kEntropy, int kThreads, int kChunks, bool kMore = false>
+__global__ __launch_bounds__(kThreads) void held_kernel(Rows r, RowOut o, Policy p, Mean mean) {
+  constexpr int kWaves = kThreads / kWave;
   __shared__ Stats parts[kWaves];
   __shared__ int totals[kWaves];
   const int64_t at = row_of_group(blockIdx.x, int64_t(r.B) * r.T);
@@ -933,7 +953,7 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Po
   const Line<X> row(row_of<X>(r, b, t), r.V);
   // (what comes first is waited for first: not behind the whole row)
   const int token = take_token(r, b, t, first), share = kOp == kPolicy ? share_of_total(r, mean) : 0;
-  Held<X, kHeldThreads, kChunks, kMore> h;
+  Held<X, kThreads, kChunks, kMore> h;
   h.load(row, threadIdx.x);
   const float x = token < 0 ? __uint_as_float(kNan) : X::load(row.x + token);
   const float k = r.inv_temp * kLog2e;
@@ -983,39 +1003,41 @@ __global__ __launch_bounds__(kHeldThreads) void held_kernel(Rows r, RowOut o, Po
     return;
   }
   write_held<kEntropy>(row, h, g, threadIdx.x, s.m, k, f);
-  if (token >= 0 && row.owner(token, kHeldThreads) == int(threadIdx.x))
+  if (token >= 0 && row.owner(token, kThreads) == int(threadIdx.x))
     X::store(g + token, f.token + gradient_at<kEntropy>(fmaf(x, k, -scaled(s.m, k)), f));
 }
 
 // ---- distillation on rows in registers --------------------------------------------------------
 
-// kThreads threads a row, kEntries entries of the teacher each: a workgroup, or one of four wavefronts
-// that then take several rows.  While the row is on its way to the registers, its threads look for ids
+// kThreads threads a row, kEntries entries of the teacher each: a workgroup, or a wavefront or 16 lanes of
+// one that then take several rows.  While the row is on its way to the registers, its threads look for ids
 // that come up twice; entry j's thread writes the gradient at id j behind the others' stores, with the
 // sum of the probabilities of this id if it does.
 template <typename X, int kThreads, int kChunks, int kEntries, bool kMore = false>
-__global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void distill_kernel(Rows r, RowOut o, Mean mean,
+__global__ __launch_bounds__(kThreads <= kWave ? kLaneThreads : kThreads) void distill_kernel(Rows r, RowOut o, Mean mean,
                                                                                            Teacher q) {
-  constexpr int kTeams = kThreads == kWave ? 4 : 1, kWaves = kThreads / kWave, kRoom = kThreads * kEntries;
+  constexpr bool kAlone = kThreads > kWave;  // (the workgroup has one row)
+  constexpr int kTeams = kAlone ? 1 : kLaneThreads / kThreads, kWaves = kAlone ? kThreads / kWave : 1;
+  constexpr int kLanes = kAlone ? kWave : kThreads, kRoom = kThreads * kEntries;
   __shared__ __attribute__((aligned(16))) int ids[kTeams][kRoom];
   __shared__ __attribute__((aligned(16))) float shares[kTeams][kRoom];
   __shared__ Stats parts[kTeams][kWaves], teachers[kTeams][kWaves];
   __shared__ float losses[kTeams][kWaves];
-  __shared__ int totals[kTeams * kWaves];
+  __shared__ int totals[kAlone ? kWaves : kLaneThreads / kWave];
   const int team = threadIdx.x / kThreads, thread = threadIdx.x % kThreads, wave = thread / kWave;
   const bool first = thread == 0;
   const int64_t rows = int64_t(r.B) * r.T;
   const float k = r.inv_temp * kLog2e;
   int total = 0;
-  if constexpr (kThreads == kWave) {
+  if constexpr (!kAlone) {
     const int part = full_wave_sum(share_of_total(r, mean));
-    if (first) totals[team] = part;
+    if (threadIdx.x % kWave == 0) totals[threadIdx.x / kWave] = part;
     __syncthreads();
-    for (int w = 0; w < kTeams; ++w) total += totals[w];
+    for (int w = 0; w < kLaneThreads / kWave; ++w) total += totals[w];
   }
   double sum = 0;
   auto take_row = [&](int64_t i) {
-    const int64_t at = kThreads == kWave ? i : row_of_group(i, rows);
+    const int64_t at = kAlone ? row_of_group(i, rows) : i;
     const At pos = position(r, at);
     const int b = pos.b, t = pos.t;
     if (first && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
@@ -1043,7 +1065,7 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
         wide[e] = load_id(q.ids, q.long_ids, at * q.K + j);
       }
     }
-    const int share = kThreads == kWave ? 0 : share_of_total(r, mean);
+    const int share = kAlone ? share_of_total(r, mean) : 0;
     Held<X, kThreads, kChunks, kMore> h;
     h.load(row, thread);
     Stats teacher = {kLowest, 0.f, 0.f};
@@ -1064,8 +1086,8 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
     if (wrong && r.status) atomicOr(r.status, TB_DEV_TOKEN_RANGE);
 #pragma unroll
     for (int e = 0; e < kEntries; ++e) teacher.s += exp2_fast((v[e] - teacher.m) * k);
-    teacher = joined_lanes<false, kWave>(teacher, [k](const Stats& a, const Stats& c) { return joined<false>(a, c, k); });
-    if constexpr (kThreads != kWave) {
+    teacher = joined_lanes<false, kLanes>(teacher, [k](const Stats& a, const Stats& c) { return joined<false>(a, c, k); });
+    if constexpr (kAlone) {
       const int part = full_wave_sum(share);
       if (thread % kWave == 0) {
         totals[wave] = part;
@@ -1087,7 +1109,7 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
     }
     const Stats mine = wave_stats<false>(row, h, thread, k);
     Stats s = mine;
-    if constexpr (kThreads != kWave) {
+    if constexpr (kAlone) {
       if (thread % kWave == 0) parts[team][wave] = mine;
       __syncthreads();
       s = block_stats<false, kWaves>(parts[team], k);
@@ -1113,7 +1135,7 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
       x[e] = z;
       shares[team][thread + e * kThreads] = share_e;
     }
-    d = wave_sum(d);
+    d = lanes_sum<kThreads>(d);
     if (thread % kWave == 0) losses[team][wave] = d;
     const float w = teacher.s == 0.f ? 0.f : weight_of(r, mean, b, total);
     Slope f = {0.f, 0.f, q.tau * w * r.g_scale};
@@ -1145,7 +1167,7 @@ __global__ __launch_bounds__(kThreads == kWave ? 4 * kWave : kThreads) void dist
     sum += double(w) * d;
   };
   // (a workgroup takes one row: what lives from row to row would cost it registers)
-  if constexpr (kThreads == kWave) {
+  if constexpr (!kAlone) {
     for (int64_t i = int64_t(blockIdx.x) * kTeams + team; i < rows; i += int64_t(gridDim.x) * kTeams) {
       take_row(i);
       meet<kThreads>();  // (before the next row takes the shared memory)
@@ -1172,8 +1194,8 @@ int grid_of(const Rows& r) {
 }
 int threads_of(const Rows& r, int per) {
   const int chunks = (r.V + per - 1) / per;
-  const int t = (chunks + kWave - 1) / kWave * kWave;
-  return t > 512 ? 512 : t;
+  const int t = (chunks / 4 + kWave - 1) / kWave * kWave;  // (four chunks a thread at least, where there are so many)
+  return t > 512 ? 512 : t < kWave ? kWave : t;
 }
 
 // Workgroups that the card holds at a time take all rows: 8 of 4 wavefronts on each of 256 units.
@@ -1191,13 +1213,11 @@ bool launch_lanes(Call& c) {
   };
   const int chunks = (r.V + X::kPer - 1) / X::kPer;
   if (r.V < X::kPer) return false;
-  if (chunks <= 8) return go(lanes_kernel<X, kOp, kEntropy, 2, 4>, 2);
-  if (chunks <= 16) return go(lanes_kernel<X, kOp, kEntropy, 4, 4>, 4);
-  if (chunks <= 32) return go(lanes_kernel<X, kOp, kEntropy, 8, 4>, 8);
-  if (chunks <= 64) return go(lanes_kernel<X, kOp, kEntropy, 16, 4>, 16);
-  if (chunks <= 128) return go(lanes_kernel<X, kOp, kEntropy, 32, 4>, 32);
-  if (chunks <= 256) return go(lanes_kernel<X, kOp, kEntropy, 64, 4>, 64);
-  if (chunks <= 512) return go(lanes_kernel<X, kOp, kEntropy, 64, 8>, 64);
+#define LANES(lanes, n) \
+  if (chunks <= lanes * n) return go(lanes_kernel<X, kOp, kEntropy, lanes, n>, lanes);
+  LANES(2, 3) LANES(2, 4) LANES(4, 3) LANES(4, 4) LANES(8, 3) LANES(8, 4) LANES(16, 3) LANES(16, 4) LANES(32, 3) LANES(32, 4)
+  LANES(64, 3) LANES(64, 4) LANES(64, 5) LANES(64, 6) LANES(64, 7) LANES(64, 8)
+#undef LANES
   return false;
 }
 
@@ -1224,29 +1244,36 @@ bool launch_held(Call& c) {
       kernel<<<int(rows), kHeldThreads, bytes, c.stream>>>(r, c.out, c.policy, c.mean);
       return true;
     };
-    return need - kFewer <= kMostMore ? go(held_kernel<X, kPolicy, kEntropy, kFewer, true>, kFewer)
-                                      : go(held_kernel<X, kPolicy, kEntropy, kMostHeld, true>, kMostHeld);
+    return need - kFewer <= kMostMore ? go(held_kernel<X, kPolicy, kEntropy, kHeldThreads, kFewer, true>, kFewer)
+                                      : go(held_kernel<X, kPolicy, kEntropy, kHeldThreads, kMostHeld, true>, kMostHeld);
   }
 #define HELD(n) \
-  case n: held_kernel<X, kOp, kEntropy, n><<<int(rows), kHeldThreads, 0, c.stream>>>(r, c.out, c.policy, c.mean); return true;
+  case n: held_kernel<X, kOp, kEntropy, kHeldThreads, n><<<int(rows), kHeldThreads, 0, c.stream>>>(r, c.out, c.policy, c.mean); return true;
+#define HALF(n) \
+  case n: held_kernel<X, kOp, kEntropy, kHeldThreads / 2, n><<<int(rows), kHeldThreads / 2, 0, c.stream>>>(r, c.out, c.policy, c.mean); return true;
+  // rows of up to 2048 chunks by half as many threads, which more of them keep busy (policy
+  // loss on 26840 rows of 5000 values in bfloat16: 170 us with all, 107 so)
+  switch ((r.V / X::kPer + kHeldThreads / 2 - 1) / (kHeldThreads / 2)) { HALF(1) HALF(2) HALF(3) HALF(4) HALF(5) HALF(6) HALF(7) HALF(8) }
   switch (need) {
     HELD(1) HELD(2) HELD(3) HELD(4) HELD(5) HELD(6) HELD(7) HELD(8) HELD(9) HELD(10) HELD(11) HELD(12) HELD(13) HELD(14)
     HELD(15) HELD(16) HELD(17) HELD(18) HELD(19) HELD(20) HELD(21) HELD(22) HELD(23) HELD(24) HELD(25) HELD(26) HELD(27)
     HELD(28) HELD(29) HELD(30) HELD(31) HELD(32)
   }
+#undef HALF
 #undef HELD
   return false;
 }
 
-// A wavefront a row of up to 512 chunks, a workgroup one of more.
-template <typename X, int kEntries>
-bool launch_distill_wave(Call& c) {
+// 16 lanes of a wavefront a row of up to 128 chunks, a wavefront one of up to 512, a workgroup one of more.
+template <typename X, int kThreads, int kEntries>
+bool launch_distill_lanes(Call& c) {
   const Rows& r = c.rows;
-  const int64_t groups = (int64_t(r.B) * r.T + 3) / 4;
+  constexpr int kTeams = kLaneThreads / kThreads;
+  const int64_t groups = (int64_t(r.B) * r.T + kTeams - 1) / kTeams;
   c.groups = int(groups < kLaneGroups ? groups : kLaneGroups);
 #define HELD(n) \
-  case n: distill_kernel<X, kWave, n, kEntries><<<c.groups, 4 * kWave, 0, c.stream>>>(r, c.out, c.mean, c.teacher); return true;
-  switch ((r.V / X::kPer + kWave - 1) / kWave) { HELD(1) HELD(2) HELD(3) HELD(4) HELD(5) HELD(6) HELD(7) HELD(8) }
+  case n: distill_kernel<X, kThreads, n, kEntries><<<c.groups, kLaneThreads, 0, c.stream>>>(r, c.out, c.mean, c.teacher); return true;
+  switch ((r.V / X::kPer + kThreads - 1) / kThreads) { HELD(1) HELD(2) HELD(3) HELD(4) HELD(5) HELD(6) HELD(7) HELD(8) }
 #undef HELD
   return false;
 }
@@ -1268,6 +1295,10 @@ bool launch_distill_block(Call& c) {
     return need - kFewer <= kMostMore ? go(distill_kernel<X, kHeldThreads, kFewer, kEntries, true>, kFewer)
                                       : go(distill_kernel<X, kHeldThreads, kMostHeld, kEntries, true>, kMostHeld);
   }
+#define HALF(n) \
+  case n: distill_kernel<X, kHeldThreads / 2, n, 2 * kEntries><<<c.groups, kHeldThreads / 2, 0, c.stream>>>(r, c.out, c.mean, c.teacher); return true;
+  switch ((r.V / X::kPer + kHeldThreads / 2 - 1) / (kHeldThreads / 2)) { HALF(1) HALF(2) HALF(3) HALF(4) HALF(5) HALF(6) HALF(7) HALF(8) }
+#undef HALF
   switch (need) {
     HELD(1) HELD(2) HELD(3) HELD(4) HELD(5) HELD(6) HELD(7) HELD(8) HELD(9) HELD(10) HELD(11) HELD(12) HELD(13) HELD(14)
     HELD(15) HELD(16) HELD(17) HELD(18) HELD(19) HELD(20) HELD(21) HELD(22) HELD(23) HELD(24) HELD(25) HELD(26) HELD(27)
@@ -1280,10 +1311,10 @@ template <typename X>
 bool launch_distill(Call& c) {
   if (c.rows.V < 2 * X::kPer) return false;
   const int K = c.teacher.K;
-  return K <= 64    ? launch_distill_wave<X, 1>(c) || launch_distill_block<X, 1>(c)
-         : K <= 256 ? launch_distill_wave<X, 4>(c) || launch_distill_block<X, 1>(c)
-         : K <= 512 ? launch_distill_wave<X, 16>(c) || launch_distill_block<X, 1>(c)
-                    : launch_distill_wave<X, 16>(c) || launch_distill_block<X, 2>(c);
+  if (K <= 16 && launch_distill_lanes<X, 16, 1>(c)) return true;
+  if (K <= 64) return launch_distill_lanes<X, 16, 4>(c) || launch_distill_lanes<X, kWave, 1>(c) || launch_distill_block<X, 1>(c);
+  if (K <= 256) return launch_distill_lanes<X, kWave, 4>(c) || launch_distill_block<X, 1>(c);
+  return launch_distill_lanes<X, kWave, 16>(c) || (K <= 512 ? launch_distill_block<X, 1>(c) : launch_distill_block<X, 2>(c));
 }
 
 template <typename X, int kOp, bool kEntropy>
