@@ -17,10 +17,10 @@
  *     any other overlap of the two is refused.
  *   - Arrays over positions are contiguous [B, T]; tokens may have a row stride of their own.
  *   - Position (b, t) counts iff t < lengths[b] (or lengths is NULL) and mask[b, t] is not 0 (or mask
- *     is NULL).  What stands at other positions -- logits, tokens, values -- is not read, whatever it
- *     is; log-probabilities, entropies and gradients there are 0.
+ *     is NULL).  What stands at other positions -- logits, tokens, values -- has no part in anything,
+ *     whatever it is; log-probabilities, entropies and gradients there are 0.
  *   - Arithmetic is in float32, sums over positions in float64; gradients are rounded once to the
- *     logits' type.  A logit of -inf is a token that cannot be: it has probability and gradient 0.  A
+ *     logits' type.  The order of a row's sum goes by the row's length and by its address modulo 128.  A logit of -inf is a token that cannot be: it has probability and gradient 0.  A
  *     row that has no finite logit, or one of +inf or NaN, has no distribution: its values are NaN.
  *   - Results do not depend on the order in which workgroups run.
  *   - Problems that the host can see come back as tb_status_t before any work is enqueued.  A token
@@ -62,8 +62,8 @@ typedef struct tb_gradient {
   float scale;                    /* the gradient is that of scale * loss */
 } tb_gradient_t;
 
-/* What the backward pass needs of a row: largest logit, sum of exp(z - largest z), entropy (0 where it
- * was not asked for), log-probability of the token.  float32 [B, T, 4]. */
+/* What the backward pass needs of a row: a reference logit m, the sum of exp(z - m / temperature), the
+ * entropy (0 where it was not asked for), the log-probability of the token.  float32 [B, T, 4]. */
 enum { TB_ROW_STATE = 4 };
 
 /* Log-probabilities of the tokens, and entropies where `entropy` is not NULL: float32 [B, T].

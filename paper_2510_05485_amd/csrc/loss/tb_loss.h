@@ -79,7 +79,9 @@ struct Given {  // the backward pass: cotangents of lp and H (or of the row's di
 // ---- types ------------------------------------------------------------------------------------
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef u32x4 u32x4_any __attribute__((aligned(2)));  // a 16-byte access at any address of a value
+// Accesses of 16 bytes to rows, which are arrays of values: at any address of a value, and at multiples of 16.
+typedef u32x4 u32x4_any __attribute__((aligned(2), may_alias));
+typedef u32x4 u32x4_at16 __attribute__((aligned(16), may_alias));
 
 struct F32 {
   template <int kFirst>
@@ -238,7 +240,7 @@ struct Span {
     chunks = (values - head) / X::kPer;
   }
   __device__ __forceinline__ int at(int chunk) const { return head + chunk * X::kPer; }
-  __device__ __forceinline__ u32x4 chunk(int i) const { return *reinterpret_cast<const u32x4*>(x + at(i)); }
+  __device__ __forceinline__ u32x4 chunk(int i) const { return *reinterpret_cast<const u32x4_at16*>(x + at(i)); }
   // the j-th value of head and rest, or -1
   __device__ __forceinline__ int edge(int j) const {
     if (j < head) return j;

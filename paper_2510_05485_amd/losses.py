@@ -23,7 +23,7 @@ Common arguments
   grad_scale   the gradient is that of grad_scale * loss (loss scaling, gradient accumulation)
   status       int32 [1] on the GPU; TB_DEV_TOKEN_RANGE / TB_DEV_LENGTH_RANGE are OR-ed into it
 
-Positions that do not count are not read, whatever stands there; what is returned for them is 0.
+What stands at positions that do not count has no part in anything; what is returned for them is 0.
 Everything runs on the current stream of the logits' GPU, and nothing synchronises.  See
 include/tensorloss.h for the formulas and for what wrong ids and infinite logits give.
 """
