@@ -114,17 +114,19 @@ template <typename T>
 T* in(void* workspace, size_t offset) {
   return reinterpret_cast<T*>(static_cast<char*>(workspace) + offset);
 }
-// What a mean divides by is added up by every workgroup while its row is on its way, from the lengths, or
-// from the numbers that a launch (4 us) counts in a mask; beyond so many numbers a launch more leaves the
-// weights.  (Policy loss on 4096 sequences of 512 positions of 64 logits: 12 us less.)
-constexpr int kMostParts = 8192;
+// What a mean divides by is added up by every workgroup while its row is on its way, from the lengths, from
+// the mask of few positions, or from the numbers that a launch (4 us) counts in a mask; beyond so many
+// numbers a launch more leaves the weights.  (Policy loss on 4096 sequences of 512 positions of 64 logits: 12 us less.)
+constexpr int kMostParts = 8192, kMostMasked = 4096;
 hipError_t set_mean(Call& c, int average, const Workspace& w, void* workspace) {
   const Rows& r = c.rows;
   int32_t* n = in<int32_t>(workspace, w.counts);
   c.mean = {nullptr, nullptr, r.B, average};
   if (average == TB_SUM || (!r.mask && !r.lengths)) return hipSuccess;
-  if (r.mask && (average == TB_MEAN_TOKENS || r.B == 1)) {
-    c.mean = {nullptr, n, kCountParts, TB_MEAN_TOKENS};  // (one sequence's mean is that of its positions)
+  if (r.mask && (average == TB_MEAN_TOKENS || r.B == 1)) {  // (one sequence's mean is that of its positions)
+    c.mean = {nullptr, nullptr, 0, TB_MEAN_TOKENS};
+    if (r.B * r.T <= kMostMasked) return hipSuccess;
+    c.mean = {nullptr, n, kCountParts, TB_MEAN_TOKENS};
     return run_part_counts(r, n, c.stream);
   }
   if (r.mask) {

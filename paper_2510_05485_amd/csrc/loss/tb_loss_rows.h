@@ -112,7 +112,15 @@ __device__ __forceinline__ int share_of_total(const Rows& r, const Mean& mean) {
   constexpr int kAhead = 8;  // loads under way
   const int32_t* from = mean.n ? mean.n : r.lengths;
   int n = 0;
-  if (mean.weight || mean.average == TB_SUM || !from) return n;
+  if (mean.weight || mean.average == TB_SUM) return n;
+  if (r.mask && !mean.n) {  // (few positions)
+    for (int i = threadIdx.x; i < r.B * r.T; i += blockDim.x) {
+      const At pos = position(r, i);
+      n += counts(r, pos.b, pos.t);
+    }
+    return n;
+  }
+  if (!from) return n;
   const int most = mean.n ? INT32_MAX : r.T, threads = blockDim.x;
   for (int i = threadIdx.x; i < mean.parts; i += kAhead * threads) {
     int m[kAhead];
@@ -129,7 +137,7 @@ __device__ __forceinline__ int share_of_total(const Rows& r, const Mean& mean) {
 __device__ __forceinline__ float weight_of(const Rows& r, const Mean& mean, int b, int length, int total) {
   if (mean.weight) return mean.weight[b];
   if (mean.average == TB_SUM) return 1.f;
-  if (!mean.n && !r.lengths) total = mean.average == TB_MEAN_TOKENS ? r.B * r.T : r.B;
+  if (!mean.n && !r.lengths && !r.mask) total = mean.average == TB_MEAN_TOKENS ? r.B * r.T : r.B;
   if (mean.average == TB_MEAN_TOKENS) return 1.f / float(total);
   return reciprocal(float(total) * float(mean.n ? mean.n[b] : length));
 }
