@@ -37,7 +37,7 @@ Workspace workspace_of(int64_t B, int64_t T) {
   const int64_t groups = B * T < kMostGroups ? B * T : kMostGroups;
   w.partial = take(8 * 4 * size_t(groups > B ? groups : B));
   w.state = take(16 * B * T);  // (of pairs only, as what follows)
-  w.lp = take(4 * B * T);
+  w.lp = take(8 * B * T);
   w.d_sequence = take(4 * B);
   w.bytes = at;
   return w;
@@ -223,7 +223,7 @@ extern "C" int tensorloss_policy(const tb_logits_t* logits, const tb_positions_t
   double *partial = in<double>(workspace, w.partial), *more = in<double>(workspace, w.more);
   if (empty(r)) return done(run_terms(0, partial, more, terms, 4, c.stream));
   c.rows.status = status;
-  c.out = {logprobs, nullptr, reinterpret_cast<float4*>(row_state), d_logprobs, d_entropy, partial};
+  c.out = {logprobs, nullptr, nullptr, reinterpret_cast<float4*>(row_state), d_logprobs, d_entropy, partial};
   c.policy = {policy->old_logprobs, policy->ref_logprobs, policy->advantages, policy->each, policy->clip_low,
               policy->clip_high, policy->kl_coef, policy->entropy_coef};
   c.entropy = policy->entropy_coef != 0.f;
@@ -254,10 +254,10 @@ extern "C" int tensorloss_preference(const tb_logits_t* logits, const tb_positio
   if (!empty(r)) {
     r.g = nullptr;
     r.status = status;
-    c.out = {in<float>(workspace, w.lp), nullptr, state, nullptr, nullptr, nullptr};
+    c.out = {nullptr, nullptr, in<double>(workspace, w.lp), state, nullptr, nullptr, nullptr};
     if (run_rows(kScore, c) != hipSuccess) return TB_ERR_HIP;
   }
-  const Pairs pairs = {preference->ref_logprobs, in<float>(workspace, w.lp), terms, sequence_logprobs, margins, d_sequence,
+  const Pairs pairs = {preference->ref_logprobs, in<double>(workspace, w.lp), terms, sequence_logprobs, margins, d_sequence,
                        in<double>(workspace, w.partial), preference->kind, preference->beta, preference->label_smoothing};
   if (run_pairs(r, pairs, c.stream) != hipSuccess) return TB_ERR_HIP;
   if (!g || empty(r)) return TB_OK;
@@ -282,7 +282,7 @@ extern "C" int tensorloss_distill(const tb_logits_t* logits, const tb_positions_
   double *partial = in<double>(workspace, w.partial), *more = in<double>(workspace, w.more);
   if (empty(r)) return done(run_terms(0, partial, more, terms, 1, c.stream));
   c.rows.status = status;
-  c.out = {row_loss, nullptr, reinterpret_cast<float4*>(row_state), d_row, nullptr, partial};
+  c.out = {row_loss, nullptr, nullptr, reinterpret_cast<float4*>(row_state), d_row, nullptr, partial};
   c.teacher = teacher_of(*teacher, r);
   if (set_mean(c, teacher->average, w, workspace) != hipSuccess || run_rows(kDistill, c) != hipSuccess)
     return TB_ERR_HIP;

@@ -44,7 +44,8 @@ constexpr int kMoreSums = 256;
 hipError_t run_terms(int64_t groups, const double* partial, double* more, float* terms, int n, hipStream_t stream);
 
 struct Pairs {
-  const float *ref_lp, *lp;  // [B, T]
+  const float* ref_lp;  // [B, T]
+  const double* lp;     // [B, T]
   float *terms, *sequence_lp, *margins, *d_sequence;
   double* partial;  // [B / 2, 3]
   int kind;

@@ -98,9 +98,9 @@ __device__ __forceinline__ Sequence sequence_part(const Rows& r, const Pairs& p,
   for (int t = thread; t < length; t += threads) {
     const int64_t at = b * r.T + t;
     if (r.mask && !r.mask[at]) continue;
-    const float lp = p.lp[at];
+    const double lp = p.lp[at];
     s.lp += lp;
-    s.d += double(lp) - p.ref_lp[at];
+    s.d += lp - p.ref_lp[at];
     s.n += 1;
   }
   return {wave_sum(s.lp), wave_sum(s.d), wave_sum(s.n)};
