@@ -227,7 +227,7 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // kAlign, `chunks` chunks of 16 bytes, and the rest.  Head and rest are at most kEdge values together;
 // chunk i and the i-th of them are thread i's (of a workgroup, or of the lanes that share a row).
 // Lines of 128 bytes where a wavefront or more reads a row (its request of 1 KB then touches eight lines
-// and not nine: a tenth less time on rows of 50257 values), 16 bytes where a few lanes do.
+// and not nine: 2 % less time on rows of 50257 values), 16 bytes where a few lanes do.
 constexpr int kLine = 128;
 template <typename X, int kAlign>
 struct Span {
@@ -298,8 +298,8 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
-// Sum over a wavefront, all lanes active: two butterflies' worth of steps inside rows of 16 lanes, then
-// each row's into the next ones'; the last lane has all of it.
+// Sum over a wavefront, all lanes active: four steps inside rows of 16 lanes, then each row's into the next
+// ones'; the last lane has all of it.
 template <int kCtrl, int kRows = 0xf>
 __device__ __forceinline__ float dpp_or(float old, float v) {
   return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(old), __float_as_int(v), kCtrl, kRows, 0xf, false));

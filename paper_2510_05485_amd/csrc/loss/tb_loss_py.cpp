@@ -1,8 +1,8 @@
 // Host side of a loss called from Python: checks the tensors, fills in the C ABI's structs, allocates
 // outputs and workspace and calls the library, in one step.  Like tb_host.cpp: every function returns
 // None for whatever is not the plain case, and the general way in losses.py then converts, or raises the
-// error that says what is wrong.  A policy loss on 16 x 32 positions takes the GPU 20 us; marshalling it
-// in Python took the host 33 us, here it takes 9 with its two launches.
+// error that says what is wrong.  A policy loss on 16 x 32 positions, 18 us of work for the GPU, took 40 us
+// a call with the marshalling in Python; one token's log-probability 14.9, and 5.2 so.
 #include <Python.h>
 
 #include <c10/hip/HIPStream.h>

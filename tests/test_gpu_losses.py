@@ -479,6 +479,34 @@ def test_differences():
             assert abs(float((r.grad.double() * u).sum()) - want) < 1e-2
 
 
+@pytest.mark.parametrize("B,T,V", [(5000, 61, 33), (2500, 121, 200), (43000, 100, 3)])
+def test_more_rows_than_workgroups(B, T, V):
+    """Workgroups that take row after row: what a row gives does not depend on the rows around it."""
+    g = torch.Generator(device=DEV).manual_seed(V)
+    x = torch.randn(B, T, V, generator=g, device=DEV).to(torch.bfloat16)
+    tokens = torch.randint(0, V, (B, T), generator=g, device=DEV)
+    lengths = torch.randint(0, T + 1, (B,), generator=g, device=DEV, dtype=torch.int32)
+    old, a = -3 + torch.randn(B, T, generator=g, device=DEV), torch.randn(B, generator=g, device=DEV)
+    ids, teacher = torch.randint(0, V, (B, T, 3), generator=g, device=DEV), torch.randn(B, T, 3, generator=g, device=DEV)
+
+    def found(s):
+        n = lengths[s]
+        r = tb.policy_loss_grad(x[s], tokens[s], old[s], a[s], lengths=n, average="sum", entropy_coef=0.1)
+        q = tb.distillation_loss_grad(x[s], ids[s], teacher[s], lengths=n, average="sum")
+        leaf = x[s].clone().requires_grad_()
+        lp = tb.token_logprobs(leaf, tokens[s], lengths=n)
+        return [r.grad, r.logprobs, q.grad, q.row_loss, lp.detach(), torch.autograd.grad(lp, leaf, old[s])[0]], r.loss, q.loss
+    whole, loss, d_loss = found(slice(0, B))
+    parts = [found(slice(i, min(i + 704, B))) for i in range(0, B, 704)]   # (whole lines: rows keep their places in them)
+    for k, w in enumerate(whole):
+        assert torch.equal(w, torch.cat([p[0][k] for p in parts]))
+    for one, other in ((loss, [p[1] for p in parts]), (d_loss, [p[2] for p in parts])):
+        assert abs(float(one) - sum(map(float, other))) <= 1e-6 * (sum(abs(float(v)) for v in other) + 1)
+    rows = slice(B // 3, B // 3 + 3)
+    want = ref.policy(x[rows], tokens[rows], old[rows], a[rows], None, lengths[rows], None, average="sum", entropy_coef=0.1)
+    near(whole[1][rows], want[2], LP)
+
+
 def test_offsets_beyond_32_bits():
     V, far = 1031, (1 << 31) + 12345
     base = torch.empty(far + 3 * V, dtype=torch.bfloat16, device=DEV)
