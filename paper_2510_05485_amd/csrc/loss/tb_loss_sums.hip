@@ -136,27 +136,31 @@ __device__ __forceinline__ Pair pair_values(const Pairs& p, int pairs, int i, Se
   return {loss, margin};
 }
 
-// One workgroup a pair.
+// One workgroup a pair; several pairs where there are more than a launch may have workgroups.
 __global__ __launch_bounds__(kThreads) void pair_kernel(Rows r, Pairs p) {
   __shared__ Sequence part[2][kWaves];
-  const int pairs = r.B / 2, i = blockIdx.x;
-  for (int side = 0; side < 2; ++side) {
-    const Sequence s = sequence_part(r, p, i + int64_t(side) * pairs, threadIdx.x, kThreads);
-    if (threadIdx.x % kWave == 0) part[side][threadIdx.x / kWave] = s;
-  }
-  __syncthreads();
-  if (threadIdx.x) return;
-  Sequence s[2] = {};
-  for (int side = 0; side < 2; ++side)
-    for (int w = 0; w < kWaves; ++w) {
-      s[side].lp += part[side][w].lp;
-      s[side].d += part[side][w].d;
-      s[side].n += part[side][w].n;
+  const int pairs = r.B / 2;
+  for (int i = blockIdx.x; i < pairs; i += gridDim.x) {
+    for (int side = 0; side < 2; ++side) {
+      const Sequence s = sequence_part(r, p, i + int64_t(side) * pairs, threadIdx.x, kThreads);
+      if (threadIdx.x % kWave == 0) part[side][threadIdx.x / kWave] = s;
     }
-  const Pair v = pair_values(p, pairs, i, s[0], s[1]);
-  p.partial[3 * i] = v.loss;
-  p.partial[3 * i + 1] = v.margin > 0;
-  p.partial[3 * i + 2] = v.margin;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      Sequence s[2] = {};
+      for (int side = 0; side < 2; ++side)
+        for (int w = 0; w < kWaves; ++w) {
+          s[side].lp += part[side][w].lp;
+          s[side].d += part[side][w].d;
+          s[side].n += part[side][w].n;
+        }
+      const Pair v = pair_values(p, pairs, i, s[0], s[1]);
+      p.partial[3 * int64_t(i)] = v.loss;
+      p.partial[3 * int64_t(i) + 1] = v.margin > 0;
+      p.partial[3 * int64_t(i) + 2] = v.margin;
+    }
+    __syncthreads();  // (before the next pair's parts)
+  }
 }
 
 // All pairs in one workgroup, a wavefront a sequence, and the means over them.
@@ -228,7 +232,7 @@ hipError_t run_pairs(const Rows& r, const Pairs& p, hipStream_t stream) {
     few_pairs_kernel<<<1, 1024, 0, stream>>>(r, p);
     return hipGetLastError();
   }
-  if (pairs) pair_kernel<<<pairs, kThreads, 0, stream>>>(r, p);
+  if (pairs) pair_kernel<<<int(pairs < kMostGroups ? pairs : kMostGroups), kThreads, 0, stream>>>(r, p);
   sum_kernel<<<1, 1024, 0, stream>>>(pairs, p.partial, 3, 3, pairs ? 1.0 / pairs : 0.0, nullptr, p.terms);
   return hipGetLastError();
 }

@@ -507,6 +507,24 @@ def test_more_rows_than_workgroups(B, T, V):
     near(whole[1][rows], want[2], LP)
 
 
+def test_more_pairs_than_a_launch_has_threads():
+    """2^24 pairs of single positions: a workgroup of 256 each would be 2^32 threads."""
+    B, V = 1 << 25, 8
+    g = torch.Generator(device=DEV).manual_seed(2)
+    x = torch.randn(B, 1, V, generator=g, device=DEV).to(torch.bfloat16)
+    tokens = torch.randint(0, V, (B, 1), generator=g, device=DEV, dtype=torch.int32)
+    reference = -2 + torch.randn(B, 1, generator=g, device=DEV)
+    r = tb.preference_loss_grad(x, tokens, reference, grad_scale=float(B))
+    for rows in (slice(0, 50), slice(B // 4 - 7, B // 4 + 50), slice(B // 2 - 50, B // 2)):
+        pair = torch.arange(B, device=DEV)[rows]
+        both = torch.cat([pair, pair + B // 2])
+        _, grad, sums, margins = ref.preference(x[both], tokens[both], reference[both])
+        near(r.margins[pair], margins, 2 * LP)
+        near(r.sequence_logprobs[both], sums, LP)
+        near_gradient(r.grad[both].double() / 2, grad * len(pair), 1.0, torch.bfloat16)
+    assert abs(float(r.loss) - float(torch.nn.functional.softplus(-0.1 * r.margins.double()).mean())) < 1e-6
+
+
 def test_offsets_beyond_32_bits():
     V, far = 1031, (1 << 31) + 12345
     base = torch.empty(far + 3 * V, dtype=torch.bfloat16, device=DEV)
