@@ -64,11 +64,10 @@ struct Call {
     *to = t->data_ptr<float>();
     return true;
   }
-  bool take(PyObject* logits_, PyObject* tokens_, PyObject* lengths_, PyObject* mask_, PyObject* temperature_,
-            PyObject* status_) {
-    x = tensor(logits_);
+  bool take_rows(const at::Tensor* t) {
+    x = t;
     if (!x || !x->is_cuda() || x->layout() != at::kStrided || (x->dim() != 2 && x->dim() != 3)) return false;
-    if (!type_of(x->scalar_type(), &logits.type) || !take_float(temperature_, &logits.temperature)) return false;
+    if (!type_of(x->scalar_type(), &logits.type)) return false;
     const auto s = c10::hip::getCurrentHIPStream();
     if (s.device_index() != x->device().index()) return false;
     stream = static_cast<void*>(s.stream());
@@ -81,31 +80,52 @@ struct Call {
     logits.B = int32_t(B);
     logits.T = int32_t(T);
     logits.V = int32_t(V);
-    if (tokens_) {
-      const at::Tensor* t = tensor(tokens_);
-      if (!here(t) || !id_type(t->scalar_type()) || t->dim() != x->dim() - 1 || t->size(-1) != T ||
-          (!packed && t->size(0) != B) || (T > 1 && t->stride(-1) != 1))
-        return false;
-      tokens = t;
-      at.tokens = t->data_ptr();
-      at.token_stride = packed ? T : t->stride(0);
-      at.token_bytes = t->scalar_type() == at::kLong ? 8 : 4;
-    }
-    if (lengths_ != Py_None) {
-      const at::Tensor* t = tensor(lengths_);
-      if (packed || !here(t) || t->scalar_type() != at::kInt || t->dim() != 1 || t->size(0) != B || !t->is_contiguous())
-        return false;
-      lengths = t;
-      at.lengths = t->data_ptr<int32_t>();
-    }
-    if (mask_ != Py_None) {
-      const at::Tensor* t = tensor(mask_);
-      if (!here(t) || (t->scalar_type() != at::kBool && t->scalar_type() != at::kByte) || t->dim() != x->dim() - 1 ||
-          t->size(-1) != T || (!packed && t->size(0) != B) || !t->is_contiguous())
-        return false;
-      mask = t;
-      at.mask = static_cast<const uint8_t*>(t->data_ptr());
-    }
+    return true;
+  }
+  bool take_tokens(const at::Tensor* t) {
+    if (!here(t) || !id_type(t->scalar_type()) || t->dim() != x->dim() - 1 || t->size(-1) != logits.T ||
+        (!packed && t->size(0) != logits.B) || (logits.T > 1 && t->stride(-1) != 1))
+      return false;
+    tokens = t;
+    at.tokens = t->data_ptr();
+    at.token_stride = packed ? logits.T : t->stride(0);
+    at.token_bytes = t->scalar_type() == at::kLong ? 8 : 4;
+    return true;
+  }
+  bool take_lengths(const at::Tensor* t) {
+    if (packed || !here(t) || t->scalar_type() != at::kInt || t->dim() != 1 || t->size(0) != logits.B ||
+        !t->is_contiguous())
+      return false;
+    lengths = t;
+    at.lengths = t->data_ptr<int32_t>();
+    return true;
+  }
+  bool take_mask(const at::Tensor* t) {
+    if (!here(t) || (t->scalar_type() != at::kBool && t->scalar_type() != at::kByte) || t->dim() != x->dim() - 1 ||
+        t->size(-1) != logits.T || (!packed && t->size(0) != logits.B) || !t->is_contiguous())
+      return false;
+    mask = t;
+    at.mask = static_cast<const uint8_t*>(t->data_ptr());
+    return true;
+  }
+  // a teacher's entries of all positions
+  bool take_teacher(const at::Tensor* ids, const at::Tensor* t, tb_teacher_t* q) const {
+    if (!here(ids) || !here(t) || !id_type(ids->scalar_type()) || !type_of(t->scalar_type(), &q->type) ||
+        ids->dim() != x->dim() || ids->sizes() != t->sizes() || !ids->is_contiguous() || !t->is_contiguous() ||
+        ids->sizes().slice(0, ids->dim() - 1) != positions() || ids->size(-1) > TB_TEACHER_MOST)
+      return false;
+    q->ids = ids->data_ptr();
+    q->logits = t->data_ptr();
+    q->id_bytes = ids->scalar_type() == at::kLong ? 8 : 4;
+    q->K = int32_t(ids->size(-1));
+    return true;
+  }
+  bool take(PyObject* logits_, PyObject* tokens_, PyObject* lengths_, PyObject* mask_, PyObject* temperature_,
+            PyObject* status_) {
+    if (!take_float(temperature_, &logits.temperature) || !take_rows(tensor(logits_))) return false;
+    if (tokens_ && !take_tokens(tensor(tokens_))) return false;
+    if (lengths_ != Py_None && !take_lengths(tensor(lengths_))) return false;
+    if (mask_ != Py_None && !take_mask(tensor(mask_))) return false;
     if (status_ != Py_None) {
       const at::Tensor* t = tensor(status_);
       if (!here(t) || t->scalar_type() != at::kInt || t->numel() != 1) return false;
@@ -143,17 +163,19 @@ struct Call {
 
 // The backward pass of all operators: the gradient of rows whose statistics and cotangents the forward
 // pass has left.  Incoming gradients are of the log-probabilities and entropies themselves (kValues), or
-// of a scalar loss that `d_lp`, `d_entropy` are the cotangents of.
+// of a scalar loss that `d_lp`, `d_entropy` are the cotangents of.  Everything that the kernels read comes from
+// the saved tensors as they are unpacked: where hooks are active (checkpointing, offloading), these are other
+// tensors than the forward pass's, whose memory may be gone, and their strides may be others.
 struct RowsBackward : public torch::autograd::Node {
   using Saved = torch::autograd::SavedVariable;
   enum Kind { kValues, kLoss, kSequences, kDistill } kind;
-  tb_logits_t logits_of;
-  tb_positions_t at;
-  tb_teacher_t teacher = {};
+  tb_logits_t logits_of;  // (shape, type and temperature)
+  int32_t average = 0;    // of a distillation
+  int64_t dims;
   Saved logits, tokens, lengths, mask, state, d_lp, d_entropy, ids, teacher_logits;
 
   static Saved kept(const at::Tensor* t) { return t && t->defined() ? Saved(*t, false) : Saved(); }
-  RowsBackward(Kind k, const Call& c, const at::Tensor& row_state) : kind(k), logits_of(c.logits), at(c.at) {
+  RowsBackward(Kind k, const Call& c, const at::Tensor& row_state) : kind(k), logits_of(c.logits), dims(c.x->dim()) {
     logits = kept(c.x);
     tokens = kept(c.tokens);
     lengths = kept(c.lengths);
@@ -161,6 +183,8 @@ struct RowsBackward : public torch::autograd::Node {
     state = kept(&row_state);
     set_next_edges(torch::autograd::collect_next_edges(*c.x));
   }
+  static constexpr const char* kHooks =
+      "a tensor saved for the losses' backward pass has come back from its hooks with another shape, type or device";
   std::string name() const override { return "TensorLossBackward"; }
   void release_variables() override {
     std::lock_guard<std::mutex> lock(mutex_);
@@ -171,8 +195,26 @@ struct RowsBackward : public torch::autograd::Node {
     TORCH_CHECK(!at::GradMode::is_enabled(), "the losses over logits cannot be differentiated twice");
     if (!in[0].defined() && (in.size() < 2 || !in[1].defined())) return {at::Tensor()};
     // (unpacking checks that nothing has been written over since)
-    const at::Tensor x = logits.unpack(), s = state.unpack(), held[] = {tokens.unpack(), lengths.unpack(), mask.unpack()};
-    at::Tensor d = d_lp.unpack(), dh = d_entropy.unpack(), up;
+    auto rows = [](const at::Tensor& t) {
+      return t.defined() && t.dim() > 0 && t.stride(-1) != 1 && t.size(-1) > 1 ? t.contiguous() : t;
+    };
+    auto whole = [](const at::Tensor& t) { return t.defined() ? t.contiguous() : t; };
+    const at::Tensor x = rows(logits.unpack()), ids_of_rows = rows(tokens.unpack()), n = whole(lengths.unpack()),
+                     m = whole(mask.unpack()), s = whole(state.unpack());
+    at::Tensor d = whole(d_lp.unpack()), dh = whole(d_entropy.unpack()), up;
+    const c10::OptionalDeviceGuard guard(x.device());
+    Call c;
+    c.logits.temperature = logits_of.temperature;
+    bool alike = x.dim() == dims && c.take_rows(&x) && c.logits.B == logits_of.B && c.logits.T == logits_of.T &&
+                 c.logits.V == logits_of.V && c.logits.type == logits_of.type;
+    auto values = [&](const at::Tensor& t, int64_t count) {
+      return c.here(&t) && t.scalar_type() == at::kFloat && t.numel() == count;
+    };
+    const int64_t count = int64_t(logits_of.B) * logits_of.T;
+    alike = alike && (!ids_of_rows.defined() || c.take_tokens(&ids_of_rows)) && (!n.defined() || c.take_lengths(&n)) &&
+            (!m.defined() || c.take_mask(&m)) && values(s, TB_ROW_STATE * count) &&
+            (!d.defined() || values(d, kind == kSequences ? logits_of.B : count)) && (!dh.defined() || values(dh, count));
+    TORCH_CHECK(alike, kHooks);
     if (kind == kValues) {
       if (in[0].defined()) d = in[0].to(at::kFloat).contiguous();
       if (in.size() > 1 && in[1].defined()) dh = in[1].to(at::kFloat).contiguous();
@@ -180,20 +222,22 @@ struct RowsBackward : public torch::autograd::Node {
     } else {
       up = in[0].to(at::kFloat).contiguous();
     }
-    const c10::DeviceGuard guard(x.device());
     at::Tensor out = at::empty(x.sizes(), x.options().requires_grad(false));
     tb_gradient_t g = {out.data_ptr(), x.dim() == 2 ? 0 : out.stride(0), out.stride(x.dim() - 2), 1.f};
-    void* stream = static_cast<void*>(c10::hip::getCurrentHIPStream().stream());
     const float* upstream = up.defined() ? up.data_ptr<float>() : nullptr;
     int rc;
     if (kind == kDistill) {
-      const at::Tensor i = ids.unpack(), q = teacher_logits.unpack();
-      rc = tensorloss_distill_grad(&logits_of, &at, &teacher, s.data_ptr<float>(), d.data_ptr<float>(), upstream, &g, stream);
+      const at::Tensor i = whole(ids.unpack()), q = whole(teacher_logits.unpack());
+      tb_teacher_t teacher = {};
+      TORCH_CHECK(c.take_teacher(&i, &q, &teacher), kHooks);
+      teacher.average = average;
+      rc = tensorloss_distill_grad(&c.logits, &c.at, &teacher, s.data_ptr<float>(), d.data_ptr<float>(), upstream, &g,
+                                   c.stream);
     } else {
       const bool each = kind != kSequences;
-      rc = tensorloss_token_logprobs_grad(&logits_of, &at, s.data_ptr<float>(), d.data_ptr<float>(),
+      rc = tensorloss_token_logprobs_grad(&c.logits, &c.at, s.data_ptr<float>(), d.data_ptr<float>(),
                                           dh.defined() ? dh.data_ptr<float>() : nullptr, each ? logits_of.T : 1, each,
-                                          upstream, &g, stream);
+                                          upstream, &g, c.stream);
     }
     TORCH_CHECK(rc == TB_OK, "tensorloss gradient: ", tensorbleu_status_string(rc));
     return {out};
@@ -355,15 +399,7 @@ PyObject* distill(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (n != 10 || !c.take(args[0], nullptr, args[1], args[2], args[3], args[4])) Py_RETURN_NONE;
   const at::Tensor *ids = tensor(args[7]), *t = tensor(args[8]);
   tb_teacher_t q = {};
-  if (!c.here(ids) || !c.here(t) || !id_type(ids->scalar_type()) || !type_of(t->scalar_type(), &q.type) ||
-      ids->dim() != c.x->dim() || ids->sizes() != t->sizes() || !ids->is_contiguous() || !t->is_contiguous() ||
-      ids->sizes().slice(0, ids->dim() - 1) != c.positions() || ids->size(-1) > TB_TEACHER_MOST ||
-      !take_int(args[9], &q.average))
-    Py_RETURN_NONE;
-  q.ids = ids->data_ptr();
-  q.logits = t->data_ptr();
-  q.id_bytes = ids->scalar_type() == at::kLong ? 8 : 4;
-  q.K = int32_t(ids->size(-1));
+  if (!c.take_teacher(ids, t, &q) || !take_int(args[9], &q.average)) Py_RETURN_NONE;
   const bool scalar = args[6] == Py_None, backward = scalar && differentiated(*c.x);
   at::Tensor out, state, d_row;
   tb_gradient_t g = {};
@@ -389,7 +425,7 @@ PyObject* distill(PyObject*, PyObject* const* args, Py_ssize_t n) {
       node->d_lp = RowsBackward::kept(&d_row);
       node->ids = RowsBackward::kept(ids);
       node->teacher_logits = RowsBackward::kept(t);
-      node->teacher = q;
+      node->average = q.average;
       torch::autograd::set_history(loss, node);
     }
     return THPVariable_Wrap(std::move(loss));

@@ -293,6 +293,11 @@ def _score(call, want_entropy, keep_state):
 
 def _rows_gradient(call, state, d_lp, d_entropy, d_strides, upstream, out=None, scale=1.0):
     out, g = call.gradient(out, scale)
+    # (hooks on saved tensors give back the same values, in what strides they like)
+    state = call.values(state, "the rows' state", (*call.shape, 4))
+    over = call.shape if d_strides[1] else (call.B,)
+    d_lp = call.values(d_lp, "d_lp", over)
+    d_entropy = None if d_entropy is None else call.values(d_entropy, "d_entropy", over)
     call.run("tensorloss_token_logprobs_grad", state, d_lp, d_entropy, *d_strides, upstream, g)
     return out
 
@@ -533,6 +538,7 @@ class _DistillationLoss(torch.autograd.Function):
         call = _Call(logits, None, lengths, mask, ctx.temperature, None)
         q = _teacher(call, teacher_ids, teacher_logits, ctx.average)
         out, g = call.gradient(None, 1.0)
+        state, d_row = call.values(state, "the rows' state", (*call.shape, 4)), call.values(d_row, "d_row")
         call.run("tensorloss_distill_grad", q, state, d_row, d_loss.to(torch.float32), g)
         return (out, *(None,) * 7)
 

@@ -1,0 +1,170 @@
+"""The losses over logits as parts of torch's graph: saved tensors that hooks replace.
+
+A hook gives back other memory than the forward pass's, which is gone by then, with other strides; the
+gradient is the one without hooks, bit by bit where rows begin at the same addresses modulo 128 (the
+clones here do: every allocation begins at a multiple of 512, and strides are kept or all rows are read
+in the same order)."""
+import math
+
+import pytest
+import torch
+from torch.utils.checkpoint import checkpoint
+
+import paper_2510_05485_amd as tb
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def apart(v):
+    """The same values, not contiguous: the general way of marshalling."""
+    return torch.stack([v, v], -1)[..., 0]
+
+
+def operators(V, seed=0, B=4, T=6, native=True):
+    """Logits, and functions of logits: a scalar each, through every operator."""
+    g = torch.Generator().manual_seed(seed + V)
+    x = (torch.randn(B, T, V, generator=g) * 2).to(DEV)
+    tokens = torch.randint(0, V, (B, T), generator=g).to(DEV)
+    old, reference = (-3 + torch.randn(B, T, generator=g).to(DEV) for _ in range(2))
+    a = torch.randn(B, generator=g).to(DEV)
+    K = min(V, 5)
+    ids, teacher = torch.randint(0, V, (B, T, K), generator=g).to(DEV), torch.randn(B, T, K, generator=g).to(DEV)
+    d = torch.randn(2, B, T, generator=g).to(DEV)
+    lengths = torch.tensor([6, 0, 4, 5], device=DEV, dtype=torch.int32)
+    mask = (torch.rand(B, T, generator=g) < 0.8).to(DEV)
+    if not native:
+        lengths, old, reference, teacher = lengths.long(), apart(old), apart(reference), apart(teacher)
+    where = dict(lengths=lengths, mask=mask, temperature=0.9)
+
+    def scores(y):
+        lp, h = tb.token_logprobs(y, tokens, want_entropy=True, **where)
+        return (lp * d[0]).sum() + (h * d[1]).sum()
+    return x, dict(
+        scores=scores,
+        logprobs=lambda y: (tb.token_logprobs(y, tokens, **where) * d[0]).sum(),
+        policy=lambda y: tb.policy_loss(y, tokens, old, a, ref_logprobs=reference, kl_coef=0.1, entropy_coef=0.1, **where),
+        preference=lambda y: tb.preference_loss(y, tokens, reference, beta=0.5, **where),
+        distillation=lambda y: tb.distillation_loss(y, ids, teacher, **where))
+
+
+def gradient_of(f, x):
+    leaf = x.clone().requires_grad_()
+    # (logits are the product of a layer, so that nothing but the loss's saved tensors holds them)
+    return torch.autograd.grad(3 * f(leaf * 1.5), leaf)[0]
+
+
+class Replaced(torch.autograd.graph.saved_tensors_hooks):
+    """Saved tensors live on the host and come back through `restore`."""
+
+    def __init__(self, restore=lambda t: t):
+        self.saved = 0
+
+        def pack(t):
+            self.saved += 1
+            return t.detach().cpu().clone()
+        super().__init__(pack, lambda t: restore(t.to(DEV)))
+
+
+def litter(x):
+    """What the forward pass's memory holds next: NaN, in every size that it may have come from."""
+    rows = x.numel() // x.shape[-1]
+    return [torch.full((n,), math.nan, device=DEV) for n in (1, rows, 2 * rows, 4 * rows, 5 * rows, x.numel()) for _ in range(4)]
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("V", [3, 64, 1031, 9001])
+def test_saved_tensors_from_the_host(V, native):
+    x, all_of = operators(V, native=native)
+    for name, f in all_of.items():
+        want = gradient_of(f, x)
+        leaf = x.clone().requires_grad_()
+        hooks = Replaced()
+        with hooks:
+            loss = 3 * f(leaf * 1.5)
+        assert hooks.saved
+        over = litter(x)
+        got, = torch.autograd.grad(loss, leaf)
+        assert torch.equal(got, want), name
+        del over
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("V", [64, 1031])
+def test_saved_tensors_with_other_strides(V, native):
+    """What a hook gives back need not be laid out as it was."""
+    def turned(t):
+        if t.dim() < 2:
+            return apart(t) if t.dim() else t
+        return t.transpose(-1, -2).contiguous().transpose(-1, -2)
+    x, all_of = operators(V, native=native)
+    for name, f in all_of.items():
+        want = gradient_of(f, x)
+        leaf = x.clone().requires_grad_()
+        with Replaced(turned):
+            loss = 3 * f(leaf * 1.5)
+        got, = torch.autograd.grad(loss, leaf)
+        assert torch.equal(got, want), name
+
+
+def test_views_that_come_back_whole():
+    """Logits that are a view of a longer model output: a copy of them has other strides."""
+    x, all_of = operators(64)
+    for name, f in all_of.items():
+        wide = torch.zeros(4, 7, 64, device=DEV)
+        wide[:, :6] = x
+        leaf = wide.requires_grad_()
+        want, = torch.autograd.grad(f((leaf * 1.0)[:, :-1]), leaf)
+        with Replaced():
+            loss = f((leaf * 1.0)[:, :-1])
+        over = litter(wide)
+        got, = torch.autograd.grad(loss, leaf)
+        assert torch.equal(got, want) and not got[:, 6:].any(), name
+        del over
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("V", [64, 1031, 9001])
+def test_checkpoint(V, native):
+    """The head and its loss computed anew in the backward pass, twice in a row."""
+    x, all_of = operators(V, native=native)
+    for name, f in all_of.items():
+        want = gradient_of(f, x)
+        leaf = x.clone().requires_grad_()
+        losses = [checkpoint(lambda y: f(y * 1.5), leaf, use_reentrant=False) for _ in range(2)]
+        over = litter(x)
+        got, = torch.autograd.grad(3 * losses[0], leaf)
+        assert torch.equal(got, want), name
+        (3 * losses[1]).backward()
+        assert torch.equal(leaf.grad, want), name
+        del over
+
+
+def test_save_on_cpu():
+    x, all_of = operators(300)
+    for name, f in all_of.items():
+        want = gradient_of(f, x)
+        leaf = x.clone().requires_grad_()
+        with torch.autograd.graph.save_on_cpu():
+            loss = 3 * f(leaf * 1.5)
+        over = litter(x)
+        assert torch.equal(torch.autograd.grad(loss, leaf)[0], want), name
+        del over
+
+
+def test_hooks_that_give_back_something_else():
+    """Another shape or type than was saved is refused, not read."""
+    x, all_of = operators(64)
+    for cut in (lambda t: t[..., :-1] if t.dim() == 3 and t.shape[-1] == 64 else t,
+                lambda t: t.double() if t.dim() == 3 and t.shape[-1] == 64 else t,
+                lambda t: t[:-1] if t.dtype == torch.int32 else t,
+                lambda t: t[:, :-1] if t.dtype == torch.bool else t,
+                lambda t: t[:, :3] if t.dim() == 3 and t.shape[-1] == 4 else t,
+                lambda t: t.cpu() if t.dtype == torch.int32 else t):
+        for name, f in all_of.items():
+            leaf = x.clone().requires_grad_()
+            y = leaf * 1.5
+            with Replaced(cut):
+                loss = f(y)
+            with pytest.raises(RuntimeError):
+                torch.autograd.grad(loss, leaf)
