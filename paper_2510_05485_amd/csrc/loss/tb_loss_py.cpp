@@ -247,6 +247,11 @@ std::shared_ptr<RowsBackward> backward_of(RowsBackward::Kind kind, const Call& c
   return std::shared_ptr<RowsBackward>(new RowsBackward(kind, c, state), torch::autograd::deleteNode);
 }
 bool differentiated(const at::Tensor& x) { return at::GradMode::is_enabled() && x.requires_grad(); }
+// A caller's tensor has been written over: torch notices it where the tensor, or one that shares its memory, is
+// saved for a backward pass.  (Tensors of inference mode count no versions and are not saved.)
+void written(PyObject* out, const at::Tensor& t) {
+  if (out != Py_None && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 // the loss, terms[0], as a tensor of its own that shares its memory
 at::Tensor first_of(const at::Tensor& terms) {
   at::AutoDispatchBelowADInplaceOrView guard;
@@ -349,6 +354,7 @@ PyObject* policy(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
     return THPVariable_Wrap(std::move(loss));
   }
+  written(args[6], out);
   return results({terms, out, lp}, args[6], 1);
 }
 
@@ -389,6 +395,7 @@ PyObject* preference(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
     return THPVariable_Wrap(std::move(loss));
   }
+  written(args[6], out);
   return results({terms, out, sums, margins}, args[6], 1);
 }
 
@@ -430,6 +437,7 @@ PyObject* distill(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
     return THPVariable_Wrap(std::move(loss));
   }
+  written(args[5], out);
   return results({terms, out, rows}, args[5], 1);
 }
 

@@ -19,7 +19,8 @@ Common arguments
   lengths      [B]: position t of sequence b counts if t < lengths[b].  Not for packed positions
   mask         bool or uint8, of the tokens' shape: a position counts if it is not 0
   temperature  divides the logits
-  out          where the gradient goes (default: a new tensor); may be the logits themselves
+  out          where the gradient goes (default: a new tensor); may be the logits themselves, which then
+               count as changed in place: what has saved them for a backward pass raises there
   grad_scale   the gradient is that of grad_scale * loss (loss scaling, gradient accumulation)
   status       int32 [1] on the GPU; TB_DEV_TOKEN_RANGE / TB_DEV_LENGTH_RANGE are OR-ed into it
 
@@ -258,6 +259,13 @@ class _Call:
         g.scale = float(scale)
         return out, g
 
+    @staticmethod
+    def written(out, to):
+        """The caller's tensor `out` has been written over: torch's checks of saved tensors notice it.
+        (Tensors of inference mode count no versions and are not saved.)"""
+        if out is not None and not to.is_inference():
+            torch.autograd.graph.increment_version(to)
+
     def new(self, *shape):
         return torch.empty(*shape, dtype=torch.float32, device=self.device)
 
@@ -416,10 +424,11 @@ def policy_loss_grad(logits, tokens, old_logprobs, advantages, *, ref_logprobs=N
     if found is not None:
         return PolicyLoss(*found)
     call = _Call(logits, tokens, lengths, mask, temperature, status)
-    out, g = call.gradient(out, grad_scale)
+    to, g = call.gradient(out, grad_scale)
     terms, lp, *_ = _policy(call, old_logprobs, advantages, ref_logprobs, clip_low, clip_high, kl_coef,
                             entropy_coef, average, g, False)
-    return PolicyLoss(terms, out, lp)
+    call.written(out, to)
+    return PolicyLoss(terms, to, lp)
 
 
 # ---- preference loss ----------------------------------------------------------------------------
@@ -490,9 +499,10 @@ def preference_loss_grad(logits, tokens, ref_logprobs, *, lengths=None, mask=Non
     if found is not None:
         return PreferenceLoss(*found)
     call = _Call(logits, tokens, lengths, mask, temperature, status)
-    out, g = call.gradient(out, grad_scale)
+    to, g = call.gradient(out, grad_scale)
     terms, lp, margins, *_ = _preference(call, ref_logprobs, beta, kind, label_smoothing, g, False)
-    return PreferenceLoss(terms, out, lp, margins)
+    call.written(out, to)
+    return PreferenceLoss(terms, to, lp, margins)
 
 
 # ---- distillation -------------------------------------------------------------------------------
@@ -573,6 +583,7 @@ def distillation_loss_grad(logits, teacher_ids, teacher_logits, *, lengths=None,
         return DistillationLoss(*found)
     call = _Call(logits, None, lengths, mask, temperature, status)
     q = _teacher(call, teacher_ids, teacher_logits, average)
-    out, g = call.gradient(out, grad_scale)
+    to, g = call.gradient(out, grad_scale)
     terms, rows, *_ = _distill(call, q, g, False)
-    return DistillationLoss(terms, out, rows)
+    call.written(out, to)
+    return DistillationLoss(terms, to, rows)

@@ -1,4 +1,5 @@
-"""The losses over logits as parts of torch's graph: saved tensors that hooks replace.
+"""The losses over logits as parts of torch's graph: saved tensors that hooks replace, gradients written over
+what is saved.
 
 A hook gives back other memory than the forward pass's, which is gone by then, with other strides; the
 gradient is the one without hooks, bit by bit where rows begin at the same addresses modulo 128 (the
@@ -168,3 +169,56 @@ def test_hooks_that_give_back_something_else():
                 loss = f(y)
             with pytest.raises(RuntimeError):
                 torch.autograd.grad(loss, leaf)
+
+
+def with_gradient(native):
+    """Every operator that returns its gradient, as a function of logits and `out`."""
+    x, _ = operators(64)
+    g = torch.Generator().manual_seed(1)
+    tokens, ids = torch.randint(0, 64, (4, 6), generator=g).to(DEV), torch.randint(0, 64, (4, 6, 5), generator=g).to(DEV)
+    v, a, teacher = torch.full((4, 6), -4.0, device=DEV), torch.ones(4, device=DEV), torch.zeros(4, 6, 5, device=DEV)
+    if not native:
+        v, teacher = apart(v), apart(teacher)
+    return x, tokens, [lambda y, out: tb.policy_loss_grad(y, tokens, v, a, out=out),
+                       lambda y, out: tb.preference_loss_grad(y, tokens, v, out=out),
+                       lambda y, out: tb.distillation_loss_grad(y, ids, teacher, out=out)]
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_a_gradient_written_over_saved_logits_is_noticed(native):
+    x, tokens, all_of = with_gradient(native)
+    for f in all_of:
+        for of in (lambda y: y.detach(), lambda y: y):
+            leaf = x.clone().requires_grad_()
+            y = leaf * 1.5
+            loss = tb.token_logprobs(y, tokens).sum() + torch.logsumexp(y, -1).sum()
+            want, = torch.autograd.grad(loss, leaf, retain_graph=True)
+            before = y._version
+            r = f(of(y), of(y))
+            assert y._version > before and r.grad.data_ptr() == y.data_ptr()
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                torch.autograd.grad(loss, leaf)
+        # the gradient itself goes on into the model from there
+        leaf = x.clone().requires_grad_()
+        y = leaf * 1.5
+        expected = f(y.detach(), None).grad
+        f(y.detach(), y.detach())
+        y.backward(y.detach().clone())
+        assert torch.equal(leaf.grad, 1.5 * expected)
+        # elsewhere than the logits: these have not changed
+        out = torch.empty_like(x)
+        before, at = x._version, out._version
+        f(x, out)
+        assert out._version > at and x._version == before
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_out_in_inference_mode(native):
+    """Tensors of inference mode have no version to count."""
+    x, tokens, all_of = with_gradient(native)
+    for f in all_of:
+        want = f(x, None).grad
+        with torch.inference_mode():
+            out = torch.empty_like(x)
+            assert torch.equal(f(x, out).grad, want)
+        assert torch.equal(f(x, out).grad, want)
