@@ -67,7 +67,7 @@ struct Call {
   bool take_rows(const at::Tensor* t) {
     x = t;
     if (!x || !x->is_cuda() || x->layout() != at::kStrided || (x->dim() != 2 && x->dim() != 3)) return false;
-    if (!type_of(x->scalar_type(), &logits.type)) return false;
+    if (!type_of(x->scalar_type(), &logits.type) || x->_fw_grad(0).defined()) return false;
     const auto s = c10::hip::getCurrentHIPStream();
     if (s.device_index() != x->device().index()) return false;
     stream = static_cast<void*>(s.stream());

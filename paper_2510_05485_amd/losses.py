@@ -25,6 +25,7 @@ Common arguments
   status       int32 [1] on the GPU; TB_DEV_TOKEN_RANGE / TB_DEV_LENGTH_RANGE are OR-ed into it
 
 What stands at positions that do not count has no part in anything; what is returned for them is 0.
+Gradients are for reverse mode, and of first order; logits with a forward-mode tangent are refused.
 Everything runs on the current stream of the logits' GPU, and nothing synchronises.  See
 include/tensorloss.h for the formulas and for what wrong ids and infinite logits give.
 """
@@ -170,6 +171,11 @@ def _on(t: torch.Tensor, device, name: str) -> None:
                               f"(got {getattr(t, 'device', type(t).__name__)})")
 
 
+def _refuse_tangent(logits: torch.Tensor) -> None:
+    if torch.autograd.forward_ad.unpack_dual(logits).tangent is not None:
+        raise TensorBLEUError("the losses have no forward-mode derivative (the logits carry a tangent)")
+
+
 class _Call:
     """A call's logits and positions, checked, as the C structs; keeps what was converted alive."""
 
@@ -181,6 +187,7 @@ class _Call:
             raise TensorBLEUError(f"logits must be float32, bfloat16 or float16 (got {logits.dtype})")
         if logits.dim() not in (2, 3) or logits.shape[-1] < 1:
             raise TensorBLEUError(f"expected logits [B, T, V] or [N, V] (got {tuple(logits.shape)})")
+        _refuse_tangent(logits)
         logits = logits.detach()
         if logits.shape[-1] > 1 and logits.stride(-1) != 1:
             logits = logits.contiguous()
@@ -286,7 +293,10 @@ class _Call:
 
 
 def _needs_grad(logits) -> bool:
-    return torch.is_grad_enabled() and isinstance(logits, torch.Tensor) and logits.requires_grad
+    if not isinstance(logits, torch.Tensor):
+        return False
+    _refuse_tangent(logits)                # (not to be seen any more inside a Function's forward)
+    return torch.is_grad_enabled() and logits.requires_grad
 
 
 # ---- log-probabilities --------------------------------------------------------------------------

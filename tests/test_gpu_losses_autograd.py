@@ -1,5 +1,5 @@
 """The losses over logits as parts of torch's graph: saved tensors that hooks replace, gradients written over
-what is saved.
+what is saved, tangents.
 
 A hook gives back other memory than the forward pass's, which is gone by then, with other strides; the
 gradient is the one without hooks, bit by bit where rows begin at the same addresses modulo 128 (the
@@ -222,3 +222,18 @@ def test_out_in_inference_mode(native):
             out = torch.empty_like(x)
             assert torch.equal(f(x, out).grad, want)
         assert torch.equal(f(x, out).grad, want)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_tangents_are_refused(native):
+    """Forward-mode differentiation: a result without a tangent would stand for one of 0."""
+    x, _, given = with_gradient(native)
+    _, all_of = operators(64, native=native)
+    with torch.autograd.forward_ad.dual_level():
+        for leaf in (x, x.clone().requires_grad_()):
+            dual = torch.autograd.forward_ad.make_dual(leaf, torch.ones_like(x))
+            for f in list(all_of.values()) + [lambda y, f=f: f(y, None) for f in given]:
+                with pytest.raises(tb.TensorBLEUError, match="forward-mode"):
+                    f(dual)
+        for f in all_of.values():                # without a tangent, as outside
+            assert torch.isfinite(f(x))
