@@ -14,7 +14,7 @@ namespace loss {
 
 constexpr int kWave = 64;
 constexpr float kLowest = -3.402823466e38f;
-constexpr float kExtreme = 1e37f;  // a row's largest logit beyond it: products with log2(e) might overflow
+constexpr float kExtreme = 1e37f;  // stands for the reference of values all below it, whose product with log2(e) is finite
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // What a row's workgroup does behind the softmax statistics.

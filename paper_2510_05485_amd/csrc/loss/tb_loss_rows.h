@@ -32,14 +32,16 @@ __device__ __forceinline__ float scaled(float m, float k) {
 #pragma clang fp contract(off)
   return m * k;
 }
+// M is off by half a unit in its last place: by 8 at most below 2^28, from where on weights are formed as
+// 2^((x - m) k) only.
+__device__ __forceinline__ bool scales(float m, float k) { return fabsf(scaled(m, k)) < 0x1p28f; }
 // Kernels that form weights as 2^((x - m) k) have sums that differ from those of 2^(x k - M) by a factor
-// that rounds M; the state of a row that is kept for the backward pass is of the latter, where M can be
-// formed at all.
+// that rounds M; the state of a row that is kept for the backward pass is of the latter, where M is used.
 __device__ __forceinline__ float to_scaled(float m, float k) {
-  return fabsf(m) < kExtreme ? exp2_fast(fmaf(m, k, -scaled(m, k))) : 1.f;
+  return scales(m, k) ? exp2_fast(fmaf(m, k, -scaled(m, k))) : 1.f;
 }
 __device__ __forceinline__ float from_scaled(float m, float k) {
-  return fabsf(m) < kExtreme ? exp2_fast(-fmaf(m, k, -scaled(m, k))) : 1.f;
+  return scales(m, k) ? exp2_fast(-fmaf(m, k, -scaled(m, k))) : 1.f;
 }
 // 1 / x, to 1 unit in the last place
 __device__ __forceinline__ float reciprocal(float x) { return __builtin_amdgcn_rcpf(x); }
@@ -894,8 +896,8 @@ __device__ __forceinline__ Stats wave_stats(const typename Held<X, kThreads, kCh
   if (kEntropy) mine.t = lanes_sum<kThreads>(mine.t);
   return mine;
 }
-__device__ __forceinline__ bool fine(const Stats& s) {
-  return fabsf(s.m) < kExtreme && s.s > 0x1p-40f && s.s < 0x1p40f;
+__device__ __forceinline__ bool fine(const Stats& s, float k) {
+  return scales(s.m, k) && s.s > 0x1p-40f && s.s < 0x1p40f;
 }
 
 template <bool kEntropy, typename X, int kThreads, int kChunks, bool kMore>
@@ -984,7 +986,7 @@ __global__ __launch_bounds__(kThreads) void held_kernel(Rows r, RowOut o, Policy
   if (threadIdx.x % kWave == 0) parts[threadIdx.x / kWave] = part;
   __syncthreads();
   Stats s = block_stats<kEntropy, kWaves>(parts, k);
-  const bool extreme = !fine(s);
+  const bool extreme = !fine(s, k);
   if (extreme) {
     __syncthreads();
     s = row_stats<X, kEntropy>(row, k, threadIdx.x, parts);
@@ -1139,7 +1141,7 @@ __global__ __launch_bounds__(kThreads <= kWave ? kLaneThreads : kThreads) void d
       total = 0;
       for (int w = 0; w < kWaves; ++w) total += totals[w];
     }
-    const bool extreme = !fine(s);
+    const bool extreme = !fine(s, k);
     if (extreme) {
       meet<kThreads>();
       s = row_stats<X, false, kThreads>(row, k, thread, parts[team]);

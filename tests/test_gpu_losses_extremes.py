@@ -1,0 +1,88 @@
+"""Losses over logits of extreme size: rows whose numbers are too large for their products with log2(e) to
+be exact, parts of a row that lie far apart, infinite margins, huge cotangents, wide lengths."""
+import math
+
+import pytest
+import torch
+
+import loss_bounds as bounds
+import loss_reference as ref
+import paper_2510_05485_amd as tb
+from loss_bounds import LP
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def near(got, want, tol, what=""):
+    off = (got.detach().cpu().double() - want).abs()
+    assert (off <= tol).all(), (what, got, want)
+
+
+def large_rows(base, V, dtype, T=4):
+    """Rows around `base`: all alike, half of them impossible, some one step below, one step above the rest."""
+    g = torch.Generator().manual_seed(V)
+    b = torch.tensor(base, dtype=torch.float32).to(dtype)
+    below, above = (torch.nextafter(b, torch.tensor(s * math.inf, dtype=dtype)) for s in (-1, 1))
+    x = b.expand(2, T, V).clone()
+    tokens = torch.randint(0, V, (2, T), generator=g)
+    some = torch.rand(2, T, V, generator=g) < 0.5
+    some = some.scatter(-1, tokens.unsqueeze(-1), False)
+    x[:, 1] = torch.where(some[:, 1], torch.full_like(x[:, 1], -math.inf), x[:, 1])
+    x[:, 2] = torch.where(some[:, 2], below.expand_as(x[:, 2]), x[:, 2])
+    x[:, 3] = x[:, 3].scatter(-1, tokens[:, 3:], above.expand(2, 1))
+    return x.to(DEV), tokens.to(DEV)
+
+
+BASES = [1e6, -1e8, 3e8, 1e10, -1e10, 3e12, 1e20, -1e20, -1e30, 1e36]
+
+
+@pytest.mark.parametrize("base", BASES)
+@pytest.mark.parametrize("dtype,V", [(torch.float32, 64), (torch.float32, 2500), (torch.float32, 20011),
+                                     (torch.bfloat16, 3), (torch.bfloat16, 1031), (torch.bfloat16, 5000),
+                                     (torch.bfloat16, 50257), (torch.float32, 140000)])
+def test_large_logits(dtype, V, base):
+    x, tokens = large_rows(base, V, dtype)
+    valid = torch.ones(2, 4, dtype=torch.bool)
+    rx, logp = ref.rows(x, valid, 1.0)
+    p = logp.detach()
+    # what is far below has probability 0 in either: keep infinities out of the bounds
+    p = p.clamp(min=-1e4)
+    lp, h = ref.chosen(logp, tokens, valid), ref.entropies(logp, valid)
+    d, d_h = torch.tensor([1.0, -0.5, 2.0, 0.7]).double().expand(2, 4), torch.tensor([0.3, 1.0, -1.0, 0.5]).double().expand(2, 4)
+    leaf = x.clone().requires_grad_()
+    got_lp, got_h = tb.token_logprobs(leaf, tokens, want_entropy=True)
+    near(got_lp, lp.detach(), LP, "log-probabilities")
+    near(got_h, h.detach(), bounds.H, "entropies")
+    want, = torch.autograd.grad((lp * d).sum() + (h * d_h).sum(), rx, retain_graph=True)
+    got, = torch.autograd.grad((got_lp, got_h), leaf, (d.float().to(DEV), d_h.float().to(DEV)))
+    bounds.check(got, want, bounds.of_softmax(p, d, bounds.at_tokens(p, tokens.cpu(), d), d_h), dtype, "of both")
+    want, = torch.autograd.grad((lp * d).sum(), rx)
+    got, = torch.autograd.grad(tb.token_logprobs(leaf, tokens), leaf, d.float().to(DEV))
+    bounds.check(got, want, bounds.of_softmax(p, d, bounds.at_tokens(p, tokens.cpu(), d)), dtype, "of log-probabilities")
+
+    one = torch.ones(2, 4).double()
+    old, a = (lp.detach() - 0.1).float().to(DEV), torch.tensor([1.0, -1.0], device=DEV)
+    terms, want, _ = ref.policy(x, tokens, old, a, average="sum")
+    bound = bounds.of_softmax(p, 1.2 * one, bounds.at_tokens(p, tokens.cpu(), 1.2 * one))
+    bounds.check(tb.policy_loss_grad(x, tokens, old, a, average="sum").grad, want, bound, dtype, "policy")
+    got, = torch.autograd.grad(tb.policy_loss(leaf, tokens, old, a, average="sum"), leaf)
+    bounds.check(got, want, bound, dtype, "policy, backward")
+
+    reference = (lp.detach() + 0.2).float().to(DEV)
+    terms, want, _, margins = ref.preference(x, tokens, reference)
+    bound = bounds.of_softmax(p, 0.1 * one, bounds.at_tokens(p, tokens.cpu(), 0.1 * one))
+    r = tb.preference_loss_grad(x, tokens, reference)
+    near(r.margins, margins, 8 * LP, "margins")
+    bounds.check(r.grad, want, bound, dtype, "preference")
+    got, = torch.autograd.grad(tb.preference_loss(leaf, tokens, reference), leaf)
+    bounds.check(got, want, bound, dtype, "preference, backward")
+
+    ids, teacher = tokens.unsqueeze(-1), torch.zeros(2, 4, 1, device=DEV)
+    terms, want, rows = ref.distillation(x, ids, teacher, average="sum")
+    bound = bounds.of_softmax(p, one, bounds.at_tokens(p, tokens.cpu(), one))
+    r = tb.distillation_loss_grad(x, ids, teacher, average="sum")
+    near(r.row_loss, rows, 2 * LP, "rows")
+    bounds.check(r.grad, want, bound, dtype, "distillation")
+    got, = torch.autograd.grad(tb.distillation_loss(leaf, ids, teacher, average="sum"), leaf)
+    bounds.check(got, want, bound, dtype, "distillation, backward")
