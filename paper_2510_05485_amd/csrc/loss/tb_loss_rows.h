@@ -854,7 +854,9 @@ __device__ __forceinline__ float lanes_sum(float v) {
 // m need not be the largest value: any that keeps the weights in range does.  It is the largest of the
 // lanes' own, found on the packed values as signed integers: right where a lane has a value above 0, else
 // the lane's smallest (half an instruction a value instead of two and a half).  Where that takes the sum
-// out of range, `fine` is false and the row has to be swept.
+// out of range, `fine` is false and the row has to be swept.  So it is where a wavefront's part of a row has
+// a sum beyond 2^88: another part's reference may be so much larger that this one's factor, 2^-126 and
+// below, is 0, and what is lost no longer negligible (otherwise it is below 2^-30 of the row's sum).
 template <bool kEntropy, typename X, int kThreads, int kChunks, bool kMore>
 __device__ __forceinline__ Stats wave_stats(const typename Held<X, kThreads, kChunks, kMore>::Row& row,
                                             Held<X, kThreads, kChunks, kMore>& h, int thread, float k) {
@@ -894,6 +896,7 @@ __device__ __forceinline__ Stats wave_stats(const typename Held<X, kThreads, kCh
   }
   mine.s = lanes_sum<kThreads>(mine.s);
   if (kEntropy) mine.t = lanes_sum<kThreads>(mine.t);
+  if (kThreads > kWave && mine.s > 0x1p88f) mine.s = __uint_as_float(kNan);
   return mine;
 }
 __device__ __forceinline__ bool fine(const Stats& s, float k) {

@@ -86,3 +86,43 @@ def test_large_logits(dtype, V, base):
     bounds.check(r.grad, want, bound, dtype, "distillation")
     got, = torch.autograd.grad(tb.distillation_loss(leaf, ids, teacher, average="sum"), leaf)
     bounds.check(got, want, bound, dtype, "distillation, backward")
+
+
+def two_peaks(V, dtype, gap):
+    """All values below 0; two that share the probability, in parts of the row that different wavefronts hold:
+    the one in a lane whose other values are far below, the other where a workgroup looks at every value."""
+    per = 4 if dtype == torch.float32 else 8
+    chunks = V // per
+    threads = 256 if -(-chunks // 256) <= 8 else 512
+    first, second = 3 * per + 1, per * ((min(-(-chunks // threads), 32) - 2) * threads + 100)
+    x = torch.full((2, 1, V), -1.0 - gap)
+    x[..., first] = x[..., second] = -1.0
+    tokens = torch.tensor([[first], [second]])
+    return x.to(dtype).to(DEV), tokens.to(DEV)
+
+
+@pytest.mark.parametrize("gap", [20.0, 60.0, 86.5, 87.5, 88.0, 88.5, 89.0, 95.0, 120.0])
+@pytest.mark.parametrize("dtype,V", [(torch.float32, 5000), (torch.bfloat16, 5000), (torch.bfloat16, 20011),
+                                     (torch.float16, 50257), (torch.float32, 50257), (torch.bfloat16, 200000)])
+def test_parts_of_a_row_that_lie_far_apart(dtype, V, gap):
+    x, tokens = two_peaks(V, dtype, gap)
+    valid = torch.ones(2, 1, dtype=torch.bool)
+    rx, logp = ref.rows(x, valid, 1.0)
+    p, one = logp.detach(), torch.ones(2, 1).double()
+    lp, h = ref.chosen(logp, tokens, valid).detach(), ref.entropies(logp, valid).detach()
+    got_lp, got_h = tb.token_logprobs(x, tokens, want_entropy=True)
+    near(got_lp, lp, LP)
+    near(got_h, h, bounds.H)
+    near(tb.token_logprobs(x, tokens), lp, LP)
+    old, a = lp.float().to(DEV) - 0.1, torch.ones(2, device=DEV)
+    for kw in (dict(), dict(entropy_coef=0.1)):
+        terms, want, _ = ref.policy(x, tokens, old, a, **kw)
+        r = tb.policy_loss_grad(x, tokens, old, a, **kw)
+        near(r.logprobs, lp, LP)
+        bound = bounds.of_softmax(p, one, bounds.at_tokens(p, tokens.cpu(), one), 0.1 * one if kw else None)
+        bounds.check(r.grad, want, bound, dtype, "policy")
+    ids, teacher = tokens.unsqueeze(-1), torch.zeros(2, 1, 1, device=DEV)
+    terms, want, rows = ref.distillation(x, ids, teacher)
+    r = tb.distillation_loss_grad(x, ids, teacher)
+    near(r.row_loss, rows, 2 * LP)
+    bounds.check(r.grad, want, bounds.of_softmax(p, one, bounds.at_tokens(p, tokens.cpu(), one)), dtype, "distillation")
