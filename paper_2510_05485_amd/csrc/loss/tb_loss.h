@@ -344,8 +344,9 @@ struct Stats {
   float m, s, t;
 };
 
-// a without -inf, whose product with its weight 0 would be NaN
-__device__ __forceinline__ float finite(float a) { return fmaxf(a, -1e30f); }
+// a without -inf, whose product with its weight 0 would be NaN; all below -1000 alike, where weights are 0, so
+// that a product with a cotangent is not infinite either
+__device__ __forceinline__ float finite(float a) { return fmaxf(a, -1e3f); }
 
 template <bool kEntropy>
 __device__ __forceinline__ Stats joined(const Stats& p, const Stats& q, float k) {

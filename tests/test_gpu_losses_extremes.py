@@ -126,3 +126,26 @@ def test_parts_of_a_row_that_lie_far_apart(dtype, V, gap):
     r = tb.distillation_loss_grad(x, ids, teacher)
     near(r.row_loss, rows, 2 * LP)
     bounds.check(r.grad, want, bounds.of_softmax(p, one, bounds.at_tokens(p, tokens.cpu(), one)), dtype, "distillation")
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [64, 700, 5000, 20011, 140000])
+def test_huge_cotangents_of_entropies(V, dtype):
+    """Tokens that cannot be have no part in an entropy's gradient, however large its cotangent is."""
+    g = torch.Generator().manual_seed(V)
+    x, tokens = 2 * torch.randn(2, 3, V, generator=g), torch.randint(0, V, (2, 3), generator=g)
+    dead = (torch.rand(2, 3, V, generator=g) < 0.3).scatter(-1, tokens.unsqueeze(-1), False)
+    x = x.masked_fill(dead, -math.inf).to(dtype)
+    valid, d_h = torch.ones(2, 3, dtype=torch.bool), torch.full((2, 3), 1e15)
+    rx, logp = ref.rows(x, valid, 1.0)
+    want, = torch.autograd.grad((ref.entropies(logp, valid) * d_h).sum(), rx)
+    p = logp.detach().clamp(min=-1e4)
+    bound = bounds.of_softmax(p, torch.zeros(2, 3).double(), torch.zeros_like(p), d_h.double())
+    leaf = x.to(DEV).requires_grad_()
+    lp, h = tb.token_logprobs(leaf, tokens.to(DEV), want_entropy=True)
+    got, = torch.autograd.grad(h, leaf, d_h.to(DEV))
+    assert not got[dead.to(DEV)].any()
+    bounds.check(got, want, bound, dtype, "backward")
+    r = tb.policy_loss_grad(x.to(DEV), tokens.to(DEV), lp.detach(), torch.zeros(2, device=DEV), entropy_coef=-1e15, average="sum")
+    assert not r.grad[dead.to(DEV)].any()
+    bounds.check(r.grad, want, bound, dtype, "policy")
