@@ -124,7 +124,7 @@ __device__ __forceinline__ Pair pair_values(const Pairs& p, int pairs, int i, Se
     slope = h < 1 ? -beta : (h == h ? 0.0 : h);
   } else {
     const double low = log1p(exp(-fabs(h))), e = p.smooth;  // softplus(-h) and softplus(h) without overflow
-    loss = low + (1 - e) * fmax(-h, 0.0) + e * fmax(h, 0.0);
+    loss = low + (1 - e) * fmax(-h, 0.0) + (e > 0 ? e * fmax(h, 0.0) : 0.0);  // (h may be infinite)
     slope = beta * (e / (1 + exp(-h)) - (1 - e) / (1 + exp(h)));
   }
   slope /= pairs;

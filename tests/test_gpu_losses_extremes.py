@@ -149,3 +149,40 @@ def test_huge_cotangents_of_entropies(V, dtype):
     r = tb.policy_loss_grad(x.to(DEV), tokens.to(DEV), lp.detach(), torch.zeros(2, device=DEV), entropy_coef=-1e15, average="sum")
     assert not r.grad[dead.to(DEV)].any()
     bounds.check(r.grad, want, bound, dtype, "policy")
+
+
+@pytest.mark.parametrize("B,T", [(4, 3), (4, 700), (300, 2)])
+@pytest.mark.parametrize("kw", [dict(), dict(beta=0.7), dict(kind="hinge"), dict(label_smoothing=0.1)])
+def test_infinite_margins(B, T, kw):
+    """A token of logit -inf has probability 0.  In a rejected sequence the margin is +inf: no loss (unless the
+    smoothed part asks for the opposite), and no gradient; in a chosen one -inf, and the loss infinite."""
+    V = 40
+    g = torch.Generator().manual_seed(B + T)
+    x, tokens = torch.randn(B, T, V, generator=g), torch.randint(0, V, (B, T), generator=g)
+    reference = torch.full((B, T), -4.0)
+    near_all = lambda r, want: near(r, want, 2 * LP * T)
+    for at in (B - 1, 0):
+        y = x.clone()
+        y[at, 1, tokens[at, 1]] = -math.inf
+        pair, pairs = at % (B // 2), B // 2
+        others = [i for i in range(B) if i % pairs != pair]
+        terms, grad, _, margins = ref.preference(x[others], tokens[others], reference[others], **kw)
+        keep = 1.0 - 1.0 / pairs
+        r = tb.preference_loss_grad(y.to(DEV), tokens.to(DEV), reference.to(DEV), **kw)
+        rest = [i for i in range(pairs) if i != pair]
+        near_all(r.margins[rest], margins)
+        sign = 1.0 if at else -1.0
+        assert float(r.margins[pair]) == sign * math.inf and float(r.terms[2]) == sign * math.inf
+        if at and not kw.get("label_smoothing"):
+            near_all(r.loss, float(terms[0]) * keep)
+            near(r.terms[1], float(terms[1]) * keep + 1.0 / pairs, 1e-6)
+            assert not r.grad[[pair, pair + pairs]].any()
+            leaf = y.to(DEV).requires_grad_()
+            loss = tb.preference_loss(leaf, tokens.to(DEV), reference.to(DEV), **kw)
+            near_all(loss, float(terms[0]) * keep)
+            assert torch.isfinite(torch.autograd.grad(loss, leaf)[0]).all()
+        else:
+            assert float(r.loss) == math.inf
+        logp, d = torch.log_softmax(x[others].double(), -1), torch.full((len(others), T), 1.0 / pairs).double()
+        bounds.check(r.grad[others], grad * keep, T * bounds.of_softmax(logp, d, bounds.at_tokens(logp, tokens[others], d)),
+                     torch.float32, "the other pairs")
