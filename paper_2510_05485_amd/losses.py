@@ -215,7 +215,9 @@ class _Call:
             if lengths.dtype not in (torch.int32, torch.int64) or tuple(lengths.shape) != (self.B,):
                 raise TensorBLEUError(f"lengths must be int32 or int64 of shape {(self.B,)} "
                                       f"(got {lengths.dtype} {tuple(lengths.shape)})")
-            at.lengths = self._kept(lengths.to(torch.int32).contiguous()).data_ptr()
+            if lengths.dtype == torch.int64:       # (wrong ones stay wrong when they are narrowed)
+                lengths = lengths.clamp(-1, self.T + 1).to(torch.int32)
+            at.lengths = self._kept(lengths.contiguous()).data_ptr()
         if mask is not None:
             _on(mask, self.device, "mask")
             if mask.dtype not in (torch.bool, torch.uint8) or tuple(mask.shape) != self.shape:

@@ -186,3 +186,23 @@ def test_infinite_margins(B, T, kw):
         logp, d = torch.log_softmax(x[others].double(), -1), torch.full((len(others), T), 1.0 / pairs).double()
         bounds.check(r.grad[others], grad * keep, T * bounds.of_softmax(logp, d, bounds.at_tokens(logp, tokens[others], d)),
                      torch.float32, "the other pairs")
+
+
+def test_lengths_beyond_32_bits():
+    """Lengths of 64 bits are held to [0, T] as what they are, not as their lower half."""
+    V, T = 64, 5
+    g = torch.Generator().manual_seed(3)
+    x, tokens = torch.randn(6, T, V, generator=g).to(DEV), torch.randint(0, V, (6, T), generator=g).to(DEV)
+    wide = torch.tensor([(1 << 32) + 2, -(1 << 32), 3, 1 << 40, -(1 << 32) + 3, (1 << 63) - 1], device=DEV)
+    held = torch.tensor([T, 0, 3, T, 0, T], device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    assert torch.equal(tb.token_logprobs(x, tokens, lengths=wide, status=status), tb.token_logprobs(x, tokens, lengths=held))
+    assert int(status) == tb.TB_DEV_LENGTH_RANGE
+    status.zero_()
+    tb.token_logprobs(x, tokens, lengths=held, status=status)
+    assert int(status) == 0
+    v, a = torch.full((6, T), -4.0, device=DEV), torch.ones(6, device=DEV)
+    for f in (lambda n: tb.policy_loss_grad(x, tokens, v, a, lengths=n), lambda n: tb.preference_loss_grad(x, tokens, v, lengths=n),
+              lambda n: tb.distillation_loss_grad(x, tokens.unsqueeze(-1), v.unsqueeze(-1), lengths=n)):
+        for one, other in zip(f(wide), f(held)):
+            assert torch.equal(one, other)
