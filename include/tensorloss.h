@@ -45,7 +45,7 @@ typedef struct tb_logits {
   int64_t seq_stride, pos_stride; /* in elements */
   int32_t B, T, V;                /* V >= 1; B*T and V below 2^31 */
   int32_t type;                   /* tb_type_t */
-  float temperature;              /* > 0 */
+  float temperature;              /* > 0, and log2(e) / temperature finite in float32 */
 } tb_logits_t;
 
 typedef struct tb_positions {

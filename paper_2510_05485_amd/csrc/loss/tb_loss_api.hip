@@ -84,7 +84,7 @@ int check(const tb_logits_t* l, const tb_positions_t* at, bool tokens, const tb_
   r.t_magic = uint32_t((((uint64_t(1) << r.t_shift) - uint32_t(r.T)) << 32) / uint32_t(r.T) + 1);
   r.inv_temp = 1.f / l->temperature;
   r.g_scale = 1.f;
-  if (!(r.inv_temp < INFINITY) || r.inv_temp == 0.f) return TB_ERR_INVALID_ARG;
+  if (!(r.inv_temp * kLog2e < INFINITY) || r.inv_temp == 0.f) return TB_ERR_INVALID_ARG;
   if (!g) return TB_OK;
   if (!g->data || reinterpret_cast<uintptr_t>(g->data) % size || !extent(g->seq_stride, g->pos_stride, *l, size, &g_span))
     return TB_ERR_INVALID_ARG;
