@@ -1279,10 +1279,10 @@ bool launch_held(Call& c) {
 #define HALF(n) \
   case n: held_kernel<X, kOp, kEntropy, kHeldThreads / 2, n><<<int(rows), kHeldThreads / 2, 0, c.stream>>>(r, c.out, c.policy, c.mean); return true;
   // rows of up to 2048 chunks by half as many threads, which more of them keep busy (policy
-  // loss on 26840 rows of 5000 values in bfloat16: 170 us with all, 107 so)
-  switch ((r.V / X::kPer + kHeldThreads / 2 - 1) / (kHeldThreads / 2)) { HALF(1) HALF(2) HALF(3) HALF(4) HALF(5) HALF(6) HALF(7) HALF(8) }
+  // loss on 26840 rows of 5000 values in bfloat16: 170 us with all, 107 so); rows of up to 512 chunks have gone to lanes
+  switch ((r.V / X::kPer + kHeldThreads / 2 - 1) / (kHeldThreads / 2)) { HALF(2) HALF(3) HALF(4) HALF(5) HALF(6) HALF(7) HALF(8) }
   switch (need) {
-    HELD(1) HELD(2) HELD(3) HELD(4) HELD(5) HELD(6) HELD(7) HELD(8) HELD(9) HELD(10) HELD(11) HELD(12) HELD(13) HELD(14)
+    HELD(5) HELD(6) HELD(7) HELD(8) HELD(9) HELD(10) HELD(11) HELD(12) HELD(13) HELD(14)
     HELD(15) HELD(16) HELD(17) HELD(18) HELD(19) HELD(20) HELD(21) HELD(22) HELD(23) HELD(24) HELD(25) HELD(26) HELD(27)
     HELD(28) HELD(29) HELD(30) HELD(31) HELD(32)
   }
@@ -1292,14 +1292,15 @@ bool launch_held(Call& c) {
 }
 
 // 16 lanes of a wavefront a row of up to 128 chunks, a wavefront one of up to 512, a workgroup one of more.
-template <typename X, int kThreads, int kEntries>
+// kFrom: chunks a lane that shorter rows leave to fewer lanes.
+template <typename X, int kThreads, int kEntries, int kFrom = 1>
 bool launch_distill_lanes(Call& c) {
   const Rows& r = c.rows;
   constexpr int kTeams = kLaneThreads / kThreads;
   const int64_t groups = (int64_t(r.B) * r.T + kTeams - 1) / kTeams;
   c.groups = int(groups < kLaneGroups ? groups : kLaneGroups);
 #define HELD(n) \
-  case n: distill_kernel<X, kThreads, n, kEntries><<<c.groups, kLaneThreads, 0, c.stream>>>(r, c.out, c.mean, c.teacher); return true;
+  case n: if constexpr (n >= kFrom) { distill_kernel<X, kThreads, n, kEntries><<<c.groups, kLaneThreads, 0, c.stream>>>(r, c.out, c.mean, c.teacher); return true; } else break;
   switch ((r.V / X::kPer + kThreads - 1) / kThreads) { HELD(1) HELD(2) HELD(3) HELD(4) HELD(5) HELD(6) HELD(7) HELD(8) }
 #undef HELD
   return false;
@@ -1324,10 +1325,11 @@ bool launch_distill_block(Call& c) {
   }
 #define HALF(n) \
   case n: distill_kernel<X, kHeldThreads / 2, n, 2 * kEntries><<<c.groups, kHeldThreads / 2, 0, c.stream>>>(r, c.out, c.mean, c.teacher); return true;
-  switch ((r.V / X::kPer + kHeldThreads / 2 - 1) / (kHeldThreads / 2)) { HALF(1) HALF(2) HALF(3) HALF(4) HALF(5) HALF(6) HALF(7) HALF(8) }
+  // (rows of up to 512 whole chunks have gone to wavefronts)
+  switch ((r.V / X::kPer + kHeldThreads / 2 - 1) / (kHeldThreads / 2)) { HALF(3) HALF(4) HALF(5) HALF(6) HALF(7) HALF(8) }
 #undef HALF
   switch (need) {
-    HELD(1) HELD(2) HELD(3) HELD(4) HELD(5) HELD(6) HELD(7) HELD(8) HELD(9) HELD(10) HELD(11) HELD(12) HELD(13) HELD(14)
+    HELD(5) HELD(6) HELD(7) HELD(8) HELD(9) HELD(10) HELD(11) HELD(12) HELD(13) HELD(14)
     HELD(15) HELD(16) HELD(17) HELD(18) HELD(19) HELD(20) HELD(21) HELD(22) HELD(23) HELD(24) HELD(25) HELD(26) HELD(27)
     HELD(28) HELD(29) HELD(30) HELD(31) HELD(32)
   }
@@ -1339,7 +1341,7 @@ bool launch_distill(Call& c) {
   if (c.rows.V < 2 * X::kPer) return false;
   const int K = c.teacher.K;
   if (K <= 16 && launch_distill_lanes<X, 16, 1>(c)) return true;
-  if (K <= 64) return launch_distill_lanes<X, 16, 4>(c) || launch_distill_lanes<X, kWave, 1>(c) || launch_distill_block<X, 1>(c);
+  if (K <= 64) return launch_distill_lanes<X, 16, 4>(c) || launch_distill_lanes<X, kWave, 1, 3>(c) || launch_distill_block<X, 1>(c);
   if (K <= 256) return launch_distill_lanes<X, kWave, 4>(c) || launch_distill_block<X, 1>(c);
   return launch_distill_lanes<X, kWave, 16>(c) || (K <= 512 ? launch_distill_block<X, 1>(c) : launch_distill_block<X, 2>(c));
 }

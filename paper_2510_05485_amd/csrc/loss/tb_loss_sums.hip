@@ -45,7 +45,7 @@ __global__ __launch_bounds__(kThreads) void part_count_kernel(Rows r, int32_t* n
   if (threadIdx.x == 0) n[blockIdx.x] = part[0] + part[1] + part[2] + part[3];
 }
 
-// One workgroup: weights from the counts.
+// One workgroup: weights of means (over tokens or sequences) from the counts.
 __global__ __launch_bounds__(1024) void weight_kernel(int B, int average, const int32_t* n, float* weight) {
   __shared__ long long part[16];
   long long sum = 0;
@@ -56,10 +56,7 @@ __global__ __launch_bounds__(1024) void weight_kernel(int B, int average, const 
   sum = 0;
   for (int w = 0; w < 16; ++w) sum += part[w];
   for (int b = threadIdx.x; b < B; b += 1024) {
-    float w = 0.f;
-    if (n[b] > 0)
-      w = average == TB_SUM ? 1.f : float(1.0 / (average == TB_MEAN_TOKENS ? double(sum) : double(sum) * n[b]));
-    weight[b] = w;
+    weight[b] = n[b] > 0 ? float(1.0 / (average == TB_MEAN_TOKENS ? double(sum) : double(sum) * n[b])) : 0.f;
   }
 }
 

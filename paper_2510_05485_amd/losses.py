@@ -311,8 +311,8 @@ def _score(call, want_entropy, keep_state):
     return lp, entropy, state
 
 
-def _rows_gradient(call, state, d_lp, d_entropy, d_strides, upstream, out=None, scale=1.0):
-    out, g = call.gradient(out, scale)
+def _rows_gradient(call, state, d_lp, d_entropy, d_strides, upstream):
+    out, g = call.gradient(None, 1.0)
     # (hooks on saved tensors give back the same values, in what strides they like)
     state = call.values(state, "the rows' state", (*call.shape, 4))
     over = call.shape if d_strides[1] else (call.B,)
