@@ -41,7 +41,7 @@ def in_registers(V, per, long):
         return None
     need, half = up(V // per, 512), up(V // per, 256)
     if long and need > 32:
-        return (512, 32, True) if need - 32 <= 18 else (512, 46, True) if need - 46 <= 18 else None
+        return (512, 32, True) if need <= 46 else (512, 46, True) if need - 46 <= 18 else None
     if half <= 8:
         return 256, half, False
     return (512, need, False) if need <= 32 else None
