@@ -115,11 +115,23 @@ T* in(void* workspace, size_t offset) {
   return reinterpret_cast<T*>(static_cast<char*>(workspace) + offset);
 }
 // What a mean divides by is added up by every workgroup while its row is on its way, from the lengths, from
-// the mask of few positions, or from the numbers that a launch (4 us) counts in a mask; beyond so many
-// numbers a launch more leaves the weights.  (Policy loss on 4096 sequences of 512 positions of 64 logits: 12 us less.)
-constexpr int kMostParts = 8192, kMostMasked = 4096;
-hipError_t set_mean(Call& c, int average, const Workspace& w, void* workspace) {
+// the mask of few positions, or from the numbers that a launch counts in a mask; where that is too much for so
+// many workgroups, launches before leave the counts, or the weights.  Policy losses in bfloat16, us:
+//   sequences x positions x values    lengths in each workgroup   weights from two launches
+//   1024 x 8 x 5000 (8 million)        41.5                        41.6
+//   2048 x 8 x 5000 (34 million)      104.9                        91.2
+//   8000 x 8 x 5000                   539                         272
+//   512 x 16 x 50257 (4 million)      281.6                       288.1
+//   8000 x 64 x 64 (16 million)        49.3                        45.1
+//   positions x values                mask in each workgroup      counts from a launch
+//   1024 x 5000                        12.1                        13.6
+//   2048 x 1000, x 5000                11.9, 18.3                  13.0, 18.7
+//   4096 x 1000, x 5000                15.0, 31.4                  14.8, 26.4
+constexpr int kMostParts = 8192, kMostMasked = 2048;
+constexpr int64_t kMostReads = 1 << 23;  // of lengths (or counts), by all workgroups together
+hipError_t set_mean(Op op, Call& c, int average, const Workspace& w, void* workspace) {
   const Rows& r = c.rows;
+  const bool few = r.B <= kMostParts && r.B * workgroups_of(op, c) <= kMostReads;
   int32_t* n = in<int32_t>(workspace, w.counts);
   c.mean = {nullptr, nullptr, r.B, average};
   if (average == TB_SUM || (!r.mask && !r.lengths)) return hipSuccess;
@@ -129,16 +141,10 @@ hipError_t set_mean(Call& c, int average, const Workspace& w, void* workspace) {
     c.mean = {nullptr, n, kCountParts, TB_MEAN_TOKENS};
     return run_part_counts(r, n, c.stream);
   }
-  if (r.mask) {
-    c.mean.n = n;
-    const hipError_t e = run_counts(r, n, c.stream);
-    if (e != hipSuccess || r.B <= kMostParts) return e;
-  } else if (r.B <= kMostParts) {
-    return hipSuccess;
-  } else {
-    const hipError_t e = run_counts(r, n, c.stream);
-    if (e != hipSuccess) return e;
-  }
+  if (!r.mask && few) return hipSuccess;
+  if (r.mask) c.mean.n = n;
+  const hipError_t e = run_counts(r, n, c.stream);
+  if (e != hipSuccess || few) return e;
   c.mean.weight = in<float>(workspace, w.weight);
   return run_weights(r.B, average, n, in<float>(workspace, w.weight), c.stream);
 }
@@ -227,7 +233,7 @@ extern "C" int tensorloss_policy(const tb_logits_t* logits, const tb_positions_t
   c.policy = {policy->old_logprobs, policy->ref_logprobs, policy->advantages, policy->each, policy->clip_low,
               policy->clip_high, policy->kl_coef, policy->entropy_coef};
   c.entropy = policy->entropy_coef != 0.f;
-  if (set_mean(c, policy->average, w, workspace) != hipSuccess || run_rows(kPolicy, c) != hipSuccess)
+  if (set_mean(kPolicy, c, policy->average, w, workspace) != hipSuccess || run_rows(kPolicy, c) != hipSuccess)
     return TB_ERR_HIP;
   return done(run_terms(c.groups, partial, more, terms, 4, c.stream));
 }
@@ -284,7 +290,7 @@ extern "C" int tensorloss_distill(const tb_logits_t* logits, const tb_positions_
   c.rows.status = status;
   c.out = {row_loss, nullptr, nullptr, reinterpret_cast<float4*>(row_state), d_row, nullptr, partial};
   c.teacher = teacher_of(*teacher, r);
-  if (set_mean(c, teacher->average, w, workspace) != hipSuccess || run_rows(kDistill, c) != hipSuccess)
+  if (set_mean(kDistill, c, teacher->average, w, workspace) != hipSuccess || run_rows(kDistill, c) != hipSuccess)
     return TB_ERR_HIP;
   return done(run_terms(c.groups, partial, more, terms, 1, c.stream));
 }

@@ -24,6 +24,20 @@ struct Call {
 
 // A launch has less than 2^32 threads: from so many rows on, workgroups take several.
 constexpr int64_t kMostGroups = 1 << 22;
+// Workgroups that the card holds at a time take all rows of up to kLaneChunks chunks: 8 of 4 wavefronts on each of
+// 256 units.
+constexpr int kLaneGroups = 2048, kLaneChunks = 512;
+
+// About how many workgroups the launch of rows_of has.
+inline int64_t workgroups_of(Op op, const Call& c) {
+  const int64_t rows = int64_t(c.rows.B) * c.rows.T;
+  const int chunks = c.rows.V / (c.type == TB_FLOAT32 ? 4 : 8);
+  if (chunks < (op == kDistill ? 2 : 1) || chunks > kLaneChunks) return rows < kMostGroups ? rows : kMostGroups;
+  // a workgroup's rows at a time: of two to four chunks a lane; of 16 lanes or a wavefront
+  const int at_a_time = op != kDistill ? (chunks < 256 ? 1024 / chunks : 4) : chunks <= 128 && c.teacher.K <= 64 ? 16 : 4;
+  const int64_t groups = (rows + at_a_time - 1) / at_a_time;
+  return groups < kLaneGroups ? groups : kLaneGroups;
+}
 
 // A pass over all rows: statistics, the operator's values, and the gradient where rows.g is set.
 template <typename X>

@@ -1225,9 +1225,6 @@ int threads_of(const Rows& r, int per) {
   return chunks >= 1280 ? 512 : chunks >= 768 ? 256 : chunks >= 256 ? 128 : kWave;
 }
 
-// Workgroups that the card holds at a time take all rows: 8 of 4 wavefronts on each of 256 units.
-constexpr int kLaneGroups = 2048;
-
 template <typename X, int kOp, bool kEntropy>
 bool launch_lanes(Call& c) {
   const Rows& r = c.rows;
