@@ -283,7 +283,9 @@ PyObject* results(std::initializer_list<at::Tensor> all, PyObject* out, int out_
 PyObject* logprobs(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Call c;
   if (n != 7 || !c.take(args[0], args[1], args[2], args[3], args[4], args[5])) Py_RETURN_NONE;
-  const bool entropy = args[6] == Py_True;
+  const int wanted = PyObject_IsTrue(args[6]);
+  if (wanted < 0) return nullptr;
+  const bool entropy = wanted;
   at::Tensor lp = c.values(c.positions()), h, state;
   if (entropy) h = c.values(c.positions());
   const bool backward = differentiated(*c.x);

@@ -237,3 +237,14 @@ def test_tangents_are_refused(native):
                     f(dual)
         for f in all_of.values():                # without a tangent, as outside
             assert torch.isfinite(f(x))
+
+
+def test_entropies_that_any_true_value_asks_for():
+    x, _ = operators(64)
+    tokens = torch.zeros(4, 6, dtype=torch.int64, device=DEV)
+    lp, h = tb.token_logprobs(x, tokens, want_entropy=True)
+    for yes in (1, "yes"):
+        found = tb.token_logprobs(x, tokens, want_entropy=yes)
+        assert isinstance(found, tuple) and torch.equal(found[0], lp) and torch.equal(found[1], h)
+    for no in (0, None):
+        assert torch.equal(tb.token_logprobs(x, tokens, want_entropy=no), lp)
