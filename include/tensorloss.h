@@ -20,8 +20,10 @@
  *     is NULL).  What stands at other positions -- logits, tokens, values -- has no part in anything,
  *     whatever it is; log-probabilities, entropies and gradients there are 0.
  *   - Arithmetic is in float32, sums over positions in float64; gradients are rounded once to the
- *     logits' type.  The order of a row's sum goes by the row's length and by its address modulo 128.  A logit of -inf is a token that cannot be: it has probability and gradient 0.  A
- *     row that has no finite logit, or one of +inf or NaN, has no distribution: its values are NaN.
+ *     logits' type.  The order of a row's sum goes by the row's length and by its address modulo 128.
+ *   - A logit of -inf is a token that cannot be: it has probability 0 and, unless it is the position's
+ *     own token, gradient 0.  A row that has no finite logit, or one of +inf or NaN, has no
+ *     distribution: its values are NaN.  Finite logits may be of any size.
  *   - Results do not depend on the order in which workgroups run.
  *   - Problems that the host can see come back as tb_status_t before any work is enqueued.  A token
  *     (or teacher's) id outside [0, V) makes the values of its row NaN and sets TB_DEV_TOKEN_RANGE, a

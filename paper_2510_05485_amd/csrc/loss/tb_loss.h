@@ -46,7 +46,7 @@ struct At {
 struct RowOut {  // per position, any may be null
   float *logprobs, *entropy;
   double* exact;  // log-probabilities (kScore) whose logarithm is not rounded to 32 bits
-  float4* state;  // largest logit, sum of exponentials, entropy, log-probability
+  float4* state;  // reference logit (the largest, or one near it), sum of exponentials, entropy, log-probability
   float *d_logprobs, *d_entropy;
   double* partial;  // [workgroup][4]: the weighted terms of its rows
 };

@@ -9,9 +9,10 @@
 //   distill_kernel   the same with a teacher's entries: 16 lanes, a wavefront or a workgroup
 //   sweep_kernel     a workgroup reads the row from memory in each of two sweeps (any length)
 //   gradient_kernel  the second sweep alone, with statistics given
-// On one MI355X, with their gradients: the policy loss of 32 x 1024 rows of 50257 values in bfloat16, 62 % of
-// which count, 1034 us (5.2 TB/s; rows copied alone 5.2 to 5.7), of 16384 rows of 8191 94 us (5.7), of 1048576
-// rows of 64 69 us (3.9); distillation of 4096 rows of 32000 94 us (4.9).  Statistics alone: 6.2 to 6.9 TB/s.
+// Calls on one MI355X, with their gradients: the policy loss of 32 x 1024 rows of 50257 values in bfloat16, 62 % of
+// which count, 1014 us (5.3 TB/s; rows copied alone 5.2 to 5.7), of 16384 rows of 8191 110 us (4.9), of 1048576
+// rows of 64 71 us (3.8); distillation of 4096 rows of 32000 106 us (5.0).  Statistics alone: 6.2 to 6.9 TB/s.
+// Cards differ by 2 to 5 %; single launches under the profiler take 3 to 5 % longer.
 #pragma once
 
 #include <type_traits>
@@ -1247,9 +1248,10 @@ bool launch_lanes(Call& c) {
 
 // Longer rows than 32 chunks a thread: 32 or 46 of them in registers and up to 18 in LDS, one workgroup a unit.
 // 46 are as many as a thread has registers for beside its work, with which rows of 64 fit; they have to be there in
-// every thread, so that rows of up to 46 hold 32.  Where both would do, 47 to 50, 46 take 1 to 2 % less (2048 rows of 200003
-// values in bfloat16, of which three quarters count: policy loss 329 and 332 us, distilled 348 and 354).
-// 2047 rows of 262144 values in bfloat16, distilled: 655 us with sweeps, 443 so (4.6 TB/s).
+// every thread, so that rows of up to 46 hold 32.  Where both would do, 47 to 50, 46 take 1 to 4 % less (2048 rows of 200003
+// values in bfloat16, of which three quarters count: policy loss 325 and 331 us, distilled 342 and 356).
+// 2047 rows of 262144 values in bfloat16, distilled: 655 us with sweeps and 443 so, on one card; 449 to 482 on others
+// (4.2 to 4.6 TB/s).
 constexpr int kMoreFrom = 32, kFewer = 32, kMostHeld = 46, kMostMore = 18;
 template <typename Kernel>
 bool more_in_lds(Kernel kernel, int chunks, size_t* bytes) {
