@@ -2,8 +2,8 @@
  * tensorloss.h -- C ABI of the losses over a policy's logits (same library as tensorbleu.h).
  *
  * What a training loop does with the rewards that tensorbleu.h computes: log-probabilities of the
- * sampled tokens, the clipped policy loss, the loss of paired log ratios, and the distillation of a
- * teacher's best logits, each with its gradient in the logits.
+ * sampled tokens, the likeliest tokens beside them, the clipped policy loss, the loss of paired log ratios,
+ * and the distillation of a teacher's best logits, each with its gradient in the logits.
  *
  * Notation: row r = (sequence b, position t) of the logits holds V values x; z = x / temperature,
  * p = softmax(z), lp = z[token] - log sum exp z, H = -sum p log p.
@@ -82,6 +82,37 @@ int tensorloss_token_logprobs_grad(const tb_logits_t* logits, const tb_positions
                                    const float* d_entropy, int64_t d_seq_stride,
                                    int64_t d_pos_stride, const float* upstream,
                                    const tb_gradient_t* grad, void* hip_stream);
+
+typedef struct tb_top {
+  void* ids;          /* [B, T, K], of id_bytes 4 or 8 */
+  float* logprobs;    /* [B, T, K] (not used by the gradient) */
+  int32_t id_bytes, K; /* K in 1..min(V, TB_TOP_MOST) */
+} tb_top_t;
+
+enum { TB_TOP_MOST = 1024 };
+
+/* The K likeliest tokens of every position in descending order of their logits, equal ones (0 and -0 among
+ * them) by their ids, with their log-probabilities.  Logits of -inf are none of them: entries that are not
+ * there, and all of a position that does not count, have the id -1 and the log-probability -inf.  A row
+ * without a distribution has ids of -1 and log-probabilities of NaN.
+ * Beside them the log-probabilities of the tokens (logprobs NULL: at->tokens is not read) and entropies (NULL
+ * for none): float32 [B, T].  row_state: NULL, or float32 [B, T, 4] for the backward pass.
+ * workspace: of tensorloss_top_workspace_bytes (NULL where that is 0). */
+int tensorloss_top_logprobs(const tb_logits_t* logits, const tb_positions_t* at, const tb_top_t* top,
+                            float* logprobs, float* entropy, float* row_state, int32_t* status,
+                            void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradient of scale * sum over positions of (sum_k d_top_k lp(ids_k) + d_logprobs lp + d_entropy H) in the
+ * logits, ids and row_state as the forward pass left them for the same logits.  Entries with an id outside
+ * [0, V) have no part in it; no id comes twice.  d_top: float32 [B, T, K]; d_logprobs (NULL: tokens are not
+ * read) and d_entropy (or NULL): float32 [B, T].  The gradient may not overlap the logits. */
+int tensorloss_top_logprobs_grad(const tb_logits_t* logits, const tb_positions_t* at, const tb_top_t* top,
+                                 const float* row_state, const float* d_top, const float* d_logprobs,
+                                 const float* d_entropy, const tb_gradient_t* grad, void* hip_stream);
+
+/* Workspace of the forward pass, 256-byte aligned device memory that needs no initialisation: 0 for most
+ * shapes (and for invalid arguments), some bytes for rows so long that workgroups share them. */
+size_t tensorloss_top_workspace_bytes(int32_t B, int32_t T, int32_t V, int32_t type, int32_t K);
 
 /* How positions are averaged: weight w of a position that counts is 1/N (N: positions that count),
  * 1/(S n_b) (n_b: those of its sequence, S: sequences that have any), or 1. */

@@ -16,6 +16,6 @@ from .api import (  # noqa: F401
     sentence_bleu,
 )
 from .losses import (  # noqa: F401
-    DistillationLoss, PolicyLoss, PreferenceLoss, distillation_loss, distillation_loss_grad,
-    policy_loss, policy_loss_grad, preference_loss, preference_loss_grad, token_logprobs,
+    DistillationLoss, PolicyLoss, PreferenceLoss, TopLogprobs, distillation_loss, distillation_loss_grad,
+    policy_loss, policy_loss_grad, preference_loss, preference_loss_grad, token_logprobs, top_logprobs,
 )

@@ -1,6 +1,6 @@
 // Entry points of the losses: argument checks, workspace, launches.  Nothing here allocates,
 // synchronises or keeps state between calls.
-#include "tb_loss_host.h"
+#include "tb_loss_top_host.h"
 
 namespace tb {
 namespace loss {
@@ -171,11 +171,88 @@ Teacher teacher_of(const tb_teacher_t& q, const Rows& r) {
   return t;
 }
 
+// How many workgroups share a row of top log-probabilities.  One holds 32 chunks of 16 bytes a thread at most.
+constexpr int kHeldBytes = 512 * 32 * 16;
+constexpr int kSharedBytes = 65536;  // of a part where there are few rows
+int top_parts(int64_t rows, int V, int type) {
+  const int64_t bytes = int64_t(V) * value_bytes(type);
+  int64_t parts = bytes <= kHeldBytes ? 1 : (bytes + kHeldBytes / 2 - 1) / (kHeldBytes / 2);
+  if (rows * parts <= 128 && bytes >= 2 * kSharedBytes) parts = std::max(parts, std::min(256 / std::max(rows, int64_t(1)), bytes / kSharedBytes));
+  return int(parts);
+}
+size_t top_bytes(int64_t rows, int V, int type, int K, size_t* stats) {
+  const int parts = top_parts(rows, V, type);
+  *stats = aligned(size_t(rows) * parts * K * 8);
+  return parts == 1 ? 0 : *stats + aligned(size_t(rows) * parts * sizeof(float4));
+}
+bool top_fits(int V, int K) { return K >= 1 && K <= TB_TOP_MOST && K <= V; }
+// (call: rows and type are there)
+int check_top(const tb_top_t* top, TopCall* c, const Call& call) {
+  c->rows = call.rows;
+  c->type = call.type;
+  const Rows& r = c->rows;
+  if (!top || !top_fits(r.V, top->K) || (top->id_bytes != 4 && top->id_bytes != 8)) return TB_ERR_INVALID_ARG;
+  c->top = {top->ids, top->logprobs, top->K, top->id_bytes == 8};
+  if (empty(r)) return TB_OK;
+  return !top->ids || reinterpret_cast<uintptr_t>(top->ids) % top->id_bytes ? TB_ERR_INVALID_ARG : TB_OK;
+}
+
 }  // namespace
 }  // namespace loss
 }  // namespace tb
 
 using namespace tb::loss;
+
+extern "C" size_t tensorloss_top_workspace_bytes(int32_t B, int32_t T, int32_t V, int32_t type, int32_t K) {
+  if (!positions_fit(B, T) || V < 1 || type < TB_FLOAT32 || type > TB_FLOAT16 || !top_fits(V, K)) return 0;
+  size_t stats;
+  return top_bytes(int64_t(B) * T, V, type, K, &stats);
+}
+
+extern "C" int tensorloss_top_logprobs(const tb_logits_t* logits, const tb_positions_t* at, const tb_top_t* top,
+                                       float* logprobs, float* entropy, float* row_state, int32_t* status,
+                                       void* workspace, size_t workspace_bytes, void* hip_stream) {
+  Call call = {};
+  if (int rc = check(logits, at, logprobs != nullptr, nullptr, &call)) return rc;
+  TopCall c = {};
+  if (int rc = check_top(top, &c, call)) return rc;
+  if (empty(c.rows)) return TB_OK;
+  if (!top->logprobs) return TB_ERR_INVALID_ARG;
+  c.rows.status = status;
+  c.out.logprobs = logprobs;
+  c.out.entropy = entropy;
+  c.out.state = reinterpret_cast<float4*>(row_state);
+  c.entropy = entropy != nullptr;
+  c.stream = static_cast<hipStream_t>(hip_stream);
+  const int64_t rows = int64_t(c.rows.B) * c.rows.T;
+  size_t stats;
+  const size_t bytes = top_bytes(rows, c.rows.V, c.type, c.top.K, &stats);
+  c.split.parts = top_parts(rows, c.rows.V, c.type);
+  if (bytes) {
+    if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign || workspace_bytes < bytes) return TB_ERR_WORKSPACE;
+    c.split.keys = in<uint64_t>(workspace, 0);
+    c.split.stats = in<float4>(workspace, stats);
+  }
+  return done(c.type == TB_FLOAT32 ? top_of<F32>(c) : c.type == TB_BFLOAT16 ? top_of<BF16>(c) : top_of<F16>(c));
+}
+
+extern "C" int tensorloss_top_logprobs_grad(const tb_logits_t* logits, const tb_positions_t* at, const tb_top_t* top,
+                                            const float* row_state, const float* d_top, const float* d_logprobs,
+                                            const float* d_entropy, const tb_gradient_t* grad, void* hip_stream) {
+  Call call = {};
+  if (!grad) return TB_ERR_INVALID_ARG;
+  if (int rc = check(logits, at, d_logprobs != nullptr, grad, &call)) return rc;
+  TopCall c = {};
+  if (int rc = check_top(top, &c, call)) return rc;
+  if (empty(c.rows)) return TB_OK;
+  if (!row_state || !d_top || c.rows.g == c.rows.x) return TB_ERR_INVALID_ARG;
+  c.given = {reinterpret_cast<const float4*>(row_state), d_top, d_logprobs, d_entropy};
+  c.entropy = d_entropy != nullptr;
+  c.stream = static_cast<hipStream_t>(hip_stream);
+  return done(c.type == TB_FLOAT32    ? top_gradient_of<F32>(c)
+              : c.type == TB_BFLOAT16 ? top_gradient_of<BF16>(c)
+                                      : top_gradient_of<F16>(c));
+}
 
 extern "C" size_t tensorloss_workspace_bytes(int32_t B, int32_t T) {
   return positions_fit(B, T) ? workspace_of(B, T).bytes + kAlign : 0;

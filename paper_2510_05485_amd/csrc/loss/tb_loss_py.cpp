@@ -305,6 +305,37 @@ PyObject* logprobs(PyObject*, PyObject* const* args, Py_ssize_t n) {
   return results({lp, h}, Py_None, -1);
 }
 
+// top(logits, k, tokens, lengths, mask, temperature, status, want_entropy, id_bytes): (ids, log-probabilities,
+// those of the tokens or None, entropies or None) or None; not where the logits are differentiated
+PyObject* top(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  Call c;
+  if (n != 9 || !c.take(args[0], args[2] == Py_None ? nullptr : args[2], args[3], args[4], args[5], args[6])) Py_RETURN_NONE;
+  tb_top_t q = {};
+  if (differentiated(*c.x) || !take_int(args[1], &q.K) || !take_int(args[8], &q.id_bytes) || q.K < 1 ||
+      q.K > TB_TOP_MOST || q.K > c.logits.V || (q.id_bytes != 4 && q.id_bytes != 8))
+    Py_RETURN_NONE;
+  const int wanted = PyObject_IsTrue(args[7]);
+  if (wanted < 0) return nullptr;
+  at::DimVector shape(c.positions().begin(), c.positions().end());
+  shape.push_back(q.K);
+  at::Tensor ids = at::empty(shape, at::TensorOptions().dtype(q.id_bytes == 8 ? at::kLong : at::kInt).device(c.x->device()));
+  at::Tensor values = c.values(shape), lp, h, workspace;
+  if (c.tokens) lp = c.values(c.positions());
+  if (wanted) h = c.values(c.positions());
+  q.ids = ids.data_ptr();
+  q.logprobs = values.data_ptr<float>();
+  const size_t bytes = tensorloss_top_workspace_bytes(c.logits.B, c.logits.T, c.logits.V, c.logits.type, q.K);
+  if (bytes) workspace = at::empty({int64_t(bytes)}, at::TensorOptions().dtype(at::kByte).device(c.x->device()));
+  int rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = tensorloss_top_logprobs(&c.logits, &c.at, &q, c.tokens ? lp.data_ptr<float>() : nullptr,
+                               wanted ? h.data_ptr<float>() : nullptr, nullptr, c.status,
+                               bytes ? workspace.data_ptr() : nullptr, bytes, c.stream);
+  Py_END_ALLOW_THREADS
+  if (rc != TB_OK) Py_RETURN_NONE;
+  return results({ids, values, lp, h}, Py_None, -1);
+}
+
 // policy(logits, tokens, lengths, mask, temperature, status, out, grad_scale, old_logprobs, advantages,
 // ref_logprobs, clip_low, clip_high, kl_coef, entropy_coef, average): (terms, gradient, logprobs) or None;
 // grad_scale None: the loss, for torch to differentiate, and out is not used
@@ -453,6 +484,7 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t n) {
 
 PyMethodDef methods[] = {
     {"logprobs", reinterpret_cast<PyCFunction>(guarded<logprobs>), METH_FASTCALL, nullptr},
+    {"top", reinterpret_cast<PyCFunction>(guarded<top>), METH_FASTCALL, nullptr},
     {"policy", reinterpret_cast<PyCFunction>(guarded<policy>), METH_FASTCALL, nullptr},
     {"preference", reinterpret_cast<PyCFunction>(guarded<preference>), METH_FASTCALL, nullptr},
     {"distill", reinterpret_cast<PyCFunction>(guarded<distill>), METH_FASTCALL, nullptr},

@@ -1,0 +1,847 @@
+// The K likeliest tokens of every position, with their log-probabilities, beside those of given tokens and
+// entropies; and the gradient of all of these in the logits.
+//
+// z = x / temperature, lp = z - log sum exp z.  The order of the alternatives is that of x, equal ones by their
+// ids.  A row is read once.  Nothing of it is sorted: the K-th largest of the maxima that lanes have of
+// their parts of the row is a bound that K values reach at least, and about K (1 + K / 2 maxima) do; these are
+// collected, and each one's place is the number of those before it.  Kernels by the length of a row:
+//   short_kernel  up to 64 chunks of 16 bytes: 2 to 64 lanes of a wavefront hold a row, a chunk each, and the best
+//                 of the lanes' best is taken K times
+//   top_kernel    a wavefront, or a workgroup, holds a row (or a part of a long one) in its registers
+//   join_kernel   joins the parts of long rows
+#pragma once
+
+#include "tb_loss_rows.h"
+#include "tb_loss_top_host.h"
+
+namespace tb {
+namespace loss {
+namespace {
+
+// ---- the order of logits as one of whole numbers ----------------------------------------------
+
+// Order: value x -> int32 that grows with x, -0 and 0 alike: sign and magnitude as two's complement.
+template <typename X>
+struct Order;
+template <>
+struct Order<F32> {
+  static constexpr int kNone = -0x7F800000;  // of -inf
+  static constexpr int kShift = 16;          // of a bound in 16 bits
+  static __device__ __forceinline__ uint32_t of_packed(uint32_t u) {
+    const int mask = int(u) >> 31;
+    return uint32_t((int(u & 0x7FFFFFFFu) ^ mask) - mask);
+  }
+  static __device__ __forceinline__ float value(int t) {
+    return __uint_as_float(t < 0 ? 0x80000000u | uint32_t(-t) : uint32_t(t));
+  }
+  static __device__ __forceinline__ int raw(float v) { return __float_as_int(v); }
+  template <typename Take>
+  static __device__ __forceinline__ void each(u32x4 c, Take take) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) take(i, int(c[i]));
+  }
+  static __device__ __forceinline__ int largest(u32x4 c) { return max(max(int(c[0]), int(c[1])), max(int(c[2]), int(c[3]))); }
+};
+struct Order16 {
+  static constexpr int kShift = 0;
+  static __device__ __forceinline__ uint32_t of_packed(uint32_t u) {
+    i16x2 v;
+    __builtin_memcpy(&v, &u, 4);
+    const i16x2 mask = v >> 15, t = ((v & i16x2{0x7FFF, 0x7FFF}) ^ mask) - mask;
+    __builtin_memcpy(&u, &t, 4);
+    return u;
+  }
+  template <typename Take>
+  static __device__ __forceinline__ void each(u32x4 c, Take take) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      take(2 * i, int(short(c[i] & 0xFFFFu)));
+      take(2 * i + 1, int(c[i]) >> 16);
+    }
+  }
+  static __device__ __forceinline__ int largest(u32x4 c) {
+    const i16x2 top = upper_pair<1>(&c);
+    return max(int(top[0]), int(top[1]));
+  }
+};
+template <>
+struct Order<BF16> : Order16 {
+  static constexpr int kNone = -0x7F80;
+  static __device__ __forceinline__ float value(int t) { return Order<F32>::value(t * 65536); }
+  static __device__ __forceinline__ int raw(float v) { return __float_as_int(v) >> 16; }
+};
+template <>
+struct Order<F16> : Order16 {
+  static constexpr int kNone = -0x7C00;
+  static __device__ __forceinline__ float value(int t) {
+    const uint16_t u = uint16_t(t < 0 ? 0x8000 | -t : t);
+    _Float16 h;
+    __builtin_memcpy(&h, &u, 2);
+    return float(h);
+  }
+  static __device__ __forceinline__ int raw(float v) {
+    const _Float16 h = _Float16(v);
+    short s;
+    __builtin_memcpy(&s, &h, 2);
+    return s;
+  }
+};
+// Logits before others have larger keys; no key of a logit is 0.
+__device__ __forceinline__ uint64_t key_of(int t, int at) {
+  return uint64_t(uint32_t(t) ^ 0x80000000u) << 32 | uint32_t(~at);
+}
+__device__ __forceinline__ int order_in(uint64_t key) { return int(uint32_t(key >> 32) ^ 0x80000000u); }
+__device__ __forceinline__ int place_in(uint64_t key) { return int(~uint32_t(key)); }
+
+// ---- what a row leaves ------------------------------------------------------------------------
+
+__device__ __forceinline__ void put_id(const Top& q, int64_t i, int id) {
+  if (q.long_ids) static_cast<int64_t*>(q.ids)[i] = id;
+  else static_cast<int32_t*>(q.ids)[i] = id;
+}
+// Entries from `from` on that are not there.
+__device__ __forceinline__ void put_none(const Top& q, int64_t at, int from, float lp, int thread, int threads) {
+  for (int j = from + thread; j < q.K; j += threads) {
+    put_id(q, at * q.K + j, -1);
+    q.logprobs[at * q.K + j] = lp;
+  }
+}
+
+// Statistics of a row and how its log-probabilities follow: of weights 2^(x k - M), or 2^((x - m) k).
+struct Found {
+  float m, s, t;
+  bool apart;  // the second
+};
+__device__ __forceinline__ float scaled_logit(const Found& f, float x, float k) {
+  return f.apart ? (x - f.m) * k : fmaf(x, k, -scaled(f.m, k));
+}
+__device__ __forceinline__ float logprob(const Found& f, float x, float k, float inv_temp, float log_s) {
+  return (f.apart ? (x - f.m) * inv_temp : scaled_logit(f, x, k) * kLn2) - log_s;
+}
+// A row without a finite logit, or with +inf or NaN
+__device__ __forceinline__ bool lost(const Found& f) { return !(f.s > 0.f); }
+
+template <bool kEntropy>
+__device__ __forceinline__ void put_values(const Rows& r, const RowOut& o, const Found& f, float x, float k, float log_s,
+                                           int64_t at) {
+  const float lp = logprob(f, x, k, r.inv_temp, log_s), H = kEntropy ? log_s - kLn2 * f.t / f.s : 0.f;
+  if (o.logprobs) o.logprobs[at] = lp;
+  if (o.entropy) o.entropy[at] = H;
+  if (o.state) o.state[at] = {f.m, f.apart ? f.s * to_scaled(f.m, k) : f.s, H, lp};
+}
+
+// ---- rows in registers ------------------------------------------------------------------------
+
+// Chunks k kThreads + thread of a row, k < kChunks, of which all but the last kStep + 2 are there in every thread
+// (kStep: how many lengths one kernel serves; one for the row's head, one for parts that differ in length).
+template <typename X, int kThreads, int kChunks, int kStep>
+struct Taken {
+  using Row = Span<X, kThreads <= kWave ? 16 : kLine>;
+  using O = Order<X>;
+  static_assert(Row::kEdge <= kThreads);
+  static constexpr int kSure = kChunks - kStep - 2 > 0 ? kChunks - kStep - 2 : 0;
+  u32x4 c[kChunks];
+  float edge;
+  int edge_at;
+
+  static __device__ __forceinline__ bool there(const Row& row, int thread, int k) { return thread + k * kThreads < row.chunks; }
+  __device__ __forceinline__ void load(const Row& row, int thread) {
+    const char* from = reinterpret_cast<const char*>(row.x + row.head);
+    const uint32_t lane = thread * 16u;
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) {
+      if (k >= kSure) c[k] = u32x4{X::kNone, X::kNone, X::kNone, X::kNone};
+      if (k < kSure || there(row, thread, k)) c[k] = *reinterpret_cast<const u32x4_at16*>(from + k * (kThreads * 16) + lane);
+    }
+    edge_at = row.edge(thread);
+    edge = edge_at >= 0 ? X::load(row.x + edge_at) : -INFINITY;
+  }
+  __device__ __forceinline__ void keep_packed() {  // (as in Held)
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) asm volatile("" : "+v"(c[k]));
+  }
+  // The chunks as whole numbers in the order of their values.
+  __device__ __forceinline__ void to_order() {
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[k][i] = O::of_packed(c[k][i]);
+    keep_packed();
+  }
+  static __device__ __forceinline__ int order_of_edge(float v) {
+    const uint32_t bits = uint32_t(O::raw(v));
+    return O::kShift ? int(O::of_packed(bits)) : int(short(O::of_packed(bits)));
+  }
+  // The largest of the thread's values, in kParts groups.
+  static constexpr int kParts = 4;
+  __device__ __forceinline__ void largest(int* most, int edge_order) const {
+    most[0] = edge_order;
+#pragma unroll
+    for (int j = 1; j < kParts; ++j) most[j] = INT32_MIN;
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) most[k % kParts] = max(most[k % kParts], O::largest(c[k]));
+  }
+  // take(order, place) for each of the thread's values.
+  template <typename Take>
+  __device__ __forceinline__ void each(const Row& row, int thread, int edge_order, Take take) const {
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) {
+      const int at = row.at(thread + k * kThreads);
+      O::each(c[k], [&](int i, int t) { take(t, at + i); });
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    take(edge_order, edge_at);
+  }
+};
+
+// Statistics of a wavefront's part of a row, as in wave_stats; most: what its lanes' largest values are, as raw bits.
+template <bool kEntropy, typename X, int kThreads, int kChunks, int kStep>
+__device__ __forceinline__ Stats taken_stats(Taken<X, kThreads, kChunks, kStep>& h, float k) {
+  Stats mine = {fmaxf(h.edge, -kExtreme), 0.f, 0.f};
+  constexpr int kSure = Taken<X, kThreads, kChunks, kStep>::kSure;
+  if constexpr (kSure > 0) mine.m = fmaxf(mine.m, X::template upper<kSure>(h.c));
+#pragma unroll
+  for (int j = kSure; j < kChunks; ++j) {  // (with what lies beyond the row)
+    float v[X::kPer];
+    X::unpack(h.c[j], v);
+#pragma unroll
+    for (int i = 0; i < X::kPer; i += 2) mine.m = max3(mine.m, v[i], v[i + 1]);
+  }
+  mine.m = full_wave_max(mine.m);
+  const float M = scaled(mine.m, k);
+  auto take = [&](float x) {
+    const float a = fmaf(x, k, -M), w = exp2_fast(a);
+    mine.s += w;
+    if (kEntropy) mine.t += w * finite(a);
+  };
+#pragma unroll
+  for (int j = 0; j < kChunks; ++j) {
+    float v[X::kPer];
+    X::unpack(h.c[j], v);
+#pragma unroll
+    for (int i = 0; i < X::kPer; ++i) take(v[i]);
+  }
+  take(h.edge);
+  h.keep_packed();
+  mine.s = full_wave_sum(mine.s);
+  if (kEntropy) mine.t = full_wave_sum(mine.t);
+  if (kThreads > kWave && mine.s > 0x1p88f) mine.s = __uint_as_float(kNan);
+  return mine;
+}
+
+// A number that `need` of a wavefront's lanes' largest values reach (in all lanes), 16 bits of it: these, or those of
+// the four groups that each lane has where more are needed.  The least number if there are not so many.
+template <typename X>
+__device__ __forceinline__ int wave_bound(const int* most, int need) {
+  constexpr int kBias = 32768, kParts = 4;
+  int u[kParts];
+#pragma unroll
+  for (int j = 0; j < kParts; ++j) u[j] = (most[j] >> Order<X>::kShift) + kBias;
+  int b = 0;
+  if (need <= kWave / 2) {
+    const int v = max(max(u[0], u[1]), max(u[2], u[3]));
+    for (int bit = 1 << 15; bit; bit >>= 1)
+      if (__popcll(__ballot(v >= (b | bit))) >= need) b |= bit;
+  } else {
+    for (int bit = 1 << 15; bit; bit >>= 1) {
+      int n = 0;
+#pragma unroll
+      for (int j = 0; j < kParts; ++j) n += __popcll(__ballot(u[j] >= (b | bit)));
+      if (n >= need) b |= bit;
+    }
+  }
+  return (b - kBias) * (1 << Order<X>::kShift);
+}
+
+// What the threads that share a row leave for one another; counted: two, taken in turn.
+template <int kWaves>
+struct TopShared {
+  Stats parts[kWaves];
+  int bounds[2][kWaves], counts[kWaves], counted[2][kWaves];
+};
+
+// How many of the row's values fulfil `holds`, in all threads.
+template <int kThreads, typename H, typename Row, typename Holds>
+__device__ __forceinline__ int row_count(const H& h, const Row& row, int thread, int edge_order, int* counted, Holds holds) {
+  int n = 0;
+  h.each(row, thread, edge_order, [&](int t, int at) { n += holds(t, at); });
+  n = full_wave_sum(n);
+  if constexpr (kThreads > kWave) {
+    if (thread % kWave == 0) counted[thread / kWave] = n;
+    __syncthreads();
+    n = 0;
+    for (int w = 0; w < kThreads / kWave; ++w) n += counted[w];
+  }
+  return n;
+}
+
+// Where the values that the bound lets through are too many (ties, masks of the lowest value, a few places that have
+// all large values): the K-th value itself and up to which place its equals are taken, by halving.  Slow, and right for
+// every row: about 50 passes over the registers.
+template <int kThreads, typename H, typename Row, typename Shared>
+__device__ __forceinline__ void exact_bound(const H& h, const Row& row, int thread, int edge_order, int K, int V,
+                                            Shared& shared, int* bound, int* before) {
+  int turn = 0;
+  auto count = [&](auto holds) {
+    turn ^= 1;
+    return row_count<kThreads>(h, row, thread, edge_order, shared.counted[turn], holds);
+  };
+  // the largest b that K values reach, above -inf
+  int64_t low = H::O::kNone + 1, high = int64_t(INT32_MAX) + 1;
+  while (high - low > 1) {
+    const int mid = int((low + high) >> 1);
+    if (count([mid](int t, int) { return t >= mid; }) >= K) low = mid;
+    else high = mid;
+  }
+  const int b = int(low), above = count([b](int t, int) { return t > b; });
+  // the first place before which there are enough of its equals (b or less: fewer finite values than K)
+  int64_t none = 0, enough = V;
+  while (enough - none > 1) {
+    const int mid = int((none + enough) >> 1);
+    if (count([b, mid](int t, int at) { return t == b && at < mid; }) >= K - above) enough = mid;
+    else none = mid;
+  }
+  *bound = b;
+  *before = int(enough);
+}
+
+// Joined parts of a row, of weights 2^((x - m) k) (apart), for parts that a kernel after this one joins.
+__device__ __forceinline__ Found moved_apart(const Found& f, float k) {
+  if (f.apart || !scales(f.m, k)) return {f.m, f.s, f.t, true};
+  const float d = -fmaf(f.m, k, -scaled(f.m, k)), e = exp2_fast(d);
+  return {f.m, e * f.s, e * (f.t + d * f.s), true};
+}
+
+constexpr int kTopThreads = 256;  // of a workgroup whose wavefronts have rows of their own
+
+// The first value of a part of a long row: multiples of 64, so that parts are alike in length up to 64 values.
+__device__ __forceinline__ int part_from(int V, int part, int parts) {
+  return part == parts ? V : int(int64_t(V) * part / parts) & ~63;
+}
+
+// kThreads threads a row, or a part of one: a wavefront of four in a workgroup, or a workgroup.
+// room: candidates that a wavefront may find, K at least, an even number.
+template <typename X, bool kEntropy, int kThreads, int kChunks, int kStep>
+__global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void top_kernel(Rows r, RowOut o, Top q, Split split,
+                                                                                      int room) {
+  constexpr bool kAlone = kThreads > kWave;
+  constexpr int kTeams = kAlone ? 1 : kTopThreads / kThreads, kWaves = kAlone ? kThreads / kWave : 1;
+  using H = Taken<X, kThreads, kChunks, kStep>;
+  using O = Order<X>;
+  extern __shared__ __attribute__((aligned(16))) uint64_t candidates[];  // [team][wave][room]
+  __shared__ TopShared<kWaves> all[kTeams];
+  const int team = threadIdx.x / kThreads, thread = threadIdx.x % kThreads, wave = thread / kWave, lane = threadIdx.x % kWave;
+  const bool first = thread == 0;
+  TopShared<kWaves>& shared = all[team];
+  uint64_t* keys = candidates + team * kWaves * room;
+  const int64_t rows = int64_t(r.B) * r.T, units = rows * split.parts;
+  const float k = r.inv_temp * kLog2e;
+  for (int64_t unit = int64_t(blockIdx.x) * kTeams + team; unit < units; unit += int64_t(gridDim.x) * kTeams) {
+    const int64_t which = split.parts == 1 ? unit : unit / split.parts;
+    const int part = int(unit - which * split.parts);
+    const int64_t at = kAlone && split.parts == 1 ? row_of_group(which, rows) : which;
+    const At pos = position(r, at);
+    const int b = pos.b, t = pos.t;
+    if (first && part == 0 && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
+    if (!counts(r, b, t)) {
+      if (part == 0) {
+        if (first) leave_nothing(o, at);
+        put_none(q, at, 0, -INFINITY, thread, kThreads);
+      }
+      continue;
+    }
+    const int from = part_from(r.V, part, split.parts), V = part_from(r.V, part + 1, split.parts) - from;
+    const typename H::Row row(row_of<X>(r, b, t) + from, V);
+    // (what comes first is waited for first: not behind the whole row)
+    const int token = r.tokens && part == 0 ? take_token(r, b, t, first) : -1;
+    H h;
+    h.load(row, thread);
+    const float x = token < 0 ? __uint_as_float(kNan) : X::load(row_of<X>(r, b, t) + token);
+    // Raw bits as signed integers are in the values' order from 0 on, with all others below: they do as long as
+    // the bound is above 0.
+    bool raw = true;
+    int most[H::kParts], edge_order = O::raw(h.edge);
+    h.largest(most, edge_order);
+    const int need = (q.K + kWaves - 1) / kWaves;
+    int bound = wave_bound<X>(most, need);
+    Stats s = taken_stats<kEntropy>(h, k);
+    if constexpr (kAlone) {
+      if (lane == 0) {
+        shared.parts[wave] = s;
+        shared.bounds[0][wave] = bound;
+      }
+      __syncthreads();
+      s = block_stats<kEntropy, kWaves>(shared.parts, k);
+      for (int w = 0; w < kWaves; ++w) bound = min(bound, shared.bounds[0][w]);
+    }
+    const bool extreme = !fine(s, k);
+    if (extreme) {
+      meet<kThreads>();
+      s = row_stats<X, kEntropy, kThreads>(row, k, thread, shared.parts);
+    }
+    const Found f = {s.m, s.s, s.t, extreme};
+    const bool none = f.s != f.s || (split.parts == 1 && lost(f));
+    auto to_order = [&] {
+      h.to_order();
+      edge_order = H::order_of_edge(h.edge);
+      raw = false;
+    };
+    if (bound < 1) {
+      to_order();
+      h.largest(most, edge_order);
+      bound = wave_bound<X>(most, need);
+      if constexpr (kAlone) {
+        if (lane == 0) shared.bounds[1][wave] = bound;
+        __syncthreads();
+        for (int w = 0; w < kWaves; ++w) bound = min(bound, shared.bounds[1][w]);
+      }
+      bound = max(bound, O::kNone + 1);
+    }
+    // The values from the bound on (its equals up to a place), as keys in LDS, a part for each wavefront.
+    int before = INT32_MAX, found = 0, total = 0;
+    uint64_t* own = keys + wave * room;
+    for (int attempt = 0; !none; ++attempt) {
+      found = 0;
+      auto take = [&](int t, int place) {
+        const bool is = t > bound || (t == bound && place < before);
+        const uint64_t mask = __ballot(is);
+        if (mask == 0) return;
+        const int slot = found + __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
+        if (is && slot < room) own[slot] = key_of(t, from + place);
+        found += __popcll(mask);
+      };
+#pragma unroll
+      for (int j = 0; j < kChunks; ++j) {
+        if (!__any(O::largest(h.c[j]) >= bound)) continue;
+        const int place = row.at(thread + j * kThreads);
+        O::each(h.c[j], [&](int i, int t) { take(t, place + i); });
+      }
+      take(edge_order, h.edge_at);
+      if (lane == 0) {
+        if (found < room) own[found] = 0;  // (keys are read in pairs)
+        if (kAlone) shared.counts[wave] = found;
+      }
+      meet<kThreads>();
+      total = found;
+      bool much = found > room;
+      if constexpr (kAlone) {
+        total = 0;
+        for (int w = 0; w < kWaves; ++w) {
+          const int n = shared.counts[w];
+          total += n;
+          much = much || n > room;
+        }
+      }
+      if (!much || attempt > 0) break;
+      if (raw) to_order();
+      exact_bound<kThreads>(h, row, thread, edge_order, q.K, V, shared, &bound, &before);
+      meet<kThreads>();
+    }
+    // Each one's place is the number of larger keys.
+    const float log_s = logf(f.s);
+    for (int i = lane; i < found; i += kWave) {
+      const uint64_t key = own[i];
+      int rank = 0;
+      for (int w = 0; w < kWaves; ++w) {
+        const uint64_t* others = keys + w * room;
+        const int n = kAlone ? shared.counts[w] : found;
+        for (int j = 0; j < n; j += 2) {
+          const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(others + j);
+          rank += (two.x > key) + (two.y > key);
+        }
+      }
+      if (rank >= q.K) continue;
+      if (split.parts > 1) {
+        split.keys[unit * q.K + rank] = key;
+      } else {
+        put_id(q, at * q.K + rank, place_in(key));
+        q.logprobs[at * q.K + rank] = logprob(f, O::value(order_in(key)), k, r.inv_temp, log_s);
+      }
+    }
+    if (split.parts > 1) {
+      for (int j = min(total, q.K) + thread; j < q.K; j += kThreads) split.keys[unit * q.K + j] = 0;
+      const Found g = moved_apart(f, k);
+      if (first) split.stats[unit] = {g.m, g.s, g.t, x};
+    } else {
+      put_none(q, at, min(total, q.K), none ? __uint_as_float(kNan) : -INFINITY, thread, kThreads);
+      if (first) put_values<kEntropy>(r, o, f, x, k, log_s, at);
+    }
+    meet<kThreads>();  // (before the next row takes the shared memory)
+  }
+}
+
+// ---- the parts of long rows -------------------------------------------------------------------
+
+// `last`: over the workgroup's threads, the largest or smallest key.
+template <bool kLargest>
+__device__ __forceinline__ uint64_t block_key(uint64_t v, uint64_t* part) {
+#pragma unroll
+  for (int d = kWave / 2; d; d >>= 1) {
+    const uint64_t u = __shfl_xor(static_cast<unsigned long long>(v), d);
+    v = (u > v) == kLargest ? u : v;
+  }
+  if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
+  __syncthreads();
+  v = part[0];
+  for (int w = 1; w < kTopThreads / kWave; ++w) v = (part[w] > v) == kLargest ? part[w] : v;
+  return v;
+}
+
+// One workgroup a row.  Every part's keys are in descending order: the largest of the parts' K-th keys is reached by K
+// keys, and so is the smallest of their (K / parts)-th ones.
+constexpr int kJoinRoom = 2048;
+template <typename X, bool kEntropy>
+__global__ __launch_bounds__(kTopThreads) void join_kernel(Rows r, RowOut o, Top q, Split split) {
+  __shared__ __attribute__((aligned(16))) uint64_t keys[kJoinRoom + 2];
+  __shared__ uint64_t tops[kTopThreads / kWave], lows[kTopThreads / kWave];
+  __shared__ int counted[2][kTopThreads / kWave], slots;
+  const int thread = threadIdx.x;
+  const int64_t rows = int64_t(r.B) * r.T;
+  const float k = r.inv_temp * kLog2e;
+  for (int64_t at = blockIdx.x; at < rows; at += gridDim.x) {
+    const At pos = position(r, at);
+    if (!counts(r, pos.b, pos.t)) continue;  // (the kernel before has written what is left of it)
+    const uint64_t* from = split.keys + at * split.parts * q.K;
+    const float4* stats = split.stats + at * split.parts;
+    const int K = q.K, share = (K + split.parts - 1) / split.parts;
+    const int64_t n = int64_t(split.parts) * K;
+    if (thread == 0) slots = 0;
+    uint64_t top = 0, low = ~uint64_t(0);
+    for (int p = thread; p < split.parts; p += kTopThreads) {
+      top = max(top, from[int64_t(p) * K + K - 1]);
+      low = min(low, from[int64_t(p) * K + share - 1]);
+    }
+    top = block_key<true>(top, tops);
+    low = block_key<false>(low, lows);
+    uint64_t bound = max(max(top, low), uint64_t(1));
+    Stats s = {kLowest, 0.f, 0.f};
+    for (int p = 0; p < split.parts; ++p) {
+      const float4 v = stats[p];
+      s = joined<kEntropy>(s, Stats{v.x, v.y, v.z}, k);
+    }
+    const Found f = {s.m, s.s, s.t, true};
+    const float x = stats[0].w, log_s = logf(f.s);
+    const bool none = lost(f);
+    int total = 0;
+    while (!none) {
+      for (int64_t i = thread; i < n; i += kTopThreads) {
+        const uint64_t key = from[i];
+        if (key < bound) continue;
+        const int slot = atomicAdd(&slots, 1);
+        if (slot < kJoinRoom) keys[slot] = key;
+      }
+      __syncthreads();
+      total = slots;
+      if (total <= kJoinRoom) break;
+      // the K-th key itself, by halving: keys differ from one another
+      uint64_t high = ~uint64_t(0);
+      int turn = 0;
+      while (high - bound > 1) {
+        const uint64_t mid = bound + (high - bound) / 2;
+        int c = 0;
+        for (int64_t i = thread; i < n; i += kTopThreads) c += from[i] >= mid;
+        c = full_wave_sum(c);
+        turn ^= 1;
+        if (thread % kWave == 0) counted[turn][thread / kWave] = c;
+        __syncthreads();
+        c = 0;
+        for (int w = 0; w < kTopThreads / kWave; ++w) c += counted[turn][w];
+        if (c >= K) bound = mid;
+        else high = mid;
+      }
+      if (thread == 0) slots = 0;
+      __syncthreads();
+    }
+    if (thread == 0) keys[total] = 0;  // (read in pairs)
+    __syncthreads();
+    for (int i = thread; i < total; i += kTopThreads) {
+      const uint64_t key = keys[i];
+      int rank = 0;
+      for (int j = 0; j < total; j += 2) {
+        const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(keys + j);
+        rank += (two.x > key) + (two.y > key);
+      }
+      if (rank >= K) continue;
+      put_id(q, at * K + rank, place_in(key));
+      q.logprobs[at * K + rank] = logprob(f, Order<X>::value(order_in(key)), k, r.inv_temp, log_s);
+    }
+    put_none(q, at, min(total, K), none ? __uint_as_float(kNan) : -INFINITY, thread, kTopThreads);
+    if (thread == 0) put_values<kEntropy>(r, o, f, x, k, log_s, at);
+    __syncthreads();  // (before the next row takes the shared memory)
+  }
+}
+
+// ---- short rows -------------------------------------------------------------------------------
+
+// The largest key of the lanes that share a row, in all of them.
+template <int kLanes, int kStep = 1>
+__device__ __forceinline__ uint32_t lanes_most(uint32_t v) {
+  if constexpr (kStep == kLanes) return v;
+  else return lanes_most<kLanes, kStep * 2>(max(v, __float_as_uint(neighbour<kStep>(__uint_as_float(v)))));
+}
+template <int kLanes, int kStep = 1>
+__device__ __forceinline__ uint64_t lanes_most(uint64_t v) {
+  if constexpr (kStep == kLanes) return v;
+  else {
+    const uint32_t high = __float_as_uint(neighbour<kStep>(__uint_as_float(uint32_t(v >> 32))));
+    const uint32_t low = __float_as_uint(neighbour<kStep>(__uint_as_float(uint32_t(v))));
+    return lanes_most<kLanes, kStep * 2>(max(v, uint64_t(high) << 32 | low));
+  }
+}
+
+// Keys in descending order: Batcher's exchanges (1968) for four and eight.
+template <typename Key>
+__device__ __forceinline__ void exchange(Key* v, int i, int j) {
+  const Key a = v[i], b = v[j];
+  v[i] = max(a, b);
+  v[j] = min(a, b);
+}
+template <typename Key, int kN>
+__device__ __forceinline__ void sort_keys(Key* v) {
+  static_assert(kN == 4 || kN == 8);
+#pragma unroll
+  for (int h = 0; h < kN; h += 4) {
+    exchange(v, h, h + 1);
+    exchange(v, h + 2, h + 3);
+    exchange(v, h, h + 2);
+    exchange(v, h + 1, h + 3);
+    exchange(v, h + 1, h + 2);
+  }
+  if constexpr (kN == 8) {
+    exchange(v, 0, 4);
+    exchange(v, 1, 5);
+    exchange(v, 2, 6);
+    exchange(v, 3, 7);
+    exchange(v, 2, 4);
+    exchange(v, 3, 5);
+    exchange(v, 1, 2);
+    exchange(v, 3, 4);
+    exchange(v, 5, 6);
+  }
+}
+
+// Keys of short rows: in 32 bits with the place in the lower half where values have 16.
+template <typename X>
+struct ShortKey {
+  using type = uint32_t;
+  static __device__ __forceinline__ type of(int t, int place) { return uint32_t(t + 32768) << 16 | uint32_t(0xFFFF - place); }
+  static __device__ __forceinline__ int order(type key) { return int(key >> 16) - 32768; }
+  static __device__ __forceinline__ int place(type key) { return 0xFFFF - int(key & 0xFFFFu); }
+};
+template <>
+struct ShortKey<F32> {
+  using type = uint64_t;
+  static __device__ __forceinline__ type of(int t, int place) { return key_of(t, place); }
+  static __device__ __forceinline__ int order(type key) { return order_in(key); }
+  static __device__ __forceinline__ int place(type key) { return place_in(key); }
+};
+
+// kLanes lanes of a wavefront a row, a chunk each, whose values each lane puts in order; the best of the lanes' best is
+// the row's next one.
+template <typename X, bool kEntropy, int kLanes>
+__global__ __launch_bounds__(kTopThreads) void short_kernel(Rows r, RowOut o, Top q) {
+  constexpr int kTeams = kTopThreads / kLanes;
+  using O = Order<X>;
+  using Key = ShortKey<X>;
+  const int lane = threadIdx.x % kLanes;
+  const int64_t rows = int64_t(r.B) * r.T;
+  const float k = r.inv_temp * kLog2e;
+  const int V = max(r.V, X::kPer);  // (a chunk at least, with nothing behind the row)
+  for (int64_t round = blockIdx.x; round * kTeams < rows; round += gridDim.x) {
+    const int64_t at = round * kTeams + threadIdx.x / kLanes;
+    const bool inside = at < rows;
+    const At pos = position(r, inside ? at : rows - 1);
+    const int b = pos.b, t = pos.t;
+    const bool live = inside && counts(r, b, t);
+    if (inside && lane == 0 && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
+    const typename X::type* values = row_of<X>(r, b, t);
+    Part<X, kLanes, 1> part;
+    if (r.V >= X::kPer) {
+      part.load(values, V, lane, live);
+    } else {
+      float v[X::kPer];
+#pragma unroll
+      for (int i = 0; i < X::kPer; ++i) v[i] = live && lane == 0 && i < r.V ? X::load(values + i) : -INFINITY;
+      part.c[0] = X::pack(v);
+    }
+    const int token = live && r.tokens ? take_token(r, b, t, lane == 0) : -1;
+    const float x = token < 0 ? __uint_as_float(kNan) : X::load(values + token);
+    const Stats s = part_stats<kEntropy, kLanes>(part, V, lane, k);
+    const Found f = {s.m, s.s, s.t, true};
+    const bool none = lost(f);
+    const float log_s = logf(f.s);
+    typename Key::type keys[X::kPer];
+    {
+      float v[X::kPer];
+      part.once(V, lane, 0, v);
+      const int place = Part<X, kLanes, 1>::at(V, lane, 0);
+#pragma unroll
+      for (int i = 0; i < X::kPer; ++i) {
+        const int order = Taken<X, kWave, 1, 1>::order_of_edge(v[i]);
+        keys[i] = order > O::kNone && live && !none ? Key::of(order, place + i) : 0;
+      }
+    }
+    sort_keys<typename Key::type, X::kPer>(keys);
+    typename Key::type kept = 0;
+    for (int j = 0; j < q.K; ++j) {
+      const typename Key::type best = lanes_most<kLanes>(keys[0]);
+      if (j % kLanes == lane) kept = best;
+      const bool mine = keys[0] == best;
+#pragma unroll
+      for (int i = 0; i < X::kPer - 1; ++i) keys[i] = mine ? keys[i + 1] : keys[i];
+      keys[X::kPer - 1] = mine ? 0 : keys[X::kPer - 1];
+      if (j % kLanes != kLanes - 1 && j != q.K - 1) continue;
+      if (inside && lane <= j % kLanes) {
+        const int64_t to = at * q.K + (j - j % kLanes + lane);
+        put_id(q, to, kept ? Key::place(kept) : -1);
+        q.logprobs[to] = kept          ? logprob(f, O::value(Key::order(kept)), k, r.inv_temp, log_s)
+                         : live && none ? __uint_as_float(kNan)
+                                        : -INFINITY;
+      }
+    }
+    if (lane == 0 && live) put_values<kEntropy>(r, o, f, x, k, log_s, at);
+    else if (lane == 0 && inside) leave_nothing(o, at);
+  }
+}
+
+// ---- gradient ---------------------------------------------------------------------------------
+
+// kThreads threads a row: the softmax's part from one reading of the row, then the entries' and the token's places
+// written over with what they get beside it.
+template <typename X, bool kEntropy, int kThreads>
+__global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void top_gradient_kernel(Rows r, Top q, TopGiven v) {
+  constexpr bool kAlone = kThreads > kWave;
+  constexpr int kTeams = kAlone ? 1 : kTopThreads / kThreads;
+  __shared__ float sums[kAlone ? kThreads / kWave : 1];
+  const int team = threadIdx.x / kThreads, thread = threadIdx.x % kThreads;
+  const int64_t rows = int64_t(r.B) * r.T;
+  const float k = r.inv_temp * kLog2e, scale = r.g_scale * r.inv_temp;
+  for (int64_t i = int64_t(blockIdx.x) * kTeams + team; i < rows; i += int64_t(gridDim.x) * kTeams) {
+    const int64_t at = kAlone ? row_of_group(i, rows) : i;
+    const At pos = position(r, at);
+    const int b = pos.b, t = pos.t;
+    if (!counts(r, b, t)) {
+      write_zeros<X>(r, b, t, thread, kThreads);
+      continue;
+    }
+    using Row = Span<X, kThreads <= kWave ? 16 : kLine>;
+    const Row row(row_of<X>(r, b, t), r.V);
+    typename X::type* g = gradient_of<X>(r, b, t);
+    const float4 state = v.state[at];
+    const float d_lp = v.d_lp ? v.d_lp[at] : 0.f, d_H = kEntropy ? v.d_entropy[at] : 0.f;
+    const int token = r.tokens && v.d_lp ? take_token(r, b, t, false) : -1;
+    auto entry = [&](int j) {
+      const int64_t id = load_id(q.ids, q.long_ids, at * q.K + j);
+      return id >= 0 && id < r.V ? int(id) : -1;
+    };
+    float sum = 0.f;
+    for (int j = thread; j < q.K; j += kThreads) sum += entry(j) < 0 ? 0.f : v.d_top[at * q.K + j];
+#pragma unroll
+    for (int d = 1; d < (kAlone ? kWave : kThreads); d <<= 1) sum += __shfl_xor(sum, d);
+    if constexpr (kAlone) {
+      if (thread % kWave == 0) sums[thread / kWave] = sum;
+      __syncthreads();
+      sum = 0.f;
+      for (int w = 0; w < kThreads / kWave; ++w) sum += sums[w];
+    }
+    // (a wrong token makes the row NaN)
+    const float all = r.tokens && v.d_lp && token < 0 ? __uint_as_float(kNan) : sum + d_lp;
+    const Slope f = slope_of(state.y * from_scaled(state.x, k), state.z, all, d_H, scale);
+    write_gradient<X, kEntropy, kThreads>(row, g, thread, state.x, k, f);
+    meet<kThreads>();  // (what it has stored comes before what follows)
+    auto over = [&](int id, float d) {
+      const float a = (X::load(row.x + id) - state.x) * k;
+      X::store(g + id, scale * d + gradient_at<kEntropy>(a, f));
+    };
+    if (thread == 0 && token >= 0) over(token, d_lp);
+    meet<kThreads>();
+    for (int j = thread; j < q.K; j += kThreads) {
+      const int id = entry(j);
+      if (id >= 0) over(id, v.d_top[at * q.K + j] + (id == token ? d_lp : 0.f));
+    }
+    meet<kThreads>();
+  }
+}
+
+// ---- launches ---------------------------------------------------------------------------------
+
+template <typename X, bool kEntropy>
+hipError_t launch_top(const TopCall& c) {
+  const Rows& r = c.rows;
+  const int64_t rows = int64_t(r.B) * r.T;
+  const int chunks = (r.V + X::kPer - 1) / X::kPer;
+  auto groups_of = [](int64_t units, int at_a_time) {
+    const int64_t groups = (units + at_a_time - 1) / at_a_time;
+    return int(groups < kMostGroups ? groups : kMostGroups);
+  };
+#define SHORT(lanes)                                                                                          \
+  if (chunks <= lanes) {                                                                                      \
+    short_kernel<X, kEntropy, lanes>                                                                          \
+        <<<std::min(groups_of(rows, kTopThreads / lanes), kLaneGroups), kTopThreads, 0, c.stream>>>(r, c.out, c.top); \
+    return hipGetLastError();                                                                                 \
+  }
+  SHORT(2) SHORT(4) SHORT(8) SHORT(16) SHORT(32) SHORT(64)
+#undef SHORT
+  // the longest part
+  const int64_t most = r.V / c.split.parts + (c.split.parts > 1 ? 64 : 0);
+  const int whole = int(most / X::kPer);
+  const int room = c.top.K <= 256 ? 256 : 1024;
+  auto go = [&](auto kernel, int threads) {
+    const int teams = threads <= kWave ? kTopThreads / threads : 1, waves = std::max(threads, kTopThreads * (teams > 1)) / kWave;
+    const size_t bytes = size_t(waves) * room * sizeof(uint64_t);
+    if (bytes > kPlainLds) {
+      const hipError_t e = grant_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes);
+      if (e != hipSuccess) return e;
+    }
+    kernel<<<groups_of(rows * c.split.parts, teams), waves * kWave, bytes, c.stream>>>(r, c.out, c.top, c.split, room);
+    return hipGetLastError();
+  };
+  auto need = [&](int threads) { return (whole + threads - 1) / threads; };
+#define HELD(threads, n, step) \
+  if (need(threads) <= n) return go(top_kernel<X, kEntropy, threads, n, step>, threads);
+  if (c.split.parts == 1) {
+    HELD(64, 2, 2) HELD(64, 4, 2) HELD(64, 6, 2) HELD(64, 8, 2)
+    HELD(256, 4, 2) HELD(256, 6, 2) HELD(256, 8, 2)
+  }
+  HELD(512, 6, 4) HELD(512, 8, 2) HELD(512, 10, 2) HELD(512, 12, 2) HELD(512, 14, 2) HELD(512, 16, 2) HELD(512, 20, 4)
+  HELD(512, 24, 4) HELD(512, 28, 4) HELD(512, 32, 4)
+#undef HELD
+  return hipErrorInvalidValue;  // (the host splits longer rows)
+}
+
+template <typename X, bool kEntropy>
+hipError_t launch_top_gradient(const TopCall& c) {
+  const Rows& r = c.rows;
+  const int64_t rows = int64_t(r.B) * r.T;
+  const int chunks = (r.V + X::kPer - 1) / X::kPer;
+  auto go = [&](auto kernel, int threads) {
+    const int teams = threads <= kWave ? kTopThreads / threads : 1;
+    const int64_t groups = (rows + teams - 1) / teams;
+    kernel<<<int(groups < kMostGroups ? groups : kMostGroups), threads * teams, 0, c.stream>>>(r, c.top, c.given);
+    return hipGetLastError();
+  };
+  if (chunks <= 32) return go(top_gradient_kernel<X, kEntropy, 8>, 8);
+  if (chunks <= 512) return go(top_gradient_kernel<X, kEntropy, 64>, 64);
+  if (chunks <= 2048) return go(top_gradient_kernel<X, kEntropy, 256>, 256);
+  return go(top_gradient_kernel<X, kEntropy, 512>, 512);
+}
+
+}  // namespace
+
+template <typename X>
+hipError_t top_of(const TopCall& c) {
+  hipError_t e = c.entropy ? launch_top<X, true>(c) : launch_top<X, false>(c);
+  if (e != hipSuccess || c.split.parts == 1) return e;
+  const int64_t rows = int64_t(c.rows.B) * c.rows.T;
+  const int groups = int(rows < kMostGroups ? rows : kMostGroups);
+  if (c.entropy) join_kernel<X, true><<<groups, kTopThreads, 0, c.stream>>>(c.rows, c.out, c.top, c.split);
+  else join_kernel<X, false><<<groups, kTopThreads, 0, c.stream>>>(c.rows, c.out, c.top, c.split);
+  return hipGetLastError();
+}
+template <typename X>
+hipError_t top_gradient_of(const TopCall& c) {
+  return c.entropy ? launch_top_gradient<X, true>(c) : launch_top_gradient<X, false>(c);
+}
+
+}  // namespace loss
+}  // namespace tb

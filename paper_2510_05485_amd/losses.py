@@ -1,12 +1,13 @@
 """Losses over a policy's logits, with their gradients: what a training loop does with its rewards.
 
     lp = token_logprobs(logits, tokens, lengths=lengths)                 # differentiable, float32 [B, T]
+    best = top_logprobs(logits, 20, tokens, lengths=lengths)             # the likeliest beside them: ids, logprobs
     r = policy_loss_grad(logits, tokens, old_lp, advantages, ref_logprobs=ref_lp, kl_coef=0.04,
                          lengths=lengths)                                # value and gradient in one pass
     logits.backward(r.grad)                                              # on into the model
     policy_loss(...).backward()                                          # the same through autograd
 
-`token_logprobs`, `policy_loss`, `preference_loss` and `distillation_loss` return tensors that torch can
+`token_logprobs`, `top_logprobs`, `policy_loss`, `preference_loss` and `distillation_loss` return tensors that torch can
 differentiate in the logits; their backward pass reads the logits a second time.  The functions whose
 names end in `_grad` return the gradient at once.  For the policy loss and the distillation this is
 one pass over the logits: half to two thirds of the traffic of the other way.
@@ -42,11 +43,12 @@ from .binding import TensorBLEUError
 TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 AVERAGES = {"token": 0, "sequence": 1, "sum": 2}
 PAIRS = {"sigmoid": 0, "hinge": 1, "ipo": 2}
-TEACHER_MOST = 1024
+TEACHER_MOST = TOP_MOST = 1024
 
 EXPORTS = [
     "tensorloss_distill", "tensorloss_distill_grad", "tensorloss_policy", "tensorloss_preference",
-    "tensorloss_token_logprobs", "tensorloss_token_logprobs_grad", "tensorloss_workspace_bytes",
+    "tensorloss_token_logprobs", "tensorloss_token_logprobs_grad", "tensorloss_top_logprobs",
+    "tensorloss_top_logprobs_grad", "tensorloss_top_workspace_bytes", "tensorloss_workspace_bytes",
 ]
 
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
@@ -79,6 +81,17 @@ class tb_preference_t(ctypes.Structure):
 class tb_teacher_t(ctypes.Structure):
     _fields_ = [("ids", _vp), ("logits", _vp), ("id_bytes", _i32), ("type", _i32), ("K", _i32),
                 ("average", _i32)]
+
+
+class tb_top_t(ctypes.Structure):
+    _fields_ = [("ids", _vp), ("logprobs", _vp), ("id_bytes", _i32), ("K", _i32)]
+
+
+class TopLogprobs(NamedTuple):
+    ids: torch.Tensor          # [B, T, K] or [N, K]; -1: none
+    logprobs: torch.Tensor     # float32, of the same shape; -inf: none
+    token_logprobs: Optional[torch.Tensor]   # float32, of the tokens' shape
+    entropy: Optional[torch.Tensor]          # float32, one for each position
 
 
 class PolicyLoss(NamedTuple):
@@ -125,6 +138,8 @@ def _library() -> ctypes.CDLL:
         for name, rest in (
                 ("token_logprobs", [_vp] * 5),
                 ("token_logprobs_grad", [_vp, _vp, _vp, _i64, _i64, _vp, p(tb_gradient_t), _vp]),
+                ("top_logprobs", [p(tb_top_t)] + [_vp] * 3 + end),
+                ("top_logprobs_grad", [p(tb_top_t)] + [_vp] * 4 + [p(tb_gradient_t), _vp]),
                 ("policy", [p(tb_policy_t), p(tb_gradient_t)] + [_vp] * 5 + end),
                 ("preference", [p(tb_preference_t), p(tb_gradient_t)] + [_vp] * 5 + end),
                 ("distill", [p(tb_teacher_t), p(tb_gradient_t)] + [_vp] * 4 + end),
@@ -133,6 +148,8 @@ def _library() -> ctypes.CDLL:
             f.restype, f.argtypes = ctypes.c_int, head + rest
         lib.tensorloss_workspace_bytes.restype = ctypes.c_size_t
         lib.tensorloss_workspace_bytes.argtypes = [_i32, _i32]
+        lib.tensorloss_top_workspace_bytes.restype = ctypes.c_size_t
+        lib.tensorloss_top_workspace_bytes.argtypes = [_i32] * 5
         _lib = lib
     return _lib
 
@@ -278,15 +295,15 @@ class _Call:
     def new(self, *shape):
         return torch.empty(*shape, dtype=torch.float32, device=self.device)
 
-    def run(self, entry, *args, workspace=False):
+    def run(self, entry, *args, workspace=None):
         def c(a):
             if isinstance(a, torch.Tensor):
                 return a.data_ptr()
             return ctypes.byref(a) if isinstance(a, ctypes.Structure) else a
         args = [c(a) for a in args]
         with torch.cuda.device(self.device):
-            if workspace:
-                n = workspace_bytes(self.B, self.T)
+            if workspace is not None:
+                n = workspace(self.B, self.T)
                 w = torch.empty(n, dtype=torch.uint8, device=self.device)
                 args += [w.data_ptr(), n]
             args.append(int(torch.cuda.current_stream().cuda_stream))
@@ -360,6 +377,79 @@ def token_logprobs(logits, tokens, *, lengths=None, mask=None, temperature: floa
     return (lp, entropy) if want_entropy else lp
 
 
+# ---- top log-probabilities ----------------------------------------------------------------------
+
+def _top(call, k, tokens, want_entropy, id_dtype, keep_state):
+    if isinstance(k, bool) or not isinstance(k, int) or not 1 <= k <= min(call.V, TOP_MOST):
+        raise TensorBLEUError(f"k must be a number from 1 to {min(call.V, TOP_MOST)} (got {k!r})")
+    if id_dtype not in (torch.int32, torch.int64):
+        raise TensorBLEUError(f"id_dtype must be int32 or int64 (got {id_dtype})")
+    ids = torch.empty(*call.shape, k, dtype=id_dtype, device=call.device)
+    top = tb_top_t()
+    values = call.new(*call.shape, k)
+    top.ids, top.logprobs, top.id_bytes, top.K = ids.data_ptr(), values.data_ptr(), ids.element_size(), k
+    lp = call.new(call.shape) if tokens is not None else None
+    entropy = call.new(call.shape) if want_entropy else None
+    state = call.new(*call.shape, 4) if keep_state else None
+    call.run("tensorloss_top_logprobs", top, lp, entropy, state, call.status,
+             workspace=lambda B, T: int(_library().tensorloss_top_workspace_bytes(B, T, call.V, call.l.type, k)))
+    return ids, values, lp, entropy, state
+
+
+class _TopLogprobs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, k, tokens, lengths, mask, temperature, want_entropy, id_dtype, status):
+        call = _Call(logits, tokens, lengths, mask, temperature, status)
+        ids, values, lp, entropy, state = _top(call, k, tokens, want_entropy, id_dtype, True)
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(logits, tokens, lengths, mask, state, ids)
+        ctx.temperature = temperature
+        ctx.mark_non_differentiable(ids)
+        return ids, values, lp, entropy
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, _, d_top, d_lp, d_entropy):
+        none = (None,) * 8
+        if d_top is None and d_lp is None and d_entropy is None:
+            return (None, *none)
+        logits, tokens, lengths, mask, state, ids = ctx.saved_tensors
+        call = _Call(logits, tokens, lengths, mask, ctx.temperature, None)
+        out, g = call.gradient(None, 1.0)
+        # (hooks on saved tensors give back the same values, in what strides they like)
+        _on(ids, call.device, "ids")
+        ids = ids.contiguous()
+        top = tb_top_t()
+        top.ids, top.id_bytes, top.K = ids.data_ptr(), ids.element_size(), ids.shape[-1]
+        shape = (*call.shape, top.K)
+        as32 = lambda d, name, over: None if d is None else call.values(d.to(torch.float32), name, over)
+        d_top = torch.zeros(shape, dtype=torch.float32, device=call.device) if d_top is None else d_top
+        call.run("tensorloss_top_logprobs_grad", top, call.values(state, "the rows' state", (*call.shape, 4)),
+                 as32(d_top, "d_top", shape), as32(d_lp, "d_lp", call.shape), as32(d_entropy, "d_entropy", call.shape), g)
+        return (out, *none)
+
+
+def top_logprobs(logits, k: int, tokens=None, *, lengths=None, mask=None, temperature: float = 1.0,
+                 want_entropy: bool = False, id_dtype: torch.dtype = torch.int64,
+                 status: Optional[torch.Tensor] = None) -> TopLogprobs:
+    """The k likeliest tokens of every position with their log-probabilities, in descending order, equal
+    ones by their ids; with `tokens` their log-probabilities beside them, and with want_entropy the entropies
+    of the rows.  Log-probabilities and entropies are differentiable in the logits.
+
+    Tokens whose logit is -inf are none of the k: entries that are not there have the id -1 and the
+    log-probability -inf, as at positions that do not count.  distillation_loss takes them so: ids and
+    logprobs (at temperature 1) are a teacher's ids and logits."""
+    found = native().top(logits, k, tokens, lengths, mask, temperature, status, want_entropy,
+                         8 if id_dtype is torch.int64 else 4 if id_dtype is torch.int32 else 0)
+    if found is not None:
+        return TopLogprobs(*found)
+    if _needs_grad(logits):
+        return TopLogprobs(*_TopLogprobs.apply(logits, k, tokens, lengths, mask, temperature, want_entropy, id_dtype,
+                                               status))
+    call = _Call(logits, tokens, lengths, mask, temperature, status)
+    return TopLogprobs(*_top(call, k, tokens, want_entropy, id_dtype, False)[:4])
+
+
 # ---- policy loss --------------------------------------------------------------------------------
 
 def _policy(call, old_logprobs, advantages, ref_logprobs, clip_low, clip_high, kl_coef, entropy_coef,
@@ -381,7 +471,7 @@ def _policy(call, old_logprobs, advantages, ref_logprobs, clip_low, clip_high, k
     terms, lp = call.new(4), call.new(call.shape)
     state, d_lp, d_entropy = (call.new(*call.shape, 4), call.new(call.shape), call.new(call.shape)) \
         if keep else (None,) * 3
-    call.run("tensorloss_policy", p, grad, terms, lp, state, d_lp, d_entropy, call.status, workspace=True)
+    call.run("tensorloss_policy", p, grad, terms, lp, state, d_lp, d_entropy, call.status, workspace=workspace_bytes)
     return terms, lp, state, d_lp, d_entropy if p.entropy_coef != 0 else None
 
 
@@ -459,7 +549,7 @@ def _preference(call, ref_logprobs, beta, kind, label_smoothing, grad, keep):
     terms, lp, margins = call.new(3), call.new(call.B), call.new(call.B // 2)
     state, d_sequence = (call.new(*call.shape, 4), call.new(call.B)) if keep else (None, None)
     call.run("tensorloss_preference", p, grad, terms, lp, margins, state, d_sequence, call.status,
-             workspace=True)
+             workspace=workspace_bytes)
     return terms, lp, margins, state, d_sequence
 
 
@@ -540,7 +630,7 @@ def _teacher(call, teacher_ids, teacher_logits, average):
 def _distill(call, q, grad, keep):
     terms, rows = call.new(1), call.new(call.shape)
     state, d_row = (call.new(*call.shape, 4), call.new(call.shape)) if keep else (None, None)
-    call.run("tensorloss_distill", q, grad, terms, rows, state, d_row, call.status, workspace=True)
+    call.run("tensorloss_distill", q, grad, terms, rows, state, d_row, call.status, workspace=workspace_bytes)
     return terms, rows, state, d_row
 
 
