@@ -34,7 +34,9 @@ struct Order<F32> {
   static __device__ __forceinline__ float value(int t) {
     return __uint_as_float(t < 0 ? 0x80000000u | uint32_t(-t) : uint32_t(t));
   }
+  static constexpr int kMost = 0x7F7FFFFF;  // of the largest value
   static __device__ __forceinline__ int raw(float v) { return __float_as_int(v); }
+  static __device__ __forceinline__ int of(float v) { return int(of_packed(__float_as_uint(v))); }
   template <typename Take>
   static __device__ __forceinline__ void each(u32x4 c, Take take) {
 #pragma unroll
@@ -66,13 +68,14 @@ struct Order16 {
 };
 template <>
 struct Order<BF16> : Order16 {
-  static constexpr int kNone = -0x7F80;
+  static constexpr int kNone = -0x7F80, kMost = 0x7F7F;
   static __device__ __forceinline__ float value(int t) { return Order<F32>::value(t * 65536); }
   static __device__ __forceinline__ int raw(float v) { return __float_as_int(v) >> 16; }
+  static __device__ __forceinline__ int of(float v) { return short(of_packed(uint32_t(raw(v)))); }
 };
 template <>
 struct Order<F16> : Order16 {
-  static constexpr int kNone = -0x7C00;
+  static constexpr int kNone = -0x7C00, kMost = 0x7BFF;
   static __device__ __forceinline__ float value(int t) {
     const uint16_t u = uint16_t(t < 0 ? 0x8000 | -t : t);
     _Float16 h;
@@ -85,6 +88,7 @@ struct Order<F16> : Order16 {
     __builtin_memcpy(&s, &h, 2);
     return s;
   }
+  static __device__ __forceinline__ int of(float v) { return short(of_packed(uint32_t(raw(v)))); }
 };
 // Logits before others have larger keys; no key of a logit is 0.
 __device__ __forceinline__ uint64_t key_of(int t, int at) {
@@ -168,10 +172,6 @@ struct Taken {
       for (int i = 0; i < 4; ++i) c[k][i] = O::of_packed(c[k][i]);
     keep_packed();
   }
-  static __device__ __forceinline__ int order_of_edge(float v) {
-    const uint32_t bits = uint32_t(O::raw(v));
-    return O::kShift ? int(O::of_packed(bits)) : int(short(O::of_packed(bits)));
-  }
   // The largest of the thread's values, in kParts groups.
   static constexpr int kParts = 4;
   __device__ __forceinline__ void largest(int* most, int edge_order) const {
@@ -181,14 +181,18 @@ struct Taken {
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) most[k % kParts] = max(most[k % kParts], O::largest(c[k]));
   }
-  // take(order, place) for each of the thread's values.
+  // take(order, place) for each of the thread's values; a wavefront leaves out chunks without any from `least` on.
+  // (Unpacked anew each time, places too: the compiler would hold all of them.)
   template <typename Take>
-  __device__ __forceinline__ void each(const Row& row, int thread, int edge_order, Take take) const {
+  __device__ __forceinline__ void each(const Row& row, int thread, int edge_order, int least, Take take) {
+    int at = row.at(thread);
+    keep_packed();
+    asm volatile("" : "+v"(at));
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
-      const int at = row.at(thread + k * kThreads);
-      O::each(c[k], [&](int i, int t) { take(t, at + i); });
-      __builtin_amdgcn_sched_barrier(0);
+      if (__any(O::largest(c[k]) >= least)) O::each(c[k], [&](int i, int t) { take(t, at + i); });
+      at += kThreads * X::kPer;
+      asm volatile("" : "+v"(at));
     }
     take(edge_order, edge_at);
   }
@@ -260,49 +264,90 @@ struct TopShared {
   int bounds[2][kWaves], counts[kWaves], counted[2][kWaves];
 };
 
-// How many of the row's values fulfil `holds`, in all threads.
-template <int kThreads, typename H, typename Row, typename Holds>
-__device__ __forceinline__ int row_count(const H& h, const Row& row, int thread, int edge_order, int* counted, Holds holds) {
-  int n = 0;
-  h.each(row, thread, edge_order, [&](int t, int at) { n += holds(t, at); });
-  n = full_wave_sum(n);
-  if constexpr (kThreads > kWave) {
-    if (thread % kWave == 0) counted[thread / kWave] = n;
-    __syncthreads();
-    n = 0;
-    for (int w = 0; w < kThreads / kWave; ++w) n += counted[w];
+// take(order, place) for each of a thread's values of a row, read from memory; some threads may call it less often.
+template <typename X, int kThreads, typename Row, typename Take>
+__device__ __forceinline__ void sweep_orders(const Row& row, int thread, Take take) {
+  using O = Order<X>;
+#pragma unroll 1
+  for (int c = thread; c < row.chunks; c += kThreads) {
+    u32x4 u = row.chunk(c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = O::of_packed(u[i]);
+    const int at = row.at(c);
+    O::each(u, [&](int i, int t) { take(t, at + i); });
   }
-  return n;
+  for (int j = thread; j < row.kEdge; j += kThreads) {
+    const int e = row.edge(j);
+    if (e >= 0) take(O::of(X::load(row.x + e)), e);
+  }
 }
 
-// Where the values that the bound lets through are too many (ties, masks of the lowest value, a few places that have
-// all large values): the K-th value itself and up to which place its equals are taken, by halving.  Slow, and right for
-// every row: about 50 passes over the registers.
-template <int kThreads, typename H, typename Row, typename Shared>
-__device__ __forceinline__ void exact_bound(const H& h, const Row& row, int thread, int edge_order, int K, int V,
-                                            Shared& shared, int* bound, int* before) {
+// Where the values that a bound lets through are too many (ties, masks of the lowest value, a few places that have
+// all large values): the K-th value itself and up to which place its equals are taken, by halving; about 40 sweeps over
+// the row, which comes from the caches.  Then keys of the K, in any order, from own[0] on in the order of wavefronts: how
+//many are there.
+template <typename X, int kThreads, typename Row, typename Shared>
+__device__ __forceinline__ int exact_keys(const Row& row, int thread, int K, int V, int from, Shared& shared, uint64_t* keys) {
+  using O = Order<X>;
+  const int wave = thread / kWave;
   int turn = 0;
   auto count = [&](auto holds) {
-    turn ^= 1;
-    return row_count<kThreads>(h, row, thread, edge_order, shared.counted[turn], holds);
+    int n = 0;
+    sweep_orders<X, kThreads>(row, thread, [&](int t, int at) { n += holds(t, at); });
+    n = full_wave_sum(n);
+    if constexpr (kThreads > kWave) {
+      turn ^= 1;
+      if (thread % kWave == 0) shared.counted[turn][wave] = n;
+      __syncthreads();
+      n = 0;
+      for (int w = 0; w < kThreads / kWave; ++w) n += shared.counted[turn][w];
+    }
+    return n;
   };
   // the largest b that K values reach, above -inf
-  int64_t low = H::O::kNone + 1, high = int64_t(INT32_MAX) + 1;
+  int64_t low = O::kNone + 1, high = int64_t(O::kMost) + 1;
   while (high - low > 1) {
     const int mid = int((low + high) >> 1);
     if (count([mid](int t, int) { return t >= mid; }) >= K) low = mid;
     else high = mid;
   }
   const int b = int(low), above = count([b](int t, int) { return t > b; });
-  // the first place before which there are enough of its equals (b or less: fewer finite values than K)
+  // the first place before which there are enough of its equals (all of them: fewer finite values than K)
   int64_t none = 0, enough = V;
   while (enough - none > 1) {
     const int mid = int((none + enough) >> 1);
     if (count([b, mid](int t, int at) { return t == b && at < mid; }) >= K - above) enough = mid;
     else none = mid;
   }
-  *bound = b;
-  *before = int(enough);
+  const int before = int(enough);
+  auto taken = [b, before](int t, int at) { return t > b || (t == b && at < before); };
+  int mine = 0;
+  sweep_orders<X, kThreads>(row, thread, [&](int t, int at) { mine += taken(t, at); });
+  // each thread's keys behind those of the threads before
+  int slot = mine;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int v = __shfl_up(slot, d);
+    if (thread % kWave >= d) slot += v;
+  }
+  int total = __shfl(slot, kWave - 1);
+  slot -= mine;
+  if constexpr (kThreads > kWave) {
+    turn ^= 1;
+    if (thread % kWave == 0) shared.counted[turn][wave] = total;
+    __syncthreads();
+    total = 0;
+    for (int w = 0; w < kThreads / kWave; ++w) {
+      const int n = shared.counted[turn][w];
+      if (w < wave) slot += n;
+      total += n;
+    }
+  }
+  sweep_orders<X, kThreads>(row, thread, [&](int t, int at) {
+    if (taken(t, at)) keys[slot++] = key_of(t, from + at);
+  });
+  if (thread == 0) keys[total] = 0;  // (read in pairs)
+  return total;
 }
 
 // Joined parts of a row, of weights 2^((x - m) k) (apart), for parts that a kernel after this one joins.
@@ -320,7 +365,7 @@ __device__ __forceinline__ int part_from(int V, int part, int parts) {
 }
 
 // kThreads threads a row, or a part of one: a wavefront of four in a workgroup, or a workgroup.
-// room: candidates that a wavefront may find, K at least, an even number.
+// room: candidates that a wavefront may find, more than K, an even number.
 template <typename X, bool kEntropy, int kThreads, int kChunks, int kStep>
 __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void top_kernel(Rows r, RowOut o, Top q, Split split,
                                                                                       int room) {
@@ -334,9 +379,9 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
   const bool first = thread == 0;
   TopShared<kWaves>& shared = all[team];
   uint64_t* keys = candidates + team * kWaves * room;
-  const int64_t rows = int64_t(r.B) * r.T, units = rows * split.parts;
+  const int64_t rows = int64_t(r.B) * r.T;
   const float k = r.inv_temp * kLog2e;
-  for (int64_t unit = int64_t(blockIdx.x) * kTeams + team; unit < units; unit += int64_t(gridDim.x) * kTeams) {
+  auto take_unit = [&](int64_t unit) {
     const int64_t which = split.parts == 1 ? unit : unit / split.parts;
     const int part = int(unit - which * split.parts);
     const int64_t at = kAlone && split.parts == 1 ? row_of_group(which, rows) : which;
@@ -348,7 +393,7 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
         if (first) leave_nothing(o, at);
         put_none(q, at, 0, -INFINITY, thread, kThreads);
       }
-      continue;
+      return;
     }
     const int from = part_from(r.V, part, split.parts), V = part_from(r.V, part + 1, split.parts) - from;
     const typename H::Row row(row_of<X>(r, b, t) + from, V);
@@ -359,7 +404,6 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
     const float x = token < 0 ? __uint_as_float(kNan) : X::load(row_of<X>(r, b, t) + token);
     // Raw bits as signed integers are in the values' order from 0 on, with all others below: they do as long as
     // the bound is above 0.
-    bool raw = true;
     int most[H::kParts], edge_order = O::raw(h.edge);
     h.largest(most, edge_order);
     const int need = (q.K + kWaves - 1) / kWaves;
@@ -374,20 +418,9 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
       s = block_stats<kEntropy, kWaves>(shared.parts, k);
       for (int w = 0; w < kWaves; ++w) bound = min(bound, shared.bounds[0][w]);
     }
-    const bool extreme = !fine(s, k);
-    if (extreme) {
-      meet<kThreads>();
-      s = row_stats<X, kEntropy, kThreads>(row, k, thread, shared.parts);
-    }
-    const Found f = {s.m, s.s, s.t, extreme};
-    const bool none = f.s != f.s || (split.parts == 1 && lost(f));
-    auto to_order = [&] {
-      h.to_order();
-      edge_order = H::order_of_edge(h.edge);
-      raw = false;
-    };
     if (bound < 1) {
-      to_order();
+      h.to_order();
+      edge_order = O::of(h.edge);
       h.largest(most, edge_order);
       bound = wave_bound<X>(most, need);
       if constexpr (kAlone) {
@@ -397,44 +430,44 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
       }
       bound = max(bound, O::kNone + 1);
     }
-    // The values from the bound on (its equals up to a place), as keys in LDS, a part for each wavefront.
-    int before = INT32_MAX, found = 0, total = 0;
+    // The values from the bound on, as keys in LDS, a part for each wavefront.
+    int found = 0;
     uint64_t* own = keys + wave * room;
-    for (int attempt = 0; !none; ++attempt) {
-      found = 0;
-      auto take = [&](int t, int place) {
-        const bool is = t > bound || (t == bound && place < before);
-        const uint64_t mask = __ballot(is);
-        if (mask == 0) return;
-        const int slot = found + __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
-        if (is && slot < room) own[slot] = key_of(t, from + place);
-        found += __popcll(mask);
-      };
-#pragma unroll
-      for (int j = 0; j < kChunks; ++j) {
-        if (!__any(O::largest(h.c[j]) >= bound)) continue;
-        const int place = row.at(thread + j * kThreads);
-        O::each(h.c[j], [&](int i, int t) { take(t, place + i); });
+    h.each(row, thread, edge_order, bound, [&](int t, int place) {
+      const uint64_t mask = __ballot(t >= bound);
+      if (mask == 0) return;
+      const int slot = found + __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
+      if (t >= bound && slot < room) own[slot] = key_of(t, from + place);
+      found += __popcll(mask);
+    });
+    if (lane == 0) {
+      if (found < room) own[found] = 0;  // (keys are read in pairs)
+      if (kAlone) shared.counts[wave] = found;
+    }
+    meet<kThreads>();
+    int total = found;
+    bool much = found > room;
+    if constexpr (kAlone) {
+      total = 0;
+      for (int w = 0; w < kWaves; ++w) {
+        const int n = shared.counts[w];
+        total += n;
+        much = much || n > room;
       }
-      take(edge_order, h.edge_at);
-      if (lane == 0) {
-        if (found < room) own[found] = 0;  // (keys are read in pairs)
-        if (kAlone) shared.counts[wave] = found;
-      }
+    }
+    const bool extreme = !fine(s, k);
+    if (extreme) {
       meet<kThreads>();
-      total = found;
-      bool much = found > room;
-      if constexpr (kAlone) {
-        total = 0;
-        for (int w = 0; w < kWaves; ++w) {
-          const int n = shared.counts[w];
-          total += n;
-          much = much || n > room;
-        }
-      }
-      if (!much || attempt > 0) break;
-      if (raw) to_order();
-      exact_bound<kThreads>(h, row, thread, edge_order, q.K, V, shared, &bound, &before);
+      s = row_stats<X, kEntropy, kThreads>(row, k, thread, shared.parts);
+    }
+    const Found f = {s.m, s.s, s.t, extreme};
+    const bool none = f.s != f.s || (split.parts == 1 && lost(f));
+    if (none) total = found = 0;
+    else if (much) {
+      meet<kThreads>();
+      total = exact_keys<X, kThreads>(row, thread, q.K, V, from, shared, keys);  // (in the first wavefronts' parts)
+      found = kAlone ? max(min(total - wave * room, room), 0) : total;
+      if (kAlone && lane == 0) shared.counts[wave] = found;
       meet<kThreads>();
     }
     // Each one's place is the number of larger keys.
@@ -466,7 +499,15 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
       put_none(q, at, min(total, q.K), none ? __uint_as_float(kNan) : -INFINITY, thread, kThreads);
       if (first) put_values<kEntropy>(r, o, f, x, k, log_s, at);
     }
-    meet<kThreads>();  // (before the next row takes the shared memory)
+  };
+  // (a workgroup takes one row: what lives from row to row would cost it registers)
+  if constexpr (kAlone) {
+    take_unit(split.first + blockIdx.x);
+  } else {
+    for (int64_t unit = int64_t(blockIdx.x) * kTeams + team; unit < rows; unit += int64_t(gridDim.x) * kTeams) {
+      take_unit(unit);
+      meet<kThreads>();  // (before the next row takes the shared memory)
+    }
   }
 }
 
@@ -677,7 +718,7 @@ __global__ __launch_bounds__(kTopThreads) void short_kernel(Rows r, RowOut o, To
       const int place = Part<X, kLanes, 1>::at(V, lane, 0);
 #pragma unroll
       for (int i = 0; i < X::kPer; ++i) {
-        const int order = Taken<X, kWave, 1, 1>::order_of_edge(v[i]);
+        const int order = O::of(v[i]);
         keys[i] = order > O::kNone && live && !none ? Key::of(order, place + i) : 0;
       }
     }
@@ -785,7 +826,7 @@ hipError_t launch_top(const TopCall& c) {
   // the longest part
   const int64_t most = r.V / c.split.parts + (c.split.parts > 1 ? 64 : 0);
   const int whole = int(most / X::kPer);
-  const int room = c.top.K <= 256 ? 256 : 1024;
+  const int room = c.top.K < 256 ? 256 : c.top.K < 512 ? 512 : 1088;
   auto go = [&](auto kernel, int threads) {
     const int teams = threads <= kWave ? kTopThreads / threads : 1, waves = std::max(threads, kTopThreads * (teams > 1)) / kWave;
     const size_t bytes = size_t(waves) * room * sizeof(uint64_t);
@@ -793,7 +834,11 @@ hipError_t launch_top(const TopCall& c) {
       const hipError_t e = grant_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes);
       if (e != hipSuccess) return e;
     }
-    kernel<<<groups_of(rows * c.split.parts, teams), waves * kWave, bytes, c.stream>>>(r, c.out, c.top, c.split, room);
+    Split split = c.split;
+    const int64_t units = teams > 1 ? 1 : rows * split.parts;
+    for (split.first = 0; split.first < units; split.first += kMostGroups)  // (a workgroup for each)
+      kernel<<<groups_of(teams > 1 ? rows : units - split.first, teams), waves * kWave, bytes, c.stream>>>(r, c.out, c.top, split,
+                                                                                                         room);
     return hipGetLastError();
   };
   auto need = [&](int threads) { return (whole + threads - 1) / threads; };
