@@ -2,7 +2,8 @@
 
 The computation lives in `libtensorbleu.so` (hand-written HIP for gfx950, built from `csrc/` by
 `python -m paper_2510_05485_amd.build`); `binding` marshals PyTorch device tensors into it.
-`losses` holds what a training loop does with such rewards: losses over a policy's logits.
+`losses` holds what a training loop does with such rewards: losses over a policy's logits.  `embeddings`
+is where a policy over token ids begins: rows of a table by ids, and their gradient.
 """
 from .binding import (  # noqa: F401
     LIB_PATH, TB_DEV_LENGTH_RANGE, TB_DEV_TABLE_OVERFLOW, TB_DEV_TOKEN_RANGE, Stats, TensorBLEUError, allocate_workspace, load_library, make_config,
@@ -19,3 +20,4 @@ from .losses import (  # noqa: F401
     DistillationLoss, PolicyLoss, PreferenceLoss, TopLogprobs, distillation_loss, distillation_loss_grad,
     policy_loss, policy_loss_grad, preference_loss, preference_loss_grad, token_logprobs, top_logprobs,
 )
+from .embeddings import embedding, embedding_grad  # noqa: F401

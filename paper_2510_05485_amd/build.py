@@ -1,8 +1,9 @@
 """Build the gfx950 shared library (libtensorbleu.so) and the Python module that calls it in-tree.
 
 `python -m paper_2510_05485_amd.build` compiles every HIP translation unit under csrc/ for
-gfx950 and links them into one C-ABI library next to this file, and csrc/tb_host.cpp and
-csrc/loss/tb_loss_py.cpp (host code, against PyTorch's headers) into the modules _host and _loss_host.
+gfx950 and links them into one C-ABI library next to this file, and csrc/tb_host.cpp,
+csrc/loss/tb_loss_py.cpp and csrc/embed/tb_embed_py.cpp (host code, against PyTorch's headers) into the modules
+_host, _loss_host and _embed_host.
 hipcc cross-compiles without a GPU, so this runs anywhere the ROCm toolchain is installed.
 """
 from __future__ import annotations
@@ -22,7 +23,9 @@ LIB = os.path.join(PKG, "libtensorbleu.so")
 HOST_SRC = os.path.join(CSRC, "tb_host.cpp")
 HOST_LIB = os.path.join(PKG, "_host.so")
 HOST_MODULES = [(HOST_SRC, HOST_LIB),
-                (os.path.join(CSRC, "loss", "tb_loss_py.cpp"), os.path.join(PKG, "_loss_host.so"))]
+                (os.path.join(CSRC, "loss", "tb_loss_py.cpp"), os.path.join(PKG, "_loss_host.so")),
+                (os.path.join(CSRC, "embed", "tb_embed_py.cpp"), os.path.join(PKG, "_embed_host.so"))]
+FOLDERS = [CSRC, os.path.join(CSRC, "loss"), os.path.join(CSRC, "embed")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 PRELOADED_WORDS = 14  # of a kernel's plain arguments
@@ -36,7 +39,7 @@ FLAGS = [
 
 
 def sources():
-    return sorted(glob.glob(os.path.join(CSRC, "*.hip")) + glob.glob(os.path.join(CSRC, "loss", "*.hip")))
+    return sorted(f for folder in FOLDERS for f in glob.glob(os.path.join(folder, "*.hip")))
 
 
 def needs_build() -> bool:
@@ -44,8 +47,8 @@ def needs_build() -> bool:
     if not all(os.path.exists(f) for f in built):
         return True
     t = min(os.path.getmtime(f) for f in built)
-    deps = sources() + [src for src, _ in HOST_MODULES] + glob.glob(os.path.join(CSRC, "*.h")) + \
-        glob.glob(os.path.join(CSRC, "loss", "*.h")) + glob.glob(os.path.join(INCLUDE, "*.h"))
+    deps = sources() + [src for src, _ in HOST_MODULES] + \
+        [f for folder in (*FOLDERS, INCLUDE) for f in glob.glob(os.path.join(folder, "*.h"))]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
@@ -71,7 +74,7 @@ def build(verbose: bool = True) -> str:
 
 
 def build_host(verbose: bool = True, src: str = HOST_SRC, lib: str = HOST_LIB) -> str:
-    """A module that marshals calls (_host, _loss_host): links against the library and PyTorch."""
+    """A module that marshals calls (_host, _loss_host, _embed_host): links against the library and PyTorch."""
     import sysconfig
 
     import torch

@@ -1,0 +1,76 @@
+// Rows of a table by token ids, scaled.
+#include "tb_embed.h"
+
+namespace tb {
+namespace embed {
+namespace {
+
+constexpr int kThreads = 256, kMostGroups = 1 << 22;
+constexpr uint32_t kNan = 0x7FC00000u;
+
+// kLanes lanes a position, chunks of 16 bytes; the last chunk of a row ends with it (values that two chunks hold
+// are written twice alike).  kWide: rows of a chunk at least.  Bound by HBM: a row is read and written once.
+template <typename X, int kLanes, bool kWide>
+__global__ __launch_bounds__(kThreads) void lookup_kernel(Rows r, int D, float scale) {
+  using T = typename X::type;
+  constexpr int kTeams = kThreads / kLanes;
+  const int lane = threadIdx.x % kLanes;
+  const int64_t rows = int64_t(r.B) * r.T;
+  for (int64_t at = int64_t(blockIdx.x) * kTeams + threadIdx.x / kLanes; at < rows; at += int64_t(gridDim.x) * kTeams) {
+    const At pos = loss::position(r, at);
+    if (lane == 0 && pos.t == 0 && r.lengths) loss::held_length(r.lengths[pos.b], r.T, r.status);
+    T* out = static_cast<T*>(r.g) + at * D;
+    const bool live = loss::counts(r, pos.b, pos.t);
+    const int64_t id = live ? loss::load_id(r.tokens, r.long_tokens, pos.b * r.token_seq + pos.t) : 0;
+    const bool fits = id >= 0 && id < r.V;
+    if (live && !fits && lane == 0 && r.status) atomicOr(r.status, TB_DEV_TOKEN_RANGE);
+    const T* row = static_cast<const T*>(r.x) + (live && fits ? id : 0) * r.x_pos;
+    const float by = live && fits ? scale : 0.f, none = live && !fits ? __uint_as_float(kNan) : 0.f;
+    const bool read = live && fits;
+    if constexpr (kWide) {
+      const int chunks = (D + X::kPer - 1) / X::kPer;
+      for (int c = lane; c < chunks; c += kLanes) {
+        const int i = min(c * X::kPer, D - X::kPer);
+        float v[X::kPer];
+        if (read) {
+          X::unpack(*reinterpret_cast<const u32x4_any*>(row + i), v);
+#pragma unroll
+          for (int j = 0; j < X::kPer; ++j) v[j] *= by;
+        } else {
+#pragma unroll
+          for (int j = 0; j < X::kPer; ++j) v[j] = none;
+        }
+        *reinterpret_cast<u32x4_any*>(out + i) = X::pack(v);
+      }
+    } else {
+      if (lane < D) X::store(out + lane, read ? X::load(row + lane) * by : none);
+    }
+  }
+}
+
+template <typename X>
+hipError_t launch(const Lookup& c) {
+  const int64_t rows = int64_t(c.r.B) * c.r.T;
+  const int chunks = (c.D + X::kPer - 1) / X::kPer;
+  auto go = [&](auto kernel, int lanes) {
+    const int64_t teams = kThreads / lanes, groups = (rows + teams - 1) / teams;
+    kernel<<<int(groups < kMostGroups ? groups : kMostGroups), kThreads, 0, c.stream>>>(c.r, c.D, c.scale);
+    return hipGetLastError();
+  };
+  if (c.D < X::kPer) return go(lookup_kernel<X, 8, false>, 8);
+  if (chunks <= 2) return go(lookup_kernel<X, 2, true>, 2);
+  if (chunks <= 8) return go(lookup_kernel<X, 8, true>, 8);
+  if (chunks <= 16) return go(lookup_kernel<X, 16, true>, 16);
+  if (chunks <= 32) return go(lookup_kernel<X, 32, true>, 32);
+  if (chunks <= 512) return go(lookup_kernel<X, 64, true>, 64);
+  return go(lookup_kernel<X, 256, true>, 256);
+}
+
+}  // namespace
+
+hipError_t run_lookup(const Lookup& c) {
+  return c.type == TB_FLOAT32 ? launch<F32>(c) : c.type == TB_BFLOAT16 ? launch<BF16>(c) : launch<F16>(c);
+}
+
+}  // namespace embed
+}  // namespace tb

@@ -42,6 +42,11 @@ struct Rows {
 struct At {
   int b, t;
 };
+inline void set_division(Rows& r) {  // (T > 0)
+  r.t_shift = 0;
+  while ((uint64_t(1) << r.t_shift) < uint32_t(r.T)) ++r.t_shift;
+  r.t_magic = uint32_t((((uint64_t(1) << r.t_shift) - uint32_t(r.T)) << 32) / uint32_t(r.T) + 1);
+}
 
 struct RowOut {  // per position, any may be null
   float *logprobs, *entropy;

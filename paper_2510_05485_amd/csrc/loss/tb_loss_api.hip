@@ -80,8 +80,7 @@ int check(const tb_logits_t* l, const tb_positions_t* at, bool tokens, const tb_
   r.long_tokens = at->token_bytes == 8;
   r.lengths = at->lengths;
   r.mask = at->mask;
-  while ((uint64_t(1) << r.t_shift) < uint32_t(r.T)) ++r.t_shift;
-  r.t_magic = uint32_t((((uint64_t(1) << r.t_shift) - uint32_t(r.T)) << 32) / uint32_t(r.T) + 1);
+  set_division(r);
   r.inv_temp = 1.f / l->temperature;
   r.g_scale = 1.f;
   if (!(r.inv_temp * kLog2e < INFINITY) || r.inv_temp == 0.f) return TB_ERR_INVALID_ARG;

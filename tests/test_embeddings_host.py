@@ -1,0 +1,109 @@
+"""Host side of the embeddings' C ABI: symbols, struct layouts, argument checks before any launch, workspace sizes."""
+import ctypes
+import os
+import re
+import subprocess
+
+import pytest
+import torch
+
+import paper_2510_05485_amd as tb
+from paper_2510_05485_amd import embeddings
+from test_losses_host import HERE, ROOT, positions
+
+HEADER = os.path.join(ROOT, "include", "tensorembed.h")
+ref = ctypes.byref
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(tb.LIB_PATH):
+        from paper_2510_05485_amd import build
+        build.build(verbose=False)
+    return embeddings._library()
+
+
+def test_every_declared_symbol_is_exported(lib):
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    assert sorted(set(re.findall(r"\b(tensorembed_\w+)\s*\(", text))) == sorted(embeddings.EXPORTS)
+    for name in embeddings.EXPORTS:
+        assert hasattr(lib, name)
+
+
+def test_struct_sizes_match_the_header(tmp_path):
+    names = ["tb_table_t", "tb_embedding_rows_t", "tb_table_gradient_t"]
+    lines = []
+    for n in names:
+        lines.append(f'printf("%zu", sizeof({n}));')
+        lines += [f'printf(" %zu", offsetof({n}, {field}));' for field, _ in getattr(embeddings, n)._fields_]
+        lines.append('printf("\\n");')
+    src = tmp_path / "sizes.c"
+    src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "tensorembed.h"\nint main(void) {' + "".join(lines) +
+                   'printf("%d", TB_WIDTH_MOST); return 0;}\n')
+    exe = tmp_path / "sizes"
+    subprocess.check_call(["gcc", "-std=c99", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)])
+    *found, most = subprocess.check_output([str(exe)], text=True).splitlines()
+    for n, line in zip(names, found):
+        s = getattr(embeddings, n)
+        assert [int(v) for v in line.split()] == [ctypes.sizeof(s)] + [getattr(s, f).offset for f, _ in s._fields_], n
+    assert int(most) == embeddings.WIDTH_MOST
+
+
+def test_workspace(lib):
+    n = embeddings.workspace_bytes
+    for bad in ((-1, 1, 5, 5), (1, -1, 5, 5), (1 << 16, 1 << 15, 5, 5), (1, 1, 0, 5), (1, 1, 5, 0), (1, 1, 5, (1 << 20) + 1)):
+        assert n(*bad) == 0, bad
+    for V in (1, 64, 50257, 262144, 5_000_000, 2 ** 31 - 1):
+        for D in (1, 64, 4096, 1 << 20):
+            for rows in (0, 1, 16, 17, 4096, 65536, 65537, 1 << 21):
+                b = n(rows, 1, V, D)
+                assert b == n(1, rows, V, D)
+                slices = rows / 256
+                assert b >= 8 * rows + (8 * slices * D if rows > 256 else 0)
+                assert b <= (1 << 20) + 16 * rows + 8 * D * (rows / 16 + 1) + (4 << 11) * (rows / 4096 + 2)
+
+
+def test_lookup_arguments(lib):
+    def rc(p=None, B=2, T=3, out=HERE << 24, **kw):
+        t = embeddings.tb_table_t(data=HERE << 20, row_stride=8, V=10, D=8, type=0)
+        for k, v in kw.items():
+            setattr(t, k, v)
+        return lib.tensorembed_lookup(ref(t), ref(p or positions()), B, T, 1.0, out, None, None)
+    assert lib.tensorembed_lookup(None, ref(positions()), 1, 1, 1.0, HERE, None, None) == 1
+    for kw in (dict(V=0), dict(D=0), dict(D=(1 << 20) + 1), dict(type=3), dict(type=-1), dict(data=None), dict(data=HERE + 2),
+               dict(row_stride=-1), dict(row_stride=1 << 62), dict(B=-1), dict(T=-1), dict(B=1 << 16, T=1 << 16), dict(out=None),
+               dict(out=HERE + 1), dict(out=HERE << 20), dict(out=(HERE << 20) + 316), dict(out=(HERE << 20) - 188),
+               dict(p=positions(tokens=None)), dict(p=positions(tokens=HERE + 4)), dict(p=positions(token_bytes=2)),
+               dict(p=positions(token_stride=-1))):
+        assert rc(**kw) == 1, kw
+    assert rc(B=0, out=None) == rc(T=0, out=None) == 0
+
+
+def test_gradient_arguments(lib):
+    n = embeddings.workspace_bytes(2, 3, 10, 8)
+
+    def rc(p=None, workspace=HERE, bytes_=n, rows=None, **kw):
+        r = embeddings.tb_embedding_rows_t(data=HERE << 20, seq_stride=24, pos_stride=8, B=2, T=3, D=8, type=1)
+        for k, v in (rows or {}).items():
+            setattr(r, k, v)
+        g = embeddings.tb_table_gradient_t(data=HERE << 24, row_stride=8, V=10, type=1, scale=1.0, accumulate=1)
+        for k, v in kw.items():
+            setattr(g, k, v)
+        return lib.tensorembed_gradient(ref(r), ref(p or positions()), ref(g), None, workspace, bytes_, None)
+    for rows in (dict(B=-1), dict(B=1 << 16, T=1 << 16), dict(D=0), dict(D=(1 << 20) + 1), dict(type=3), dict(type=2), dict(data=None),
+                 dict(data=HERE + 1), dict(seq_stride=-1), dict(pos_stride=-1), dict(seq_stride=1 << 62),
+                 dict(data=HERE << 24), dict(data=(HERE << 24) + 158), dict(data=(HERE << 24) - 94)):
+        assert rc(rows=rows) == 1, rows
+    for kw in (dict(V=0), dict(type=2), dict(type=3), dict(data=None), dict(data=HERE + 1), dict(row_stride=7), dict(row_stride=-1),
+               dict(row_stride=1 << 62), dict(p=positions(tokens=None)), dict(p=positions(token_bytes=3))):
+        assert rc(**kw) == 1, kw
+    assert rc(workspace=None) == rc(workspace=HERE + 16) == rc(bytes_=n - 512) == 2
+    assert rc(rows=dict(B=0, data=None), p=positions(tokens=None)) == 0        # nothing to add
+
+
+def test_python_refuses_what_is_not_on_a_gpu():
+    table, tokens = torch.zeros(5, 4), torch.zeros(2, 3, dtype=torch.int64)
+    for f in (lambda: tb.embedding(table, tokens), lambda: tb.embedding(table.requires_grad_(), tokens),
+              lambda: tb.embedding_grad(torch.zeros(2, 3, 4), tokens, 5)):
+        with pytest.raises(tb.TensorBLEUError, match="GPU"):
+            f()
