@@ -11,6 +11,7 @@
 //   join_kernel   joins the parts of long rows
 #pragma once
 
+#include <cstdlib>
 #include "tb_loss_rows.h"
 #include "tb_loss_top_host.h"
 
@@ -19,6 +20,9 @@ namespace loss {
 namespace {
 
 // ---- the order of logits as one of whole numbers ----------------------------------------------
+
+typedef int int_alias __attribute__((may_alias));  // (values inside chunks)
+typedef short short_alias __attribute__((may_alias));
 
 // Order: value x -> int32 that grows with x, -0 and 0 alike: sign and magnitude as two's complement.
 template <typename X>
@@ -42,6 +46,7 @@ struct Order<F32> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) take(i, int(c[i]));
   }
+  static __device__ __forceinline__ int in_chunk(const u32x4* c, int i) { return reinterpret_cast<const int_alias*>(c)[i]; }
   static __device__ __forceinline__ int largest(u32x4 c) { return max(max(int(c[0]), int(c[1])), max(int(c[2]), int(c[3]))); }
 };
 struct Order16 {
@@ -61,6 +66,7 @@ struct Order16 {
       take(2 * i + 1, int(c[i]) >> 16);
     }
   }
+  static __device__ __forceinline__ int in_chunk(const u32x4* c, int i) { return reinterpret_cast<const short_alias*>(c)[i]; }
   static __device__ __forceinline__ int largest(u32x4 c) {
     const i16x2 top = upper_pair<1>(&c);
     return max(int(top[0]), int(top[1]));
@@ -136,6 +142,10 @@ __device__ __forceinline__ void put_values(const Rows& r, const RowOut& o, const
 
 // ---- rows in registers ------------------------------------------------------------------------
 
+__device__ __forceinline__ int lanes_before(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
+}
+
 // Chunks k kThreads + thread of a row, k < kChunks, of which all but the last kStep + 2 are there in every thread
 // (kStep: how many lengths one kernel serves; one for the row's head, one for parts that differ in length).
 template <typename X, int kThreads, int kChunks, int kStep>
@@ -181,20 +191,27 @@ struct Taken {
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) most[k % kParts] = max(most[k % kParts], O::largest(c[k]));
   }
-  // take(order, place) for each of the thread's values; a wavefront leaves out chunks without any from `least` on.
-  // (Unpacked anew each time, places too: the compiler would hold all of them.)
-  template <typename Take>
-  __device__ __forceinline__ void each(const Row& row, int thread, int edge_order, int least, Take take) {
-    int at = row.at(thread);
+  // Chunks with a value from `least` on, with the places of their first values, into a list of the wavefront: how many
+  // there are (of which `room` are kept).
+  __device__ __forceinline__ int hits(const Row& row, int thread, int least, u32x4* chunks, int* places, int room) {
+    int n = 0, at = row.at(thread);
     keep_packed();
-    asm volatile("" : "+v"(at));
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
-      if (__any(O::largest(c[k]) >= least)) O::each(c[k], [&](int i, int t) { take(t, at + i); });
+      const bool is = O::largest(c[k]) >= least;
+      const uint64_t mask = __ballot(is);
+      if (mask) {
+        const int slot = n + lanes_before(mask);
+        if (is && slot < room) {
+          chunks[slot] = c[k];
+          places[slot] = at;
+        }
+        n += __popcll(mask);
+      }
       at += kThreads * X::kPer;
-      asm volatile("" : "+v"(at));
+      asm volatile("" : "+v"(at));  // (the compiler would hold all places)
     }
-    take(edge_order, edge_at);
+    return n;
   }
 };
 
@@ -255,6 +272,13 @@ __device__ __forceinline__ int wave_bound(const int* most, int need) {
     }
   }
   return (b - kBias) * (1 << Order<X>::kShift);
+}
+
+// Sum over groups of kLanes neighbouring lanes, in all of them.
+template <int kLanes, int kStep = 1>
+__device__ __forceinline__ int lanes_total(int v) {
+  if constexpr (kStep == kLanes) return v;
+  else return lanes_total<kLanes, kStep * 2>(v + __float_as_int(neighbour<kStep>(__int_as_float(v))));
 }
 
 // What the threads that share a row leave for one another; counted: two, taken in turn.
@@ -357,6 +381,7 @@ __device__ __forceinline__ Found moved_apart(const Found& f, float k) {
   return {f.m, e * f.s, e * (f.t + d * f.s), true};
 }
 
+constexpr int kHits = 192, kHitBytes = sizeof(u32x4) + sizeof(int);  // chunks with candidates that a wavefront may find
 constexpr int kTopThreads = 256;  // of a workgroup whose wavefronts have rows of their own
 
 // The first value of a part of a long row: multiples of 64, so that parts are alike in length up to 64 values.
@@ -365,7 +390,7 @@ __device__ __forceinline__ int part_from(int V, int part, int parts) {
 }
 
 // kThreads threads a row, or a part of one: a wavefront of four in a workgroup, or a workgroup.
-// room: candidates that a wavefront may find, more than K, an even number.
+// room: candidates that a wavefront may find, an even number, more than K by all that share a row.
 template <typename X, bool kEntropy, int kThreads, int kChunks, int kStep>
 __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void top_kernel(Rows r, RowOut o, Top q, Split split,
                                                                                       int room) {
@@ -373,12 +398,16 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
   constexpr int kTeams = kAlone ? 1 : kTopThreads / kThreads, kWaves = kAlone ? kThreads / kWave : 1;
   using H = Taken<X, kThreads, kChunks, kStep>;
   using O = Order<X>;
-  extern __shared__ __attribute__((aligned(16))) uint64_t candidates[];  // [team][wave][room]
+  // of each wavefront: chunks with candidates, their places, the candidates' keys [room]
+  extern __shared__ __attribute__((aligned(16))) uint64_t candidates[];
   __shared__ TopShared<kWaves> all[kTeams];
   const int team = threadIdx.x / kThreads, thread = threadIdx.x % kThreads, wave = thread / kWave, lane = threadIdx.x % kWave;
   const bool first = thread == 0;
   TopShared<kWaves>& shared = all[team];
-  uint64_t* keys = candidates + team * kWaves * room;
+  constexpr int kAllWaves = kTeams * kWaves;
+  u32x4* chunks = reinterpret_cast<u32x4*>(candidates) + threadIdx.x / kWave * kHits;
+  int* places = reinterpret_cast<int*>(reinterpret_cast<u32x4*>(candidates) + kAllWaves * kHits) + threadIdx.x / kWave * kHits;
+  uint64_t* keys = candidates + kAllWaves * (kHits * kHitBytes / 8) + team * kWaves * room;
   const int64_t rows = int64_t(r.B) * r.T;
   const float k = r.inv_temp * kLog2e;
   auto take_unit = [&](int64_t unit) {
@@ -430,23 +459,32 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
       }
       bound = max(bound, O::kNone + 1);
     }
-    // The values from the bound on, as keys in LDS, a part for each wavefront.
+    // The values from the bound on, as keys in LDS, a part for each wavefront: first the chunks that have some, with
+    // one lane storing all of its chunk, then each value of these.
     int found = 0;
     uint64_t* own = keys + wave * room;
-    h.each(row, thread, edge_order, bound, [&](int t, int place) {
-      const uint64_t mask = __ballot(t >= bound);
-      if (mask == 0) return;
-      const int slot = found + __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
-      if (t >= bound && slot < room) own[slot] = key_of(t, from + place);
+    const int hits = h.hits(row, thread, bound, chunks, places, kHits);
+    meet<kWave>();
+    auto take = [&](bool is, int t, int place) {
+      const uint64_t mask = __ballot(is);
+      const int slot = found + lanes_before(mask);
+      if (is && slot < room) own[slot] = key_of(t, from + place);
       found += __popcll(mask);
-    });
+    };
+    for (int e = 0; e < min(hits, kHits); e += kWave / X::kPer) {
+      const int hit = e + lane / X::kPer, i = lane % X::kPer;
+      const bool there = hit < min(hits, kHits);
+      const int t = there ? O::in_chunk(chunks + hit, i) : O::kNone, place = there ? places[hit] + i : 0;
+      take(there && t >= bound, t, place);
+    }
+    if (__any(edge_order >= bound)) take(edge_order >= bound, edge_order, h.edge_at);
     if (lane == 0) {
       if (found < room) own[found] = 0;  // (keys are read in pairs)
-      if (kAlone) shared.counts[wave] = found;
+      if (kAlone) shared.counts[wave] = hits > kHits ? room + 1 : found;
     }
     meet<kThreads>();
     int total = found;
-    bool much = found > room;
+    bool much = hits > kHits || found > room;
     if constexpr (kAlone) {
       total = 0;
       for (int w = 0; w < kWaves; ++w) {
@@ -470,20 +508,24 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
       if (kAlone && lane == 0) shared.counts[wave] = found;
       meet<kThreads>();
     }
-    // Each one's place is the number of larger keys.
+    // Each one's place is the number of larger keys: kWaves lanes count those of a wavefront's part each.
     const float log_s = logf(f.s);
-    for (int i = lane; i < found; i += kWave) {
+    const int share = lane % kWaves;
+    const uint64_t* others = keys + share * room;
+    const int theirs = kAlone ? shared.counts[share] : found;
+    for (int i = lane / kWaves; i < found; i += kWave / kWaves) {
       const uint64_t key = own[i];
-      int rank = 0;
-      for (int w = 0; w < kWaves; ++w) {
-        const uint64_t* others = keys + w * room;
-        const int n = kAlone ? shared.counts[w] : found;
-        for (int j = 0; j < n; j += 2) {
-          const ulonglong2 two = *reinterpret_cast<const ulonglong2*>(others + j);
-          rank += (two.x > key) + (two.y > key);
-        }
+      int rank = 0, j = 0;
+      for (; j + 4 < theirs; j += 4) {
+        const ulonglong2 one = *reinterpret_cast<const ulonglong2*>(others + j), two = *reinterpret_cast<const ulonglong2*>(others + j + 2);
+        rank += (one.x > key) + (one.y > key) + (two.x > key) + (two.y > key);
       }
-      if (rank >= q.K) continue;
+      for (; j < theirs; j += 2) {
+        const ulonglong2 one = *reinterpret_cast<const ulonglong2*>(others + j);
+        rank += (one.x > key) + (one.y > key);
+      }
+      rank = lanes_total<kWaves>(rank);
+      if (rank >= q.K || share) continue;
       if (split.parts > 1) {
         split.keys[unit * q.K + rank] = key;
       } else {
@@ -826,10 +868,12 @@ hipError_t launch_top(const TopCall& c) {
   // the longest part
   const int64_t most = r.V / c.split.parts + (c.split.parts > 1 ? 64 : 0);
   const int whole = int(most / X::kPer);
-  const int room = c.top.K < 256 ? 256 : c.top.K < 512 ? 512 : 1088;
   auto go = [&](auto kernel, int threads) {
     const int teams = threads <= kWave ? kTopThreads / threads : 1, waves = std::max(threads, kTopThreads * (teams > 1)) / kWave;
-    const size_t bytes = size_t(waves) * room * sizeof(uint64_t);
+    // (not a multiple of 32 keys: the parts begin at other banks)
+    constexpr int room = 258;
+    static_assert(4 * room > TB_TOP_MOST);
+    const size_t bytes = size_t(waves) * (room * sizeof(uint64_t) + kHits * kHitBytes);
     if (bytes > kPlainLds) {
       const hipError_t e = grant_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes);
       if (e != hipSuccess) return e;
@@ -845,8 +889,9 @@ hipError_t launch_top(const TopCall& c) {
 #define HELD(threads, n, step) \
   if (need(threads) <= n) return go(top_kernel<X, kEntropy, threads, n, step>, threads);
   if (c.split.parts == 1) {
-    HELD(64, 2, 2) HELD(64, 4, 2) HELD(64, 6, 2) HELD(64, 8, 2)
+    if (c.top.K <= 128) { HELD(64, 2, 2) HELD(64, 4, 2) HELD(64, 6, 2) HELD(64, 8, 2) }
     HELD(256, 4, 2) HELD(256, 6, 2) HELD(256, 8, 2)
+    if (c.top.K < 512 && rows >= (getenv("TB_X") ? atoi(getenv("TB_X")) : 512)) { HELD(256, 12, 4) HELD(256, 16, 4) HELD(256, 20, 4) HELD(256, 26, 4) }
   }
   HELD(512, 6, 4) HELD(512, 8, 2) HELD(512, 10, 2) HELD(512, 12, 2) HELD(512, 14, 2) HELD(512, 16, 2) HELD(512, 20, 4)
   HELD(512, 24, 4) HELD(512, 28, 4) HELD(512, 32, 4)
