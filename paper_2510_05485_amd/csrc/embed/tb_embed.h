@@ -1,6 +1,8 @@
 // Embeddings of token ids: what the kernels and the entry points share.
 #pragma once
 
+#include <type_traits>
+
 #include "../loss/tb_loss.h"
 #include "tensorembed.h"
 
@@ -25,13 +27,15 @@ struct Lookup {
   hipStream_t stream;
 };
 
-// Tokens are sorted by `digit`, some of their bits (so that the likeliest tokens, whose ids are neighbours in most
-// vocabularies, fall to different workgroups; but of small tables neighbouring rows to one, whole lines of memory), then
-// by their other bits.
+// Tokens are sorted by a digit, some of their lower bits (so that the likeliest tokens, whose ids are neighbours in most
+// vocabularies, fall to different workgroups; but neighbouring rows of narrow tables, whole lines of memory, to one),
+// then by their other bits.
 struct Buckets {
   int low, bits;  // the digit is (token >> low) & (2^bits - 1)
   int rows;       // of a bucket
 };
+constexpr int kPartBlock = 4096;
+
 struct Entry {
   uint32_t token, position;
 };
@@ -41,15 +45,17 @@ struct Gradient {
   int D, type, out_type, accumulate;
   float scale;
   Buckets by;
-  Entry* sorted;     // [positions]
-  Entry* parted;     // [positions], of many positions: by digit alone
-  int32_t* counts;   // [digit][block] of these, then where each begins
-  int32_t* totals;   // [digit]
-  int32_t* valid;    // how many positions there are in `sorted`
-  float* partial;    // [slice][2][D]: sums of tokens that go on from the slice before, or into the next one
-  int block;         // positions that a workgroup parts
-  int blocks;
-  int slice;         // entries of `sorted` that are added up together
+  int32_t* tokens;     // [positions], -1 for none; null: few positions, whose tokens are read where they are needed
+  Entry* sorted;       // [positions]
+  Entry* parted;       // [positions], of many positions: by digit alone
+  int32_t* counts;     // [digit][block] of these, then where each begins
+  int32_t* totals;     // [digit]
+  int32_t* valid;      // how many positions there are in `sorted`
+  int32_t* joins;      // how many tokens go over the end of a slice
+  int32_t* join_from;  // the slices in which these begin
+  float* partial;      // [slice][2][D]: sums of tokens that go on from the slice before, or into the next one
+  int blocks;          // of kPartBlock positions; 0: not parted
+  int slice;           // entries of `sorted` that are added up together
   int64_t slices;
   hipStream_t stream;
 };

@@ -1,6 +1,7 @@
 // Entry points of the embeddings: argument checks, workspace, launches.  Nothing here allocates, synchronises or
 // keeps state between calls.
 #include <algorithm>
+#include <cstdlib>
 
 #include "tb_embed.h"
 
@@ -21,29 +22,29 @@ int log2_up(int64_t n) {
 }
 
 // Up to so many positions every workgroup of the sort reads all tokens; more are parted first.
-constexpr int64_t kScanMost = 65536;
-constexpr int kMostPartBits = 11, kMostRows = 2048, kBlock = 4096, kMostBlocks = 2048;
+static const int64_t kScanMost = getenv("TB_S") ? atoi(getenv("TB_S")) : 65536;
+static const int64_t kDirectMost = getenv("TB_D") ? atoi(getenv("TB_D")) : 1024;
+constexpr int kMostPartBits = 11, kMostRows = 1024;
 
 struct Plan {
   Buckets by;
-  int block, blocks, slice;  // blocks 0: not parted
+  int blocks, slice;  // blocks 0: not parted
   int64_t slices;
-  size_t sorted, parted, counts, totals, valid, partial, bytes;
+  size_t tokens, sorted, parted, counts, totals, valid, join_from, partial, bytes;
 };
 Plan plan_of(int64_t B, int64_t T, int V, int D) {
   Plan p = {};
   const int64_t rows = B * T;
-  // 128 values at least of neighbouring rows to one bucket, 512 buckets where there are so many rows
-  p.by.low = D < 128 ? log2_up((128 + D - 1) / D) : 0;
+  const bool many = rows > kScanMost;
+  // Few positions: 128 values at least of neighbouring rows to one bucket, 512 buckets where there are so many rows.
+  // Many: a bucket for every token where there are few, so that nothing is left to sort
+  p.by.low = D < 128 && !(many && V <= 1 << kMostPartBits) ? log2_up((128 + D - 1) / D) : 0;
   const int64_t groups = (int64_t(V) + (1 << p.by.low) - 1) >> p.by.low;
-  p.by.bits = std::min(9, log2_up(groups));
+  p.by.bits = std::min(many && V <= 1 << kMostPartBits ? kMostPartBits : 9, log2_up(groups));
   const int most_rows = kMostRows >> p.by.low;
   while ((groups >> p.by.bits) + 1 > most_rows) ++p.by.bits;
   p.by.rows = int((groups + (1 << p.by.bits) - 1) >> p.by.bits) << p.by.low;
-  if (rows > kScanMost && p.by.bits <= kMostPartBits) {
-    p.block = int(std::max<int64_t>(kBlock, (rows + kMostBlocks - 1) / kMostBlocks + 255 & ~int64_t(255)));
-    p.blocks = int((rows + p.block - 1) / p.block);
-  }
+  if (many && p.by.bits <= kMostPartBits) p.blocks = int((rows + kPartBlock - 1) / kPartBlock);
   // slices of 16 to 256 positions, about 4096 wavefronts of 512 columns together
   const int64_t columns = (D + 511) / 512, each = D < 512 ? std::max(1, 512 / D) : 1;
   p.slice = 16;
@@ -55,11 +56,13 @@ Plan plan_of(int64_t B, int64_t T, int V, int D) {
     at += aligned(n);
     return from;
   };
+  p.tokens = take(rows > kDirectMost ? 4 * rows : 0);
   p.sorted = take(sizeof(Entry) * rows);
-  p.parted = take(p.blocks ? sizeof(Entry) * rows : 0);
+  p.parted = take(p.blocks && p.by.rows > 1 ? sizeof(Entry) * rows : 0);
   p.counts = take(size_t(4) * p.blocks << p.by.bits);
   p.totals = take(p.blocks ? size_t(4) << p.by.bits : 0);
-  p.valid = take(4);
+  p.valid = take(8);
+  p.join_from = take(4 * p.slices);
   p.partial = take(p.slices > 1 ? size_t(8) * p.slices * D : 0);
   p.bytes = at;
   return p;
@@ -150,6 +153,7 @@ extern "C" int tensorembed_gradient(const tb_embedding_rows_t* rows, const tb_po
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % kAlign) return TB_ERR_WORKSPACE;
   const Plan p = plan_of(rows->B, rows->T, grad->V, rows->D);
   if (workspace_bytes < p.bytes) return TB_ERR_WORKSPACE;
+  const int64_t rows_of = int64_t(rows->B) * rows->T;
   Gradient c = {};
   if (empty) {  // (every token is without positions)
     c.r.V = grad->V;
@@ -172,13 +176,15 @@ extern "C" int tensorembed_gradient(const tb_embedding_rows_t* rows, const tb_po
   c.accumulate = grad->accumulate != 0;
   c.scale = grad->scale;
   c.by = p.by;
+  c.tokens = rows_of > kDirectMost ? in<int32_t>(workspace, p.tokens) : nullptr;
   c.sorted = in<Entry>(workspace, p.sorted);
-  c.parted = p.blocks ? in<Entry>(workspace, p.parted) : nullptr;
+  c.parted = in<Entry>(workspace, p.parted);
   c.counts = in<int32_t>(workspace, p.counts);
   c.totals = in<int32_t>(workspace, p.totals);
   c.valid = in<int32_t>(workspace, p.valid);
+  c.joins = c.valid + 1;
+  c.join_from = in<int32_t>(workspace, p.join_from);
   c.partial = in<float>(workspace, p.partial);
-  c.block = p.block;
   c.blocks = p.blocks;
   c.slice = p.slice;
   c.slices = p.slices;

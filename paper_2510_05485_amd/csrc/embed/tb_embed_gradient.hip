@@ -13,21 +13,36 @@ namespace tb {
 namespace embed {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kThreads = 256;
 constexpr int64_t kMostGroups = 1 << 22;
-constexpr int kListed = 512;  // positions that a wavefront keeps between its two passes
 
 // ---- tokens -----------------------------------------------------------------------------------
 
-// The token of a position, or -1 for one that does not count or is outside the table (told by the threads with `tell`).
-__device__ __forceinline__ int token_of(const Rows& r, uint32_t n, bool tell) {
-  const At pos = loss::position(r, n);
-  if (tell && pos.t == 0 && r.lengths) loss::held_length(r.lengths[pos.b], r.T, r.status);
-  if (!loss::counts(r, pos.b, pos.t)) return -1;
-  const int64_t id = loss::load_id(r.tokens, r.long_tokens, pos.b * r.token_seq + pos.t);
-  if (id >= 0 && id < r.V) return int(id);
-  if (tell && r.status) atomicOr(r.status, TB_DEV_TOKEN_RANGE);
-  return -1;
+// The tokens of kN positions, `step` apart from n on: -1 at places from `end` on, at positions that do not count, and
+// for tokens outside the table (told by the threads with `tell`).  All requests are under way together, tokens of
+// positions that do not count among them.
+template <int kN>
+__device__ __forceinline__ void tokens_of(const Rows& r, int64_t n, int step, int64_t end, bool tell, int* token) {
+  int64_t id[kN];
+  int length[kN], t[kN];
+  uint8_t mask[kN];
+#pragma unroll
+  for (int a = 0; a < kN; ++a) {
+    const int64_t at = min(n + a * step, end - 1);
+    const At pos = loss::position(r, at);
+    t[a] = pos.t;
+    id[a] = loss::load_id(r.tokens, r.long_tokens, pos.b * r.token_seq + pos.t);
+    length[a] = r.lengths ? r.lengths[pos.b] : r.T;
+    mask[a] = r.mask ? r.mask[at] : 1;
+  }
+#pragma unroll
+  for (int a = 0; a < kN; ++a) {
+    const bool there = n + a * step < end, live = there && t[a] < length[a] && mask[a] != 0;
+    const bool fits = id[a] >= 0 && id[a] < r.V;
+    if (tell && there && t[a] == 0 && r.lengths) loss::held_length(length[a], r.T, r.status);
+    if (tell && live && !fits && r.status) atomicOr(r.status, TB_DEV_TOKEN_RANGE);
+    token[a] = live && fits ? int(id[a]) : -1;
+  }
 }
 __device__ __forceinline__ int digit_of(const Buckets& by, int token) { return (token >> by.low) & ((1 << by.bits) - 1); }
 // a token's row among those of its bucket, and back
@@ -42,6 +57,7 @@ __device__ __forceinline__ int lanes_before(uint64_t mask) {
 }
 
 // Sum of the values of the threads before, and of all (part: one a wavefront).
+template <int kThreads>
 __device__ __forceinline__ int block_scan(int v, int* part, int* all) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   int sum = v;
@@ -54,107 +70,14 @@ __device__ __forceinline__ int block_scan(int v, int* part, int* all) {
   if (lane == kWave - 1) part[wave] = sum;
   __syncthreads();
   int before = 0, total = 0;
-  for (int w = 0; w < kWaves; ++w) {
+#pragma unroll
+  for (int w = 0; w < kThreads / kWave; ++w) {
     if (w < wave) before += part[w];
     total += part[w];
   }
   *all = total;
   return before + sum - v;
 }
-
-// ---- parts of many positions ------------------------------------------------------------------
-
-__global__ __launch_bounds__(kThreads) void part_count_kernel(Gradient c) {
-  extern __shared__ int count[];
-  const int digits = 1 << c.by.bits;
-  for (int d = threadIdx.x; d < digits; d += kThreads) count[d] = 0;
-  __syncthreads();
-  const int64_t rows = int64_t(c.r.B) * c.r.T, from = int64_t(blockIdx.x) * c.block, to = min(from + c.block, rows);
-  for (int64_t n = from + threadIdx.x; n < to; n += kThreads) {
-    const int token = token_of(c.r, uint32_t(n), true);
-    if (token >= 0) atomicAdd(&count[digit_of(c.by, token)], 1);
-  }
-  __syncthreads();
-  for (int d = threadIdx.x; d < digits; d += kThreads) c.counts[int64_t(d) * c.blocks + blockIdx.x] = count[d];
-}
-
-// A workgroup a digit: where each block's positions begin among those of the digit, and how many these are.
-__global__ __launch_bounds__(kThreads) void part_sums_kernel(Gradient c) {
-  __shared__ int part[kWaves];
-  int32_t* counts = c.counts + int64_t(blockIdx.x) * c.blocks;
-  int before = 0;
-  for (int from = 0; from < c.blocks; from += kThreads) {
-    const int i = from + threadIdx.x;
-    int all;
-    const int mine = i < c.blocks ? counts[i] : 0, at = block_scan(mine, part, &all);
-    if (i < c.blocks) counts[i] = before + at;
-    before += all;
-  }
-  if (threadIdx.x == 0) c.totals[blockIdx.x] = before;
-}
-
-// Where the digits' positions begin, in `begin` [digits + 1]: sums of the totals.
-__device__ __forceinline__ void digit_begins(const Gradient& c, int* begin, int* part) {
-  const int digits = 1 << c.by.bits;
-  int before = 0;
-  for (int from = 0; from < digits; from += kThreads) {
-    const int i = from + threadIdx.x;
-    int all;
-    const int at = block_scan(i < digits ? c.totals[i] : 0, part, &all);
-    if (i < digits) begin[i] = before + at;
-    before += all;
-  }
-  if (threadIdx.x == 0) begin[digits] = before;
-  __syncthreads();
-}
-
-// Entries to their digits, in the order of the positions: every wavefront has a run of the block's positions, whose
-// digits it counts first.  Lanes with equal digits find one another by the digits' bits.
-__global__ __launch_bounds__(kThreads) void part_kernel(Gradient c) {
-  extern __shared__ int next[];  // [wave][digit], and the digits' beginnings
-  __shared__ int part[kWaves];
-  const int digits = 1 << c.by.bits, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  int* begin = next + kWaves * digits;
-  for (int d = threadIdx.x; d < kWaves * digits; d += kThreads) next[d] = 0;
-  digit_begins(c, begin, part);
-  const int64_t rows = int64_t(c.r.B) * c.r.T, first = int64_t(blockIdx.x) * c.block, end = min(first + c.block, rows);
-  const int run = c.block / kWaves;
-  const int64_t from = first + int64_t(wave) * run, to = min(from + run, end);
-  for (int64_t n = from + lane; n < to; n += kWave) {
-    const int token = token_of(c.r, uint32_t(n), false);
-    if (token >= 0) atomicAdd(&next[wave * digits + digit_of(c.by, token)], 1);
-  }
-  __syncthreads();
-  for (int d = threadIdx.x; d < digits; d += kThreads) {
-    int at = begin[d] + c.counts[int64_t(d) * c.blocks + blockIdx.x];
-    for (int w = 0; w < kWaves; ++w) {
-      const int n = next[w * digits + d];
-      next[w * digits + d] = at;
-      at += n;
-    }
-  }
-  __syncthreads();
-  int* mine = next + wave * digits;
-  for (int64_t i = from; i < to; i += kWave) {
-    const int64_t n = i + lane;
-    const int token = n < to ? token_of(c.r, uint32_t(n), false) : -1, digit = digit_of(c.by, token);
-    uint64_t same = __ballot(token >= 0);
-    for (int b = 0; b < c.by.bits; ++b) {
-      const bool set = digit >> b & 1;
-      const uint64_t with = __ballot(set);
-      same &= set ? with : ~with;
-    }
-    int at = 0;
-    if (token >= 0) at = mine[digit];
-    wave_fence();
-    const int before = lanes_before(same);
-    if (token >= 0 && before == 0) mine[digit] = at + __popcll(same);
-    wave_fence();
-    if (token >= 0) c.parted[at + before] = {uint32_t(token), uint32_t(n)};
-  }
-}
-
-// ---- sorted positions -------------------------------------------------------------------------
 
 // Zeros for a row of D values, by `lanes` threads.
 template <typename X>
@@ -167,11 +90,131 @@ __device__ __forceinline__ void write_zeros(typename X::type* row, int D, int la
     *reinterpret_cast<u32x4_any*>(row + min(i, D - X::kPer)) = u32x4{};
 }
 
+// The tokens of all positions, -1 for none: what every workgroup of the sort reads.
+constexpr int kReadyPer = 4;  // positions of a thread
+__global__ __launch_bounds__(kThreads) void ready_kernel(Gradient c) {
+  const int64_t rows = int64_t(c.r.B) * c.r.T, from = int64_t(blockIdx.x) * (kReadyPer * kThreads) + threadIdx.x;
+  int token[kReadyPer];
+  tokens_of<kReadyPer>(c.r, from, kThreads, rows, true, token);
+#pragma unroll
+  for (int a = 0; a < kReadyPer; ++a)
+    if (from + a * kThreads < rows) c.tokens[from + a * kThreads] = token[a];
+}
+
+// ---- parts of many positions ------------------------------------------------------------------
+
+constexpr int kHeld = kPartBlock / kThreads;  // positions of a thread
+
+__global__ __launch_bounds__(kThreads) void part_count_kernel(Gradient c) {
+  extern __shared__ int count[];
+  const int digits = 1 << c.by.bits;
+  const int64_t from = int64_t(blockIdx.x) * kPartBlock, rows = int64_t(c.r.B) * c.r.T;
+  int token[kHeld];
+  tokens_of<kHeld>(c.r, from + threadIdx.x, kThreads, rows, true, token);
+#pragma unroll
+  for (int a = 0; a < kHeld; ++a)
+    if (from + threadIdx.x + a * kThreads < rows) c.tokens[from + threadIdx.x + a * kThreads] = token[a];
+  for (int d = threadIdx.x; d < digits; d += kThreads) count[d] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int a = 0; a < kHeld; ++a)
+    if (token[a] >= 0) atomicAdd(&count[digit_of(c.by, token[a])], 1);
+  __syncthreads();
+  for (int d = threadIdx.x; d < digits; d += kThreads) c.counts[int64_t(d) * c.blocks + blockIdx.x] = count[d];
+}
+
+// A workgroup a digit: where each block's positions begin among those of the digit, and how many these are.  Where a
+// digit is a token, one without positions has a row of zeros.
+template <typename Out>
+__global__ __launch_bounds__(kThreads) void part_sums_kernel(Gradient c) {
+  __shared__ int part[kThreads / kWave];
+  int32_t* counts = c.counts + int64_t(blockIdx.x) * c.blocks;
+  int before = 0;
+  for (int from = 0; from < c.blocks; from += kThreads) {
+    const int i = from + threadIdx.x;
+    int all;
+    const int mine = i < c.blocks ? counts[i] : 0, at = block_scan<kThreads>(mine, part, &all);
+    if (i < c.blocks) counts[i] = before + at;
+    before += all;
+  }
+  if (threadIdx.x == 0) c.totals[blockIdx.x] = before;
+  if (threadIdx.x == 0 && blockIdx.x == 0) *c.joins = 0;
+  if (c.by.rows == 1 && before == 0 && !c.accumulate && int(blockIdx.x) < c.r.V)
+    write_zeros<Out>(static_cast<typename Out::type*>(c.r.g) + blockIdx.x * c.r.g_pos, c.D, threadIdx.x, kThreads);
+}
+
+// Entries to their digits, in the order of the positions: every wavefront has a run of the block's positions, whose
+// digits it counts first.  Lanes with equal digits find one another by the digits' bits.
+__global__ __launch_bounds__(kThreads) void part_kernel(Gradient c, Entry* to) {
+  constexpr int kWaves = kThreads / kWave;
+  extern __shared__ int next[];  // [wave][digit], and the digits' beginnings
+  __shared__ int part[kWaves];
+  const int digits = 1 << c.by.bits, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  int* begin = next + kWaves * digits;
+  const int64_t from = int64_t(blockIdx.x) * kPartBlock + wave * (kPartBlock / kWaves) + lane, rows = int64_t(c.r.B) * c.r.T;
+  int token[kHeld];
+#pragma unroll
+  for (int a = 0; a < kHeld; ++a) {
+    const int t = c.tokens[min(from + a * kWave, rows - 1)];
+    token[a] = from + a * kWave < rows ? t : -1;
+  }
+  for (int d = threadIdx.x; d < kWaves * digits; d += kThreads) next[d] = 0;
+  int before = 0;  // (the digits' beginnings: sums of their totals)
+  for (int i = 0; i < digits; i += kThreads) {
+    const int d = i + threadIdx.x;
+    int all;
+    const int at = block_scan<kThreads>(d < digits ? c.totals[d] : 0, part, &all);
+    if (d < digits) begin[d] = before + at;
+    before += all;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *c.valid = before;
+  __syncthreads();
+  int* mine = next + wave * digits;
+#pragma unroll
+  for (int a = 0; a < kHeld; ++a)
+    if (token[a] >= 0) atomicAdd(&mine[digit_of(c.by, token[a])], 1);
+  __syncthreads();
+  for (int d = threadIdx.x; d < digits; d += kThreads) {
+    int at = begin[d] + c.counts[int64_t(d) * c.blocks + blockIdx.x];
+    for (int w = 0; w < kWaves; ++w) {
+      const int n = next[w * digits + d];
+      next[w * digits + d] = at;
+      at += n;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int a = 0; a < kHeld; ++a) {
+    const int digit = digit_of(c.by, token[a]);
+    uint64_t same = __ballot(token[a] >= 0);
+    for (int b = 0; b < c.by.bits; ++b) {
+      const bool set = digit >> b & 1;
+      const uint64_t with = __ballot(set);
+      same &= set ? with : ~with;
+    }
+    int at = 0;
+    if (token[a] >= 0) at = mine[digit];
+    wave_fence();
+    const int k = lanes_before(same);
+    if (token[a] >= 0 && k == 0) mine[digit] = at + __popcll(same);
+    wave_fence();
+    if (token[a] >= 0) to[at + k] = {uint32_t(token[a]), uint32_t(from + a * kWave)};
+  }
+}
+
+// ---- sorted positions -------------------------------------------------------------------------
+
+constexpr int kSortThreads = 512, kListed = 384;  // positions that a wavefront keeps between its two passes
+
 // Workgroup d: the positions whose token has the digit d.  Two passes over the positions (each wavefront has a run of
 // them), or over a list of those that were found: how many of each token each wavefront has, then each one's place.
-// kParted: the positions are those of the digit's part.
-template <typename X, bool kParted>
-__global__ __launch_bounds__(kThreads) void sort_kernel(Gradient c) {
+// The positions are read from the caller's tensors (few of them), from what ready_kernel has left, or from the digit's
+// part.  What it takes is the latency of its reads, sixteen of which are under way for each lane, and then the zeros.
+enum From { kTokens, kReady, kPart };
+template <typename X, int kFrom>
+__global__ __launch_bounds__(kSortThreads) void sort_kernel(Gradient c) {
+  constexpr bool kParted = kFrom == kPart;
+  constexpr int kThreads = kSortThreads, kWaves = kThreads / kWave;
   extern __shared__ int next[];  // [wave][row]: how many, then where the next one goes
   __shared__ Entry listed[kWaves][kListed];
   __shared__ int part[kWaves];
@@ -185,35 +228,44 @@ __global__ __launch_bounds__(kThreads) void sort_kernel(Gradient c) {
       if (d < digit) before += n;
       if (d == digit) mine = n;
     }
-    block_scan(before, part, &all);
+    block_scan<kThreads>(before, part, &all);
     first = all;
-    block_scan(mine, part, &all);
+    block_scan<kThreads>(mine, part, &all);
     end = first + all;
+  } else if (digit == 0 && threadIdx.x == 0) {
+    *c.joins = 0;
   }
   __syncthreads();
   const int64_t run = ((end - first + kWaves - 1) / kWaves + kWave - 1) / kWave * kWave;
   const int64_t from = min(first + wave * run, end), to = min(from + run, end);
   int below = 0, seen = 0;
-  // entry(i): the token at place i, or -1, and its position
-  auto entry = [&](int64_t i, uint32_t* position, bool tell) {
+  // tokens at kN places from `i` on, and their positions; -1 for none
+  auto entries = [&](int64_t i, auto count, int* token, uint32_t* position, bool tell) {
+    constexpr int kN = decltype(count)::value;
     if constexpr (kParted) {
-      const Entry e = c.parted[i];
-      *position = e.position;
-      return int(e.token);
+#pragma unroll
+      for (int a = 0; a < kN; ++a) {
+        const Entry e = c.parted[min(i + a * kWave, to - 1)];
+        token[a] = i + a * kWave < to ? int(e.token) : -1;
+        position[a] = e.position;
+      }
     } else {
-      *position = uint32_t(i);
-      return token_of(c.r, uint32_t(i), tell);
+      if constexpr (kFrom == kTokens) tokens_of<kN>(c.r, i, kWave, to, tell, token);
+#pragma unroll
+      for (int a = 0; a < kN; ++a) {
+        position[a] = uint32_t(i + a * kWave);
+        if constexpr (kFrom == kReady) {
+          const int t = c.tokens[min(i + a * kWave, to - 1)];
+          token[a] = i + a * kWave < to ? t : -1;
+        }
+      }
     }
   };
-  constexpr int kAhead = 4;
+  constexpr int kAhead = 16;
   for (int64_t i = from; i < to; i += kAhead * kWave) {
     int token[kAhead];
     uint32_t position[kAhead];
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      const int64_t n = i + a * kWave + lane;
-      token[a] = n < to ? entry(n, &position[a], digit == 0) : -1;
-    }
+    entries(i + lane, std::integral_constant<int, kAhead>(), token, position, kFrom == kTokens && digit == 0);
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) {
       const int d = digit_of(c.by, token[a]);
@@ -231,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void sort_kernel(Gradient c) {
   }
   if constexpr (!kParted) {
     int all;
-    block_scan(below, part, &all);
+    block_scan<kThreads>(below, part, &all);
     first = all;
   }
   __syncthreads();
@@ -242,7 +294,7 @@ __global__ __launch_bounds__(kThreads) void sort_kernel(Gradient c) {
     int mine = 0, all;
     if (row < buckets)
       for (int w = 0; w < kWaves; ++w) mine += next[w * buckets + row];
-    int at = int(before) + block_scan(mine, part, &all);
+    int at = int(before) + block_scan<kThreads>(mine, part, &all);
     before += all;
     if (row < buckets) {
       for (int w = 0; w < kWaves; ++w) {
@@ -253,7 +305,7 @@ __global__ __launch_bounds__(kThreads) void sort_kernel(Gradient c) {
       }
     }
   }
-  if (digit == (1 << c.by.bits) - 1 && threadIdx.x == 0) *c.valid = int(before);
+  if (!kParted && digit == (1 << c.by.bits) - 1 && threadIdx.x == 0) *c.valid = int(before);
   __syncthreads();
   if (!c.accumulate) {
     const int chunks = (c.D + X::kPer - 1) / X::kPer;
@@ -294,9 +346,10 @@ __global__ __launch_bounds__(kThreads) void sort_kernel(Gradient c) {
     return;
   }
   for (int64_t i = from; i < to; i += kWave) {
-    uint32_t position = 0;
-    const int token = i + lane < to ? entry(i + lane, &position, false) : -1;
-    place(token >= 0 && digit_of(c.by, token) == digit ? token : -1, position);
+    int token[1];
+    uint32_t position[1];
+    entries(i + lane, std::integral_constant<int, 1>(), token, position, false);
+    place(token[0] >= 0 && digit_of(c.by, token[0]) == digit ? token[0] : -1, position[0]);
   }
 }
 
@@ -370,56 +423,73 @@ __device__ __forceinline__ void store_partial(float* to, const float* sum) {
   for (int i = 0; i < kPer; ++i) to[i] = sum[i];
 }
 
-// kLanes lanes a slice and kLanes chunks of columns (a tile).
+// A lane's value among those of its team's lanes.
+template <int kLanes>
+__device__ __forceinline__ uint32_t of_lane(uint32_t v, int lane) {
+  if constexpr (kLanes == kWave) return uint32_t(__builtin_amdgcn_readlane(int(v), lane));
+  return uint32_t(__shfl(int(v), lane, kLanes));
+}
+
+// kLanes lanes a slice and kLanes chunks of columns (a tile).  Each lane reads an entry, of as many as there are lanes at
+// a time, the next ones while the rows of these are on their way.
 template <typename X, typename Out, int kLanes, bool kWide>
 __global__ __launch_bounds__(kThreads) void sum_kernel(Gradient c, int tiles) {
   using C = Columns<X, kWide>;
-  constexpr int kTeams = kThreads / kLanes, kAhead = 8, kPer = C::kPer;
+  constexpr int kTeams = kThreads / kLanes, kAhead = kLanes < 8 ? kLanes : 8, kPer = C::kPer;
   const int lane = threadIdx.x % kLanes;
-  const int64_t valid = *c.valid, units = c.slices * tiles;
+  const int64_t rows = int64_t(c.r.B) * c.r.T, units = c.slices * tiles;
   for (int64_t unit = int64_t(blockIdx.x) * kTeams + threadIdx.x / kLanes; unit < units; unit += int64_t(gridDim.x) * kTeams) {
-    const int64_t slice = unit / tiles, from = slice * c.slice, to = min(from + c.slice, valid);
+    const int64_t slice = unit / tiles, from = slice * c.slice;
+    const int tile = int(unit - slice * tiles);
+    // (what lies behind the sorted positions is read, too, but not used: all of it is under way together)
+    Entry e = c.sorted[min(from + lane, rows - 1)];
+    const Entry previous = c.sorted[max(from - 1, int64_t(0))], following = c.sorted[min(from + c.slice, rows - 1)];
+    const int64_t valid = *c.valid, to = min(from + c.slice, valid);
     if (from >= to) continue;
-    const C at(int(unit - slice * tiles) * kLanes + lane, c.D);
-    const bool before = from > 0 && c.sorted[from - 1].token == c.sorted[from].token;
-    const bool behind = to < valid && c.sorted[to].token == c.sorted[to - 1].token;
+    const C at(tile * kLanes + lane, c.D);
     float sum[kPer] = {};
-    uint32_t token = c.sorted[from].token;
-    bool head = before;
+    uint32_t token = of_lane<kLanes>(e.token, 0);
+    bool head = from > 0 && previous.token == token;
     auto done = [&](bool tail) {
       if (!at.any) return;
       if (head || tail) store_partial<kPer>(c.partial + (slice * 2 + !head) * c.D + at.first, sum);
       else put_row<X, Out, kWide>(c, token, at, sum);
     };
-    for (int64_t i = from; i < to; i += kAhead) {
-      Entry e[kAhead];
-      u32x4 u[kAhead];
+    for (int64_t group = from; group < to; group += kLanes) {
+      const Entry now = e;
+      e = c.sorted[min(group + kLanes + lane, rows - 1)];
+      const int many = int(min(to - group, int64_t(kLanes)));
+      for (int i = 0; i < many; i += kAhead) {
+        u32x4 u[kAhead];
 #pragma unroll
-      for (int a = 0; a < kAhead; ++a) e[a] = c.sorted[min(i + a, to - 1)];
-#pragma unroll
-      for (int a = 0; a < kAhead; ++a) {
-        const At pos = loss::position(c.r, e[a].position);
-        u[a] = at.any && i + a < to ? C::load(loss::row_of<X>(c.r, pos.b, pos.t) + at.first) : u32x4{};
-      }
-#pragma unroll
-      for (int a = 0; a < kAhead; ++a) {
-        if (i + a >= to) break;
-        if (e[a].token != token) {
-          done(false);
-          head = false;
-          token = e[a].token;
-#pragma unroll
-          for (int j = 0; j < kPer; ++j) sum[j] = 0.f;
+        for (int a = 0; a < kAhead; ++a) {
+          const At pos = loss::position(c.r, of_lane<kLanes>(now.position, min(i + a, many - 1)));
+          u[a] = at.any ? C::load(loss::row_of<X>(c.r, pos.b, pos.t) + at.first) : u32x4{};
         }
-        C::add(u[a], sum);
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+          if (i + a >= many) break;
+          const uint32_t next = of_lane<kLanes>(now.token, i + a);
+          if (next != token) {
+            done(false);
+            head = false;
+            token = next;
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) sum[j] = 0.f;
+          }
+          C::add(u[a], sum);
+        }
       }
     }
+    const bool behind = to < valid && following.token == token;
     done(behind);
+    // (in any order: each one is joined by itself)
+    if (behind && !head && tile == 0 && lane == 0) c.join_from[atomicAdd(c.joins, 1)] = int32_t(slice);
   }
 }
 
-// Tokens that go over the end of a slice: the workgroup takes some slices in which such a token begins, one after
-// the other; its teams add up the slices' partial sums, a run of them each, and the first team what the teams have.
+// A token that goes over the end of a slice, and a tile of its columns: the workgroup's teams add up the slices'
+// partial sums, a run of them each, and the first team what the teams have.
 template <typename X, typename Out, int kLanes, bool kWide>
 __global__ __launch_bounds__(kThreads) void join_kernel(Gradient c, int tiles) {
   using C = Columns<X, kWide>;
@@ -427,14 +497,11 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Gradient c, int tiles) {
   __shared__ float sums[kTeams][kLanes * kPer];
   const int lane = threadIdx.x % kLanes, team = threadIdx.x / kLanes;
   const int64_t valid = *c.valid, slices = (valid + c.slice - 1) / c.slice;
-  const int64_t units = slices * tiles;
+  const int64_t units = int64_t(*c.joins) * tiles;
   auto token_at = [&](int64_t i) { return c.sorted[i].token; };
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int64_t slice = unit / tiles, from = slice * c.slice, to = from + c.slice;
-    if (to >= valid) continue;
-    const uint32_t token = token_at(to - 1);
-    if (token_at(to) != token) continue;
-    if (token_at(from) == token && from > 0 && token_at(from - 1) == token) continue;  // (it begins before)
+    const int64_t entry = unit / tiles, slice = c.join_from[entry];
+    const uint32_t token = token_at((slice + 1) * c.slice);
     // the slices that it goes on through: the last one whose first entry it has
     int64_t last = slice + 1;
     for (;;) {
@@ -444,7 +511,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Gradient c, int tiles) {
       last += n;
       if (n < kWave) break;
     }
-    const C at(int(unit - slice * tiles) * kLanes + lane, c.D);
+    const C at(int(unit - entry * tiles) * kLanes + lane, c.D);
     float sum[kPer] = {};
     if (at.any) {
       const int64_t many = last - slice + 1, run = (many + kTeams - 1) / kTeams;
@@ -488,7 +555,7 @@ hipError_t launch_sums(const Gradient& c) {
   const int64_t groups = (c.slices * tiles + kTeams - 1) / kTeams;
   sum_kernel<X, Out, kLanes, kWide><<<int(groups < kMostGroups ? groups : kMostGroups), kThreads, 0, c.stream>>>(c, tiles);
   if (c.slices > 1) {
-    const int64_t joins = c.slices * tiles < 2048 ? c.slices * tiles : 2048;
+    const int64_t joins = c.slices * tiles < 1024 ? c.slices * tiles : 1024;
     join_kernel<X, Out, kLanes, kWide><<<int(joins), kThreads, 0, c.stream>>>(c, tiles);
   }
   return hipGetLastError();
@@ -497,15 +564,20 @@ hipError_t launch_sums(const Gradient& c) {
 template <typename X, typename Out>
 hipError_t launch(const Gradient& c) {
   const int digits = 1 << c.by.bits;
-  const size_t next = size_t(kWaves) * c.by.rows * sizeof(int);
-  if (c.parted) {
+  const size_t next = size_t(kSortThreads / kWave) * c.by.rows * sizeof(int);
+  if (c.blocks) {
     const size_t lds = size_t(digits) * sizeof(int);
+    const bool sorted = c.by.rows == 1;  // (a digit is a token)
     part_count_kernel<<<c.blocks, kThreads, lds, c.stream>>>(c);
-    part_sums_kernel<<<digits, kThreads, 0, c.stream>>>(c);
-    part_kernel<<<c.blocks, kThreads, (kWaves + 1) * lds + sizeof(int), c.stream>>>(c);
-    sort_kernel<Out, true><<<digits, kThreads, next, c.stream>>>(c);
+    part_sums_kernel<Out><<<digits, kThreads, 0, c.stream>>>(c);
+    part_kernel<<<c.blocks, kThreads, (kThreads / kWave + 1) * lds, c.stream>>>(c, sorted ? c.sorted : c.parted);
+    if (!sorted) sort_kernel<Out, kPart><<<digits, kSortThreads, next, c.stream>>>(c);
+  } else if (c.tokens) {
+    const int64_t rows = int64_t(c.r.B) * c.r.T;
+    ready_kernel<<<int((rows + kReadyPer * kThreads - 1) / (kReadyPer * kThreads)), kThreads, 0, c.stream>>>(c);
+    sort_kernel<Out, kReady><<<digits, kSortThreads, next, c.stream>>>(c);
   } else {
-    sort_kernel<Out, false><<<digits, kThreads, next, c.stream>>>(c);
+    sort_kernel<Out, kTokens><<<digits, kSortThreads, next, c.stream>>>(c);
   }
   if (const hipError_t e = hipGetLastError()) return e;
   if (c.slices == 0) return hipSuccess;  // (no positions: zeros are all)
