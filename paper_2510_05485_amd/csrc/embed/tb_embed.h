@@ -34,7 +34,7 @@ struct Buckets {
   int low, bits;  // the digit is (token >> low) & (2^bits - 1)
   int rows;       // of a bucket
 };
-constexpr int kPartBlock = 4096;
+constexpr int kPartBlock = 2048;
 
 struct Entry {
   uint32_t token, position;

@@ -502,14 +502,20 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Gradient c, int tiles) {
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const int64_t entry = unit / tiles, slice = c.join_from[entry];
     const uint32_t token = token_at((slice + 1) * c.slice);
-    // the slices that it goes on through: the last one whose first entry it has
+    // the last slice that it goes on through, whose first entry it has: one by one, and in steps of 64 where it has
+    // all that a wavefront looks at
     int64_t last = slice + 1;
-    for (;;) {
-      const int64_t i = last + 1 + threadIdx.x % kWave;
+    auto steps = [&](int step) {
+      const int64_t i = last + int64_t(step) * (1 + threadIdx.x % kWave);
       const uint64_t with = __ballot(i < slices && token_at(i * c.slice) == token);
       const int n = with == ~uint64_t(0) ? kWave : __ffsll(static_cast<unsigned long long>(~with)) - 1;
-      last += n;
-      if (n < kWave) break;
+      last += int64_t(n) * step;
+      return n == kWave;
+    };
+    if (steps(1)) {
+      while (steps(kWave)) {
+      }
+      steps(1);
     }
     const C at(int(unit - entry * tiles) * kLanes + lane, c.D);
     float sum[kPer] = {};

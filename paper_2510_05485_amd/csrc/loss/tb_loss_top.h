@@ -5,8 +5,9 @@
 // ids.  A row is read once.  Nothing of it is sorted: the K-th largest of the maxima that lanes have of
 // their parts of the row is a bound that K values reach at least, and about K (1 + K / 2 maxima) do; these are
 // collected, and each one's place is the number of those before it.  Kernels by the length of a row:
-//   short_kernel  up to 64 chunks of 16 bytes: 2 to 64 lanes of a wavefront hold a row, a chunk each, and the best
-//                 of the lanes' best is taken K times
+//   best_kernel   up to 128 chunks of 16 bytes and eight alternatives: 2 to 32 lanes of a wavefront hold a row and keep
+//                 the best of their chunks
+//   short_kernel  up to 64 chunks: 2 to 64 lanes, a chunk each, and the best of the lanes' best is taken K times
 //   top_kernel    a wavefront, or a workgroup, holds a row (or a part of a long one) in its registers
 //   join_kernel   joins the parts of long rows
 #pragma once
@@ -703,21 +704,143 @@ __device__ __forceinline__ void sort_keys(Key* v) {
   }
 }
 
+// The eight largest keys of two descending lists: no key of the one is behind its counterpart of the other in reverse,
+// and what that leaves rises and then falls (Batcher).
+template <typename Key>
+__device__ __forceinline__ void merge_keys(Key* v, const Key* u) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = max(v[i], u[7 - i]);
+#pragma unroll
+  for (int d = 4; d; d >>= 1)
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (!(i & d)) exchange(v, i, i + d);
+}
+template <int kStep>
+__device__ __forceinline__ uint32_t neighbour_key(uint32_t v) {
+  return __float_as_uint(neighbour<kStep>(__uint_as_float(v)));
+}
+template <int kStep>
+__device__ __forceinline__ uint64_t neighbour_key(uint64_t v) {
+  return uint64_t(neighbour_key<kStep>(uint32_t(v >> 32))) << 32 | neighbour_key<kStep>(uint32_t(v));
+}
+// Of the lanes that share a row, in all of them.
+template <int kLanes, int kStep = 1, typename Key>
+__device__ __forceinline__ void merge_lanes(Key* v) {
+  if constexpr (kStep < kLanes) {
+    Key u[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = neighbour_key<kStep>(v[i]);
+    merge_keys(v, u);
+    merge_lanes<kLanes, kStep * 2>(v);
+  }
+}
+
 // Keys of short rows: in 32 bits with the place in the lower half where values have 16.
 template <typename X>
 struct ShortKey {
   using type = uint32_t;
-  static __device__ __forceinline__ type of(int t, int place) { return uint32_t(t + 32768) << 16 | uint32_t(0xFFFF - place); }
   static __device__ __forceinline__ int order(type key) { return int(key >> 16) - 32768; }
   static __device__ __forceinline__ int place(type key) { return 0xFFFF - int(key & 0xFFFFu); }
+  static __device__ __forceinline__ type of(int t, int place) { return uint32_t(t + 32768) << 16 | uint32_t(0xFFFF - place); }
+  // of a chunk's values, the first of which is at `place`
+  static __device__ __forceinline__ void of_chunk(u32x4 c, int place, type* keys) {
+    const uint32_t low = uint32_t(0xFFFF - place);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t t = Order<X>::of_packed(c[i]) ^ 0x80008000u;
+      keys[2 * i] = t << 16 | (low - 2 * i);
+      keys[2 * i + 1] = (t & 0xFFFF0000u) | (low - 2 * i - 1);
+    }
+  }
 };
 template <>
 struct ShortKey<F32> {
   using type = uint64_t;
-  static __device__ __forceinline__ type of(int t, int place) { return key_of(t, place); }
   static __device__ __forceinline__ int order(type key) { return order_in(key); }
   static __device__ __forceinline__ int place(type key) { return place_in(key); }
+  static __device__ __forceinline__ type of(int t, int place) { return key_of(t, place); }
+  static __device__ __forceinline__ void of_chunk(u32x4 c, int place, type* keys) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) keys[i] = key_of(int(Order<F32>::of_packed(c[i])), place + i);
+  }
 };
+
+// Up to eight alternatives of rows of up to 1024 values: each lane keeps the eight best of its chunks, sorted eight by
+// eight and merged, and so do the lanes with one another.  Few lanes with many chunks share what is done once a row.
+constexpr int kFewest = 8;
+template <typename X, bool kEntropy, int kLanes, int kChunks>
+__global__ __launch_bounds__(kTopThreads) void best_kernel(Rows r, RowOut o, Top q) {
+  constexpr int kTeams = kTopThreads / kLanes, kOctet = 8 / X::kPer;  // chunks that are sorted together
+  static_assert(kChunks % kOctet == 0);
+  using O = Order<X>;
+  using Key = ShortKey<X>;
+  using K = typename Key::type;
+  const int lane = threadIdx.x % kLanes;
+  const int64_t rows = int64_t(r.B) * r.T;
+  const float k = r.inv_temp * kLog2e;
+  for (int64_t round = blockIdx.x; round * kTeams < rows; round += gridDim.x) {
+    int V = r.V;
+    asm volatile("" : "+s"(V));  // (as in lanes_kernel)
+    const int64_t at = round * kTeams + threadIdx.x / kLanes;
+    const bool inside = at < rows;
+    const At pos = position(r, inside ? at : rows - 1);
+    const int b = pos.b, t = pos.t;
+    const bool live = inside && counts(r, b, t);
+    if (inside && lane == 0 && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
+    K best[8] = {};
+    Found f = {0.f, 1.f, 0.f, true};
+    float x = 0.f, log_s = 0.f;
+    if (__any(live)) {
+      const typename X::type* values = row_of<X>(r, b, t);
+      Part<X, kLanes, kChunks> part;
+      part.load(values, V, lane, live);
+      const int token = live && r.tokens ? take_token(r, b, t, lane == 0) : -1;
+      x = token < 0 ? __uint_as_float(kNan) : X::load(values + token);
+      const Stats s = part_stats<kEntropy, kLanes>(part, V, lane, k);
+      f = {s.m, s.s, s.t, true};
+      log_s = logf(f.s);
+#pragma unroll
+      for (int j = 0; j < kChunks; j += kOctet) {
+        K keys[8];
+#pragma unroll
+        for (int h = 0; h < kOctet; ++h) {
+          const int place = Part<X, kLanes, kChunks>::at(V, lane, j + h);
+          Key::of_chunk(part.c[j + h], place, keys + h * X::kPer);
+          // values that are another chunk's, or beyond the row
+          if (V % X::kPer == 0 && place >= 0) continue;
+          const int again = place < 0 ? X::kPer : (lane + (j + h) * kLanes) * X::kPer - place;
+#pragma unroll
+          for (int i = 0; i < X::kPer; ++i)
+            if (i < again) keys[h * X::kPer + i] = 0;
+        }
+        sort_keys<K, 8>(keys);
+        if (j == 0) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) best[i] = keys[i];
+        } else {
+          merge_keys(best, keys);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      merge_lanes<kLanes>(best);
+    }
+    const bool none = lost(f);
+#pragma unroll
+    for (int j = 0; j < kFewest; ++j) {
+      if (j >= q.K) break;
+      if (j % kLanes != lane || !inside) continue;
+      const int order = Key::order(best[j]);
+      const bool there = live && !none && best[j] != 0 && order > O::kNone;
+      put_id(q, at * q.K + j, there ? Key::place(best[j]) : -1);
+      q.logprobs[at * q.K + j] = there          ? logprob(f, O::value(order), k, r.inv_temp, log_s)
+                                 : live && none ? __uint_as_float(kNan)
+                                                : -INFINITY;
+    }
+    if (lane == 0 && live) put_values<kEntropy>(r, o, f, x, k, log_s, at);
+    else if (lane == 0 && inside) leave_nothing(o, at);
+  }
+}
 
 // kLanes lanes of a wavefront a row, a chunk each, whose values each lane puts in order; the best of the lanes' best is
 // the row's next one.
@@ -857,6 +980,14 @@ hipError_t launch_top(const TopCall& c) {
     const int64_t groups = (units + at_a_time - 1) / at_a_time;
     return int(groups < kMostGroups ? groups : kMostGroups);
   };
+#define BEST(lanes, n)                                                                                        \
+  if (chunks <= lanes * n) {                                                                                  \
+    best_kernel<X, kEntropy, lanes, n>                                                                        \
+        <<<std::min(groups_of(rows, kTopThreads / lanes), kLaneGroups), kTopThreads, 0, c.stream>>>(r, c.out, c.top); \
+    return hipGetLastError();                                                                                 \
+  }
+  if (c.top.K <= kFewest && r.V >= X::kPer) { BEST(2, 4) BEST(4, 4) BEST(8, 4) BEST(16, 4) BEST(32, 4) }
+#undef BEST
 #define SHORT(lanes)                                                                                          \
   if (chunks <= lanes) {                                                                                      \
     short_kernel<X, kEntropy, lanes>                                                                          \

@@ -81,7 +81,7 @@ def test_ties(V, dtype):
     x = rows.to(dtype).unsqueeze(0).to(DEV)
     n = rows.shape[0]
     valid = torch.ones(1, n, dtype=torch.bool)
-    for k in (1, min(V, 20), min(V, 300)):
+    for k in (1, 8, min(V, 20), min(V, 300)):
         r = tb.top_logprobs(x, k)
         _, _, ids, lps = plain.top(x, k, valid)
         assert torch.equal(r.ids.cpu(), ids), [(i, (r.ids[0, i].cpu() != ids[0, i]).sum()) for i in range(n)]
