@@ -170,14 +170,12 @@ Teacher teacher_of(const tb_teacher_t& q, const Rows& r) {
   return t;
 }
 
-// How many workgroups share a row of top log-probabilities.  One holds 32 chunks of 16 bytes a thread at most.
-constexpr int kHeldBytes = 512 * 32 * 16;
-constexpr int kSharedBytes = 65536;  // of a part where there are few rows
+// How many workgroups share a row of top log-probabilities: where there are few rows, parts of 64 KB.
+constexpr int64_t kSharedBytes = 65536, kSharedRows = 512;
 int top_parts(int64_t rows, int V, int type) {
   const int64_t bytes = int64_t(V) * value_bytes(type);
-  int64_t parts = bytes <= kHeldBytes ? 1 : (bytes + kHeldBytes / 2 - 1) / (kHeldBytes / 2);
-  if (rows * parts <= 128 && bytes >= 2 * kSharedBytes) parts = std::max(parts, std::min(256 / std::max(rows, int64_t(1)), bytes / kSharedBytes));
-  return int(parts);
+  if (rows == 0 || bytes < 2 * kSharedBytes) return 1;
+  return int(std::max(int64_t(1), std::min(kSharedRows / rows, bytes / kSharedBytes)));
 }
 size_t top_bytes(int64_t rows, int V, int type, int K, size_t* stats) {
   const int parts = top_parts(rows, V, type);

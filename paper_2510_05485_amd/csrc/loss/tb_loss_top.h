@@ -12,7 +12,6 @@
 //   join_kernel   joins the parts of long rows
 #pragma once
 
-#include <cstdlib>
 #include "tb_loss_rows.h"
 #include "tb_loss_top_host.h"
 
@@ -289,12 +288,54 @@ __device__ __forceinline__ int lanes_total(int v) {
   else return lanes_total<kLanes, kStep * 2>(v + __float_as_int(neighbour<kStep>(__int_as_float(v))));
 }
 
+template <int kLanes, int kStep = 1>
+__device__ __forceinline__ float lanes_added(float v) {
+  if constexpr (kStep == kLanes) return v;
+  else return lanes_added<kLanes, kStep * 2>(v + neighbour<kStep>(v));
+}
+
 // What the threads that share a row leave for one another; counted: two, taken in turn.
 template <int kWaves>
 struct TopShared {
   Stats parts[kWaves];
-  int bounds[2][kWaves], counts[kWaves], counted[2][kWaves];
+  int bounds[4][kWaves], counts[kWaves], counted[2][kWaves];
 };
+
+// The same of the keys that a wavefront has found, or no number (of -inf) if there are not so many.
+constexpr int kMostKeys = 514;
+template <typename X>
+__device__ __forceinline__ int list_bound(const uint64_t* own, int found, int need) {
+  constexpr int kBias = 32768, kBlocks = (kMostKeys + kWave - 1) / kWave;
+  if (found < need) return Order<X>::kNone;
+  const int lane = threadIdx.x % kWave;
+  int u[kBlocks];
+#pragma unroll
+  for (int j = 0; j < kBlocks; ++j) {
+    const int i = j * kWave + lane;
+    u[j] = i < found ? (order_in(own[i]) >> Order<X>::kShift) + kBias : -1;
+  }
+  int b = 0;
+  for (int bit = 1 << 15; bit; bit >>= 1) {
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < kBlocks; ++j)
+      if (j * kWave < found) n += __popcll(__ballot(u[j] >= (b | bit)));
+    if (n >= need) b |= bit;
+  }
+  return (b - kBias) * (1 << Order<X>::kShift);
+}
+
+// Sums of weights 2^(x k - M) of two parts of a row, M the scaled reference of each.
+template <bool kEntropy>
+__device__ __forceinline__ Stats joined_scaled(const Stats& p, const Stats& q, float k) {
+  Stats r;
+  r.m = fmaxf(p.m, q.m);
+  const float M = scaled(r.m, k), dp = scaled(p.m, k) - M, dq = scaled(q.m, k) - M;
+  const float ep = exp2_fast(dp), eq = exp2_fast(dq);
+  r.s = ep * p.s + eq * q.s;
+  r.t = kEntropy ? ep * (p.t + finite(dp) * p.s) + eq * (q.t + finite(dq) * q.s) : 0.f;
+  return r;
+}
 
 // take(order, place) for each of a thread's values of a row, read from memory; some threads may call it less often.
 template <typename X, int kThreads, typename Row, typename Take>
@@ -389,7 +430,12 @@ __device__ __forceinline__ Found moved_apart(const Found& f, float k) {
   return {f.m, e * f.s, e * (f.t + d * f.s), true};
 }
 
-constexpr int kHits = 192, kHitBytes = sizeof(u32x4) + sizeof(int);  // chunks with candidates that a wavefront may find
+constexpr int64_t kManyRows = 512;
+// What a wavefront may find: chunks with candidates (of a tile), and candidates.
+struct Room {
+  int hits, keys;  // (keys: an even number, more than K by all that share a row, at most kMostKeys)
+};
+constexpr int kHitBytes = sizeof(u32x4) + sizeof(int);
 constexpr int kTopThreads = 256;  // of a workgroup whose wavefronts have rows of their own
 
 // The first value of a part of a long row: multiples of 64, so that parts are alike in length up to 64 values.
@@ -397,25 +443,26 @@ __device__ __forceinline__ int part_from(int V, int part, int parts) {
   return part == parts ? V : int(int64_t(V) * part / parts) & ~63;
 }
 
-// kThreads threads a row, or a part of one: a wavefront of four in a workgroup, or a workgroup.
-// room: candidates that a wavefront may find, an even number, more than K by all that share a row.
-template <typename X, bool kEntropy, int kThreads, int kChunks, int kStep>
+// kThreads threads a row, or a part of one: a wavefront of four in a workgroup, or a workgroup.  With kTiled a row (or
+// part) is longer than the registers hold, and is taken tile by tile: what has been found in those before is a
+// bound for the next ones.
+template <typename X, bool kEntropy, int kThreads, int kChunks, int kStep, bool kTiled = false>
 __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void top_kernel(Rows r, RowOut o, Top q, Split split,
-                                                                                      int room) {
+                                                                                      Room room) {
   constexpr bool kAlone = kThreads > kWave;
   constexpr int kTeams = kAlone ? 1 : kTopThreads / kThreads, kWaves = kAlone ? kThreads / kWave : 1;
   using H = Taken<X, kThreads, kChunks, kStep>;
   using O = Order<X>;
-  // of each wavefront: chunks with candidates, their places, the candidates' keys [room]
+  // of each wavefront: chunks with candidates, their places, the candidates' keys
   extern __shared__ __attribute__((aligned(16))) uint64_t candidates[];
   __shared__ TopShared<kWaves> all[kTeams];
   const int team = threadIdx.x / kThreads, thread = threadIdx.x % kThreads, wave = thread / kWave, lane = threadIdx.x % kWave;
   const bool first = thread == 0;
   TopShared<kWaves>& shared = all[team];
   constexpr int kAllWaves = kTeams * kWaves;
-  u32x4* chunks = reinterpret_cast<u32x4*>(candidates) + threadIdx.x / kWave * kHits;
-  int* places = reinterpret_cast<int*>(reinterpret_cast<u32x4*>(candidates) + kAllWaves * kHits) + threadIdx.x / kWave * kHits;
-  uint64_t* keys = candidates + kAllWaves * (kHits * kHitBytes / 8) + team * kWaves * room;
+  u32x4* chunks = reinterpret_cast<u32x4*>(candidates) + threadIdx.x / kWave * room.hits;
+  int* places = reinterpret_cast<int*>(reinterpret_cast<u32x4*>(candidates) + kAllWaves * room.hits) + threadIdx.x / kWave * room.hits;
+  uint64_t* keys = candidates + kAllWaves * (room.hits * kHitBytes / 8) + team * kWaves * room.keys;
   const int64_t rows = int64_t(r.B) * r.T;
   const float k = r.inv_temp * kLog2e;
   auto take_unit = [&](int64_t unit) {
@@ -433,74 +480,104 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
       return;
     }
     const int from = part_from(r.V, part, split.parts), V = part_from(r.V, part + 1, split.parts) - from;
-    const typename H::Row row(row_of<X>(r, b, t) + from, V);
+    const typename X::type* values = row_of<X>(r, b, t) + from;
     // (what comes first is waited for first: not behind the whole row)
     const int token = r.tokens && part == 0 ? take_token(r, b, t, first) : -1;
-    H h;
-    h.load(row, thread);
-    const float x = token < 0 ? __uint_as_float(kNan) : X::load(row_of<X>(r, b, t) + token);
-    // Raw bits as signed integers are in the values' order from 0 on, with all others below: they do as long as
-    // the bound is above 0.
-    int most[H::kParts], edge_order = O::raw(h.edge);
-    h.largest(most, edge_order);
-    const int need = (q.K + kWaves - 1) / kWaves;
-    int bound = wave_bound<X>(most, need);
-    Stats s = taken_stats<kEntropy>(h, k);
-    if constexpr (kAlone) {
-      if (lane == 0) {
-        shared.parts[wave] = s;
-        shared.bounds[0][wave] = bound;
-      }
-      __syncthreads();
-      s = block_stats<kEntropy, kWaves>(shared.parts, k);
-      for (int w = 0; w < kWaves; ++w) bound = min(bound, shared.bounds[0][w]);
-    }
-    if (bound < 1) {
-      h.to_order();
-      edge_order = O::of(h.edge);
+    float x = __uint_as_float(kNan);
+    const int need = (q.K + kWaves - 1) / kWaves, tiles = kTiled ? split.tiles : 1;
+    int found = 0, bound = O::kNone + 1;
+    bool much = false;
+    Stats s = {};
+    uint64_t* own = keys + wave * room.keys;
+    for (int tile = 0; tile < tiles; ++tile) {
+      const int start = kTiled ? part_from(V, tile, tiles) : 0;
+      const typename H::Row row(values + start, kTiled ? part_from(V, tile + 1, tiles) - start : V);
+      H h;
+      h.load(row, thread);
+      if (tile == 0 && token >= 0) x = X::load(values - from + token);
+      // Raw bits as signed integers are in the values' order from 0 on, with all others below: they do as long as
+      // the bound is above 0.
+      int most[H::kParts], edge_order = O::raw(h.edge);
       h.largest(most, edge_order);
-      bound = wave_bound<X>(most, need);
-      if constexpr (kAlone) {
-        if (lane == 0) shared.bounds[1][wave] = bound;
-        __syncthreads();
-        for (int w = 0; w < kWaves; ++w) bound = min(bound, shared.bounds[1][w]);
+      int least = wave_bound<X>(most, need);
+      const Stats mine = taken_stats<kEntropy>(h, k);
+      s = tile ? joined_scaled<kEntropy>(s, mine, k) : mine;
+      int listed = O::kNone;
+      if (kTiled && tile) listed = list_bound<X>(own, found, need);
+      // the workgroup's bound: what all wavefronts have `need` values from
+      auto shared_bound = [&](int turn) {
+        if constexpr (kTiled) least = max(least, listed);
+        if constexpr (kAlone) {
+          if (lane == 0) shared.bounds[turn][wave] = least;
+          __syncthreads();
+          for (int w = 0; w < kWaves; ++w) least = min(least, shared.bounds[turn][w]);
+        }
+        bound = max(bound, least);
+      };
+      if (least < 1) least = O::kNone;
+      shared_bound(tile % 2);
+      if (bound < 1) {
+        h.to_order();
+        edge_order = O::of(h.edge);
+        h.largest(most, edge_order);
+        least = wave_bound<X>(most, need);
+        shared_bound(2 + tile % 2);
       }
-      bound = max(bound, O::kNone + 1);
+      if (kTiled && tile) {  // (keys below the bound are not needed any more)
+        int kept = 0;
+        for (int i = 0; i < found; i += kWave) {
+          const uint64_t key = i + lane < found ? own[i + lane] : 0;
+          const bool is = i + lane < found && order_in(key) >= bound;
+          const uint64_t mask = __ballot(is);
+          meet<kWave>();
+          if (is) own[kept + lanes_before(mask)] = key;
+          kept += __popcll(mask);
+        }
+        found = kept;
+        meet<kWave>();
+      }
+      // The values from the bound on, as keys in LDS, a part for each wavefront: first the chunks that have some,
+      // with one lane storing all of its chunk, then each value of these.
+      int hits = h.hits(row, thread, bound, chunks, places, room.hits);
+      meet<kWave>();
+      auto take = [&](bool is, int order, int place) {
+        const uint64_t mask = __ballot(is);
+        const int slot = found + lanes_before(mask);
+        if (is && slot < room.keys) own[slot] = key_of(order, from + start + place);
+        found += __popcll(mask);
+      };
+      much = much || hits > room.hits;
+      hits = min(hits, room.hits);
+      for (int e = 0; e < hits; e += kWave / X::kPer) {
+        const int hit = e + lane / X::kPer, i = lane % X::kPer;
+        const bool there = hit < hits;
+        const int order = there ? O::in_chunk(chunks + hit, i) : O::kNone, place = there ? places[hit] + i : 0;
+        take(there && order >= bound, order, place);
+      }
+      if (__any(edge_order >= bound)) take(edge_order >= bound, edge_order, h.edge_at);
+      much = much || found > room.keys;
+      found = min(found, room.keys);
+      meet<kWave>();
     }
-    // The values from the bound on, as keys in LDS, a part for each wavefront: first the chunks that have some, with
-    // one lane storing all of its chunk, then each value of these.
-    int found = 0;
-    uint64_t* own = keys + wave * room;
-    const int hits = h.hits(row, thread, bound, chunks, places, kHits);
-    meet<kWave>();
-    auto take = [&](bool is, int t, int place) {
-      const uint64_t mask = __ballot(is);
-      const int slot = found + lanes_before(mask);
-      if (is && slot < room) own[slot] = key_of(t, from + place);
-      found += __popcll(mask);
-    };
-    for (int e = 0; e < min(hits, kHits); e += kWave / X::kPer) {
-      const int hit = e + lane / X::kPer, i = lane % X::kPer;
-      const bool there = hit < min(hits, kHits);
-      const int t = there ? O::in_chunk(chunks + hit, i) : O::kNone, place = there ? places[hit] + i : 0;
-      take(there && t >= bound, t, place);
-    }
-    if (__any(edge_order >= bound)) take(edge_order >= bound, edge_order, h.edge_at);
     if (lane == 0) {
-      if (found < room) own[found] = 0;  // (keys are read in pairs)
-      if (kAlone) shared.counts[wave] = hits > kHits ? room + 1 : found;
+      if (found < room.keys) own[found] = 0;  // (keys are read in pairs)
+      if (kAlone) {
+        shared.parts[wave] = s;
+        shared.counts[wave] = much ? -1 : found;
+      }
     }
     meet<kThreads>();
     int total = found;
-    bool much = hits > kHits || found > room;
     if constexpr (kAlone) {
+      s = block_stats<kEntropy, kWaves>(shared.parts, k);
       total = 0;
       for (int w = 0; w < kWaves; ++w) {
         const int n = shared.counts[w];
         total += n;
-        much = much || n > room;
+        much = much || n < 0;
       }
     }
+    const typename H::Row row(values, V);
     const bool extreme = !fine(s, k);
     if (extreme) {
       meet<kThreads>();
@@ -512,14 +589,14 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
     else if (much) {
       meet<kThreads>();
       total = exact_keys<X, kThreads>(row, thread, q.K, V, from, shared, keys);  // (in the first wavefronts' parts)
-      found = kAlone ? max(min(total - wave * room, room), 0) : total;
+      found = kAlone ? max(min(total - wave * room.keys, room.keys), 0) : total;
       if (kAlone && lane == 0) shared.counts[wave] = found;
       meet<kThreads>();
     }
     // Each one's place is the number of larger keys: kWaves lanes count those of a wavefront's part each.
     const float log_s = logf(f.s);
     const int share = lane % kWaves;
-    const uint64_t* others = keys + share * room;
+    const uint64_t* others = keys + share * room.keys;
     const int theirs = kAlone ? shared.counts[share] : found;
     for (int i = lane / kWaves; i < found; i += kWave / kWaves) {
       const uint64_t key = own[i];
@@ -782,7 +859,7 @@ __device__ __forceinline__ uint32_t place_in_round(int64_t round) {
 
 // Up to eight alternatives of rows of up to 1024 values: each lane keeps the eight best of its chunks, sorted eight by
 // eight and merged, and so do the lanes with one another.  Few lanes with many chunks share what is done once a row.
-constexpr int kFewest = 8;
+constexpr int kFewest = 8, kBestGroups = 5120;
 template <typename X, bool kEntropy, int kLanes, int kChunks>
 __global__ __launch_bounds__(kTopThreads) void best_kernel(Rows r, RowOut o, Top q) {
   constexpr int kTeams = kTopThreads / kLanes, kOctet = 8 / X::kPer;  // chunks that are sorted together
@@ -803,7 +880,7 @@ __global__ __launch_bounds__(kTopThreads) void best_kernel(Rows r, RowOut o, Top
     const bool live = inside && counts(r, b, t);
     if (inside && lane == 0 && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
     K best[8] = {};
-    Found f = {0.f, 1.f, 0.f, true};
+    Found f = {0.f, 1.f, 0.f, false};
     float x = 0.f, log_s = 0.f;
     if (__any(live)) {
       const typename X::type* values = row_of<X>(r, b, t);
@@ -811,9 +888,6 @@ __global__ __launch_bounds__(kTopThreads) void best_kernel(Rows r, RowOut o, Top
       part.load(values, V, lane, live);
       const int token = live && r.tokens ? take_token(r, b, t, lane == 0) : -1;
       x = token < 0 ? __uint_as_float(kNan) : X::load(values + token);
-      const Stats s = part_stats<kEntropy, kLanes>(part, V, lane, k);
-      f = {s.m, s.s, s.t, true};
-      log_s = logf(f.s);
 #pragma unroll
       for (int j = 0; j < kChunks; j += kOctet) {
         K keys[8];
@@ -838,7 +912,33 @@ __global__ __launch_bounds__(kTopThreads) void best_kernel(Rows r, RowOut o, Top
         __builtin_amdgcn_sched_barrier(0);
       }
       merge_lanes<kLanes>(best);
+      part.keep_packed();
+      // the best is the largest value, or the row has a NaN
+      f.m = live ? O::value(Key::order(best[0])) : 0.f;
+      f.apart = !scales(f.m, k);
+      const float M = scaled(f.m, k);
+      f.s = 0.f;
+      auto sums = [&](auto argument) {
+#pragma unroll
+        for (int j = 0; j < kChunks; ++j) {
+          float v[X::kPer];
+          part.once(V, lane, j, v);
+#pragma unroll
+          for (int i = 0; i < X::kPer; ++i) {
+            const float a = argument(v[i]), w = exp2_fast(a);
+            f.s += w;
+            if (kEntropy) f.t += w * finite(a);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      if (__any(f.apart)) sums([&](float v) { return f.apart ? (v - f.m) * k : fmaf(v, k, -M); });
+      else sums([&](float v) { return fmaf(v, k, -M); });
+      f.s = lanes_added<kLanes>(f.s);
+      if (kEntropy) f.t = lanes_added<kLanes>(f.t);
+      log_s = logf(f.s);
     }
+    // (stores of whole lines through LDS take as long)
     const bool none = lost(f);
 #pragma unroll
     for (int j = 0; j < kFewest; ++j) {
@@ -998,7 +1098,7 @@ hipError_t launch_top(const TopCall& c) {
 #define BEST(lanes, n)                                                                                        \
   if (chunks <= lanes * n) {                                                                                  \
     best_kernel<X, kEntropy, lanes, n>                                                                        \
-        <<<std::min(groups_of(rows, kTopThreads / lanes), kLaneGroups), kTopThreads, 0, c.stream>>>(r, c.out, c.top); \
+        <<<std::min(groups_of(rows, kTopThreads / lanes), kBestGroups), kTopThreads, 0, c.stream>>>(r, c.out, c.top); \
     return hipGetLastError();                                                                                 \
   }
   if (c.top.K <= kFewest && r.V >= X::kPer) { BEST(2, 4) BEST(4, 4) BEST(8, 4) BEST(16, 4) BEST(32, 4) }
@@ -1014,17 +1114,18 @@ hipError_t launch_top(const TopCall& c) {
   // the longest part
   const int64_t most = r.V / c.split.parts + (c.split.parts > 1 ? 64 : 0);
   const int whole = int(most / X::kPer);
+  Split split = c.split;
+  split.tiles = 1;
   auto go = [&](auto kernel, int threads) {
     const int teams = threads <= kWave ? kTopThreads / threads : 1, waves = std::max(threads, kTopThreads * (teams > 1)) / kWave;
-    // (not a multiple of 32 keys: the parts begin at other banks)
-    constexpr int room = 258;
-    static_assert(4 * room > TB_TOP_MOST);
-    const size_t bytes = size_t(waves) * (room * sizeof(uint64_t) + kHits * kHitBytes);
+    // (not multiples of 32 keys: the parts begin at other banks)
+    const Room room = c.top.K < 256 ? Room{192, 258} : Room{256, kMostKeys};
+    static_assert(8 * kMostKeys > TB_TOP_MOST && 4 * kMostKeys > TB_TOP_MOST);
+    const size_t bytes = size_t(waves) * (room.keys * sizeof(uint64_t) + room.hits * kHitBytes);
     if (bytes > kPlainLds) {
       const hipError_t e = grant_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes);
       if (e != hipSuccess) return e;
     }
-    Split split = c.split;
     const int64_t units = teams > 1 ? 1 : rows * split.parts;
     for (split.first = 0; split.first < units; split.first += kMostGroups)  // (a workgroup for each)
       kernel<<<groups_of(teams > 1 ? rows : units - split.first, teams), waves * kWave, bytes, c.stream>>>(r, c.out, c.top, split,
@@ -1037,12 +1138,27 @@ hipError_t launch_top(const TopCall& c) {
   if (c.split.parts == 1) {
     if (c.top.K <= 128) { HELD(64, 2, 2) HELD(64, 4, 2) HELD(64, 6, 2) HELD(64, 8, 2) }
     HELD(256, 4, 2) HELD(256, 6, 2) HELD(256, 8, 2)
-    if (c.top.K < 512 && rows >= (getenv("TB_X") ? atoi(getenv("TB_X")) : 512)) { HELD(256, 12, 4) HELD(256, 16, 4) HELD(256, 20, 4) HELD(256, 26, 4) }
+    // (one row of 50257 values takes 8.5 us by 512 threads and 9.6 by 256; 16384 rows 267 us and 223)
+    if (c.top.K < 512 && rows >= kManyRows) { 
+      HELD(256, 10, 2) HELD(256, 12, 2) HELD(256, 14, 2) HELD(256, 16, 2) HELD(256, 18, 2) HELD(256, 20, 2) HELD(256, 22, 2)
+      HELD(256, 24, 2) HELD(256, 26, 2)
+    }
   }
-  HELD(512, 6, 4) HELD(512, 8, 2) HELD(512, 10, 2) HELD(512, 12, 2) HELD(512, 14, 2) HELD(512, 16, 2) HELD(512, 20, 4)
-  HELD(512, 24, 4) HELD(512, 28, 4) HELD(512, 32, 4)
+  if (c.top.K >= 512 || rows < kManyRows) {
+    HELD(512, 6, 4) HELD(512, 8, 2) HELD(512, 10, 2) HELD(512, 12, 2) HELD(512, 14, 2) HELD(512, 16, 2)
+  }
 #undef HELD
-  return hipErrorInvalidValue;  // (the host splits longer rows)
+  // tiles that differ by up to 64 values
+  constexpr int kTileThreads = 256, kTile = 24;
+  split.tiles = (whole + kTile * kTileThreads - 1) / (kTile * kTileThreads);
+  auto chunks_of = [&] { return (whole / split.tiles + 64 / X::kPer + 2 + kTileThreads - 1) / kTileThreads; };  // the longest's
+  if (chunks_of() > kTile) ++split.tiles;
+  const int each = chunks_of();
+#define TILED(n) \
+  if (each <= n) return go(top_kernel<X, kEntropy, kTileThreads, n, 2, true>, kTileThreads);
+  TILED(14) TILED(16) TILED(18) TILED(20) TILED(22) TILED(kTile)
+#undef TILED
+  return hipErrorInvalidValue;  // (not reached)
 }
 
 template <typename X, bool kEntropy>

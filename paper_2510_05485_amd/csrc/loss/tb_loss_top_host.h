@@ -17,6 +17,7 @@ struct Split {  // of long rows; parts 1: none
   uint64_t* keys;  // [row][part][K], in descending order, 0 for none
   float4* stats;   // [row][part]: reference logit, sums of 2^((x - m) k) and of these times their logarithms, token's logit
   int parts;
+  int tiles;      // of a part, that a workgroup takes one after the other
   int64_t first;  // part of the launch
 };
 struct TopGiven {

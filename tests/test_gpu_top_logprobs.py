@@ -67,6 +67,50 @@ def test_many_alternatives(V, K, dtype):
     check_values(tb.top_logprobs(x, K, tokens, want_entropy=True), x, K, tokens, valid)
 
 
+# rows of every length that kernels for many rows tell apart: chunks of 16 bytes a thread of 256, their first and last
+LENGTHS = [c * 2048 + d for c in range(2, 27) for d in (-70, 3)] + [26 * 2048 - 1, 26 * 2048, 26 * 2048 + 1, 26 * 2048 + 9, 28 * 2048, 2 * 24 * 2048,
+                                                                   2 * 24 * 2048 - 150, 2 * 24 * 2048 + 150, 131072, 150001]
+
+
+@pytest.mark.parametrize("half", [False, True])
+@pytest.mark.parametrize("V", LENGTHS)
+def test_many_rows(V, half):
+    """Against sorted float64 on the GPU, some of the rows with large values next to one another or below 0."""
+    V, dtype, rows = (V, torch.bfloat16, 600) if half else (V // 2 + 1, torch.float32, 600)
+    g = torch.Generator(device=DEV).manual_seed(V)
+    x = torch.randn(rows, V, generator=g, device=DEV) * 3
+    x[3] -= 100
+    x[4, V // 2:V // 2 + 700] += 20
+    x[5] = x[5].sort().values
+    x[6] = x[6].sort(descending=True).values
+    x[7, :] = 1.25
+    x[8, : V - 40] = -math.inf
+    x[9, 40:] = torch.finfo(dtype).min
+    x = x.to(dtype)
+    tokens = torch.randint(0, V, (rows,), generator=g, device=DEV)
+    tokens[8] = V - 1
+    mask = torch.ones(rows, dtype=torch.bool, device=DEV)
+    mask[[0, 100, 599]] = False
+    order = (x.double() + 0.0).sort(dim=-1, descending=True, stable=True)
+    logp = torch.log_softmax(x.double(), -1)
+    for k in (20, 300):
+        r = tb.top_logprobs(x, k, tokens, mask=mask, want_entropy=True)
+        there = (order.values[:, :k] > -math.inf) & mask.unsqueeze(-1)
+        ids = torch.where(there, order.indices[:, :k], -1)
+        assert torch.equal(r.ids, ids), (k, (r.ids != ids).any(-1).nonzero()[:5].flatten().tolist())
+        want = torch.where(there, logp.gather(-1, ids.clamp(min=0)), -math.inf)
+        low = ~(want > -1e4)
+        assert torch.equal(low, ~(r.logprobs > -1e4))
+        assert ((r.logprobs.double() - want)[~low].abs() <= LP).all()
+        lp = logp.gather(-1, tokens.unsqueeze(-1)).squeeze(-1)
+        fine = mask & (lp > -1e4)
+        assert ((r.token_logprobs.double() - lp)[fine].abs() <= LP).all()
+        held = logp.clamp(min=-1e6)
+        h = -(held.exp() * held).sum(-1)
+        assert ((r.entropy.double() - h)[mask].abs() <= H).all()
+    del order, logp
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("V", [60, 500, 3000, 20011, 140000])
 def test_ties(V, dtype):

@@ -37,11 +37,12 @@ def test_workspace(lib):  # noqa: F811
         assert n(*bad) == 0, bad
     assert n(1 << 10, 1 << 10, 64, 1, 5) == 0 and n(4096, 1, 32000, 1, 64) == 0
     for V, type_ in ((262144, 0), (1 << 20, 1), (2 ** 31 - 1, 2)):
-        for rows, k in ((1, 1), (1, 1024), (3, 64), (5000, 256)):
+        for rows, k in ((1, 1), (1, 1024), (3, 64), (100, 256)):
             b = n(rows, 1, V, type_, k)
             assert b == n(1, rows, V, type_, k)
-            parts = -(-V // (65536 if type_ == 0 else 131072))
+            parts = min(512 // rows, V * (4 if type_ == 0 else 2) // 65536)
             assert b >= rows * parts * (8 * k + 16)      # (every part leaves K keys and its statistics)
+        assert n(5000, 1, V, type_, 64) == 0              # (a workgroup for each row)
 
 
 def test_arguments(lib):  # noqa: F811
