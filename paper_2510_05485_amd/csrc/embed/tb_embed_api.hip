@@ -1,7 +1,6 @@
 // Entry points of the embeddings: argument checks, workspace, launches.  Nothing here allocates, synchronises or
 // keeps state between calls.
 #include <algorithm>
-#include <cstdlib>
 
 #include "tb_embed.h"
 
@@ -22,8 +21,9 @@ int log2_up(int64_t n) {
 }
 
 // Up to so many positions every workgroup of the sort reads all tokens; more are parted first.
-static const int64_t kScanMost = getenv("TB_S") ? atoi(getenv("TB_S")) : 65536;
-static const int64_t kDirectMost = getenv("TB_D") ? atoi(getenv("TB_D")) : 1024;
+constexpr int64_t kScanMost = 65536;
+// Up to so many they read them from the caller's tensors, beyond from what a launch before has left.
+constexpr int64_t kDirectMost = 1024;
 constexpr int kMostPartBits = 11, kMostRows = 1024;
 
 struct Plan {

@@ -489,12 +489,16 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
     bool much = false;
     Stats s = {};
     uint64_t* own = keys + wave * room.keys;
+    auto start_of = [&](int tile) { return kTiled ? part_from(V, tile, tiles) : 0; };
+    auto tile_of = [&](int tile) {
+      return typename H::Row(values + start_of(tile), kTiled ? start_of(tile + 1) - start_of(tile) : V);
+    };
+    H h;
+    h.load(tile_of(0), thread);
+    if (token >= 0) x = X::load(values - from + token);
     for (int tile = 0; tile < tiles; ++tile) {
-      const int start = kTiled ? part_from(V, tile, tiles) : 0;
-      const typename H::Row row(values + start, kTiled ? part_from(V, tile + 1, tiles) - start : V);
-      H h;
-      h.load(row, thread);
-      if (tile == 0 && token >= 0) x = X::load(values - from + token);
+      const int start = start_of(tile);
+      const typename H::Row row = tile_of(tile);
       // Raw bits as signed integers are in the values' order from 0 on, with all others below: they do as long as
       // the bound is above 0.
       int most[H::kParts], edge_order = O::raw(h.edge);
@@ -539,6 +543,8 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
       // The values from the bound on, as keys in LDS, a part for each wavefront: first the chunks that have some,
       // with one lane storing all of its chunk, then each value of these.
       int hits = h.hits(row, thread, bound, chunks, places, room.hits);
+      const int edge_at = h.edge_at;
+      if (kTiled && tile + 1 < tiles) h.load(tile_of(tile + 1), thread);
       meet<kWave>();
       auto take = [&](bool is, int order, int place) {
         const uint64_t mask = __ballot(is);
@@ -554,7 +560,7 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
         const int order = there ? O::in_chunk(chunks + hit, i) : O::kNone, place = there ? places[hit] + i : 0;
         take(there && order >= bound, order, place);
       }
-      if (__any(edge_order >= bound)) take(edge_order >= bound, edge_order, h.edge_at);
+      if (__any(edge_order >= bound)) take(edge_order >= bound, edge_order, edge_at);
       much = much || found > room.keys;
       found = min(found, room.keys);
       meet<kWave>();
@@ -664,6 +670,7 @@ __global__ __launch_bounds__(kTopThreads) void join_kernel(Rows r, RowOut o, Top
   __shared__ __attribute__((aligned(16))) uint64_t keys[kJoinRoom + 2];
   __shared__ uint64_t tops[kTopThreads / kWave], lows[kTopThreads / kWave];
   __shared__ int counted[2][kTopThreads / kWave], slots;
+  __shared__ Stats joints[kTopThreads / kWave];
   const int thread = threadIdx.x;
   const int64_t rows = int64_t(r.B) * r.T;
   const float k = r.inv_temp * kLog2e;
@@ -675,26 +682,31 @@ __global__ __launch_bounds__(kTopThreads) void join_kernel(Rows r, RowOut o, Top
     const int K = q.K, share = (K + split.parts - 1) / split.parts;
     const int64_t n = int64_t(split.parts) * K;
     if (thread == 0) slots = 0;
+    // (what is read first is under way together)
+    const uint64_t own = thread < n ? from[thread] : 0;
     uint64_t top = 0, low = ~uint64_t(0);
+    Stats s = {kLowest, 0.f, 0.f};
     for (int p = thread; p < split.parts; p += kTopThreads) {
       top = max(top, from[int64_t(p) * K + K - 1]);
       low = min(low, from[int64_t(p) * K + share - 1]);
-    }
-    top = block_key<true>(top, tops);
-    low = block_key<false>(low, lows);
-    uint64_t bound = max(max(top, low), uint64_t(1));
-    Stats s = {kLowest, 0.f, 0.f};
-    for (int p = 0; p < split.parts; ++p) {
       const float4 v = stats[p];
       s = joined<kEntropy>(s, Stats{v.x, v.y, v.z}, k);
     }
+    const float x = stats[0].w;
+    s = joined_lanes<kEntropy, kWave>(s, [k](const Stats& a, const Stats& b) { return joined<kEntropy>(a, b, k); });
+    if (thread % kWave == 0) joints[thread / kWave] = s;
+    top = block_key<true>(top, tops);
+    low = block_key<false>(low, lows);
+    uint64_t bound = max(max(top, low), uint64_t(1));
+    s = joints[0];
+    for (int w = 1; w < kTopThreads / kWave; ++w) s = joined<kEntropy>(s, joints[w], k);
     const Found f = {s.m, s.s, s.t, true};
-    const float x = stats[0].w, log_s = logf(f.s);
+    const float log_s = logf(f.s);
     const bool none = lost(f);
     int total = 0;
     while (!none) {
       for (int64_t i = thread; i < n; i += kTopThreads) {
-        const uint64_t key = from[i];
+        const uint64_t key = i == thread ? own : from[i];
         if (key < bound) continue;
         const int slot = atomicAdd(&slots, 1);
         if (slot < kJoinRoom) keys[slot] = key;
