@@ -243,6 +243,73 @@ struct RowsBackward : public torch::autograd::Node {
     return {out};
   }
 };
+// The backward pass of top log-probabilities, of what else came with them: incoming gradients of the alternatives, the
+// tokens and the entropies, those of the last two only where there are some.
+struct TopBackward : public torch::autograd::Node {
+  using Saved = torch::autograd::SavedVariable;
+  tb_logits_t logits_of;  // (shape, type and temperature)
+  int64_t dims;
+  int32_t K;
+  bool tokens_too, entropy_too;
+  Saved logits, tokens, lengths, mask, state, ids;
+
+  TopBackward(const Call& c, const at::Tensor& row_state, const at::Tensor& chosen, int32_t k, bool entropy)
+      : logits_of(c.logits), dims(c.x->dim()), K(k), tokens_too(c.tokens != nullptr), entropy_too(entropy) {
+    logits = RowsBackward::kept(c.x);
+    tokens = RowsBackward::kept(c.tokens);
+    lengths = RowsBackward::kept(c.lengths);
+    mask = RowsBackward::kept(c.mask);
+    state = RowsBackward::kept(&row_state);
+    ids = RowsBackward::kept(&chosen);
+    set_next_edges(torch::autograd::collect_next_edges(*c.x));
+  }
+  std::string name() const override { return "TensorTopBackward"; }
+  void release_variables() override {
+    std::lock_guard<std::mutex> lock(mutex_);
+    for (Saved* s : {&logits, &tokens, &lengths, &mask, &state, &ids}) s->reset_data();
+  }
+  torch::autograd::variable_list apply(torch::autograd::variable_list&& in) override {
+    std::lock_guard<std::mutex> lock(mutex_);
+    TORCH_CHECK(!at::GradMode::is_enabled(), "the losses over logits cannot be differentiated twice");
+    const size_t of_tokens = 1, of_entropy = 1 + tokens_too;
+    bool any = false;
+    for (const at::Tensor& d : in) any = any || d.defined();
+    if (!any) return {at::Tensor()};
+    // (unpacking checks that nothing has been written over since)
+    auto rows = [](const at::Tensor& t) {
+      return t.defined() && t.dim() > 0 && t.stride(-1) != 1 && t.size(-1) > 1 ? t.contiguous() : t;
+    };
+    auto whole = [](const at::Tensor& t) { return t.defined() ? t.contiguous() : t; };
+    auto given = [](const at::Tensor& t) { return t.defined() ? t.to(at::kFloat).contiguous() : t; };
+    const at::Tensor x = rows(logits.unpack()), ids_of_rows = rows(tokens.unpack()), n = whole(lengths.unpack()),
+                     m = whole(mask.unpack()), s = whole(state.unpack()), i = whole(ids.unpack());
+    const c10::OptionalDeviceGuard guard(x.device());
+    Call c;
+    c.logits.temperature = logits_of.temperature;
+    bool alike = x.dim() == dims && c.take_rows(&x) && c.logits.B == logits_of.B && c.logits.T == logits_of.T &&
+                 c.logits.V == logits_of.V && c.logits.type == logits_of.type;
+    const int64_t count = int64_t(logits_of.B) * logits_of.T;
+    auto values = [&](const at::Tensor& t, int64_t numbers) {
+      return c.here(&t) && t.scalar_type() == at::kFloat && t.numel() == numbers;
+    };
+    alike = alike && (!tokens_too || (ids_of_rows.defined() && c.take_tokens(&ids_of_rows))) &&
+            (!n.defined() || c.take_lengths(&n)) && (!m.defined() || c.take_mask(&m)) && values(s, TB_ROW_STATE * count) &&
+            c.here(&i) && (i.scalar_type() == at::kLong || i.scalar_type() == at::kInt) && i.numel() == count * K;
+    TORCH_CHECK(alike, RowsBackward::kHooks);
+    at::Tensor d_top = given(in[0]), d_lp, d_h;
+    if (tokens_too && in.size() > of_tokens) d_lp = given(in[of_tokens]);
+    if (entropy_too && in.size() > of_entropy) d_h = given(in[of_entropy]);
+    if (!d_top.defined()) d_top = at::zeros({count * K}, s.options().requires_grad(false));
+    at::Tensor out = at::empty(x.sizes(), x.options().requires_grad(false));
+    const tb_gradient_t g = {out.data_ptr(), x.dim() == 2 ? 0 : out.stride(0), out.stride(x.dim() - 2), 1.f};
+    const tb_top_t q = {i.data_ptr(), nullptr, i.scalar_type() == at::kLong ? 8 : 4, K};
+    const int rc = tensorloss_top_logprobs_grad(&c.logits, &c.at, &q, s.data_ptr<float>(), d_top.data_ptr<float>(),
+                                                d_lp.defined() ? d_lp.data_ptr<float>() : nullptr,
+                                                d_h.defined() ? d_h.data_ptr<float>() : nullptr, &g, c.stream);
+    TORCH_CHECK(rc == TB_OK, "tensorloss gradient: ", tensorbleu_status_string(rc));
+    return {out};
+  }
+};
 std::shared_ptr<RowsBackward> backward_of(RowsBackward::Kind kind, const Call& c, const at::Tensor& state) {
   return std::shared_ptr<RowsBackward>(new RowsBackward(kind, c, state), torch::autograd::deleteNode);
 }
@@ -306,12 +373,12 @@ PyObject* logprobs(PyObject*, PyObject* const* args, Py_ssize_t n) {
 }
 
 // top(logits, k, tokens, lengths, mask, temperature, status, want_entropy, id_bytes): (ids, log-probabilities,
-// those of the tokens or None, entropies or None) or None; not where the logits are differentiated
+// those of the tokens or None, entropies or None) or None
 PyObject* top(PyObject*, PyObject* const* args, Py_ssize_t n) {
   Call c;
   if (n != 9 || !c.take(args[0], args[2] == Py_None ? nullptr : args[2], args[3], args[4], args[5], args[6])) Py_RETURN_NONE;
   tb_top_t q = {};
-  if (differentiated(*c.x) || !take_int(args[1], &q.K) || !take_int(args[8], &q.id_bytes) || q.K < 1 ||
+  if (!take_int(args[1], &q.K) || !take_int(args[8], &q.id_bytes) || q.K < 1 ||
       q.K > TB_TOP_MOST || q.K > c.logits.V || (q.id_bytes != 4 && q.id_bytes != 8))
     Py_RETURN_NONE;
   const int wanted = PyObject_IsTrue(args[7]);
@@ -324,15 +391,24 @@ PyObject* top(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (wanted) h = c.values(c.positions());
   q.ids = ids.data_ptr();
   q.logprobs = values.data_ptr<float>();
+  const bool backward = differentiated(*c.x);
+  at::Tensor state;
+  if (backward) state = c.row_state();
   const size_t bytes = tensorloss_top_workspace_bytes(c.logits.B, c.logits.T, c.logits.V, c.logits.type, q.K);
   if (bytes) workspace = at::empty({int64_t(bytes)}, at::TensorOptions().dtype(at::kByte).device(c.x->device()));
   int rc;
   Py_BEGIN_ALLOW_THREADS
   rc = tensorloss_top_logprobs(&c.logits, &c.at, &q, c.tokens ? lp.data_ptr<float>() : nullptr,
-                               wanted ? h.data_ptr<float>() : nullptr, nullptr, c.status,
+                               wanted ? h.data_ptr<float>() : nullptr, backward ? state.data_ptr<float>() : nullptr, c.status,
                                bytes ? workspace.data_ptr() : nullptr, bytes, c.stream);
   Py_END_ALLOW_THREADS
   if (rc != TB_OK) Py_RETURN_NONE;
+  if (backward) {
+    std::shared_ptr<TopBackward> node(new TopBackward(c, state, ids, q.K, wanted), torch::autograd::deleteNode);
+    torch::autograd::set_history(values, node);
+    if (c.tokens) torch::autograd::set_history(lp, node);
+    if (wanted) torch::autograd::set_history(h, node);
+  }
   return results({ids, values, lp, h}, Py_None, -1);
 }
 

@@ -408,13 +408,39 @@ def test_refusals():
     with pytest.raises(tb.TensorBLEUError, match="mask"):
         tb.top_logprobs(x.flatten(0, 1), 3, lengths=torch.ones(2, device=DEV))
     leaf = x.clone().requires_grad_()
-    v, = torch.autograd.grad(tb.top_logprobs(leaf, 3).logprobs.sum(), leaf, create_graph=True)
-    with pytest.raises(RuntimeError):
-        v.sum().backward()
+    with pytest.raises(RuntimeError, match="differentiated twice"):
+        torch.autograd.grad(tb.top_logprobs(leaf, 3).logprobs.sum(), leaf, create_graph=True)
     with torch.autograd.forward_ad.dual_level():
         dual = torch.autograd.forward_ad.make_dual(x, torch.ones_like(x))
         with pytest.raises(tb.TensorBLEUError, match="tangent"):
             tb.top_logprobs(dual, 3)
+
+
+def test_general_way_and_hooks():
+    """int64 lengths go through the general way, whose results and gradients are the native ones' bit by bit; hooks on saved
+    tensors may give back other memory and strides; changed logits are noticed."""
+    x, tokens, g = inputs(6, 3, 4, 700, torch.bfloat16)
+    lengths = torch.tensor([4, 1, 3], device=DEV, dtype=torch.int32)
+    d = torch.randn(3, 4, 5, generator=g).to(DEV), torch.randn(3, 4, generator=g).to(DEV)
+
+    def step(n, hooks=None):
+        leaf = x.clone().requires_grad_()
+        with hooks or torch.enable_grad():
+            r = tb.top_logprobs(leaf, 5, tokens, lengths=n, want_entropy=True)
+        return [t.detach() for t in r] + list(torch.autograd.grad([r.logprobs, r.token_logprobs, r.entropy], leaf, [*d, d[1]]))
+    want = step(lengths)
+    moved = torch.autograd.graph.saved_tensors_hooks(
+        lambda t: t.cpu(), lambda t: t.to(DEV).transpose(0, -1).contiguous().transpose(0, -1))
+    for got in (step(lengths.long()), step(lengths, moved), step(lengths.long(), torch.autograd.graph.save_on_cpu())):
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+    leaf = x.clone().requires_grad_()
+    y = leaf * 1
+    r = tb.top_logprobs(y, 5)
+    y.add_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        r.logprobs.sum().backward()
+    r = tb.top_logprobs(leaf, 5, tokens)
+    assert not r.ids.requires_grad and r.logprobs.requires_grad and r.token_logprobs.requires_grad and r.entropy is None
 
 
 @pytest.mark.parametrize("V", [64, 700, 9001, 300000])
