@@ -198,6 +198,22 @@ struct Taken {
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) most[k % kParts] = max(most[k % kParts], O::largest(c[k]));
   }
+  // A number that `need` of a wavefront's values reach, 16 bits of it, when the chunks are whole numbers in the values'
+  // order: the largest such, by halving; three instructions a value and step, two of them scalar.
+  __device__ __forceinline__ int value_bound(int edge_order, int need) {
+    constexpr int kBias = 32768;
+    int b = 0;
+#pragma unroll 1
+    for (int bit = 1 << 15; bit; bit >>= 1) {
+      keep_packed();
+      const int least = ((b | bit) - kBias) * (1 << O::kShift);
+      int n = __popcll(__ballot(edge_order >= least));
+#pragma unroll
+      for (int k = 0; k < kChunks; ++k) O::each(c[k], [&](int, int t) { n += __popcll(__ballot(t >= least)); });
+      if (n >= need) b |= bit;
+    }
+    return (b - kBias) * (1 << O::kShift);
+  }
   // Chunks with a value from `least` on, with the places of their first values, into a list of the wavefront: how many
   // there are (of which `room` are kept).
   __device__ __forceinline__ int hits(const Row& row, int thread, int least, u32x4* chunks, int* places, int room) {
@@ -337,6 +353,27 @@ __device__ __forceinline__ Stats joined_scaled(const Stats& p, const Stats& q, f
   return r;
 }
 
+// A wavefront's keys in descending order, `found` of them in room for the next power of two (Batcher's exchanges).
+__device__ __forceinline__ void sort_list(uint64_t* own, int found) {
+  const int lane = threadIdx.x % kWave;
+  int n = 2;
+  while (n < found) n *= 2;
+  for (int i = found + lane; i < n; i += kWave) own[i] = 0;
+  meet<kWave>();
+  for (int size = 2; size <= n; size *= 2)
+    for (int d = size / 2; d; d /= 2) {
+      for (int i = lane; i < n / 2; i += kWave) {
+        const int lo = 2 * i - (i & (d - 1)), hi = lo + d;
+        const uint64_t a = own[lo], b = own[hi];
+        if ((a < b) == !(lo & size)) {
+          own[lo] = b;
+          own[hi] = a;
+        }
+      }
+      meet<kWave>();
+    }
+}
+
 // take(order, place) for each of a thread's values of a row, read from memory; some threads may call it less often.
 template <typename X, int kThreads, typename Row, typename Take>
 __device__ __forceinline__ void sweep_orders(const Row& row, int thread, Take take) {
@@ -353,6 +390,37 @@ __device__ __forceinline__ void sweep_orders(const Row& row, int thread, Take ta
     const int e = row.edge(j);
     if (e >= 0) take(O::of(X::load(row.x + e)), e);
   }
+}
+
+// Statistics of a row from one sweep over it, as row_stats, with few registers: for rows that are rare.
+template <typename X, bool kEntropy, int kThreads, typename Row>
+__device__ __forceinline__ Stats swept_stats(const Row& row, float k, int thread, Stats* parts) {
+  Stats mine = {kLowest, 0.f, 0.f};
+  auto take = [&](float v) { mine = joined<kEntropy>(mine, v == -INFINITY ? Stats{kLowest, 0.f, 0.f} : Stats{v, v == v ? 1.f : v, 0.f}, k); };
+#pragma unroll 1
+  for (int c = thread; c < row.chunks; c += kThreads) {
+    float v[X::kPer];
+    X::unpack(row.chunk(c), v);
+#pragma unroll 1
+    for (int i = 0; i < X::kPer; ++i) {
+      float one = v[0];
+#pragma unroll
+      for (int j = 1; j < X::kPer; ++j) one = j == i ? v[j] : one;
+      take(one);
+    }
+  }
+#pragma unroll 1
+  for (int j = thread; j < row.kEdge; j += kThreads) {
+    const int e = row.edge(j);
+    if (e >= 0) take(X::load(row.x + e));
+  }
+  mine = joined_lanes<kEntropy, kWave>(mine, [k](const Stats& a, const Stats& b) { return joined<kEntropy>(a, b, k); });
+  if constexpr (kThreads <= kWave) return mine;
+  if (thread % kWave == 0) parts[thread / kWave] = mine;
+  __syncthreads();
+  Stats all = parts[0];
+  for (int w = 1; w < kThreads / kWave; ++w) all = joined<kEntropy>(all, parts[w], k);
+  return all;
 }
 
 // Where the values that a bound lets through are too many (ties, masks of the lowest value, a few places that have
@@ -431,6 +499,7 @@ __device__ __forceinline__ Found moved_apart(const Found& f, float k) {
 }
 
 constexpr int64_t kManyRows = 512;
+constexpr int kCounted = 128;
 // What a wavefront may find: chunks with candidates (of a tile), and candidates.
 struct Room {
   int hits, keys;  // (keys: an even number, more than K by all that share a row, at most kMostKeys)
@@ -465,7 +534,7 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
   uint64_t* keys = candidates + kAllWaves * (room.hits * kHitBytes / 8) + team * kWaves * room.keys;
   const int64_t rows = int64_t(r.B) * r.T;
   const float k = r.inv_temp * kLog2e;
-  auto take_unit = [&](int64_t unit) {
+  auto take_unit = [&](int64_t unit, int thread, int lane) {
     const int64_t which = split.parts == 1 ? unit : unit / split.parts;
     const int part = int(unit - which * split.parts);
     const int64_t at = kAlone && split.parts == 1 ? row_of_group(which, rows) : which;
@@ -479,7 +548,9 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
       }
       return;
     }
-    const int from = part_from(r.V, part, split.parts), V = part_from(r.V, part + 1, split.parts) - from;
+    const int from = kAlone ? part_from(r.V, part, split.parts) : 0;
+    int V = kAlone ? part_from(r.V, part + 1, split.parts) - from : r.V;
+    if constexpr (!kAlone) asm volatile("" : "+s"(V));
     const typename X::type* values = row_of<X>(r, b, t) + from;
     // (what comes first is waited for first: not behind the whole row)
     const int token = r.tokens && part == 0 ? take_token(r, b, t, first) : -1;
@@ -519,8 +590,16 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
         bound = max(bound, least);
       };
       if (least < 1) least = O::kNone;
+      bool ordered = false;
+      if constexpr (!kAlone)
+        if (split.by_values) {
+          h.to_order();
+          edge_order = O::of(h.edge);
+          least = max(h.value_bound(edge_order, need), O::kNone);
+          ordered = true;
+        }
       shared_bound(tile % 2);
-      if (bound < 1) {
+      if (bound < 1 && !ordered) {
         h.to_order();
         edge_order = O::of(h.edge);
         h.largest(most, edge_order);
@@ -587,7 +666,7 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
     const bool extreme = !fine(s, k);
     if (extreme) {
       meet<kThreads>();
-      s = row_stats<X, kEntropy, kThreads>(row, k, thread, shared.parts);
+      s = swept_stats<X, kEntropy, kThreads>(row, k, thread, shared.parts);
     }
     const Found f = {s.m, s.s, s.t, extreme};
     const bool none = f.s != f.s || (split.parts == 1 && lost(f));
@@ -599,8 +678,23 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
       if (kAlone && lane == 0) shared.counts[wave] = found;
       meet<kThreads>();
     }
-    // Each one's place is the number of larger keys: kWaves lanes count those of a wavefront's part each.
     const float log_s = logf(f.s);
+    auto put_key = [&](int rank, uint64_t key) {
+      if (split.parts > 1) {
+        split.keys[unit * q.K + rank] = key;
+      } else {
+        put_id(q, at * q.K + rank, place_in(key));
+        q.logprobs[at * q.K + rank] = logprob(f, O::value(order_in(key)), k, r.inv_temp, log_s);
+      }
+    };
+    // Each one's place is the number of larger keys: kWaves lanes count those of a wavefront's part each.  Many of a
+    // wavefront are sorted: counting takes found^2 / 64 comparisons.
+    const bool sorted = !kAlone && found > kCounted && found <= (room.keys & ~3);  // (the next power of two fits)
+    if (sorted) {
+      sort_list(own, found);
+      for (int i = lane; i < min(found, q.K); i += kWave) put_key(i, own[i]);
+      found = 0;
+    }
     const int share = lane % kWaves;
     const uint64_t* others = keys + share * room.keys;
     const int theirs = kAlone ? shared.counts[share] : found;
@@ -616,13 +710,7 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
         rank += (one.x > key) + (one.y > key);
       }
       rank = lanes_total<kWaves>(rank);
-      if (rank >= q.K || share) continue;
-      if (split.parts > 1) {
-        split.keys[unit * q.K + rank] = key;
-      } else {
-        put_id(q, at * q.K + rank, place_in(key));
-        q.logprobs[at * q.K + rank] = logprob(f, O::value(order_in(key)), k, r.inv_temp, log_s);
-      }
+      if (rank < q.K && !share) put_key(rank, key);
     }
     if (split.parts > 1) {
       for (int j = min(total, q.K) + thread; j < q.K; j += kThreads) split.keys[unit * q.K + j] = 0;
@@ -635,11 +723,13 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
   };
   // (a workgroup takes one row: what lives from row to row would cost it registers)
   if constexpr (kAlone) {
-    take_unit(split.first + blockIdx.x);
+    take_unit(split.first + blockIdx.x, thread, lane);
   } else {
     for (int64_t group = blockIdx.x; group * kTeams < rows; group += gridDim.x) {
       const int64_t unit = turned(group, (rows + kTeams - 1) / kTeams) * kTeams + team;
-      if (unit < rows) take_unit(unit);
+      int now = thread;  // (keeps the compiler from working out places and masks once for all rows, 50 registers)
+      asm volatile("" : "+v"(now));
+      if (unit < rows) take_unit(unit, now, now);
       meet<kThreads>();  // (before the next row takes the shared memory)
     }
   }
@@ -871,7 +961,7 @@ __device__ __forceinline__ uint32_t place_in_round(int64_t round) {
 
 // Up to eight alternatives of rows of up to 1024 values: each lane keeps the eight best of its chunks, sorted eight by
 // eight and merged, and so do the lanes with one another.  Few lanes with many chunks share what is done once a row.
-constexpr int kFewest = 8, kBestGroups = 5120;
+constexpr int kFewest = 8, kBestGroups = 5120, kShortSteps = 2048;
 template <typename X, bool kEntropy, int kLanes, int kChunks>
 __global__ __launch_bounds__(kTopThreads) void best_kernel(Rows r, RowOut o, Top q) {
   constexpr int kTeams = kTopThreads / kLanes, kOctet = 8 / X::kPer;  // chunks that are sorted together
@@ -1115,8 +1205,9 @@ hipError_t launch_top(const TopCall& c) {
   }
   if (c.top.K <= kFewest && r.V >= X::kPer) { BEST(2, 4) BEST(4, 4) BEST(8, 4) BEST(16, 4) BEST(32, 4) }
 #undef BEST
+  // (K steps for 64 / lanes rows: 21846 rows of 285 values, K = 171, took 197 us, and 125 by top_kernel)
 #define SHORT(lanes)                                                                                          \
-  if (chunks <= lanes) {                                                                                      \
+  if (chunks <= lanes && (c.top.K * lanes <= kShortSteps || r.V < X::kPer)) {                                  \
     short_kernel<X, kEntropy, lanes>                                                                          \
         <<<std::min(groups_of(rows, kTopThreads / lanes), kLaneGroups), kTopThreads, 0, c.stream>>>(r, c.out, c.top); \
     return hipGetLastError();                                                                                 \
@@ -1131,8 +1222,8 @@ hipError_t launch_top(const TopCall& c) {
   auto go = [&](auto kernel, int threads) {
     const int teams = threads <= kWave ? kTopThreads / threads : 1, waves = std::max(threads, kTopThreads * (teams > 1)) / kWave;
     // (not multiples of 32 keys: the parts begin at other banks)
-    const Room room = c.top.K < 256 ? Room{192, 258} : Room{256, kMostKeys};
-    static_assert(8 * kMostKeys > TB_TOP_MOST && 4 * kMostKeys > TB_TOP_MOST);
+    const Room room = c.top.K <= 128 ? Room{192, 258} : teams == 1 && c.top.K < 256 ? Room{192, 258} : Room{256, kMostKeys};
+    static_assert(4 * kMostKeys > TB_TOP_MOST);
     const size_t bytes = size_t(waves) * (room.keys * sizeof(uint64_t) + room.hits * kHitBytes);
     if (bytes > kPlainLds) {
       const hipError_t e = grant_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes);
@@ -1148,7 +1239,11 @@ hipError_t launch_top(const TopCall& c) {
 #define HELD(threads, n, step) \
   if (need(threads) <= n) return go(top_kernel<X, kEntropy, threads, n, step>, threads);
   if (c.split.parts == 1) {
-    if (c.top.K <= 128) { HELD(64, 2, 2) HELD(64, 4, 2) HELD(64, 6, 2) HELD(64, 8, 2) }
+    // Rows of a wavefront: where the lanes' groups of chunks are less than twice the alternatives, so that what K of
+    // their largest reach lets most values through, the bound is that of the values themselves.
+    const int groups = std::min(whole, 4 * kWave);
+    split.by_values = 2 * c.top.K > groups;
+    if (c.top.K <= 128 || (c.top.K <= 256 && whole <= 4 * kWave)) { HELD(64, 2, 2) HELD(64, 4, 2) HELD(64, 6, 2) HELD(64, 8, 2) }
     HELD(256, 4, 2) HELD(256, 6, 2) HELD(256, 8, 2)
     // (one row of 50257 values takes 8.5 us by 512 threads and 9.6 by 256; 16384 rows 267 us and 223)
     if (c.top.K < 512 && rows >= kManyRows) { 

@@ -19,6 +19,7 @@ struct Split {  // of long rows; parts 1: none
   int parts;
   int tiles;      // of a part, that a workgroup takes one after the other
   int64_t first;  // part of the launch
+  int by_values;  // a wavefront's bound goes by its values, not by what lanes have the largest
 };
 struct TopGiven {
   const float4* state;

@@ -112,6 +112,27 @@ def test_many_rows(V, half):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [33, 130, 255, 285, 300, 511, 600, 635, 1000, 1023, 1100, 2000, 2047, 2512, 4000])
+def test_many_alternatives_of_short_rows(V, dtype):
+    """Every number of alternatives that the kernels for wavefronts tell apart, with ties and masked tokens."""
+    x, tokens, g = inputs(V, 3, 40, V, dtype)
+    x[0, 0] = x[0, 0].abs() * -1
+    x[0, 1] = (x[0, 1] * 0.5).round()
+    x[0, 2] = 3.0
+    x[0, 3, torch.randperm(V, generator=g)[: V - 20].to(DEV)] = -math.inf
+    x[0, 4] = torch.where(x[0, 4] > 1, x[0, 4], torch.full_like(x[0, 4], torch.finfo(dtype).min))
+    valid = torch.ones(3, 40, dtype=torch.bool)
+    for k in sorted({min(V, k) for k in (9, 16, 17, 32, 33, 64, 65, 100, 127, 128, 129, 192, 200, 255, 256, 257)}):
+        r = tb.top_logprobs(x, k)
+        _, _, ids, lps = plain.top(x, k, valid)
+        assert torch.equal(r.ids.cpu(), ids), (k, (r.ids.cpu() != ids).any(-1).nonzero()[:4].tolist())
+        got, want = r.logprobs.cpu().double(), lps.detach()
+        low = ~(want > -1e4)
+        assert torch.equal(low, ~(got > -1e4))
+        near(got.masked_fill(low, 0.0), want.masked_fill(low, 0.0), LP, k)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("V", [60, 500, 3000, 20011, 140000])
 def test_ties(V, dtype):
     """Equal logits are taken by their ids, 0 and -0 alike: few values, one value, values of both signs."""
