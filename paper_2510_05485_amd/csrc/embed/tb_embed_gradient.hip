@@ -261,7 +261,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Gradient c) {
       }
     }
   };
-  constexpr int kAhead = 16;
+  constexpr int kAhead = kFrom == kTokens ? 2 : 16;  // (kDirectMost positions are two for each lane)
   for (int64_t i = from; i < to; i += kAhead * kWave) {
     int token[kAhead];
     uint32_t position[kAhead];
