@@ -13,7 +13,7 @@ constexpr uint32_t kNan = 0x7FC00000u;
 template <typename X, int kLanes, bool kWide>
 __global__ __launch_bounds__(kThreads) void lookup_kernel(Rows r, int D, float scale) {
   using T = typename X::type;
-  constexpr int kTeams = kThreads / kLanes;
+  constexpr int kTeams = kThreads / kLanes, kAhead = kLanes < 64 ? 1 : 4;  // chunks of a lane under way
   const int lane = threadIdx.x % kLanes;
   const int64_t rows = int64_t(r.B) * r.T;
   for (int64_t at = int64_t(blockIdx.x) * kTeams + threadIdx.x / kLanes; at < rows; at += int64_t(gridDim.x) * kTeams) {
@@ -25,25 +25,33 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(Rows r, int D, float s
     const bool fits = id >= 0 && id < r.V;
     if (live && !fits && lane == 0 && r.status) atomicOr(r.status, TB_DEV_TOKEN_RANGE);
     const T* row = static_cast<const T*>(r.x) + (live && fits ? id : 0) * r.x_pos;
-    const float by = live && fits ? scale : 0.f, none = live && !fits ? __uint_as_float(kNan) : 0.f;
     const bool read = live && fits;
+    const float none = live && !fits ? __uint_as_float(kNan) : 0.f;
     if constexpr (kWide) {
       const int chunks = (D + X::kPer - 1) / X::kPer;
-      for (int c = lane; c < chunks; c += kLanes) {
-        const int i = min(c * X::kPer, D - X::kPer);
-        float v[X::kPer];
-        if (read) {
-          X::unpack(*reinterpret_cast<const u32x4_any*>(row + i), v);
+      for (int c = lane; c < chunks; c += kAhead * kLanes) {
+        u32x4 u[kAhead];
+        if (read)
 #pragma unroll
-          for (int j = 0; j < X::kPer; ++j) v[j] *= by;
-        } else {
+          for (int a = 0; a < kAhead; ++a)
+            u[a] = *reinterpret_cast<const u32x4_any*>(row + min((c + a * kLanes) * X::kPer, D - X::kPer));
 #pragma unroll
-          for (int j = 0; j < X::kPer; ++j) v[j] = none;
+        for (int a = 0; a < kAhead; ++a) {
+          if (a > 0 && c + a * kLanes >= chunks) break;
+          float v[X::kPer];
+          if (read) {
+            X::unpack(u[a], v);
+#pragma unroll
+            for (int j = 0; j < X::kPer; ++j) v[j] *= scale;
+          } else {
+#pragma unroll
+            for (int j = 0; j < X::kPer; ++j) v[j] = none;
+          }
+          *reinterpret_cast<u32x4_any*>(out + min((c + a * kLanes) * X::kPer, D - X::kPer)) = X::pack(v);
         }
-        *reinterpret_cast<u32x4_any*>(out + i) = X::pack(v);
       }
     } else {
-      if (lane < D) X::store(out + lane, read ? X::load(row + lane) * by : none);
+      if (lane < D) X::store(out + lane, read ? X::load(row + lane) * scale : none);
     }
   }
 }
