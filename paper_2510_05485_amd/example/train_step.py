@@ -1,11 +1,11 @@
 """A training loop around the scorer: sampled sequences are rewarded by their BLEU and a small policy
-learns from that, with every loss of `paper_2510_05485_amd.losses`.
+learns from that, with every loss of `paper_2510_05485_amd.losses`, from its embeddings on.
 
 Prompts are class numbers, and each class has a reference sequence.  The policy is a table of
 embeddings and a linear layer, so that the loop fits a page; a language model takes their place
 without a change to the calls.
 
-  distil   the policy follows a teacher's best logits (a teacher that is right most of the time)
+  distil   the policy follows a teacher's eight likeliest tokens (a teacher that is right most of the time)
   prefer   of two samples of a prompt the one with the higher BLEU is preferred
   reward   eight samples of a prompt compete: advantages are their BLEU against the group's mean
 
@@ -30,8 +30,8 @@ class Policy(torch.nn.Module):
 
     def forward(self, prompts):
         """Logits [B, T, V] of the answers' positions."""
-        x = torch.tanh(self.prompt(prompts).unsqueeze(1) * self.place.weight)
-        return self.head(x)
+        prompt = tb.embedding(self.prompt.weight, prompts)
+        return self.head(torch.tanh(prompt.unsqueeze(1) * self.place.weight))
 
 
 def sample(logits, generator):
@@ -72,14 +72,13 @@ def run(steps: int = 60, seed: int = 0, say=print):
 
     report("untrained")
 
-    # a teacher whose best logits hold the right token, at a wrong place in the order now and then
-    ids = torch.rand(CLASSES, T, V, generator=gen, device=DEVICE).topk(8).indices
-    ids[..., 0] = references
-    best = torch.sort(torch.randn(CLASSES, T, 8, generator=gen, device=DEVICE), descending=True).values
-    best[..., 0] += torch.where(torch.rand(CLASSES, T, generator=gen, device=DEVICE) < 0.7, 2.0, -1.0)
+    # a teacher that has the right token first, or among the others now and then
+    teacher = torch.randn(CLASSES, T, V, generator=gen, device=DEVICE)
+    right = torch.where(torch.rand(CLASSES, T, 1, generator=gen, device=DEVICE) < 0.7, 5.0, 1.0)
+    best = tb.top_logprobs(teacher.scatter(-1, references.unsqueeze(-1), right), 8, lengths=lengths)
     for _ in range(steps):
         logits = policy(every)
-        r = tb.distillation_loss_grad(logits.detach(), ids, best, lengths=lengths)
+        r = tb.distillation_loss_grad(logits.detach(), best.ids, best.logprobs, lengths=lengths)
         update(logits, r.grad)
     report("distilled")
 

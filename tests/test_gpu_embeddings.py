@@ -310,6 +310,37 @@ def test_saved_tensor_hooks_and_changed_ids():
         out.sum().backward()
 
 
+def test_two_streams_at_once():
+    """Gradients of the same rows on several streams at the same time."""
+    _, tokens, rows, _ = inputs(8, 3, 30000, 4000, 40, torch.bfloat16)
+    want = tb.embedding_grad(rows, tokens, 4000), tb.embedding_grad(rows[:, :500], tokens[:, :500], 4000)
+    torch.cuda.synchronize()
+    streams, found = [torch.cuda.Stream() for _ in range(3)], []
+    for i in range(9):
+        with torch.cuda.stream(streams[i % 3]):
+            found.append((tb.embedding_grad(rows, tokens, 4000), tb.embedding_grad(rows[:, :500], tokens[:, :500], 4000)))
+    for s in streams:
+        torch.cuda.current_stream().wait_stream(s)
+    assert all(torch.equal(a, b) for calls in found for a, b in zip(calls, want))
+
+
+def test_wide_offsets():
+    """A table and a gradient whose last values lie beyond 2^31 (and their bytes beyond 2^32)."""
+    V, D = 280_000, 8192
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB of the GPU's memory")
+    table = torch.empty(V, D, dtype=torch.bfloat16, device=DEV)
+    g = torch.Generator().manual_seed(1)
+    tokens = torch.tensor([V - 1, 0, V - 2, V - 1, 262145, V - 1], device=DEV)
+    table[tokens] = torch.randn(6, D, generator=g).bfloat16().to(DEV)
+    out = tb.embedding(table, tokens)
+    assert torch.equal(out, table[tokens])
+    grad = tb.embedding_grad(out, tokens, V, out=table)           # (over the table: its rows are not needed any more)
+    rows, size, counts = plain.embedding_grad(out, torch.tensor([3, 0, 2, 3, 1, 3]), 4, torch.ones(6, dtype=torch.bool))
+    check_sums(grad[[0, 262145, V - 2, V - 1]], rows, size, counts)
+    assert not grad[1:262145].any() and not grad[262146:V - 2].any()
+
+
 @pytest.mark.parametrize("N,V,D", [(14, 50, 24), (900, 40000, 33), (70000, 300, 20)])
 def test_streams_and_graphs(N, V, D):
     """On a stream of its own; captured, forward and backward, and replayed with eager work between."""

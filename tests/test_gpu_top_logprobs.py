@@ -381,6 +381,25 @@ def test_alternatives_teach():
             near(tb.distillation_loss_grad(x, best.ids, best.logprobs, lengths=lengths).row_loss, torch.zeros(3, 4).double(), 2 * LP)
 
 
+def test_two_streams_at_once():
+    """Calls that share nothing but the logits, on two streams at the same time, and results that are read on a third."""
+    x, tokens, _ = inputs(9, 4, 300, 50257, torch.bfloat16)
+    few = x[:1, :3].clone()
+    big = torch.randn(2, 1, 400000, device=DEV)
+    want = tb.top_logprobs(x, 20, tokens, want_entropy=True), tb.top_logprobs(few, 300), tb.top_logprobs(big, 9)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    found = []
+    for i in range(9):
+        with torch.cuda.stream(streams[i % 3]):
+            found.append((tb.top_logprobs(x, 20, tokens, want_entropy=True), tb.top_logprobs(few, 300), tb.top_logprobs(big, 9)))
+    for s in streams:
+        torch.cuda.current_stream().wait_stream(s)
+    for calls in found:
+        for got, ref_ in zip(calls, want):
+            assert all(a is b or torch.equal(a, b) for a, b in zip(got, ref_))
+
+
 def test_wrong_tokens_and_lengths():
     x, tokens, _ = inputs(3, 2, 3, 5000)
     status = torch.zeros(1, dtype=torch.int32, device=DEV)
@@ -464,10 +483,10 @@ def test_general_way_and_hooks():
     assert not r.ids.requires_grad and r.logprobs.requires_grad and r.token_logprobs.requires_grad and r.entropy is None
 
 
-@pytest.mark.parametrize("V", [64, 700, 9001, 300000])
-def test_streams_graphs_and_order(V):
+@pytest.mark.parametrize("V,k", [(64, 9), (700, 9), (700, 200), (9001, 9), (50257, 300), (300000, 9)])
+def test_streams_graphs_and_order(V, k):
     """On a stream of its own; captured and replayed with eager work between; the same bits every time."""
-    k, T = 9, 7
+    T = 7
     x, tokens, g = inputs(V, 2, T, V, torch.bfloat16)
     others = [inputs(V + i, 2, T, V, torch.bfloat16)[0] for i in (1, 2, 3)]
     eager = [tb.top_logprobs(y, k, tokens, want_entropy=True) for y in others]
