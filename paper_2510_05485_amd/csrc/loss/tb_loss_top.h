@@ -556,7 +556,7 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
     const int token = r.tokens && part == 0 ? take_token(r, b, t, first) : -1;
     float x = __uint_as_float(kNan);
     const int need = (q.K + kWaves - 1) / kWaves, tiles = kTiled ? split.tiles : 1;
-    int found = 0, bound = O::kNone + 1;
+    int found = 0, bound = O::kNone + 1, turn = 0;
     bool much = false;
     Stats s = {};
     uint64_t* own = keys + wave * room.keys;
@@ -570,18 +570,11 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
     for (int tile = 0; tile < tiles; ++tile) {
       const int start = start_of(tile);
       const typename H::Row row = tile_of(tile);
-      // Raw bits as signed integers are in the values' order from 0 on, with all others below: they do as long as
-      // the bound is above 0.
-      int most[H::kParts], edge_order = O::raw(h.edge);
-      h.largest(most, edge_order);
-      int least = wave_bound<X>(most, need);
       const Stats mine = taken_stats<kEntropy>(h, k);
       s = tile ? joined_scaled<kEntropy>(s, mine, k) : mine;
-      int listed = O::kNone;
-      if (kTiled && tile) listed = list_bound<X>(own, found, need);
       // the workgroup's bound: what all wavefronts have `need` values from
+      int least;
       auto shared_bound = [&](int turn) {
-        if constexpr (kTiled) least = max(least, listed);
         if constexpr (kAlone) {
           if (lane == 0) shared.bounds[turn][wave] = least;
           __syncthreads();
@@ -589,24 +582,23 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
         }
         bound = max(bound, least);
       };
-      if (least < 1) least = O::kNone;
-      bool ordered = false;
-      if constexpr (!kAlone)
-        if (split.by_values) {
-          h.to_order();
-          edge_order = O::of(h.edge);
-          least = max(h.value_bound(edge_order, need), O::kNone);
-          ordered = true;
+      // Raw bits as signed integers are in the values' order from 0 on, with all others below: they do as long as
+      // the bound is above 0.
+      int most[H::kParts], edge_order = O::raw(h.edge);
+      bool by_values = false;
+      if constexpr (!kAlone) by_values = split.by_values;
+      if (tile == 0) {
+        if (!by_values) {
+          h.largest(most, edge_order);
+          least = wave_bound<X>(most, need);
+          if (least < 1) least = O::kNone;
+          shared_bound(0);
         }
-      shared_bound(tile % 2);
-      if (bound < 1 && !ordered) {
-        h.to_order();
-        edge_order = O::of(h.edge);
-        h.largest(most, edge_order);
-        least = wave_bound<X>(most, need);
-        shared_bound(2 + tile % 2);
-      }
-      if (kTiled && tile) {  // (keys below the bound are not needed any more)
+      } else {
+        // a new bound from what has been found: all tiles together find about K log(tiles) candidates
+        least = list_bound<X>(own, found, need);
+        shared_bound(2 + turn);
+        turn ^= 1;
         int kept = 0;
         for (int i = 0; i < found; i += kWave) {
           const uint64_t key = i + lane < found ? own[i + lane] : 0;
@@ -619,9 +611,33 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
         found = kept;
         meet<kWave>();
       }
+      if (bound < 1) {
+        h.to_order();
+        edge_order = O::of(h.edge);
+        if (tile == 0) {
+          if (by_values) {
+            least = h.value_bound(edge_order, need);
+          } else {
+            h.largest(most, edge_order);
+            least = wave_bound<X>(most, need);
+          }
+          shared_bound(1);
+        }
+      }
       // The values from the bound on, as keys in LDS, a part for each wavefront: first the chunks that have some,
       // with one lane storing all of its chunk, then each value of these.
-      int hits = h.hits(row, thread, bound, chunks, places, room.hits);
+      int from_here = bound;
+      int hits = h.hits(row, thread, from_here, chunks, places, room.hits);
+      if (kTiled && tile > 0 && hits > room.hits / 2) {
+        // more than the tiles before let expect (rising values): no wavefront needs more than its own K largest
+        h.largest(most, edge_order);
+        const int local = wave_bound<X>(most, q.K);
+        if (local > from_here) {
+          from_here = local;
+          meet<kWave>();
+          hits = h.hits(row, thread, from_here, chunks, places, room.hits);
+        }
+      }
       const int edge_at = h.edge_at;
       if (kTiled && tile + 1 < tiles) h.load(tile_of(tile + 1), thread);
       meet<kWave>();
@@ -637,9 +653,9 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
         const int hit = e + lane / X::kPer, i = lane % X::kPer;
         const bool there = hit < hits;
         const int order = there ? O::in_chunk(chunks + hit, i) : O::kNone, place = there ? places[hit] + i : 0;
-        take(there && order >= bound, order, place);
+        take(there && order >= from_here, order, place);
       }
-      if (__any(edge_order >= bound)) take(edge_order >= bound, edge_order, edge_at);
+      if (__any(edge_order >= from_here)) take(edge_order >= from_here, edge_order, edge_at);
       much = much || found > room.keys;
       found = min(found, room.keys);
       meet<kWave>();
@@ -1256,7 +1272,7 @@ hipError_t launch_top(const TopCall& c) {
   }
 #undef HELD
   // tiles that differ by up to 64 values
-  constexpr int kTileThreads = 256, kTile = 24;
+  constexpr int kTileThreads = 256, kTile = 24;  // (as many chunks as leave registers for three workgroups a unit)
   split.tiles = (whole + kTile * kTileThreads - 1) / (kTile * kTileThreads);
   auto chunks_of = [&] { return (whole / split.tiles + 64 / X::kPer + 2 + kTileThreads - 1) / kTileThreads; };  // the longest's
   if (chunks_of() > kTile) ++split.tiles;
