@@ -60,7 +60,8 @@ def test_workspace(lib):
                 assert b == n(1, rows, V, D)
                 slices = rows / 256
                 assert b >= 8 * rows + (8 * slices * D if rows > 256 else 0)
-                assert b <= (1 << 20) + 16 * rows + 8 * D * (rows / 16 + 1) + (4 << 11) * (rows / 4096 + 2)
+                # tokens, entries twice, slices' partial sums, and the parts' counts of up to 2048 digits
+                assert b <= (1 << 20) + 21 * rows + 8 * D * (rows / 16 + 1) + (4 << 11) * (rows / 2048 + 2)
 
 
 def test_lookup_arguments(lib):
