@@ -282,8 +282,13 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Gradient c) {
       if (!kParted) below += token[a] >= 0 && d < digit;
       const uint64_t mask = __ballot(mine);
       if (mask == 0) continue;
+      // (lanes with the first one's token are counted together: 64 additions to one place of LDS take as many turns, and
+      // 200000 positions of one token took 494 us so)
+      const int row = mine ? row_in(c.by, token[a]) : -1, leader = __ffsll(static_cast<unsigned long long>(mask)) - 1;
+      const int row0 = __builtin_amdgcn_readlane(row, leader);
+      const uint64_t alike = __ballot(row == row0);
       if (mine) {
-        atomicAdd(&next[wave * buckets + row_in(c.by, token[a])], 1);
+        if (row != row0 || lane == leader) atomicAdd(&next[wave * buckets + row], row != row0 ? 1 : __popcll(alike));
         const int slot = seen + lanes_before(mask);
         if (slot < kListed) listed[wave][slot] = {uint32_t(token[a]), position[a]};
       }
@@ -354,11 +359,23 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Gradient c) {
     }
     return;
   }
-  for (int64_t i = from; i < to; i += kWave) {
-    int token[1];
-    uint32_t position[1];
-    entries(i + lane, std::integral_constant<int, 1>(), token, position, false);
-    place(token[0] >= 0 && digit_of(c.by, token[0]) == digit ? token[0] : -1, position[0]);
+  constexpr int kAgain = 8;
+  for (int64_t i = from; i < to; i += kAgain * kWave) {
+    int token[kAgain];
+    uint32_t position[kAgain];
+    entries(i + lane, std::integral_constant<int, kAgain>(), token, position, false);
+#pragma unroll 1
+    for (int a = 0; a < kAgain; ++a) {
+      int t = -1;
+      uint32_t p = 0;
+#pragma unroll
+      for (int j = 0; j < kAgain; ++j)
+        if (j == a) {
+          t = token[j];
+          p = position[j];
+        }
+      place(t >= 0 && digit_of(c.by, t) == digit ? t : -1, p);
+    }
   }
 }
 

@@ -381,7 +381,7 @@ __device__ __forceinline__ void sort_list(uint64_t* own, int found) {
     }
 }
 
-// take(order, place) for each of a thread's values of a row, read from memory; some threads may call it less often.
+// take(order, place) for each of a thread's values of a row, read from memory.
 template <typename X, int kThreads, typename Row, typename Take>
 __device__ __forceinline__ void sweep_orders(const Row& row, int thread, Take take) {
   using O = Order<X>;
@@ -393,33 +393,46 @@ __device__ __forceinline__ void sweep_orders(const Row& row, int thread, Take ta
     const int at = row.at(c);
     O::each(u, [&](int i, int t) { take(t, at + i); });
   }
+#pragma unroll 1
   for (int j = thread; j < row.kEdge; j += kThreads) {
     const int e = row.edge(j);
     if (e >= 0) take(O::of(X::load(row.x + e)), e);
   }
 }
 
-// Statistics of a row from one sweep over it, as row_stats, with few registers: for rows that are rare.
+// Statistics of a row from one sweep over it, as row_stats, with few registers: rows whose reference is out of range, as
+// where a mask of -inf leaves some of a wavefront's part, all below 0.
 template <typename X, bool kEntropy, int kThreads, typename Row>
 __device__ __forceinline__ Stats swept_stats(const Row& row, float k, int thread, Stats* parts) {
   Stats mine = {kLowest, 0.f, 0.f};
-  auto take = [&](float v) { mine = joined<kEntropy>(mine, v == -INFINITY ? Stats{kLowest, 0.f, 0.f} : Stats{v, v == v ? 1.f : v, 0.f}, k); };
+  auto take = [&](const float* v, auto count) {
+    constexpr int n = decltype(count)::value;
+    float top = mine.m;
+#pragma unroll
+    for (int i = 0; i < n; ++i) top = fmaxf(top, v[i]);
+    const float d = (mine.m - top) * k, e = exp2_fast(d);
+    mine.t = kEntropy ? e * (mine.t + finite(d) * mine.s) : 0.f;
+    mine.s *= e;
+    mine.m = top;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float a = (v[i] - top) * k, w = exp2_fast(a);
+      mine.s += w;
+      if (kEntropy) mine.t += w * finite(a);
+    }
+  };
 #pragma unroll 1
   for (int c = thread; c < row.chunks; c += kThreads) {
     float v[X::kPer];
     X::unpack(row.chunk(c), v);
-#pragma unroll 1
-    for (int i = 0; i < X::kPer; ++i) {
-      float one = v[0];
-#pragma unroll
-      for (int j = 1; j < X::kPer; ++j) one = j == i ? v[j] : one;
-      take(one);
-    }
+    take(v, std::integral_constant<int, X::kPer>());
   }
 #pragma unroll 1
   for (int j = thread; j < row.kEdge; j += kThreads) {
     const int e = row.edge(j);
-    if (e >= 0) take(X::load(row.x + e));
+    if (e < 0) continue;
+    const float v[1] = {X::load(row.x + e)};
+    take(v, std::integral_constant<int, 1>());
   }
   mine = joined_lanes<kEntropy, kWave>(mine, [k](const Stats& a, const Stats& b) { return joined<kEntropy>(a, b, k); });
   if constexpr (kThreads <= kWave) return mine;
@@ -430,72 +443,139 @@ __device__ __forceinline__ Stats swept_stats(const Row& row, float k, int thread
   return all;
 }
 
-// Where the values that a bound lets through are too many (ties, masks of the lowest value, a few places that have
-// all large values): the K-th value itself and up to which place its equals are taken, by halving; about 40 sweeps over
-// the row, which comes from the caches.  Then keys of the K, in any order, from own[0] on in the order of wavefronts: how
-//many are there.
+// Where the values that a bound lets through are too many: keys of the K before all others, in any order, from keys[0] on;
+// returns how many there are.  Ties and masks of the lowest value, where the smallest of these values has less than K
+// above it, take two sweeps over the row, which comes from the caches; others (large values all in one place) as many more
+// as it takes to find the K-th value by quarters, 8 or 16.
 template <typename X, int kThreads, typename Row, typename Shared>
-__device__ __forceinline__ int exact_keys(const Row& row, int thread, int K, int V, int from, Shared& shared, uint64_t* keys) {
+__device__ __forceinline__ int exact_keys(const Row& row, int thread, int K, int from, int bound, Shared& shared, uint64_t* keys) {
   using O = Order<X>;
-  const int wave = thread / kWave;
+  constexpr int kWaves = kThreads > kWave ? kThreads / kWave : 1;
+  const int wave = thread / kWave, lane = thread % kWave;
   int turn = 0;
-  auto count = [&](auto holds) {
-    int n = 0;
-    sweep_orders<X, kThreads>(row, thread, [&](int t, int at) { n += holds(t, at); });
-    n = full_wave_sum(n);
+  // over all threads
+  auto over_all = [&](int v, auto join) {
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) v = join(v, __shfl_xor(v, d));
     if constexpr (kThreads > kWave) {
       turn ^= 1;
-      if (thread % kWave == 0) shared.counted[turn][wave] = n;
+      if (lane == 0) shared.counted[turn][wave] = v;
       __syncthreads();
-      n = 0;
-      for (int w = 0; w < kThreads / kWave; ++w) n += shared.counted[turn][w];
+      v = shared.counted[turn][0];
+      for (int w = 1; w < kWaves; ++w) v = join(v, shared.counted[turn][w]);
     }
-    return n;
+    return v;
   };
-  // the largest b that K values reach, above -inf
-  int64_t low = O::kNone + 1, high = int64_t(O::kMost) + 1;
-  while (high - low > 1) {
-    const int mid = int((low + high) >> 1);
-    if (count([mid](int t, int) { return t >= mid; }) >= K) low = mid;
-    else high = mid;
-  }
-  const int b = int(low), above = count([b](int t, int) { return t > b; });
-  // the first place before which there are enough of its equals (all of them: fewer finite values than K)
-  int64_t none = 0, enough = V;
-  while (enough - none > 1) {
-    const int mid = int((none + enough) >> 1);
-    if (count([b, mid](int t, int at) { return t == b && at < mid; }) >= K - above) enough = mid;
-    else none = mid;
-  }
-  const int before = int(enough);
-  auto taken = [b, before](int t, int at) { return t > b || (t == b && at < before); };
-  int mine = 0;
-  sweep_orders<X, kThreads>(row, thread, [&](int t, int at) { mine += taken(t, at); });
-  // each thread's keys behind those of the threads before
-  int slot = mine;
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const int v = __shfl_up(slot, d);
-    if (thread % kWave >= d) slot += v;
-  }
-  int total = __shfl(slot, kWave - 1);
-  slot -= mine;
-  if constexpr (kThreads > kWave) {
-    turn ^= 1;
-    if (thread % kWave == 0) shared.counted[turn][wave] = total;
-    __syncthreads();
-    total = 0;
-    for (int w = 0; w < kThreads / kWave; ++w) {
-      const int n = shared.counted[turn][w];
-      if (w < wave) slot += n;
-      total += n;
-    }
-  }
-  sweep_orders<X, kThreads>(row, thread, [&](int t, int at) {
-    if (taken(t, at)) keys[slot++] = key_of(t, from + at);
+  auto sum = [](int a, int b) { return a + b; };
+  int least = INT32_MAX, at_least = 0, count = 0;
+  sweep_orders<X, kThreads>(row, thread, [&](int t, int) {
+    if (t < bound) return;
+    ++count;
+    at_least = t < least ? 1 : at_least + (t == least);
+    least = min(least, t);
   });
-  if (thread == 0) keys[total] = 0;  // (read in pairs)
-  return total;
+  const int mine = least;
+  least = over_all(least, [](int a, int b) { return min(a, b); });
+  count = over_all(count, sum);
+  int above = count - over_all(mine == least ? at_least : 0, sum);
+  if (above >= K) {  // the K-th value: `least` is reached by K, `high` by `above` less than K
+    int64_t low = least, high = int64_t(O::kMost) + 1;
+    above = 0;
+    while (high - low > 1) {
+      const int64_t step = max((high - low) / 4, int64_t(1));
+      const int m0 = int(low + step), m1 = int(min(low + 2 * step, high - 1)), m2 = int(min(low + 3 * step, high - 1));
+      int n0 = 0, n1 = 0, n2 = 0;
+      sweep_orders<X, kThreads>(row, thread, [&](int t, int) {
+        n0 += t >= m0;
+        n1 += t >= m1;
+        n2 += t >= m2;
+      });
+      n0 = over_all(n0, sum);
+      n1 = over_all(n1, sum);
+      n2 = over_all(n2, sum);
+      if (n2 >= K) {
+        low = m2;
+      } else if (n1 >= K) {
+        low = m1;
+        high = m2;
+        above = n2;
+      } else if (n0 >= K) {
+        low = m0;
+        high = m1;
+        above = n1;
+      } else {
+        high = m0;
+        above = n0;
+      }
+    }
+    least = int(low);
+  }
+  // those above it, and of its equals the first ones: their numbers among all threads' values in the order of places
+  int equals = K - above, slots = 0;
+  auto take = [&](const int* t, int n, int at) {
+    int larger = 0, same = 0;
+    for (int i = 0; i < n; ++i) {
+      larger += t[i] > least;
+      same += t[i] == least;
+    }
+    int before = same << 16 | larger;  // (both at once: 4096 values at most)
+    const int own = before;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+      const int v = __shfl_up(before, d);
+      if (lane >= d) before += v;
+    }
+    int all = __shfl(before, kWave - 1);
+    before -= own;
+    if constexpr (kThreads > kWave) {
+      turn ^= 1;
+      if (lane == 0) shared.counted[turn][wave] = all;
+      __syncthreads();
+      all = 0;
+      for (int w = 0; w < kWaves; ++w) {
+        const int v = shared.counted[turn][w];
+        if (w < wave) before += v;
+        all += v;
+      }
+    }
+    // (the larger ones first, then as many of the equals as are wanted still)
+    const int taken = min(all >> 16, equals);
+    int to = slots + (before & 0xFFFF), rank = before >> 16;
+    const int equal_slots = slots + (all & 0xFFFF);
+    for (int i = 0; i < n; ++i) {
+      if (t[i] > least) keys[to++] = key_of(t[i], from + at + i);
+      if (t[i] == least) {
+        if (rank < taken) keys[equal_slots + rank] = key_of(t[i], from + at + i);
+        ++rank;
+      }
+    }
+    equals -= taken;
+    slots = equal_slots + taken;
+  };
+  // (a thread's values of the row's head, then of its chunks, then of what is behind these)
+  const int none = INT32_MIN;
+  {
+    const int t[1] = {thread < row.head ? O::of(X::load(row.x + thread)) : none};
+    take(t, 1, thread);
+  }
+#pragma unroll 1
+  for (int c = 0; c < row.chunks; c += kThreads) {
+    int t[X::kPer];
+    const bool there = c + thread < row.chunks;
+    u32x4 u = {};
+    if (there) u = row.chunk(c + thread);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = O::of_packed(u[i]);
+    O::each(u, [&](int i, int order) { t[i] = there ? order : none; });
+    take(t, X::kPer, row.at(c + thread));
+  }
+  {
+    const int e = row.head + row.chunks * X::kPer + thread;
+    const int t[1] = {e < row.V ? O::of(X::load(row.x + e)) : none};
+    take(t, 1, e);
+  }
+  if (thread == 0) keys[slots] = 0;  // (read in pairs)
+  return slots;
 }
 
 // Joined parts of a row, of weights 2^((x - m) k) (apart), for parts that a kernel after this one joins.
@@ -696,7 +776,7 @@ __global__ __launch_bounds__(kThreads <= kWave ? kTopThreads : kThreads) void to
     if (none) total = found = 0;
     else if (much) {
       meet<kThreads>();
-      total = exact_keys<X, kThreads>(row, thread, q.K, V, from, shared, keys);  // (in the first wavefronts' parts)
+      total = exact_keys<X, kThreads>(row, thread, q.K, from, bound, shared, keys);  // (in the first wavefronts' parts)
       found = kAlone ? max(min(total - wave * room.keys, room.keys), 0) : total;
       if (kAlone && lane == 0) shared.counts[wave] = found;
       meet<kThreads>();
