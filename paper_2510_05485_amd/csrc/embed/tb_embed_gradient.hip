@@ -514,12 +514,13 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(Gradient c, int tiles) {
   }
 }
 
+constexpr int kJoinThreads = 512;
 // A token that goes over the end of a slice, and a tile of its columns: the workgroup's teams add up the slices'
 // partial sums, a run of them each, and the first team what the teams have.
 template <typename X, typename Out, int kLanes, bool kWide>
-__global__ __launch_bounds__(kThreads) void join_kernel(Gradient c, int tiles) {
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(Gradient c, int tiles) {
   using C = Columns<X, kWide>;
-  constexpr int kTeams = kThreads / kLanes, kPer = C::kPer, kAhead = 4;
+  constexpr int kTeams = kJoinThreads / kLanes, kPer = C::kPer, kAhead = 8;
   __shared__ float sums[kTeams][kLanes * kPer];
   const int lane = threadIdx.x % kLanes, team = threadIdx.x / kLanes;
   const int64_t valid = *c.valid, slices = (valid + c.slice - 1) / c.slice;
@@ -588,7 +589,7 @@ hipError_t launch_sums(const Gradient& c) {
   sum_kernel<X, Out, kLanes, kWide><<<int(groups < kMostGroups ? groups : kMostGroups), kThreads, 0, c.stream>>>(c, tiles);
   if (c.slices > 1) {
     const int64_t joins = c.slices * tiles < 1024 ? c.slices * tiles : 1024;
-    join_kernel<X, Out, kLanes, kWide><<<int(joins), kThreads, 0, c.stream>>>(c, tiles);
+    join_kernel<X, Out, kLanes, kWide><<<int(joins), kJoinThreads, 0, c.stream>>>(c, tiles);
   }
   return hipGetLastError();
 }
