@@ -90,7 +90,9 @@ def test_values_and_gradient(D, dtype):
                                      (5, 333, 1000, 129), (16, 256, 32000, 33), (3, 1000, 2, 600), (7, 2000, 5000, 16),
                                      (2, 40000, 64, 8), (5, 20000, 300, 5), (3, 30000, 50257, 12), (100, 700, 7, 70),
                                      (1, 131073, 1, 16), (4, 9, 262144, 8), (2, 33000, 262144, 4), (40000, 2, 700, 16),
-                                     (3, 5, 5_000_000, 4), (1, 70000, 5_000_000, 4)])
+                                     (3, 5, 5_000_000, 4), (1, 70000, 5_000_000, 4),
+                                     (300, 512, 64, 64), (90, 1000, 100, 37), (150, 500, 31, 131),
+                                     (2, 40000, 255, 16), (3, 30000, 16, 256), (1, 2_000_000, 3, 9), (66000, 2, 256, 8), (70, 1000, 1, 129)])
 def test_gradient(B, T, V, D, dtype, out):
     """One position to many, one token to many, tokens with one position to all: tokens inside a slice, over the end
     of one, over many slices."""
