@@ -10,6 +10,7 @@
 #include <torch/csrc/autograd/saved_variable.h>
 #include <ATen/ATen.h>
 
+#include "../tb_py_capture.h"
 #include "tensorembed.h"
 
 namespace {
@@ -134,6 +135,7 @@ struct EmbeddingBackward : public torch::autograd::Node {
   torch::autograd::variable_list apply(torch::autograd::variable_list&& in) override {
     std::lock_guard<std::mutex> lock(mutex_);
     TORCH_CHECK(!at::GradMode::is_enabled(), "the embedding cannot be differentiated twice");
+    TORCH_CHECK(!tb::leaves_capture(next_edges()), tb::kLeavesCapture);
     if (!in[0].defined()) return {at::Tensor()};
     at::Tensor ids = tokens.unpack(), n = lengths.unpack(), m = mask.unpack(), rows = in[0];
     if (ids.defined() && ids.dim() > 0 && ids.size(-1) > 1 && ids.stride(-1) != 1) ids = ids.contiguous();

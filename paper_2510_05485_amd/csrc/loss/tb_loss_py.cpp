@@ -8,10 +8,12 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/function.h>
 #include <torch/csrc/autograd/functions/utils.h>
+#include <torch/csrc/autograd/python_cpp_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/autograd/saved_variable.h>
 #include <ATen/ATen.h>
 
+#include "../tb_py_capture.h"
 #include "tensorloss.h"
 
 namespace {
@@ -271,6 +273,7 @@ struct TopBackward : public torch::autograd::Node {
   torch::autograd::variable_list apply(torch::autograd::variable_list&& in) override {
     std::lock_guard<std::mutex> lock(mutex_);
     TORCH_CHECK(!at::GradMode::is_enabled(), "the losses over logits cannot be differentiated twice");
+    TORCH_CHECK(!tb::leaves_capture(next_edges()), tb::kLeavesCapture);
     const size_t of_tokens = 1, of_entropy = 1 + tokens_too;
     bool any = false;
     for (const at::Tensor& d : in) any = any || d.defined();
@@ -558,7 +561,15 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// leaves_capture(function): whether a captured backward pass would go on to this next function outside the capture
+PyObject* leaves_capture(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != 1 || !torch::autograd::THPCppFunction_Check(args[0])) Py_RETURN_FALSE;
+  const auto* function = reinterpret_cast<torch::autograd::THPCppFunction*>(args[0]);
+  return PyBool_FromLong(tb::leaves_capture(function->cdata.get()));
+}
+
 PyMethodDef methods[] = {
+    {"leaves_capture", reinterpret_cast<PyCFunction>(guarded<leaves_capture>), METH_FASTCALL, nullptr},
     {"logprobs", reinterpret_cast<PyCFunction>(guarded<logprobs>), METH_FASTCALL, nullptr},
     {"top", reinterpret_cast<PyCFunction>(guarded<top>), METH_FASTCALL, nullptr},
     {"policy", reinterpret_cast<PyCFunction>(guarded<policy>), METH_FASTCALL, nullptr},

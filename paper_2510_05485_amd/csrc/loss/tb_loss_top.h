@@ -13,10 +13,11 @@
 //   join_kernel   joins the parts of long rows, where there are few
 //
 // Long rows are bound by HBM and, with entropies, by the vector units alike: about 9 instructions a value, an exponential
-// counted as four of them.  On one MI355X, among other calls: 3072 rows of 32000 values in bfloat16, K = 64, 47 us (4.2
-// TB/s); 10240 of 50257, K = 20, with entropies 204 us (5.1; 79 % of the vector units' time); 1842 of 262144 in float16,
-// K = 256, 248 us (3.9); 3884 of 50257 in float32, K = 20, with entropies 190 us (4.1); 1113000 of 64, K = 5, 95 us (2.9;
-// the exchanges of the sorted chunks); one row of 50257 8.3 us, on one unit; four of 262144 in float32 12 us, two launches.
+// counted as four of them.  On one MI355X, among other calls: 16 x 256 rows (three in four of which count) of 32000
+// values in bfloat16, K = 64, 47 us (4.2 TB/s); 10240 of 50257, K = 20, with entropies 204 us (5.1; 79 % of the vector
+// units' time); 1842 of 262144 in float16, K = 256, 248 us (3.9); 3884 of 50257 in float32, K = 20, with
+// entropies 190 us (4.1); 1113000 of 64, K = 5, 95 us (2.9; the exchanges of the sorted chunks); one row of 50257 8.3 us,
+// on one unit; four of 262144 in float32 12 us, two launches.
 #pragma once
 
 #include "tb_loss_rows.h"
@@ -1349,7 +1350,7 @@ hipError_t launch_top(const TopCall& c) {
     if (c.top.K <= 128 || (c.top.K <= 256 && whole <= 4 * kWave)) { HELD(64, 2, 2) HELD(64, 4, 2) HELD(64, 6, 2) HELD(64, 8, 2) }
     HELD(256, 4, 2) HELD(256, 6, 2) HELD(256, 8, 2)
     // (one row of 50257 values takes 8.5 us by 512 threads and 9.6 by 256; 16384 rows 267 us and 223)
-    if (c.top.K < 512 && rows >= kManyRows) { 
+    if (c.top.K < 512 && rows >= kManyRows) {
       HELD(256, 10, 2) HELD(256, 12, 2) HELD(256, 14, 2) HELD(256, 16, 2) HELD(256, 18, 2) HELD(256, 20, 2) HELD(256, 22, 2)
       HELD(256, 24, 2) HELD(256, 26, 2)
     }

@@ -13,8 +13,9 @@ Common arguments
 
 What stands at positions that do not count has no part in anything; their embeddings are 0.  A table's gradient is
 summed in float32 in an order that does not change from call to call.  Gradients are for reverse mode, and of first
-order; tables with a forward-mode tangent are refused.  Everything runs on the current stream of the table's (or rows')
-GPU, and nothing synchronises.  See include/tensorembed.h.
+order; tables with a forward-mode tangent are refused, and so is a backward pass that is captured into a graph while an
+eager graph holds the same table.  Everything runs on the current stream of the table's (or rows') GPU, and nothing
+synchronises.  See include/tensorembed.h.
 """
 from __future__ import annotations
 
@@ -25,7 +26,7 @@ import torch
 
 from . import binding as _b
 from .binding import TensorBLEUError
-from .losses import TYPES, tb_positions_t
+from .losses import TYPES, _stay_in_capture, tb_positions_t
 
 WIDTH_MOST = 1 << 20
 
@@ -197,6 +198,7 @@ class _Embedding(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_rows):
+        _stay_in_capture(ctx)
         tokens, lengths, mask = ctx.saved_tensors
         (V, D), dtype = ctx.table
         rows = _values(d_rows.to(dtype), (2, 3), "the embeddings' gradient")
@@ -246,7 +248,7 @@ def embedding_grad(rows, tokens, V: int, *, scale: float = 1.0, lengths=None, ma
     if out.dtype != kind or tuple(out.shape) != shape or (shape[1] > 1 and out.stride(-1) != 1):
         raise TensorBLEUError(f"out must be {kind} of shape {shape} with consecutive values in a row "
                               f"(got {out.dtype} {tuple(out.shape)})")
-    if out.requires_grad and out.is_leaf and torch.is_grad_enabled():
+    if out.requires_grad and torch.is_grad_enabled():
         raise TensorBLEUError("out must not require a gradient")
     _gradient(rows, tokens, V, lengths, mask, scale, out.detach(), bool(accumulate), status)
     if not out.is_inference():

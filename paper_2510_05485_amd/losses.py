@@ -396,6 +396,13 @@ def _top(call, k, tokens, want_entropy, id_dtype, keep_state):
     return ids, values, lp, entropy, state
 
 
+def _stay_in_capture(ctx) -> None:
+    """Raises where a captured backward pass would leave the capture (as the native nodes do)."""
+    if torch.cuda.is_current_stream_capturing() and any(native().leaves_capture(f) for f, _ in ctx.next_functions):
+        raise RuntimeError("a backward pass is being captured while a graph from outside the capture holds the same "
+                           "leaf: let go of that graph (or capture with a detached leaf)")
+
+
 class _TopLogprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, k, tokens, lengths, mask, temperature, want_entropy, id_dtype, status):
@@ -410,6 +417,7 @@ class _TopLogprobs(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, _, d_top, d_lp, d_entropy):
+        _stay_in_capture(ctx)
         none = (None,) * 8
         if d_top is None and d_lp is None and d_entropy is None:
             return (None, *none)
@@ -434,7 +442,8 @@ def top_logprobs(logits, k: int, tokens=None, *, lengths=None, mask=None, temper
                  status: Optional[torch.Tensor] = None) -> TopLogprobs:
     """The k likeliest tokens of every position with their log-probabilities, in descending order, equal
     ones by their ids; with `tokens` their log-probabilities beside them, and with want_entropy the entropies
-    of the rows.  Log-probabilities and entropies are differentiable in the logits.
+    of the rows.  Log-probabilities and entropies are differentiable in the logits (a backward pass that is
+    captured into a graph while an eager graph holds the same leaf is refused).
 
     Tokens whose logit is -inf are none of the k: entries that are not there have the id -1 and the
     log-probability -inf, as at positions that do not count.  distillation_loss takes them so: ids and

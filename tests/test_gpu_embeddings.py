@@ -4,6 +4,7 @@ An embedding is a product in float32, rounded once: 2^-24 and half a step of the
 adds at most n numbers one after the other, and no more than 256 of a slice, then at most n / 16 + 130 sums of
 slices: each addition rounds by 2^-24 of a number that the sum of magnitudes bounds, and so do the product with the
 scale and an addition to what is there."""
+import gc
 import math
 
 import pytest
@@ -272,6 +273,7 @@ def test_refusals():
               lambda: tb.embedding_grad(rows, tokens, 10, accumulate=True),
               lambda: tb.embedding_grad(rows, tokens, 10, out=table[:9].clone()),
               lambda: tb.embedding_grad(rows, tokens, 10, out=table.clone().requires_grad_()),
+              lambda: tb.embedding_grad(rows, tokens, 10, out=table.clone().requires_grad_() * 2),
               lambda: tb.embedding_grad(rows.bfloat16(), tokens, 10, out=table.half()),
               lambda: tb.embedding_grad(rows, tokens, 6, out=rows.view(6, 8))):
         with pytest.raises(E):
@@ -370,3 +372,27 @@ def test_streams_and_graphs(N, V, D):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held, want))
+
+
+@pytest.mark.parametrize("lengths", [None, torch.int64])
+def test_a_capture_beside_an_eager_graph(lengths):
+    """A leaf that a graph from outside holds: the captured backward pass is refused; without that graph it runs."""
+    table, tokens, rows, _ = inputs(6, 2, 30, 50, 24, torch.float32)
+    leaf = table.clone().requires_grad_()
+    where = {} if lengths is None else dict(lengths=torch.tensor([30, 11], device=DEV, dtype=lengths))
+    held = tb.embedding(leaf, tokens, **where)
+    want, = torch.autograd.grad(held, leaf, rows, retain_graph=True)
+    torch.cuda.synchronize()
+    with pytest.raises(RuntimeError, match="outside the capture"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            torch.autograd.grad(tb.embedding(leaf, tokens, **where), leaf, rows)
+    del held
+    gc.collect()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got, = torch.autograd.grad(tb.embedding(leaf, tokens, **where), leaf, rows)
+    for _ in range(3):
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)

@@ -4,6 +4,7 @@ Ids have to be equal.  Log-probabilities and entropies are held to LP and H, whi
 derives for the same sums; gradients value by value to what tests/loss_bounds.py derives, a row's cotangents of
 K + 1 log-probabilities being as many terms of its softmax part: their sum, rounded K + 1 times at 2^-24 of its
 size, is within LP of the sum of their magnitudes for K up to 500, and of 2 LP for 1024."""
+import gc
 import math
 
 import pytest
@@ -517,3 +518,28 @@ def test_streams_graphs_and_order(V, k):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(p, q) for p, q in zip(held, want))
+
+
+@pytest.mark.parametrize("lengths", [None, torch.int64])
+def test_a_capture_beside_an_eager_graph(lengths):
+    """A leaf that a graph from outside holds: the captured backward pass is refused; without that graph it runs."""
+    x, tokens, _ = inputs(9, 2, 6, 700, torch.float32)
+    leaf = x.clone().requires_grad_()
+    where = {} if lengths is None else dict(lengths=torch.tensor([6, 2], device=DEV, dtype=lengths))
+    f = lambda: tb.top_logprobs(leaf, 5, tokens, **where).token_logprobs.sum()
+    held = f()
+    want, = torch.autograd.grad(held, leaf, retain_graph=True)
+    torch.cuda.synchronize()
+    with pytest.raises(RuntimeError, match="outside the capture"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph()):
+            torch.autograd.grad(f(), leaf)
+    del held
+    gc.collect()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got, = torch.autograd.grad(f(), leaf)
+    for _ in range(3):
+        got.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
