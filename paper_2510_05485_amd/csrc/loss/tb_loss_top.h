@@ -1027,6 +1027,48 @@ __device__ __forceinline__ void merge_lanes(Key* v) {
   }
 }
 
+// A key into the descending list `v`, of which kFilled are there, when kBefore of these are known to be larger: an
+// instruction a place.
+template <int kKeep, int kFilled, int kBefore = 0>
+__device__ __forceinline__ void insert_key(uint32_t* v, uint32_t key) {
+  uint32_t old[kKeep];
+#pragma unroll
+  for (int i = 0; i < kKeep; ++i) old[i] = v[i];
+#pragma unroll
+  for (int i = kBefore; i < kKeep; ++i) {
+    if (i > kFilled) break;
+    if (i == kFilled) v[i] = i == kBefore ? key : min(old[i - 1], key);
+    else if (i == kBefore) v[i] = max(old[i], key);
+    else v[i] = max(min(key, old[i]), min(max(key, old[i]), old[i - 1]));  // (the median of three)
+  }
+}
+template <int kKeep, int kI = 0>
+__device__ __forceinline__ void insert_keys(uint32_t* v, const uint32_t* keys, bool first) {
+  if constexpr (kI < 8) {
+    if (first) insert_key<kKeep, kI < kKeep ? kI : kKeep>(v, keys[kI]);
+    else insert_key<kKeep, kKeep>(v, keys[kI]);
+    insert_keys<kKeep, kI + 1>(v, keys, first);
+  }
+}
+// Two lists: the second one's places are known to be none before their own.
+template <int kKeep, int kI = 0>
+__device__ __forceinline__ void insert_list(uint32_t* v, const uint32_t* u) {
+  if constexpr (kI < kKeep) {
+    insert_key<kKeep, kKeep, kI>(v, u[kI]);
+    insert_list<kKeep, kI + 1>(v, u);
+  }
+}
+template <int kKeep, int kLanes, int kStep = 1>
+__device__ __forceinline__ void insert_lanes(uint32_t* v) {
+  if constexpr (kStep < kLanes) {
+    uint32_t u[kKeep];
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) u[i] = neighbour_key<kStep>(v[i]);
+    insert_list<kKeep>(v, u);
+    insert_lanes<kKeep, kLanes, kStep * 2>(v);
+  }
+}
+
 // Keys of short rows: in 32 bits with the place in the lower half where values have 16.
 template <typename X>
 struct ShortKey {
@@ -1063,29 +1105,41 @@ __device__ __forceinline__ uint32_t place_in_round(int64_t round) {
   return uint32_t((blockIdx.x + round) % gridDim.x);
 }
 
-// Up to eight alternatives of rows of up to 1024 values: each lane keeps the eight best of its chunks, sorted eight by
-// eight and merged, and so do the lanes with one another.  Few lanes with many chunks share what is done once a row.
+// Up to eight alternatives of rows of up to 1024 values: each lane keeps the best of its chunks, and the lanes join
+// theirs.  Keys of 32 bits are inserted one by one into a list of kKeep, an instruction a place (a median of three);
+// 64-bit ones are sorted eight by eight and merged (as 32-bit ones were: 2097152 positions of 64 values, 53 % of
+// which count, K = 5, 95 us, and 79 so).  Few lanes with many chunks share what is done once a row.  Five workgroups a
+// unit: with 4 (116 registers) 85 us, with 6 (spills) 110.
 constexpr int kFewest = 8, kBestGroups = 5120, kShortSteps = 2048;
-template <typename X, bool kEntropy, int kLanes, int kChunks>
-__global__ __launch_bounds__(kTopThreads) void best_kernel(Rows r, RowOut o, Top q) {
+template <typename X, bool kEntropy, int kLanes, int kChunks, int kKeep>
+__global__ __launch_bounds__(kTopThreads, 5) void best_kernel(Rows r, RowOut o, Top q) {
   constexpr int kTeams = kTopThreads / kLanes, kOctet = 8 / X::kPer;  // chunks that are sorted together
-  static_assert(kChunks % kOctet == 0);
   using O = Order<X>;
   using Key = ShortKey<X>;
   using K = typename Key::type;
-  const int lane = threadIdx.x % kLanes;
+  constexpr bool kInsert = sizeof(K) == 4;
+  static_assert(kChunks % kOctet == 0 && (kInsert || kKeep == 8));
+  constexpr int kEntries = kWave / kLanes * kKeep;
+  __shared__ K all_entries[kTopThreads / kWave][kEntries];
+  __shared__ float2 all_found[kTopThreads / kWave][kWave / kLanes];
+  K* entries = all_entries[threadIdx.x / kWave];
+  float2* found = all_found[threadIdx.x / kWave];
+  const uint32_t per_entry = (65536u + q.K - 1) / q.K;  // (of a number below 256, the quotient by K is exact so)
   const int64_t rows = int64_t(r.B) * r.T;
   const float k = r.inv_temp * kLog2e;
   for (int64_t round = 0; round * gridDim.x * kTeams < rows; ++round) {
     int V = r.V;
     asm volatile("" : "+s"(V));  // (as in lanes_kernel)
-    const int64_t at = (round * gridDim.x + place_in_round(round)) * kTeams + threadIdx.x / kLanes;
+    int thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));
+    const int lane = thread % kLanes;
+    const int64_t at = (round * gridDim.x + place_in_round(round)) * kTeams + thread / kLanes;
     const bool inside = at < rows;
     const At pos = position(r, inside ? at : rows - 1);
     const int b = pos.b, t = pos.t;
     const bool live = inside && counts(r, b, t);
     if (inside && lane == 0 && t == 0 && r.lengths) held_length(r.lengths[b], r.T, r.status);
-    K best[8] = {};
+    K best[kKeep] = {};
     Found f = {0.f, 1.f, 0.f, false};
     float x = 0.f, log_s = 0.f;
     if (__any(live)) {
@@ -1108,16 +1162,21 @@ __global__ __launch_bounds__(kTopThreads) void best_kernel(Rows r, RowOut o, Top
           for (int i = 0; i < X::kPer; ++i)
             if (i < again) keys[h * X::kPer + i] = 0;
         }
-        sort_keys<K, 8>(keys);
-        if (j == 0) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) best[i] = keys[i];
+        if constexpr (kInsert) {
+          insert_keys<kKeep>(best, keys, j == 0);
         } else {
-          merge_keys(best, keys);
+          sort_keys<K, 8>(keys);
+          if (j == 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) best[i] = keys[i];
+          } else {
+            merge_keys(best, keys);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      merge_lanes<kLanes>(best);
+      if constexpr (kInsert) insert_lanes<kKeep, kLanes>(best);
+      else merge_lanes<kLanes>(best);
       part.keep_packed();
       // the best is the largest value, or the row has a NaN
       f.m = live ? O::value(Key::order(best[0])) : 0.f;
@@ -1144,18 +1203,34 @@ __global__ __launch_bounds__(kTopThreads) void best_kernel(Rows r, RowOut o, Top
       if (kEntropy) f.t = lanes_added<kLanes>(f.t);
       log_s = logf(f.s);
     }
-    // (stores of whole lines through LDS take as long)
     const bool none = lost(f);
+    const float missing = live && none ? __uint_as_float(kNan) : -INFINITY;
+    auto put = [&](int64_t to, K key, const Found& g, float log_sum, float otherwise) {
+      put_id(q, to, key ? Key::place(key) : -1);
+      q.logprobs[to] = key ? logprob(g, O::value(Key::order(key)), k, r.inv_temp, log_sum) : otherwise;
+    };
+    auto entry = [&](int j) { return live && !none && Key::order(best[j]) > O::kNone ? best[j] : 0; };
+    if constexpr (kKeep <= 2) {
 #pragma unroll
-    for (int j = 0; j < kFewest; ++j) {
-      if (j >= q.K) break;
-      if (j % kLanes != lane || !inside) continue;
-      const int order = Key::order(best[j]);
-      const bool there = live && !none && best[j] != 0 && order > O::kNone;
-      put_id(q, at * q.K + j, there ? Key::place(best[j]) : -1);
-      q.logprobs[at * q.K + j] = there          ? logprob(f, O::value(order), k, r.inv_temp, log_s)
-                                 : live && none ? __uint_as_float(kNan)
-                                                : -INFINITY;
+      for (int j = 0; j < kKeep; ++j)
+        if (inside && j < q.K && j % kLanes == lane) put(at * q.K + j, entry(j), f, log_s, missing);
+    } else {
+      // Through LDS, from where neighbouring lanes store neighbouring entries and work out their log-probabilities.
+      // (2097152 rows of 64 values of which none counts, all, K = 5: 32 and 101 us, and 51 and 110 with each entry stored by
+      // the lane that has it; K = 1: 23 and 78, and 20 and 74.)
+      const int own = thread % kWave / kLanes;
+      if (lane == 0) found[own] = {f.m, !live ? 0.f : none ? missing : log_s};
+#pragma unroll
+      for (int j = 0; j < kKeep; ++j)
+        if (j < q.K && j % kLanes == lane) entries[own * q.K + j] = entry(j);
+      meet<kWave>();
+      const int64_t first = at - own;
+      const int n = int(min(rows - first, int64_t(kWave / kLanes))) * q.K;
+      for (int i = thread % kWave; i < n; i += kWave) {
+        const float2 of = found[i * per_entry >> 16];
+        put(first * q.K + i, entries[i], {of.x, 0.f, 0.f, !scales(of.x, k)}, of.y, of.y != of.y ? of.y : -INFINITY);
+      }
+      meet<kWave>();
     }
     if (lane == 0 && live) put_values<kEntropy>(r, o, f, x, k, log_s, at);
     else if (lane == 0 && inside) leave_nothing(o, at);
@@ -1301,13 +1376,23 @@ hipError_t launch_top(const TopCall& c) {
     const int64_t groups = (units + at_a_time - 1) / at_a_time;
     return int(groups < kMostGroups ? groups : kMostGroups);
   };
-#define BEST(lanes, n)                                                                                        \
-  if (chunks <= lanes * n) {                                                                                  \
-    best_kernel<X, kEntropy, lanes, n>                                                                        \
-        <<<std::min(groups_of(rows, kTopThreads / lanes), kBestGroups), kTopThreads, 0, c.stream>>>(r, c.out, c.top); \
-    return hipGetLastError();                                                                                 \
+  // (lists no longer than they have to be, where their length is what keys cost)
+  auto best = [&](auto lanes, auto keep) {
+    constexpr int kLanes = decltype(lanes)::value;
+    const int groups = std::min(groups_of(rows, kTopThreads / kLanes), kBestGroups);
+    best_kernel<X, kEntropy, kLanes, 4, decltype(keep)::value><<<groups, kTopThreads, 0, c.stream>>>(r, c.out, c.top);
+    return hipGetLastError();
+  };
+#define BEST(lanes)                                                                          \
+  if (chunks <= lanes * 4) {                                                                 \
+    const std::integral_constant<int, lanes> n;                                              \
+    if constexpr (X::kPer == 8) {                                                            \
+      if (c.top.K <= 2) return best(n, std::integral_constant<int, 2>());                    \
+      if (c.top.K <= 5) return best(n, std::integral_constant<int, 5>());                    \
+    }                                                                                        \
+    return best(n, std::integral_constant<int, kFewest>());                                  \
   }
-  if (c.top.K <= kFewest && r.V >= X::kPer) { BEST(2, 4) BEST(4, 4) BEST(8, 4) BEST(16, 4) BEST(32, 4) }
+  if (c.top.K <= kFewest && r.V >= X::kPer) { BEST(2) BEST(4) BEST(8) BEST(16) BEST(32) }
 #undef BEST
   // (K steps for 64 / lanes rows: 21846 rows of 285 values, K = 171, took 197 us, and 125 by top_kernel)
 #define SHORT(lanes)                                                                                          \

@@ -543,3 +543,27 @@ def test_a_capture_beside_an_eager_graph(lengths):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [8, 17, 64, 100, 256, 511, 1000])
+def test_few_alternatives_of_short_rows(V, dtype):
+    """One to eight of rows with ties, 0 and -0 and masks, some of which leave less than K; ragged, so that wavefronts
+    hold rows that do not count, and a number of rows that fills no wavefront."""
+    x, tokens, g = inputs(V, 5, 41, V, dtype)
+    x = (x * 2).round() / 2
+    x[0, :9] = x[0, :9].masked_fill((torch.rand(9, V, generator=g) < 0.9).to(DEV), -math.inf)
+    x[1, 3], x[1, 4, V // 2], x[1, 5] = -math.inf, math.nan, -0.0
+    lengths = torch.tensor([41, 7, 0, 20, 33], device=DEV, dtype=torch.int32)
+    valid = ref.valid_positions((5, 41), lengths)
+    lost = valid & ((x == -math.inf).all(-1) | x.isnan().any(-1)).cpu()           # (rows without a distribution)
+    assert lost[1, 3] and lost[1, 4]
+    for k in range(1, 9):
+        r = tb.top_logprobs(x, k, tokens, lengths=lengths, want_entropy=True)
+        assert (r.ids.cpu()[lost] == -1).all() and r.logprobs.cpu()[lost].isnan().all()
+        _, _, ids, lps = plain.top(x.masked_fill(lost.to(DEV).unsqueeze(-1), 0.0), k, valid & ~lost)
+        assert torch.equal(r.ids.cpu().long(), ids)
+        got = r.logprobs.cpu().double()
+        there, none = ids >= 0, (ids < 0) & ~lost.unsqueeze(-1)
+        assert (got[none] == -math.inf).all()
+        near(torch.where(there, got, 0.0), torch.where(there, lps.detach(), torch.zeros_like(lps)), LP, k)
