@@ -16,7 +16,7 @@
 // counted as four of them.  On one MI355X, among other calls: 16 x 256 rows (three in four of which count) of 32000
 // values in bfloat16, K = 64, 47 us (4.2 TB/s); 10240 of 50257, K = 20, with entropies 204 us (5.1; 79 % of the vector
 // units' time); 1842 of 262144 in float16, K = 256, 248 us (3.9); 3884 of 50257 in float32, K = 20, with
-// entropies 190 us (4.1); 1113000 of 64, K = 5, 95 us (2.9; the exchanges of the sorted chunks); one row of 50257 8.3 us,
+// entropies 190 us (4.1); 1113000 of 64, K = 5, 79 us (3.4; issue and stores); one row of 50257 8.3 us,
 // on one unit; four of 262144 in float32 12 us, two launches.
 #pragma once
 
