@@ -10,7 +10,7 @@
 #include <torch/csrc/autograd/saved_variable.h>
 #include <ATen/ATen.h>
 
-#include "../tb_py_capture.h"
+#include "../loss/tb_py_capture.h"
 #include "tensorembed.h"
 
 namespace {

@@ -13,7 +13,7 @@
 #include <torch/csrc/autograd/saved_variable.h>
 #include <ATen/ATen.h>
 
-#include "../tb_py_capture.h"
+#include "tb_py_capture.h"
 #include "tensorloss.h"
 
 namespace {
