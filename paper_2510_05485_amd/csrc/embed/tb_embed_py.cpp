@@ -135,7 +135,7 @@ struct EmbeddingBackward : public torch::autograd::Node {
   torch::autograd::variable_list apply(torch::autograd::variable_list&& in) override {
     std::lock_guard<std::mutex> lock(mutex_);
     TORCH_CHECK(!at::GradMode::is_enabled(), "the embedding cannot be differentiated twice");
-    TORCH_CHECK(!tb::leaves_capture(next_edges()), tb::kLeavesCapture);
+    TORCH_CHECK(!tb::leaves_capture(this), tb::kLeavesCapture);
     if (!in[0].defined()) return {at::Tensor()};
     at::Tensor ids = tokens.unpack(), n = lengths.unpack(), m = mask.unpack(), rows = in[0];
     if (ids.defined() && ids.dim() > 0 && ids.size(-1) > 1 && ids.stride(-1) != 1) ids = ids.contiguous();

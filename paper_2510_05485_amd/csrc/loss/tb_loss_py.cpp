@@ -8,7 +8,6 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/function.h>
 #include <torch/csrc/autograd/functions/utils.h>
-#include <torch/csrc/autograd/python_cpp_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/autograd/saved_variable.h>
 #include <ATen/ATen.h>
@@ -196,6 +195,7 @@ struct RowsBackward : public torch::autograd::Node {
     std::lock_guard<std::mutex> lock(mutex_);
     TORCH_CHECK(!at::GradMode::is_enabled(), "the losses over logits cannot be differentiated twice");
     if (!in[0].defined() && (in.size() < 2 || !in[1].defined())) return {at::Tensor()};
+    TORCH_CHECK(!tb::leaves_capture(this), tb::kLeavesCapture);
     // (unpacking checks that nothing has been written over since)
     auto rows = [](const at::Tensor& t) {
       return t.defined() && t.dim() > 0 && t.stride(-1) != 1 && t.size(-1) > 1 ? t.contiguous() : t;
@@ -273,7 +273,7 @@ struct TopBackward : public torch::autograd::Node {
   torch::autograd::variable_list apply(torch::autograd::variable_list&& in) override {
     std::lock_guard<std::mutex> lock(mutex_);
     TORCH_CHECK(!at::GradMode::is_enabled(), "the losses over logits cannot be differentiated twice");
-    TORCH_CHECK(!tb::leaves_capture(next_edges()), tb::kLeavesCapture);
+    TORCH_CHECK(!tb::leaves_capture(this), tb::kLeavesCapture);
     const size_t of_tokens = 1, of_entropy = 1 + tokens_too;
     bool any = false;
     for (const at::Tensor& d : in) any = any || d.defined();
@@ -561,11 +561,9 @@ PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
-// leaves_capture(function): whether a captured backward pass would go on to this next function outside the capture
-PyObject* leaves_capture(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n != 1 || !torch::autograd::THPCppFunction_Check(args[0])) Py_RETURN_FALSE;
-  const auto* function = reinterpret_cast<torch::autograd::THPCppFunction*>(args[0]);
-  return PyBool_FromLong(tb::leaves_capture(function->cdata.get()));
+// leaves_capture(): whether the backward pass that the calling Function is part of is captured and would leave the capture
+PyObject* leaves_capture(PyObject*, PyObject* const*, Py_ssize_t) {
+  return PyBool_FromLong(tb::leaves_capture(torch::autograd::get_current_node().get()));
 }
 
 PyMethodDef methods[] = {

@@ -13,9 +13,10 @@ Common arguments
 
 What stands at positions that do not count has no part in anything; their embeddings are 0.  A table's gradient is
 summed in float32 in an order that does not change from call to call.  Gradients are for reverse mode, and of first
-order; tables with a forward-mode tangent are refused, and so is a backward pass that is captured into a graph while an
-eager graph holds the same table.  Everything runs on the current stream of the table's (or rows') GPU, and nothing
-synchronises.  See include/tensorembed.h.
+order; tables with a forward-mode tangent are refused, and so is a backward pass that is captured into a HIP graph
+while a graph from outside the capture, on the default stream, holds the table or the leaf that it comes from.
+Everything runs on the current stream of the table's (or rows') GPU, and nothing synchronises.  See
+include/tensorembed.h.
 """
 from __future__ import annotations
 
@@ -198,7 +199,7 @@ class _Embedding(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_rows):
-        _stay_in_capture(ctx)
+        _stay_in_capture()
         tokens, lengths, mask = ctx.saved_tensors
         (V, D), dtype = ctx.table
         rows = _values(d_rows.to(dtype), (2, 3), "the embeddings' gradient")

@@ -26,7 +26,9 @@ Common arguments
   status       int32 [1] on the GPU; TB_DEV_TOKEN_RANGE / TB_DEV_LENGTH_RANGE are OR-ed into it
 
 What stands at positions that do not count has no part in anything; what is returned for them is 0.
-Gradients are for reverse mode, and of first order; logits with a forward-mode tangent are refused.
+Gradients are for reverse mode, and of first order; logits with a forward-mode tangent are refused.  So is a
+backward pass that is captured into a HIP graph while a graph from outside the capture, on the default stream,
+holds a leaf (or anything else) that the gradient goes on to from here: it would end the process.
 Everything runs on the current stream of the logits' GPU, and nothing synchronises.  See
 include/tensorloss.h for the formulas and for what wrong ids and infinite logits give.
 """
@@ -339,6 +341,13 @@ def _rows_gradient(call, state, d_lp, d_entropy, d_strides, upstream):
     return out
 
 
+def _stay_in_capture() -> None:
+    """Raises where a captured backward pass would leave the capture (as the native nodes do)."""
+    if torch.cuda.is_current_stream_capturing() and native().leaves_capture():
+        raise RuntimeError("a backward pass is being captured while a graph from outside the capture holds a leaf that "
+                           "it goes on to: let go of that graph (or capture with a detached leaf)")
+
+
 class _TokenLogprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, tokens, lengths, mask, temperature, want_entropy, status):
@@ -355,6 +364,7 @@ class _TokenLogprobs(torch.autograd.Function):
         none = (None,) * 6
         if d_lp is None and d_entropy is None:
             return (None, *none)
+        _stay_in_capture()
         logits, tokens, lengths, mask, state = ctx.saved_tensors
         call = _Call(logits, tokens, lengths, mask, ctx.temperature, None)
         as32 = lambda d: None if d is None else d.to(torch.float32).contiguous()
@@ -396,13 +406,6 @@ def _top(call, k, tokens, want_entropy, id_dtype, keep_state):
     return ids, values, lp, entropy, state
 
 
-def _stay_in_capture(ctx) -> None:
-    """Raises where a captured backward pass would leave the capture (as the native nodes do)."""
-    if torch.cuda.is_current_stream_capturing() and any(native().leaves_capture(f) for f, _ in ctx.next_functions):
-        raise RuntimeError("a backward pass is being captured while a graph from outside the capture holds the same "
-                           "leaf: let go of that graph (or capture with a detached leaf)")
-
-
 class _TopLogprobs(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, k, tokens, lengths, mask, temperature, want_entropy, id_dtype, status):
@@ -417,7 +420,7 @@ class _TopLogprobs(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, _, d_top, d_lp, d_entropy):
-        _stay_in_capture(ctx)
+        _stay_in_capture()
         none = (None,) * 8
         if d_top is None and d_lp is None and d_entropy is None:
             return (None, *none)
@@ -442,8 +445,7 @@ def top_logprobs(logits, k: int, tokens=None, *, lengths=None, mask=None, temper
                  status: Optional[torch.Tensor] = None) -> TopLogprobs:
     """The k likeliest tokens of every position with their log-probabilities, in descending order, equal
     ones by their ids; with `tokens` their log-probabilities beside them, and with want_entropy the entropies
-    of the rows.  Log-probabilities and entropies are differentiable in the logits (a backward pass that is
-    captured into a graph while an eager graph holds the same leaf is refused).
+    of the rows.  Log-probabilities and entropies are differentiable in the logits.
 
     Tokens whose logit is -inf are none of the k: entries that are not there have the id -1 and the
     log-probability -inf, as at positions that do not count.  distillation_loss takes them so: ids and
@@ -496,6 +498,7 @@ class _PolicyLoss(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_loss):
+        _stay_in_capture()
         logits, tokens, lengths, mask, state, d_lp, d_entropy = ctx.saved_tensors
         call = _Call(logits, tokens, lengths, mask, ctx.temperature, None)
         grad = _rows_gradient(call, state, d_lp, d_entropy, (call.T, 1), d_loss.to(torch.float32))
@@ -574,6 +577,7 @@ class _PreferenceLoss(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_loss):
+        _stay_in_capture()
         logits, tokens, lengths, mask, state, d_sequence = ctx.saved_tensors
         call = _Call(logits, tokens, lengths, mask, ctx.temperature, None)
         grad = _rows_gradient(call, state, d_sequence, None, (1, 0), d_loss.to(torch.float32))
@@ -655,6 +659,7 @@ class _DistillationLoss(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, d_loss):
+        _stay_in_capture()
         logits, teacher_ids, teacher_logits, lengths, mask, state, d_row = ctx.saved_tensors
         call = _Call(logits, None, lengths, mask, ctx.temperature, None)
         q = _teacher(call, teacher_ids, teacher_logits, ctx.average)
