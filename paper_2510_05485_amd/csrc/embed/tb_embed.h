@@ -33,6 +33,7 @@ struct Lookup {
 struct Buckets {
   int low, bits;  // the digit is (token >> low) & (2^bits - 1)
   int rows;       // of a bucket
+  int held;       // of these by a workgroup of the sort, whose counters of them are in LDS
 };
 constexpr int kPartBlock = 2048;
 

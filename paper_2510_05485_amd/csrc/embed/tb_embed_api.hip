@@ -43,9 +43,10 @@ Plan plan_of(int64_t B, int64_t T, int V, int D) {
   const int64_t groups = (int64_t(V) + (1 << p.by.low) - 1) >> p.by.low;
   p.by.bits = std::min(many && V <= 1 << kMostPartBits ? kMostPartBits : 9, log2_up(groups));
   const int most_rows = kMostRows >> p.by.low;
-  while ((groups >> p.by.bits) + 1 > most_rows) ++p.by.bits;
+  while ((groups >> p.by.bits) + 1 > most_rows && !(many && p.by.bits == kMostPartBits)) ++p.by.bits;
   p.by.rows = int((groups + (1 << p.by.bits) - 1) >> p.by.bits) << p.by.low;
-  if (many && p.by.bits <= kMostPartBits) p.blocks = int((rows + kPartBlock - 1) / kPartBlock);
+  p.by.held = std::min(p.by.rows, kMostRows);  // (fewer than a digit's in tables of more than 2 million rows)
+  if (many) p.blocks = int((rows + kPartBlock - 1) / kPartBlock);
   // slices of 16 to 256 positions, about 4096 wavefronts of 512 columns together (32768 positions, D = 2048: 86.3 us with
   // 2048 wavefronts, 86.9 with 4096, 103 with 8192; 2097152, D = 64: 79, 72 and 78)
   const int64_t columns = (D + 511) / 512, each = D < 512 ? std::max(1, 512 / D) : 1;

@@ -61,6 +61,8 @@ __device__ __forceinline__ int row_in(const Buckets& by, int token) {
 __device__ __forceinline__ int64_t token_in(const Buckets& by, int digit, int row) {
   return (int64_t(row >> by.low) << by.bits | digit) << by.low | (row & ((1 << by.low) - 1));
 }
+// how many workgroups share a digit
+__host__ __device__ inline int ranges_of(const Buckets& by) { return (by.rows + by.held - 1) / by.held; }
 __device__ __forceinline__ int lanes_before(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi(uint32_t(mask >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(mask), 0));
 }
@@ -219,15 +221,28 @@ constexpr int kSortThreads = 512, kListed = 384;  // positions that a wavefront 
 // them), or over a list of those that were found: how many of each token each wavefront has, then each one's place.
 // The positions are read from the caller's tensors (few of them), from what ready_kernel has left, or from the digit's
 // part.  What it takes is the latency of its reads, sixteen of which are under way for each lane, and then the zeros.
-enum From { kTokens, kReady, kPart };
+// Of tables of more than two million rows (kRanges) a digit has more than the counters hold: each of its workgroups takes a
+// range of its rows, and reads the digit's part.
+enum From { kTokens, kReady, kPart, kRanges };
 template <typename X, int kFrom>
 __global__ __launch_bounds__(kSortThreads) void sort_kernel(Gradient c) {
-  constexpr bool kParted = kFrom == kPart;
+  constexpr bool kParted = kFrom == kPart || kFrom == kRanges;
   constexpr int kThreads = kSortThreads, kWaves = kThreads / kWave;
   extern __shared__ int next[];  // [wave][row]: how many, then where the next one goes
   __shared__ Entry listed[kWaves][kListed];
   __shared__ int part[kWaves];
-  const int digit = blockIdx.x, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, buckets = c.by.rows;
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  int digit = blockIdx.x, low_row = 0, buckets = c.by.rows;
+  if constexpr (kFrom == kRanges) {
+    const int ranges = ranges_of(c.by);
+    digit = blockIdx.x / ranges;
+    low_row = int(blockIdx.x - digit * ranges) * c.by.held;
+    buckets = min(c.by.held, c.by.rows - low_row);
+  }
+  auto is_mine = [&](int token) {
+    if (token < 0 || digit_of(c.by, token) != digit) return false;
+    return kFrom != kRanges || uint32_t(row_in(c.by, token) - low_row) < uint32_t(buckets);
+  };
   for (int i = threadIdx.x; i < kWaves * buckets; i += kThreads) next[i] = 0;
   int64_t first = 0, end = int64_t(c.r.B) * c.r.T;
   if constexpr (kParted) {
@@ -277,14 +292,14 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Gradient c) {
     entries(i + lane, std::integral_constant<int, kAhead>(), token, position, kFrom == kTokens && digit == 0);
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) {
-      const int d = digit_of(c.by, token[a]);
-      const bool mine = token[a] >= 0 && d == digit;
-      if (!kParted) below += token[a] >= 0 && d < digit;
+      const bool mine = is_mine(token[a]);
+      if (!kParted) below += token[a] >= 0 && digit_of(c.by, token[a]) < digit;
+      if (kFrom == kRanges) below += token[a] >= 0 && row_in(c.by, token[a]) < low_row;
       const uint64_t mask = __ballot(mine);
       if (mask == 0) continue;
       // (lanes with the first one's token are counted together: 64 additions to one place of LDS take as many turns, and
       // 200000 positions of one token took 494 us so)
-      const int row = mine ? row_in(c.by, token[a]) : -1, leader = __ffsll(static_cast<unsigned long long>(mask)) - 1;
+      const int row = mine ? row_in(c.by, token[a]) - low_row : -1, leader = __ffsll(static_cast<unsigned long long>(mask)) - 1;
       const int row0 = __builtin_amdgcn_readlane(row, leader);
       const uint64_t alike = __ballot(row == row0);
       if (mine) {
@@ -295,10 +310,10 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Gradient c) {
       seen += __popcll(mask);
     }
   }
-  if constexpr (!kParted) {
+  if constexpr (kFrom != kPart) {
     int all;
     block_scan<kThreads>(below, part, &all);
-    first = all;
+    first = kParted ? first + all : all;
   }
   __syncthreads();
   // where each row's and wavefront's positions begin; rows without any
@@ -328,7 +343,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Gradient c) {
     typename X::type* out = static_cast<typename X::type*>(c.r.g);
     for (int row = threadIdx.x / lanes; row < buckets; row += kThreads / lanes) {
       if (next[row] >= 0) continue;
-      const int64_t token = token_in(c.by, digit, row);
+      const int64_t token = token_in(c.by, digit, row + low_row);
       if (token < c.r.V) write_zeros<X>(out + token * c.r.g_pos, c.D, threadIdx.x % lanes, lanes);
     }
   }
@@ -336,7 +351,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Gradient c) {
   // lanes with the token of the first of them, then those of the next
   int* mine = next + wave * buckets;
   auto place = [&](int token, uint32_t position) {
-    const int row = token >= 0 ? row_in(c.by, token) : -1;
+    const int row = token >= 0 ? row_in(c.by, token) - low_row : -1;
     uint64_t left = __ballot(token >= 0);
     while (left) {
       const int r0 = __builtin_amdgcn_readlane(row, __ffsll(static_cast<unsigned long long>(left)) - 1);
@@ -374,7 +389,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Gradient c) {
           t = token[j];
           p = position[j];
         }
-      place(t >= 0 && digit_of(c.by, t) == digit ? t : -1, p);
+      place(is_mine(t) ? t : -1, p);
     }
   }
 }
@@ -597,14 +612,16 @@ hipError_t launch_sums(const Gradient& c) {
 template <typename X, typename Out>
 hipError_t launch(const Gradient& c) {
   const int digits = 1 << c.by.bits;
-  const size_t next = size_t(kSortThreads / kWave) * c.by.rows * sizeof(int);
+  const size_t next = size_t(kSortThreads / kWave) * c.by.held * sizeof(int);
   if (c.blocks) {
     const size_t lds = size_t(digits) * sizeof(int);
     const bool sorted = c.by.rows == 1;  // (a digit is a token)
     part_count_kernel<<<c.blocks, kThreads, lds, c.stream>>>(c);
     part_sums_kernel<Out><<<digits, kThreads, 0, c.stream>>>(c);
     part_kernel<<<c.blocks, kThreads, (kThreads / kWave + 1) * lds, c.stream>>>(c, sorted ? c.sorted : c.parted);
-    if (!sorted) sort_kernel<Out, kPart><<<digits, kSortThreads, next, c.stream>>>(c);
+    const int ranges = ranges_of(c.by);
+    if (ranges > 1) sort_kernel<Out, kRanges><<<digits * ranges, kSortThreads, next, c.stream>>>(c);
+    else if (!sorted) sort_kernel<Out, kPart><<<digits, kSortThreads, next, c.stream>>>(c);
   } else if (c.tokens) {
     const int64_t rows = int64_t(c.r.B) * c.r.T;
     ready_kernel<<<int((rows + kReadyPer * kThreads - 1) / (kReadyPer * kThreads)), kThreads, 0, c.stream>>>(c);

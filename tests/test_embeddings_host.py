@@ -108,3 +108,13 @@ def test_python_refuses_what_is_not_on_a_gpu():
               lambda: tb.embedding_grad(torch.zeros(2, 3, 4), tokens, 5)):
         with pytest.raises(tb.TensorBLEUError, match="GPU"):
             f()
+
+
+@pytest.mark.parametrize("D", [1, 16, 4096])
+@pytest.mark.parametrize("V", [50257, 2_000_000, 2_500_000, 5_000_000, 1 << 26, 2 ** 31 - 1])
+def test_many_positions_are_parted_whatever_the_table(lib, V, D):
+    """Beyond 65536 positions: a list of tokens, entries in their parts and sorted ones, the parts' counts.  (Without parts
+    every workgroup of the sort reads every token, and there are as many as the table has rows, divided by 1024.)"""
+    for rows in (65537, 1 << 21):
+        slices = rows // 256
+        assert embeddings.workspace_bytes(1, rows, V, D) >= 20 * rows + 4 * (4 << 9) * (rows // 2048) // 4 + 8 * slices * D
