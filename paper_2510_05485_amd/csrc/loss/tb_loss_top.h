@@ -134,7 +134,9 @@ __device__ __forceinline__ float scaled_logit(const Found& f, float x, float k) 
   return f.apart ? (x - f.m) * k : fmaf(x, k, -scaled(f.m, k));
 }
 __device__ __forceinline__ float logprob(const Found& f, float x, float k, float inv_temp, float log_s) {
-  return (f.apart ? (x - f.m) * inv_temp : scaled_logit(f, x, k) * kLn2) - log_s;
+  const float z = (x - f.m) * inv_temp, scaled_z = f.apart ? z : scaled_logit(f, x, k) * kLn2;
+  // (x k overflows where x / temperature does not: a mask of the type's lowest value)
+  return (scaled_z == -INFINITY ? z : scaled_z) - log_s;
 }
 // A row without a finite logit, or with +inf or NaN
 __device__ __forceinline__ bool lost(const Found& f) { return !(f.s > 0.f); }
