@@ -239,10 +239,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Gradient c) {
     low_row = int(blockIdx.x - digit * ranges) * c.by.held;
     buckets = min(c.by.held, c.by.rows - low_row);
   }
-  auto is_mine = [&](int token) {
-    if (token < 0 || digit_of(c.by, token) != digit) return false;
-    return kFrom != kRanges || uint32_t(row_in(c.by, token) - low_row) < uint32_t(buckets);
-  };
+  auto in_range = [&](int token) { return kFrom != kRanges || uint32_t(row_in(c.by, token) - low_row) < uint32_t(buckets); };
   for (int i = threadIdx.x; i < kWaves * buckets; i += kThreads) next[i] = 0;
   int64_t first = 0, end = int64_t(c.r.B) * c.r.T;
   if constexpr (kParted) {
@@ -292,8 +289,9 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Gradient c) {
     entries(i + lane, std::integral_constant<int, kAhead>(), token, position, kFrom == kTokens && digit == 0);
 #pragma unroll
     for (int a = 0; a < kAhead; ++a) {
-      const bool mine = is_mine(token[a]);
-      if (!kParted) below += token[a] >= 0 && digit_of(c.by, token[a]) < digit;
+      const int d = digit_of(c.by, token[a]);
+      const bool mine = token[a] >= 0 && d == digit && in_range(token[a]);
+      if (!kParted) below += token[a] >= 0 && d < digit;
       if (kFrom == kRanges) below += token[a] >= 0 && row_in(c.by, token[a]) < low_row;
       const uint64_t mask = __ballot(mine);
       if (mask == 0) continue;
@@ -389,7 +387,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Gradient c) {
           t = token[j];
           p = position[j];
         }
-      place(is_mine(t) ? t : -1, p);
+      place(t >= 0 && digit_of(c.by, t) == digit && in_range(t) ? t : -1, p);
     }
   }
 }
