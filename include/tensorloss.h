@@ -45,10 +45,13 @@ typedef enum { TB_FLOAT32 = 0, TB_BFLOAT16 = 1, TB_FLOAT16 = 2 } tb_type_t;
 typedef struct tb_logits {
   const void* data;
   int64_t seq_stride, pos_stride; /* in elements */
-  int32_t B, T, V;                /* V >= 1; B*T and V below 2^31 */
+  int32_t B, T, V;                /* V in 1..TB_VALUES_MOST; B*T below 2^31 - 1 */
   int32_t type;                   /* tb_type_t */
   float temperature;              /* > 0, and log2(e) / temperature finite in float32 */
 } tb_logits_t;
+
+/* The end of a row and a workgroup behind it are still a number of 32 bits. */
+enum { TB_VALUES_MOST = 0x7FFFFE00 };
 
 typedef struct tb_positions {
   const void* tokens;    /* [B, T], row b at tokens + b*token_stride */

@@ -55,7 +55,7 @@ bool extent(int64_t seq, int64_t pos, const tb_logits_t& l, size_t bytes, int64_
 }
 
 int check(const tb_logits_t* l, const tb_positions_t* at, bool tokens, const tb_gradient_t* g, Call* c) {
-  if (!l || !at || l->V < 1 || !positions_fit(l->B, l->T) || l->type < TB_FLOAT32 || l->type > TB_FLOAT16 ||
+  if (!l || !at || l->V < 1 || l->V > TB_VALUES_MOST || !positions_fit(l->B, l->T) || l->type < TB_FLOAT32 || l->type > TB_FLOAT16 ||
       !(l->temperature > 0.f) || !(l->temperature < INFINITY))
     return TB_ERR_INVALID_ARG;
   Rows& r = c->rows;

@@ -46,6 +46,7 @@ TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 AVERAGES = {"token": 0, "sequence": 1, "sum": 2}
 PAIRS = {"sigmoid": 0, "hinge": 1, "ipo": 2}
 TEACHER_MOST = TOP_MOST = 1024
+VALUES_MOST = 2 ** 31 - 512
 
 EXPORTS = [
     "tensorloss_distill", "tensorloss_distill_grad", "tensorloss_policy", "tensorloss_preference",
@@ -214,7 +215,7 @@ class _Call:
         self.packed = logits.dim() == 2
         self.B, self.T = (1, self.shape[0]) if self.packed else self.shape
         self.V = int(logits.shape[-1])
-        if self.B * self.T >= 2 ** 31 - 1 or self.V >= 2 ** 31:
+        if self.B * self.T >= 2 ** 31 - 1 or self.V > VALUES_MOST:
             raise TensorBLEUError("too many positions or tokens for 32-bit counts")
         self.keep = []
         at = tb_positions_t()
