@@ -13,9 +13,11 @@
 //   join_kernel     tokens that go over the end of a slice
 //
 // Bound by HBM where there is much to move, else by four launches of 3 to 8 us.  On one MI355X, among other calls: 32 x
-// 1024 positions (62 % of which count) of 50257 tokens distributed like words, D = 2048, bfloat16, 87 us for 290 MB: 5 to read
-// the tokens, 42 for the sort with 175 MB of zeros, 31 for the sums, 7 for 500 joins.  2097152 positions of 64 tokens, D =
-// 64: 72 us: 25 for the parts, 30 for the sums of 142 MB, 8 for the joins.  Two positions: 9 us.
+// 1024 positions (62 % of which count) of 50257 tokens distributed like words, D = 2048, bfloat16, 79 to 87 us for 290 MB: 5 to read
+// the tokens, 37 to 42 for the sort (17 of them without its 175 MB of zeros), 32 for the sums, 8 for 500 joins.  2097152 positions of 64 tokens, D =
+// 64: 72 us: 25 for the parts, 30 for the sums of 142 MB, 8 for the joins.  Two positions: 9 us.  Not fast:
+// tokens that go over the end of a slice in narrow tables, a workgroup of 512 threads each (2097152 positions of 5 million
+// rows, D = 16: 576 of 950 us).
 #include "tb_embed.h"
 
 namespace tb {

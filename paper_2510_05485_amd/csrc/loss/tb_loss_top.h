@@ -12,12 +12,14 @@
 //   top_kernel    a wavefront, or a workgroup, holds a row (or a part of a long one) in its registers, or tile by tile
 //   join_kernel   joins the parts of long rows, where there are few
 //
-// Long rows are bound by HBM and, with entropies, by the vector units alike: about 9 instructions a value, an exponential
-// counted as four of them.  On one MI355X, among other calls: 16 x 256 rows (three in four of which count) of 32000
-// values in bfloat16, K = 64, 47 us (4.2 TB/s); 10240 of 50257, K = 20, with entropies 204 us (5.1; 79 % of the vector
-// units' time); 1842 of 262144 in float16, K = 256, 248 us (3.9); 3884 of 50257 in float32, K = 20, with
-// entropies 190 us (4.1); 1113000 of 64, K = 5, 79 us (3.4; issue and stores); one row of 50257 8.3 us,
-// on one unit; four of 262144 in float32 12 us, two launches.
+// Long rows are bound by HBM and, with entropies, by the vector units alike: 10 to 11 vector instructions a value, one of
+// them an exponential at a quarter of the rate, under way for 76 % of a unit's busy cycles.  On one MI355X, among other
+// calls: 16 x 256 rows (three in four of which count) of 32000 values in bfloat16, K = 64, 47 us (4.2 TB/s); 10240 of
+// 50257, K = 20, with entropies 204 us (5.1); 1842 of 262144 in float16, K = 256, 248 us (3.9); 3884 of 50257 in float32,
+// K = 20, with entropies 190 us (4.1); 1113000 of 64, K = 5, 79 us (3.4; issue and stores); one row of 50257 8.3 us, on
+// one unit; four of 262144 in float32 12 us, two launches.  Far from that: many alternatives of short rows (66582 of 635,
+// K = 134, 338 us), and more than 512 alternatives, of rows taken tile by tile (1024 of 262144 in float32: K = 512 292 us,
+// 1024 6230, in 18 sweeps) and of others (4096 of 32000 in bfloat16, K = 1024, 1142 us: the order of the candidates).
 #pragma once
 
 #include "tb_loss_rows.h"
